@@ -354,6 +354,108 @@ fd_status fd_scatter_update(const fd_plan* plan, int32_t C, float* x, const floa
                             const int32_t* idx, const int32_t* m, const float* dt, float* vcache,
                             const uint8_t* active, int32_t skip_mode, fd_stream_t stream);
 
+/* ---------------------------------------------------------------- 8-bit rows
+ * Rows and weights in 8 bits with block scales, for the products of a served
+ * model (Sec. 4 Backend runs the active patches through the backbone's linear
+ * layers; the paper does not prescribe their number format).  A value is
+ *   code * 2^(s - 127),
+ * code an OCP e4m3 byte (largest 448, no infinities), s one byte (E8M0) per
+ * block of 128 columns of one row (activations) or of 128 rows x 128 columns
+ * (weights); the last block of a row or of the rows may be shorter.  s - 127 is
+ * the smallest power, at least -126, at which the block's largest magnitude is at
+ * most 448, and codes are rounded to nearest even, so a value is off by at most
+ * 2^-4 of itself or 2^-10 of its scale.  A block that holds an infinity or a NaN has s = 255 and
+ * NaN in every code.  Scale bytes are [rows or row blocks][fd_scale_stride(cols)]:
+ * byte kb of a row belongs to columns 128 kb ..; the padding is neither read nor
+ * written.  Row counts `m` are device int32 [1], at most n_rows (the capacity);
+ * outputs past them are untouched.  Column counts are multiples of 16.
+ */
+int32_t fd_scale_stride(int32_t cols); /* ceil(cols / 128) rounded up to a multiple of 4; 0 for cols < 1 */
+
+/*
+ * bf16 values to codes.
+ *   block_rows  1: one scale per row and 128 columns; 128: per 128 x 128 block
+ *   x     device bf16 [n_rows][cols], 16-byte aligned
+ *   m     device int32 [1] or null (all n_rows); must be null with block_rows 128
+ *   q     device e4m3 [n_rows][cols], 16-byte aligned (output)
+ *   scale device uint8 [ceil(n_rows / block_rows)][fd_scale_stride(cols)] (output)
+ */
+fd_status fd_quant_blocks(int32_t n_rows, int32_t cols, int32_t block_rows, const uint16_t* x, const int32_t* m,
+                          uint8_t* q, uint8_t* scale, fd_stream_t stream);
+
+/*
+ * The residual stream through its root-mean-square norm to 8-bit rows, for i < *m
+ * with b the row's request:
+ *   h[i] += gate_b * y[i]                                    (only with y)
+ *   a    = h[i] / sqrt(mean(h[i]^2) + eps) * weight * (1 + scale_b) + shift_b
+ *   q, q_scale = a in codes, one scale per 128 columns
+ * in fp32, a rounded once.  The squares are formed in fp32: rows whose magnitudes
+ * exceed 2^63 overflow to a norm of zero.
+ *   h      device fp32 [n_rows][D], 16-byte aligned, updated in place
+ *   y      device bf16 [n_rows][D] or null (a branch's output)
+ *   gate, scale, shift  device fp32, request b's at + b * mod_stride, or null
+ *          (gate 1, scale 0, shift 0); 16-byte aligned, mod_stride % 4 == 0 (may be
+ *          0: the same for every request)
+ *   weight device fp32 [D] or null (1)
+ *   cu_q   device int32 [n_requests + 1], m device int32 [1], from fd_select; cu_q is
+ *          not read (may be null) with one request
+ * D is a multiple of 16, at most 12288; eps >= 0.
+ */
+fd_status fd_rms_quant(int32_t n_rows, int32_t D, int32_t n_requests, float* h, const uint16_t* y, const float* gate,
+                       const float* weight, const float* shift, const float* scale, int32_t mod_stride, float eps,
+                       const int32_t* cu_q, const int32_t* m, uint8_t* q, uint8_t* q_scale, fd_stream_t stream);
+
+/* Pairs of fd_rope: (2j, 2j + 1), or (j, j + dim / 2), of an axis' section of the head. */
+enum { FD_ROPE_INTERLEAVED = 0, FD_ROPE_HALVES = 1 };
+
+/* Rotary positions on up to four axes (a video's time, height and width): the head's
+ * first dim[0] values turn with the first axis, the next dim[1] with the second, ...;
+ * values past the last section are not turned.  Pair j of axis a turns by
+ *   pos_a * step[a] * theta[a]^(-2j / dim[a])  radians. */
+typedef struct fd_rope {
+  int32_t n_axes;      /* 1 .. 4                                      */
+  int32_t pairing;     /* FD_ROPE_INTERLEAVED or FD_ROPE_HALVES       */
+  int32_t dim[4];      /* even, >= 2; their sum is at most the head dim */
+  double theta[4];     /* > 0                                         */
+  double step[4];      /* finite; 1 for unscaled positions            */
+} fd_rope;
+
+/*
+ * Rotary positions on the active rows of a fused q | k | v product (the tokens'
+ * place in the latent grid, App. "Setup and Notation"; a DiT with rotary in place
+ * of learned positions): q and k turned in fp32 by angles formed in fp64, rounded
+ * once to bf16; q to its row, k and v to the cache rows of the row's token.
+ *   heads, kv_heads  query heads and key/value heads, head dim dh in {16, 64, 128}
+ *   coord  device int32 [n_tokens][n_axes], position of every token on every axis
+ *   qkv    device bf16 [n_rows][(heads + 2 kv_heads) dh]
+ *   idx    device int32 [n_rows], token of each row (distinct, in [0, n_tokens)),
+ *          or null (row i is token i)
+ *   q      device bf16 [n_rows][heads dh] (output)
+ *   k_cache, v_cache  device bf16 [n_tokens][kv_heads dh]; rows of other tokens untouched
+ * All 16-byte aligned but coord, idx and m; the outputs must not overlap qkv or
+ * each other.
+ */
+fd_status fd_rope_axes(int32_t n_rows, int32_t n_tokens, const fd_rope* rope, int32_t heads, int32_t kv_heads, int32_t dh,
+                       const int32_t* coord, const uint16_t* qkv, const int32_t* idx, const int32_t* m, uint16_t* q,
+                       uint16_t* k_cache, uint16_t* v_cache, fd_stream_t stream);
+
+/*
+ * A linear layer on 8-bit rows and weights:
+ *   y[i] = act(a[i] w^T + bias) for i < *m, products of the values the codes stand
+ * for, sums in fp32; act GELU (tanh form) or none.
+ *   a, a_scale  device codes [n_rows][n_in] and their row scales
+ *   w, w_scale  device codes [n_out][n_in] and their 128 x 128 scales
+ *   bias        device fp32 [n_out] or null
+ *   m           device int32 [1] or null (all n_rows)
+ *   one output, 16-byte aligned: y_bf [n_rows][n_out] bf16, y_fp fp32, or y_q and
+ *   y_scale (codes and row scales)
+ * n_in and n_out are multiples of 16; weights below 2 GiB.  Codes, bias and outputs
+ * 16-byte, scales 4-byte aligned; the output must not overlap the inputs.
+ */
+fd_status fd_scaled_linear(int32_t n_rows, int32_t n_out, int32_t n_in, const uint8_t* a, const uint8_t* a_scale,
+                           const uint8_t* w, const uint8_t* w_scale, const float* bias, int32_t gelu, const int32_t* m,
+                           uint16_t* y_bf, float* y_fp, uint8_t* y_q, uint8_t* y_scale, fd_stream_t stream);
+
 /* ---------------------------------------------------------------- timing
  * Kernel timer for measurement: while armed for `kernel`, every launch of that
  * kernel records a pair of HIP events around it on its stream (up to
@@ -367,7 +469,8 @@ fd_status fd_scatter_update(const fd_plan* plan, int32_t C, float* x, const floa
 enum {
   FD_K_SCORE = 1, FD_K_SELECT, FD_K_GATHER, FD_K_EMBED, FD_K_ADALN, FD_K_LN,
   FD_K_GEMM_QKV, FD_K_ATTN, FD_K_GEMM_O, FD_K_GEMM_MLP1, FD_K_GEMM_MLP2,
-  FD_K_FINAL, FD_K_SCATTER, FD_K_IMPORTANCE, FD_K_PARTITION
+  FD_K_FINAL, FD_K_SCATTER, FD_K_IMPORTANCE, FD_K_PARTITION,
+  FD_K_QUANT, FD_K_RMS, FD_K_ROPE, FD_K_LINEAR
 };
 fd_status fd_timer_arm(int32_t kernel, int32_t capacity);
 int32_t fd_timer_read(float* ms, int32_t capacity);

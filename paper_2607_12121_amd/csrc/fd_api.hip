@@ -1,5 +1,6 @@
 // C ABI entry points: argument validation, workspace carving and launch order of
 // the region-sparse DiT step.  Nothing here allocates device memory.
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
@@ -9,6 +10,7 @@
 
 #include "fd_common.h"
 #include "fd_rules.h"
+#include "fd_scaled.h"
 
 namespace {
 
@@ -107,6 +109,32 @@ fd_status check_C(int C) {
     fd_status st_ = (expr);           \
     if (st_ != FD_OK) return st_;     \
   } while (0)
+
+// Column counts of 8-bit rows: 16-byte aligned rows.
+fd_status check_cols(int cols) {
+  if (cols % 16) return fdh::set_error("%d columns, not a multiple of 16", cols), FD_E_UNSUPPORTED;
+  return FD_OK;
+}
+
+// Checks a rotary descriptor and fills the kernel's sections and the turns of its pairs.
+fd_status rope_turns(const fd_rope* r, int dh, fdh::RopeArgs* g) {
+  FD_REQUIRE(r, "rope is null");
+  if (dh != 16 && dh != 64 && dh != 128)
+    return fdh::set_error("head dim %d not in {16, 64, 128}", dh), FD_E_UNSUPPORTED;
+  FD_REQUIRE(r->n_axes >= 1 && r->n_axes <= fdh::kMaxRopeAxes, "%d axes, not 1 to 4", r->n_axes);
+  FD_REQUIRE(r->pairing == FD_ROPE_INTERLEAVED || r->pairing == FD_ROPE_HALVES, "unknown pairing %d", r->pairing);
+  g->n_axes = r->n_axes;
+  g->pairs = 0;
+  for (int a = 0; a < r->n_axes; ++a) {
+    const int d = r->dim[a];
+    FD_REQUIRE(d >= 2 && d % 2 == 0 && d <= dh - 2 * g->pairs, "axis %d: %d values of a head of %d", a, d, dh);
+    FD_REQUIRE(r->theta[a] > 0 && isfinite(r->theta[a]) && isfinite(r->step[a]), "axis %d: theta or step", a);
+    g->dim[a] = d;
+    for (int j = 0; j < d / 2; ++j)
+      g->turns[g->pairs++] = r->step[a] * pow(r->theta[a], -2.0 * j / d) / 6.283185307179586;
+  }
+  return FD_OK;
+}
 
 #define FD_LAUNCH(kernel_id, stream, call)               \
   do {                                                   \
@@ -531,8 +559,83 @@ fd_status fd_scatter_update(const fd_plan* plan, int32_t C, float* x, const floa
   return FD_OK;
 }
 
+int32_t fd_scale_stride(int32_t cols) { return cols < 1 ? 0 : fd::scale_stride(cols); }
+
+fd_status fd_quant_blocks(int32_t n_rows, int32_t cols, int32_t block_rows, const uint16_t* x, const int32_t* m,
+                          uint8_t* q, uint8_t* scale, fd_stream_t stream) {
+  FD_REQUIRE(n_rows >= 1 && cols >= 1, "sizes must be positive");
+  FD_REQUIRE(block_rows == 1 || block_rows == fd::kScaleBlock, "block_rows = %d, not 1 or 128", block_rows);
+  FD_TRY(check_cols(cols));
+  FD_REQUIRE(x && q && scale, "null pointer");
+  FD_REQUIRE(!m || block_rows == 1, "a row count with 128-row blocks");
+  FD_REQUIRE(aligned(x, 16) && aligned(q, 16), "misaligned buffer");
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  FD_LAUNCH(FD_K_QUANT, s, fdh::launch_quant_blocks(x, n_rows, cols, block_rows, m, q, scale, s));
+  return FD_OK;
+}
+
+fd_status fd_rms_quant(int32_t n_rows, int32_t D, int32_t n_requests, float* h, const uint16_t* y, const float* gate,
+                       const float* weight, const float* shift, const float* scale, int32_t mod_stride, float eps,
+                       const int32_t* cu_q, const int32_t* m, uint8_t* q, uint8_t* q_scale, fd_stream_t stream) {
+  FD_REQUIRE(n_rows >= 1 && D >= 1 && n_requests >= 1, "sizes must be positive");
+  FD_TRY(check_cols(D));
+  if (D > 12288) return fdh::set_error("D > 12288 unsupported"), FD_E_UNSUPPORTED;
+  FD_REQUIRE(h && m && q && q_scale && (cu_q || n_requests == 1), "null pointer");
+  FD_REQUIRE(y || !gate, "a gate without a branch");
+  FD_REQUIRE(eps >= 0.f, "eps must be >= 0");
+  FD_REQUIRE(mod_stride >= 0 && mod_stride % 4 == 0, "mod_stride = %d, not a multiple of 4", mod_stride);
+  FD_REQUIRE(aligned(h, 16) && aligned(y, 16) && aligned(gate, 16) && aligned(weight, 16) && aligned(shift, 16) &&
+                 aligned(scale, 16) && aligned(q, 16),
+             "misaligned buffer");
+  fdh::RmsArgs g{};
+  g.n_rows = n_rows; g.D = D; g.n_req = n_requests; g.mod_stride = mod_stride; g.cu_q = cu_q; g.m = m; g.eps = eps;
+  g.h = h; g.y = y; g.gate = gate; g.weight = weight; g.shift = shift; g.scale = scale; g.q = q; g.q_scale = q_scale;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  FD_LAUNCH(FD_K_RMS, s, fdh::launch_rms_quant(g, s));
+  return FD_OK;
+}
+
+fd_status fd_rope_axes(int32_t n_rows, int32_t n_tokens, const fd_rope* rope, int32_t heads, int32_t kv_heads, int32_t dh,
+                       const int32_t* coord, const uint16_t* qkv, const int32_t* idx, const int32_t* m, uint16_t* q,
+                       uint16_t* k_cache, uint16_t* v_cache, fd_stream_t stream) {
+  FD_REQUIRE(n_rows >= 1 && n_rows <= n_tokens, "%d rows of %d tokens", n_rows, n_tokens);
+  FD_REQUIRE(heads >= 1 && kv_heads >= 1, "heads must be positive");
+  FD_REQUIRE(coord && qkv && m && q && k_cache && v_cache, "null pointer");
+  FD_REQUIRE(aligned(qkv, 16) && aligned(q, 16) && aligned(k_cache, 16) && aligned(v_cache, 16), "misaligned buffer");
+  fdh::RopeArgs g{};
+  FD_TRY(rope_turns(rope, dh, &g));
+  if (heads > 4096 || kv_heads > 4096) return fdh::set_error("more than 4096 heads"), FD_E_UNSUPPORTED;
+  g.n_rows = n_rows; g.hq = heads; g.hk = kv_heads; g.dh = dh; g.m = m; g.idx = idx; g.coord = coord;
+  g.qkv = qkv; g.q = q; g.k = k_cache; g.v = v_cache;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  FD_LAUNCH(FD_K_ROPE, s, fdh::launch_rope(g, rope->pairing == FD_ROPE_HALVES, s));
+  return FD_OK;
+}
+
+fd_status fd_scaled_linear(int32_t n_rows, int32_t n_out, int32_t n_in, const uint8_t* a, const uint8_t* a_scale,
+                           const uint8_t* w, const uint8_t* w_scale, const float* bias, int32_t gelu, const int32_t* m,
+                           uint16_t* y_bf, float* y_fp, uint8_t* y_q, uint8_t* y_scale, fd_stream_t stream) {
+  FD_REQUIRE(n_rows >= 1 && n_out >= 1 && n_in >= 1, "sizes must be positive");
+  FD_TRY(check_cols(n_in));
+  FD_TRY(check_cols(n_out));
+  FD_REQUIRE(a && a_scale && w && w_scale, "null pointer");
+  FD_REQUIRE((y_bf != nullptr) + (y_fp != nullptr) + (y_q != nullptr) == 1 && !y_q == !y_scale, "not one output");
+  FD_REQUIRE(gelu == 0 || gelu == 1, "gelu = %d", gelu);
+  FD_REQUIRE(aligned(a, 16) && aligned(w, 16) && aligned(a_scale, 4) && aligned(w_scale, 4) && aligned(bias, 16) &&
+                 aligned(y_bf, 16) && aligned(y_fp, 16) && aligned(y_q, 16),
+             "misaligned buffer");
+  if (static_cast<long long>(n_out) * n_in > fdh::kMaxGemmBytes)
+    return fdh::set_error("weights of 2 GiB or more (%d x %d given)", n_out, n_in), FD_E_UNSUPPORTED;
+  fdh::ScaledArgs g{};
+  g.n_rows = n_rows; g.N = n_out; g.K = n_in; g.m = m; g.a = a; g.a_scale = a_scale; g.w = w; g.w_scale = w_scale;
+  g.bias = bias; g.gelu = gelu; g.y_bf16 = y_bf; g.y_f32 = y_fp; g.y_q = y_q; g.y_scale = y_scale;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  FD_LAUNCH(FD_K_LINEAR, s, fdh::launch_scaled_linear(g, s));
+  return FD_OK;
+}
+
 fd_status fd_timer_arm(int32_t kernel, int32_t capacity) {
-  FD_REQUIRE(kernel >= FD_K_SCORE && kernel <= FD_K_PARTITION && capacity >= 1 && capacity <= (1 << 20),
+  FD_REQUIRE(kernel >= FD_K_SCORE && kernel <= FD_K_LINEAR && capacity >= 1 && capacity <= (1 << 20),
              "bad timer arguments");
   std::lock_guard<std::mutex> lk(g_timer.mu);
   for (hipEvent_t e : g_timer.ev) (void)hipEventDestroy(e);

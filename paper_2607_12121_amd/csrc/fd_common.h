@@ -157,6 +157,45 @@ size_t partition_ws_bytes(int n_tokens, int n_requests);
 hipError_t launch_partition(int n_requests, const int32_t* req_tok_off, const int32_t* req_reg_off,
                             const uint16_t* saliency, int32_t* region, void* ws, hipStream_t s);
 
+// 8-bit rows and weights with block scales (fd_scaled.h).
+hipError_t launch_quant_blocks(const uint16_t* x, int n_rows, int cols, int block_rows, const int32_t* m, uint8_t* q,
+                               uint8_t* scale, hipStream_t s);
+struct RmsArgs {
+  int n_rows, D, n_req, mod_stride;
+  const int32_t* cu_q; const int32_t* m;
+  float eps;
+  float* h;                      // [n_rows][D], += gate * y
+  const uint16_t* y;             // optional
+  const float* gate;             // optional, [n_req] rows of mod_stride, as shift and scale
+  const float* weight;           // optional [D]
+  const float* shift; const float* scale;
+  uint8_t* q; uint8_t* q_scale;
+};
+hipError_t launch_rms_quant(const RmsArgs& g, hipStream_t s);
+
+constexpr int kMaxRopeAxes = 4, kMaxRopePairs = 64;
+struct RopeArgs {
+  int n_rows, hq, hk, dh, n_axes, pairs;
+  int dim[kMaxRopeAxes];
+  const int32_t* m; const int32_t* idx; const int32_t* coord;
+  const uint16_t* qkv;           // [n_rows][(hq + 2 hk) dh]
+  uint16_t* q; uint16_t* k; uint16_t* v;
+  double turns[kMaxRopePairs];   // turns of each pair per unit of its axis' position
+};
+hipError_t launch_rope(const RopeArgs& g, bool halves, hipStream_t s);
+
+struct ScaledArgs {
+  int n_rows, N, K;
+  const int32_t* m;                             // optional: all n_rows rows without it
+  const uint8_t* a; const uint8_t* a_scale;     // [n_rows][K]
+  const uint8_t* w; const uint8_t* w_scale;     // [N][K]
+  const float* bias;                            // optional
+  int gelu;
+  uint16_t* y_bf16; float* y_f32;               // one of the outputs: [n_rows][N]
+  uint8_t* y_q; uint8_t* y_scale;
+};
+hipError_t launch_scaled_linear(const ScaledArgs& g, hipStream_t s);
+
 // Bytes of KV-split scratch the attention kernel needs for head dim dh.
 size_t attn_scratch_bytes(int dh);
 

@@ -24,7 +24,7 @@ FD_SKIP_REUSE_DRIFT = 1
 
 KERNELS = {"score": 1, "select": 2, "gather": 3, "embed": 4, "adaln": 5, "ln": 6, "gemm_qkv": 7,
            "attn": 8, "gemm_o": 9, "gemm_mlp1": 10, "gemm_mlp2": 11, "final": 12, "scatter": 13,
-           "importance": 14, "partition": 15}
+           "importance": 14, "partition": 15, "quant": 16, "rms": 17, "rope": 18, "linear": 19}
 
 _p = ctypes.c_void_p
 _i32 = ctypes.c_int32
@@ -52,6 +52,11 @@ class FdFinalWeights(ctypes.Structure):
 
 class FdGate(ctypes.Structure):
     _fields_ = [("eta", ctypes.c_double), ("max_skip", _i32)]
+
+
+class FdRope(ctypes.Structure):
+    _fields_ = [("n_axes", _i32), ("pairing", _i32), ("dim", _i32 * 4), ("theta", ctypes.c_double * 4),
+                ("step", ctypes.c_double * 4)]
 
 
 class FlashDiffError(RuntimeError):
@@ -92,6 +97,11 @@ def lib() -> ctypes.CDLL:
                                   ctypes.c_size_t, _p], _i32),
         "fd_partition_ws_size": ([_i32, _i32], ctypes.c_size_t),
         "fd_partition": ([_i32, _p, _p, _p, _p, _p, ctypes.c_size_t, _p], _i32),
+        "fd_scale_stride": ([_i32], _i32),
+        "fd_quant_blocks": ([_i32, _i32, _i32, _p, _p, _p, _p, _p], _i32),
+        "fd_rms_quant": ([_i32, _i32, _i32, _p, _p, _p, _p, _p, _p, _i32, ctypes.c_float, _p, _p, _p, _p, _p], _i32),
+        "fd_rope_axes": ([_i32, _i32, P(FdRope), _i32, _i32, _i32, _p, _p, _p, _p, _p, _p, _p, _p], _i32),
+        "fd_scaled_linear": ([_i32, _i32, _i32, _p, _p, _p, _p, _p, _i32, _p, _p, _p, _p, _p, _p], _i32),
         "fd_timer_arm": ([_i32, _i32], _i32),
         "fd_timer_read": ([_p, _i32], _i32),
         "fd_timer_disarm": ([], None),
@@ -109,7 +119,8 @@ def exported_symbols() -> Sequence[str]:
             "fd_region_score_noalloc",
             "fd_select", "fd_gather", "fd_embed", "fd_adaln", "fd_block_ws_size", "fd_block_forward", "fd_final",
             "fd_scatter_update", "fd_importance_ws_size", "fd_region_importance", "fd_partition_ws_size",
-            "fd_partition", "fd_timer_arm", "fd_timer_read", "fd_timer_disarm")
+            "fd_partition", "fd_scale_stride", "fd_quant_blocks", "fd_rms_quant", "fd_rope_axes", "fd_scaled_linear",
+            "fd_timer_arm", "fd_timer_read", "fd_timer_disarm")
 
 
 def _check(name: str, status: int) -> None:
@@ -127,7 +138,8 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 
 _DT = {"f32": (torch.float32,), "f64": (torch.float64,), "i32": (torch.int32,), "u8": (torch.uint8,),
-       "b16": (torch.bfloat16, torch.int16, torch.uint16), "bytes": None}
+       "b16": (torch.bfloat16, torch.int16, torch.uint16), "bytes": None,
+       "code": (torch.float8_e4m3fn, torch.uint8), "scale": (torch.uint8, torch.float8_e8m0fnu)}
 
 
 def _need(name: str, t: Optional[torch.Tensor], kind: str, numel: int, exact: bool = False,
@@ -390,6 +402,127 @@ def partition(saliency: torch.Tensor, req_tok_off, req_reg_off, stream=None) -> 
         ws.record_stream(stream)
         out.record_stream(stream)
     return out
+
+
+# ------------------------------------------------------------------ 8-bit rows
+
+def fd_scale_stride(cols: int) -> int:
+    """Bytes of a row of block scales: ceil(cols / 128) rounded up to a multiple of 4."""
+    return int(lib().fd_scale_stride(cols))
+
+
+def _rows(name: str, t: torch.Tensor) -> Sequence[int]:
+    if t.dim() != 2:
+        raise FlashDiffError(f"{name} must have two dimensions, got {tuple(t.shape)}")
+    return t.shape
+
+
+def _same_device(**tensors: Optional[torch.Tensor]) -> None:
+    """Every tensor of a call on the current device, whose stream the call runs on."""
+    cur = torch.cuda.current_device()
+    for name, t in tensors.items():
+        if t is not None and t.device.index != cur:
+            raise FlashDiffError(f"{name} is on {t.device}, the current device is {cur}")
+
+
+def fd_quant_blocks(x, block_rows: int, q, scale, m=None, stream=None) -> None:
+    """bf16 x [rows, cols] to e4m3 codes q [rows, cols] and scale bytes
+    [ceil(rows / block_rows), fd_scale_stride(cols)]; block_rows 1 (activations, `m` of
+    the rows when given) or 128 (weights)."""
+    rows, cols = _rows("x", x)
+    _need("x", x, "b16", rows * cols)
+    _need("q", q, "code", rows * cols)
+    _need("scale", scale, "scale", -(-rows // max(block_rows, 1)) * fd_scale_stride(cols))
+    _need("m", m, "i32", 1, optional=True)
+    _same_device(x=x, q=q, scale=scale, m=m)
+    _check("fd_quant_blocks", lib().fd_quant_blocks(rows, cols, block_rows, _ptr(x), _ptr(m), _ptr(q), _ptr(scale),
+                                                    _stream(stream)))
+
+
+def fd_rms_quant(h, q, scale, cu_q, m, y=None, gate=None, weight=None, shift=None, mod_scale=None, eps: float = 1e-6,
+                 stream=None) -> None:
+    """h [rows, D] fp32 += gate * y (with y), then its RMS norm times weight, modulated, as codes q
+    [rows, D] and scale bytes [rows, fd_scale_stride(D)].  gate, shift and mod_scale: fp32 [requests, D],
+    which may be column ranges of one modulation tensor (equal row strides)."""
+    rows, D = _rows("h", h)
+    B = int(cu_q.numel()) - 1
+    _need("h", h, "f32", rows * D)
+    _need("y", y, "b16", rows * D, optional=True)
+    _need("weight", weight, "f32", D, optional=True)
+    _need("cu_q", cu_q, "i32", 2)
+    _need("m", m, "i32", 1)
+    _need("q", q, "code", rows * D)
+    _need("scale", scale, "scale", rows * fd_scale_stride(D))
+    stride = None
+    for n_, t_ in (("gate", gate), ("shift", shift), ("mod_scale", mod_scale)):
+        if t_ is None:
+            continue
+        _need(n_, t_, "f32", B * D)
+        if tuple(_rows(n_, t_)) != (B, D) or t_.stride(1) != 1:
+            raise FlashDiffError(f"{n_} must be [{B}, {D}] with contiguous rows")
+        if stride is not None and t_.stride(0) != stride:
+            raise FlashDiffError("gate, shift and mod_scale must have the same row stride")
+        stride = t_.stride(0)
+    _same_device(h=h, y=y, gate=gate, weight=weight, shift=shift, mod_scale=mod_scale, cu_q=cu_q, m=m, q=q, scale=scale)
+    at = [None if t is None else t.data_ptr() for t in (gate, shift, mod_scale)]
+    _check("fd_rms_quant", lib().fd_rms_quant(rows, D, B, _ptr(h), _ptr(y), at[0], _ptr(weight), at[1], at[2], stride or 0,
+                                              eps, _ptr(cu_q), _ptr(m), _ptr(q), _ptr(scale), _stream(stream)))
+
+
+def rope_axes(dims: Sequence[int], theta=10000.0, step=1.0, halves: bool = False) -> FdRope:
+    """Descriptor of rotary positions: the head's values per axis, theta and step of each axis (or
+    one for all), pairs (j, j + dim / 2) with halves, else (2j, 2j + 1)."""
+    n = len(dims)
+    if not 1 <= n <= 4:
+        raise FlashDiffError(f"{n} axes, not 1 to 4")
+    th, st = ([float(v)] * n if isinstance(v, (int, float)) else [float(u) for u in v] for v in (theta, step))
+    if len(th) != n or len(st) != n:
+        raise FlashDiffError("dims, theta and step must have one entry per axis")
+    pad = (0,) * (4 - n)
+    return FdRope(n, int(bool(halves)), (_i32 * 4)(*dims, *pad), (ctypes.c_double * 4)(*th, *pad),
+                  (ctypes.c_double * 4)(*st, *pad))
+
+
+def fd_rope_axes(qkv, coord, idx, m, q, k_cache, v_cache, heads: int, kv_heads: int, head_dim: int, dims=None, theta=10000.0,
+                 step=1.0, halves: bool = False, rope: Optional[FdRope] = None, stream=None) -> None:
+    """q | k | v rows qkv [rows, (heads + 2 kv_heads) head_dim]: q and k turned by the token's
+    coord [tokens, axes]; q to [rows, heads head_dim], k and v to the caches' rows idx.  The axes
+    are given by dims, theta, step and halves, or by a descriptor from rope_axes."""
+    r = rope if rope is not None else rope_axes(dims, theta, step, halves)
+    rows, tokens = _rows("qkv", qkv)[0], _rows("coord", coord)[0]
+    _need("qkv", qkv, "b16", rows * (heads + 2 * kv_heads) * head_dim, exact=True)
+    _need("coord", coord, "i32", tokens * r.n_axes, exact=True)
+    _need("idx", idx, "i32", rows, optional=True)
+    _need("m", m, "i32", 1)
+    _need("q", q, "b16", rows * heads * head_dim)
+    _need("k_cache", k_cache, "b16", tokens * kv_heads * head_dim)
+    _need("v_cache", v_cache, "b16", tokens * kv_heads * head_dim)
+    _same_device(qkv=qkv, coord=coord, idx=idx, m=m, q=q, k_cache=k_cache, v_cache=v_cache)
+    _check("fd_rope_axes", lib().fd_rope_axes(rows, tokens, ctypes.byref(r), heads, kv_heads, head_dim, _ptr(coord), _ptr(qkv),
+                                              _ptr(idx), _ptr(m), _ptr(q), _ptr(k_cache), _ptr(v_cache), _stream(stream)))
+
+
+def fd_scaled_linear(a, a_scale, w, w_scale, y, y_scale=None, bias=None, gelu: bool = False, m=None, stream=None) -> None:
+    """y = act(a w^T + bias) of codes a [rows, n_in] and w [n_out, n_in] with their scale bytes.
+    y's type chooses the output: bf16, fp32, or codes (with y_scale [rows, fd_scale_stride(n_out)])."""
+    (rows, k), (n, kw) = _rows("a", a), _rows("w", w)
+    if k != kw:
+        raise FlashDiffError(f"a has {k} columns, w {kw}")
+    codes = y.dtype in _DT["code"]
+    _need("a", a, "code", rows * k)
+    _need("a_scale", a_scale, "scale", rows * fd_scale_stride(k))
+    _need("w", w, "code", n * k)
+    _need("w_scale", w_scale, "scale", -(-n // 128) * fd_scale_stride(k))
+    _need("bias", bias, "f32", n, optional=True)
+    _need("m", m, "i32", 1, optional=True)
+    _need("y", y, "code" if codes else "f32" if y.dtype == torch.float32 else "b16", rows * n)
+    _need("y_scale", y_scale, "scale", rows * fd_scale_stride(n), optional=not codes)
+    _same_device(a=a, a_scale=a_scale, w=w, w_scale=w_scale, y=y, y_scale=y_scale, bias=bias, m=m)
+    out = _ptr(y)
+    _check("fd_scaled_linear", lib().fd_scaled_linear(
+        rows, n, k, _ptr(a), _ptr(a_scale), _ptr(w), _ptr(w_scale), _ptr(bias), int(gelu), _ptr(m),
+        None if codes or y.dtype == torch.float32 else out, out if y.dtype == torch.float32 else None, out if codes else None,
+        _ptr(y_scale) if codes else None, _stream(stream)))
 
 
 def fd_timer_arm(kernel: str, capacity: int) -> None:

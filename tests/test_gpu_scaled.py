@@ -1,0 +1,384 @@
+"""The 8-bit operators (fd_quant_blocks, fd_rms_quant, fd_rope_axes, fd_scaled_linear) against the
+64-bit reference: sizes around their blocks and tiles, no rows, rows past the count, infinities, NaN and zeros,
+every output type, and a run of them together."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import scaled as ref
+from paper_2607_12121_amd import flashdiff as fdl
+from tests import gpu_harness as gh
+
+pytestmark = pytest.mark.gpu
+
+U32, UB, U8 = 2.0 ** -24, 2.0 ** -8, 2.0 ** -4     # half steps of fp32, bf16 and e4m3
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    fdl.lib()
+
+
+def dev(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).cuda()
+
+
+def count(m):
+    return torch.tensor([m], dtype=torch.int32, device="cuda")
+
+
+def codes(rows, cols, block_rows=1, fill=0x55):
+    return (torch.full((rows, cols), fill, dtype=torch.uint8, device="cuda"),
+            torch.full((-(-rows // block_rows), ref.stride(cols)), fill, dtype=torch.uint8, device="cuda"))
+
+
+def bf16(x):
+    return torch.from_numpy(np.asarray(x, np.float32)).to(torch.bfloat16)
+
+
+def check_codes(q, s, want, err, block_rows=1):
+    """Codes q with scale bytes s (numpy) stand for `want` [rows][cols], itself known to +- err: every scale
+    byte is that of some block maximum within the error, every value within the error and half a code step."""
+    r, c = want.shape
+    nk = -(-c // 128)
+    lo = ref.scale_bytes(ref.block_tops(np.maximum(np.abs(want) - err, 0), block_rows))
+    hi = ref.scale_bytes(ref.block_tops(np.abs(want) + err, block_rows))
+    s = s[:, :nk]
+    assert np.all((lo <= s) & (s <= hi)), "scale bytes"
+    got = ref.values(q, s, block_rows)
+    half = np.maximum(U8 * (np.abs(want) + err), 2.0 ** -10 * ref.spread(ref.powers(s), r, c, block_rows))
+    # a value whose block maximum is within the error of a scale's limit may saturate by that error
+    worst = np.max(np.abs(got - want) - (half + err))
+    assert worst <= 0, f"a value is off by {worst} more than half a step"
+
+
+# ------------------------------------------------------------------ codes
+
+@pytest.mark.parametrize("rows,cols,m", [(1, 16, None), (1, 128, 1), (3, 144, 2), (5, 1088, 0), (130, 48, 129), (67, 1536, 67), (3, 6160, 3)])
+def test_quant_rows_exact(rows, cols, m):
+    """bf16 values are exact, so codes and scales have to be the definition's, bit for bit."""
+    gh.say(f"quant rows {rows}x{cols} m={m}")
+    rng = np.random.default_rng([rows, cols])
+    x = bf16(rng.standard_normal((rows, cols)) * np.exp(3 * rng.standard_normal((rows, 1))))
+    x[0, :16] = torch.tensor([0.0, -0.0, 1.0, -1.0] * 4)
+    q, s = codes(rows, cols)
+    fdl.fd_quant_blocks(x.cuda(), 1, q, s, m=None if m is None else count(m))
+    n = rows if m is None else m
+    wq, ws = ref.quant(x.double().numpy(), 1)
+    np.testing.assert_array_equal(q.cpu().numpy()[:n], wq[:n])
+    np.testing.assert_array_equal(s.cpu().numpy()[:n, :ws.shape[1]], ws[:n])
+    assert (q[n:] == 0x55).all() and (s[n:] == 0x55).all() and (s[:, ws.shape[1]:] == 0x55).all()
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 16), (128, 128), (129, 144), (127, 1088), (300, 336)])
+def test_quant_weights_exact(rows, cols):
+    gh.say(f"quant weights {rows}x{cols}")
+    rng = np.random.default_rng([rows, cols, 1])
+    x = bf16(0.02 * rng.standard_normal((rows, cols)))
+    q, s = codes(rows, cols, 128)
+    fdl.fd_quant_blocks(x.cuda(), 128, q, s)
+    wq, ws = ref.quant(x.double().numpy(), 128)
+    np.testing.assert_array_equal(q.cpu().numpy(), wq)
+    np.testing.assert_array_equal(s.cpu().numpy()[:, :ws.shape[1]], ws)
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quant_edges(block_rows):
+    """Zeros, subnormals, the largest values, every limit of a scale, infinities and NaN: a bad block is NaN
+    throughout and its neighbours are as ever."""
+    vals = [0.0, 1e-40, 1e-38, 3e38, 448.0, 450.0, 224.0, 225.0, 1.75, 1.7578125, np.inf, -np.inf, np.nan]
+    x = np.zeros((128 * len(vals) if block_rows == 128 else len(vals), 256), np.float32)
+    for i, v in enumerate(vals):
+        r = slice(128 * i, 128 * i + 128) if block_rows == 128 else slice(i, i + 1)
+        x[r, :128] = 0.37 * (v if np.isfinite(v) else 1.0)
+        x[128 * i + 77 if block_rows == 128 else i, 100] = v
+        x[r, 128:] = 1.5
+    x = bf16(x)
+    q, s = codes(*x.shape, block_rows)
+    fdl.fd_quant_blocks(x.cuda(), block_rows, q, s)
+    wq, ws = ref.quant(x.double().numpy(), block_rows)
+    np.testing.assert_array_equal(s.cpu().numpy()[:, :2], ws)
+    got = q.cpu().numpy()
+    bad = ref.spread(ws == 255, *x.shape, block_rows)
+    assert np.all((got[bad] & 127) == 127)
+    np.testing.assert_array_equal(got[~bad], wq[~bad])
+
+
+# ------------------------------------------------------------------ residual and norm
+
+def rms_case(rows, D, B, m, parts, seed=0):
+    rng = np.random.default_rng([rows, D, B, seed])
+    h = (rng.standard_normal((rows, D)) * np.exp(rng.standard_normal((rows, 1)))).astype(np.float32)
+    y = bf16(rng.standard_normal((rows, D))) if "y" in parts else None
+    mod = (0.3 * rng.standard_normal((B, 3 * D))).astype(np.float32)
+    weight = (1 + 0.1 * rng.standard_normal(D)).astype(np.float32) if "w" in parts else None
+    cuts = np.sort(rng.integers(0, m + 1, B - 1))          # requests of any length, empty ones too
+    return h, y, mod, weight, np.concatenate([[0], cuts, [m]]).astype(np.int32)
+
+
+def run_rms(h, y, mod, weight, cu, m, parts, eps=1e-6):
+    D = h.shape[1]
+    d_h, d_mod = dev(h), dev(mod)
+    q, s = codes(*h.shape)
+    part = lambda i, on: d_mod[:, i * D:(i + 1) * D] if on in parts else None  # noqa: E731
+    fdl.fd_rms_quant(d_h, q, s, dev(cu), count(m), y=None if y is None else y.cuda(), gate=part(2, "g"),
+                     weight=None if weight is None else dev(weight), shift=part(0, "m"), mod_scale=part(1, "m"), eps=eps)
+    torch.cuda.synchronize()
+    return d_h.cpu().numpy(), q.cpu().numpy(), s.cpu().numpy()
+
+
+@pytest.mark.parametrize("parts", ["", "y", "yg", "w", "m", "ygwm"])
+@pytest.mark.parametrize("rows,D,B,m", [(1, 16, 1, 1), (5, 64, 1, 3), (9, 1088, 4, 9), (33, 1536, 7, 30), (6, 2048, 2, 6),
+                                        (5, 2064, 3, 4), (3, 6160, 2, 3), (2, 12288, 1, 2), (4, 128, 3, 0)])
+def test_rms_quant(rows, D, B, m, parts):
+    """fp32 error: the sum of squares is formed from at most 48 terms per lane and a tree of 8 levels (relative
+    error 56 half steps, halved by the root), then at most 8 roundings to the value."""
+    gh.say(f"rms {rows}x{D} B={B} m={m} parts={parts!r}")
+    h, y, mod, weight, cu = rms_case(rows, D, B, m, parts)
+    gh_, q, s = run_rms(h, y, mod, weight, cu, m, parts)
+    of_row = np.repeat(np.arange(B), np.diff(cu))
+    pick = lambda i, on: mod[of_row, i * D:(i + 1) * D].astype(np.float64) if on in parts else None  # noqa: E731
+    y64 = None if y is None else y.double().numpy()[:m]
+    gate, shift, scale = pick(2, "g"), pick(0, "m"), pick(1, "m")
+    wh, wa = ref.rms(h[:m], y64, gate, None if weight is None else weight.astype(np.float64), shift, scale, 1e-6)
+    add = 0.0 if y64 is None else np.abs(y64) * (1.0 if gate is None else np.abs(gate))
+    assert np.all(np.abs(gh_[:m] - wh) <= 2 * U32 * (np.abs(wh) + add))
+    np.testing.assert_array_equal(gh_[m:], h[m:])
+    if m:
+        base = np.abs(wa - (0 if shift is None else shift))
+        # the rounding of h reaches a through h itself and through the norm
+        h_err = 2 * U32 * (np.abs(wh) + add) / np.sqrt(np.mean(wh * wh, 1, keepdims=True))
+        w_abs = (1.0 if weight is None else np.abs(weight)) * (1.0 if scale is None else np.abs(1 + scale))
+        err = (28 + 8 + 2) * U32 * base + h_err * w_abs + 2 * U32 * np.abs(wa)
+        check_codes(q[:m], s[:m], wa, err)
+    assert np.all(q[m:] == 0x55) and np.all(s[m:] == 0x55)
+
+
+def test_rms_quant_zero_and_bad_rows():
+    """A row of zeros (eps 0: 0 * inf is NaN, as the formula says; eps > 0: codes of zero), rows with an infinity
+    or a NaN: those rows alone are NaN."""
+    rng = np.random.default_rng(5)
+    h = rng.standard_normal((6, 192)).astype(np.float32)
+    h[1] = 0
+    h[3, 100], h[4, 3] = np.inf, np.nan
+    for eps in (1e-6, 0.0):
+        _, q, s = run_rms(h, None, np.zeros((1, 576), np.float32), None, np.array([0, 6], np.int32), 6, "", eps)
+        v = ref.values(q, s)
+        assert np.all(np.isnan(v[4])) and np.all(np.isnan(v[3, :128]))
+        assert np.all(np.isnan(v[1])) if eps == 0 else np.all(v[1] == 0)
+        assert np.all(np.isfinite(v[[0, 2, 5]]))
+
+
+# ------------------------------------------------------------------ rotary positions
+
+@pytest.mark.parametrize("halves", [False, True])
+@pytest.mark.parametrize("dh,dims,hq,hk,rows,tokens,m", [
+    (16, [16], 1, 1, 1, 1, 1), (16, [4, 6, 6], 4, 4, 9, 12, 7), (64, [64], 6, 2, 5, 5, 5), (64, [32, 32], 24, 8, 33, 40, 33),
+    (64, [2, 14, 20], 3, 1, 6, 9, 6), (128, [44, 42, 42], 12, 12, 17, 50, 16), (128, [16, 56, 56], 2, 2, 4, 4, 4),
+    (128, [32, 32, 32, 32], 1, 1, 3, 8, 0), (128, [16, 32, 32], 2, 1, 5, 7, 5)])
+def test_rope(dh, dims, hq, hk, rows, tokens, m, halves):
+    """Angles err by 2^-26 of a turn, cosine and sine by two more ulp and each product by half of one: 2^-21 of the
+    pair's magnitudes covers them.  v is copied, other cache rows stay, values past the axes are copied."""
+    gh.say(f"rope dh={dh} dims={dims} heads={hq}/{hk} rows={rows} m={m} halves={halves}")
+    rng = np.random.default_rng([dh, rows, sum(dims)])
+    theta, step = [1e4, 100.0, 1e6, 10.0][:len(dims)], [1.0, 0.25, 3.0, 1.0][:len(dims)]
+    pos = rng.integers(-1000, 1 << 20, (tokens, len(dims))).astype(np.int32)
+    pos[0] = 0
+    x = bf16(rng.standard_normal((rows, (hq + 2 * hk) * dh)))
+    idx = np.sort(rng.permutation(tokens)[:rows]).astype(np.int32)
+    k0, v0 = bf16(rng.standard_normal((2, tokens, hk * dh)))
+    q, k, v = torch.full((rows, hq * dh), 7.0, dtype=torch.bfloat16, device="cuda"), k0.cuda(), v0.cuda()
+    fdl.fd_rope_axes(x.cuda(), dev(pos), dev(idx), count(m), q, k, v, heads=hq, kv_heads=hk, head_dim=dh, dims=dims, theta=theta,
+                     step=step, halves=halves)
+    x64 = x.double().numpy().reshape(rows, hq + 2 * hk, dh)[:m]
+    want = ref.rope(x64[:, :hq + hk], pos[idx[:m]], dims, theta, step, halves)
+    mag = np.abs(x64[:, :hq + hk]).max(-1, keepdims=True) * 2
+    got_k, got_v = k.double().cpu().numpy(), v.double().cpu().numpy()
+    got = np.concatenate([q.double().cpu().numpy()[:m].reshape(m, hq, dh), got_k[idx[:m]].reshape(m, hk, dh)], 1)
+    assert np.all(np.abs(got - want) <= UB * np.abs(want) + (1 + UB) * 2.0 ** -21 * mag)
+    assert np.array_equal(got[..., sum(dims):], x64[:, :hq + hk, sum(dims):])
+    assert np.array_equal(got_v[idx[:m]], x64[:, hq + hk:].reshape(m, hk * dh))
+    rest = np.setdiff1d(np.arange(tokens), idx[:m])
+    assert np.array_equal(got_k[rest], k0.double().numpy()[rest]) and np.array_equal(got_v[rest], v0.double().numpy()[rest])
+    assert (q[m:] == 7.0).all()
+
+
+def test_rope_without_index_and_infinities():
+    """idx None: row i is token i.  An infinity stays in its pair, and in values that are not turned."""
+    x = torch.ones((3, 3 * 64), dtype=torch.bfloat16)
+    x[1, 5] = float("inf")      # turned with value 4 (interleaved)
+    x[2, 63] = float("inf")     # past the axes
+    pos = torch.ones((3, 1), dtype=torch.int32, device="cuda")
+    q, k, v = (torch.zeros((3, 64), dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    fdl.fd_rope_axes(x.cuda(), pos, None, count(3), q, k, v, heads=1, kv_heads=1, head_dim=64, dims=[32])
+    q = q.cpu()
+    assert torch.isinf(q[1, 4:6]).all() and torch.isfinite(q[1, :4]).all() and torch.isfinite(q[1, 6:]).all()
+    assert torch.isinf(q[2, 63]) and torch.isfinite(q[2, :63]).all()
+    assert torch.equal(k.cpu()[0], k.cpu()[2])
+
+
+# ------------------------------------------------------------------ product
+
+def linear_case(M, N, K, seed=0):
+    rng = np.random.default_rng([M, N, K, seed])
+    a, sa = ref.quant(rng.standard_normal((max(M, 1), K)) * np.exp(rng.standard_normal((max(M, 1), 1))), 1)
+    w, sw = ref.quant(0.05 * rng.standard_normal((N, K)), 128)
+    pad = lambda s: np.concatenate([s, np.full((s.shape[0], ref.stride(K) - s.shape[1]), 255, np.uint8)], 1)  # noqa: E731
+    return a, pad(sa), w, pad(sw), (0.1 * rng.standard_normal(N)).astype(np.float32)
+
+
+def run_linear(a, sa, w, sw, bias, gelu, to, rows, m):
+    """The product with `rows` of capacity; rows past the inputs repeat the last one."""
+    up = lambda x: dev(np.concatenate([x, np.repeat(x[-1:], rows - len(x), 0)]) if rows > len(x) else x)  # noqa: E731
+    n = w.shape[0]
+    if to == "8":
+        y, ys = codes(rows, n)
+    else:
+        y, ys = torch.full((rows, n), 7.0, dtype=torch.bfloat16 if to == "bf16" else torch.float32, device="cuda"), None
+    fdl.fd_scaled_linear(up(a), up(sa), dev(w), dev(sw), y, ys, bias=None if bias is None else dev(bias), gelu=gelu,
+                         m=None if m is None else count(m))
+    torch.cuda.synchronize()
+    return y.cpu(), None if ys is None else ys.cpu().numpy()
+
+
+def check_linear(y, ys, a, sa, w, sw, bias, gelu, to, M):
+    """Products are exact; each of the K + 1 additions errs by at most an fp32 half step of the sum of magnitudes.  GELU's
+    slope is at most 1.13, and its own error below 2^-21 of its argument."""
+    va, vw = ref.values(a[:M], sa[:M]), ref.values(w, sw, 128)
+    b = np.zeros(w.shape[0]) if bias is None else bias.astype(np.float64)
+    z = va @ vw.T + b
+    err = (a.shape[1] + 2) * U32 * (np.abs(va) @ np.abs(vw).T + np.abs(b))
+    want = z
+    if gelu:
+        want, err = ref.gelu(z), 1.13 * err + 2.0 ** -21 * np.abs(z)
+    if to == "8":
+        check_codes(y.numpy()[:M], ys[:M], want, err)
+        assert (y[M:] == 0x55).all() and np.all(ys[M:] == 0x55) and np.all(ys[:, -(-w.shape[0] // 128):] == 0x55)
+        return
+    half = UB if to == "bf16" else U32
+    got = y[:M].double().numpy()
+    assert np.all(np.abs(got - want) <= err + half * (np.abs(want) + err)), float(np.max(np.abs(got - want) - err))
+    assert (y[M:] == 7.0).all()
+
+
+@pytest.mark.parametrize("to,gelu", [("bf16", False), ("f32", True), ("8", False), ("8", True)])
+@pytest.mark.parametrize("M,N,K,rows", [(1, 16, 16, 1), (1, 128, 128, 40), (15, 144, 112, 15), (16, 256, 144, 17), (17, 64, 1088, 200), (0, 64, 64, 3),
+                                        (63, 112, 512, 64), (65, 400, 640, 70), (129, 1088, 272, 300), (257, 272, 384, 257), (300, 528, 1552, 700)])
+def test_scaled_linear(M, N, K, rows, to, gelu):
+    gh.say(f"linear M={M} N={N} K={K} rows={rows} to={to} gelu={gelu}")
+    case = linear_case(M, N, K)
+    y, ys = run_linear(*case, gelu, to, rows, M)
+    check_linear(y, ys, *case, gelu, to, M)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 1536, 1536), (40, 1536, 6144), (200, 1600, 1536), (1000, 1088, 1088), (3000, 1536, 512)])
+@pytest.mark.parametrize("to", ["bf16", "8"])
+def test_scaled_linear_sizes(M, N, K, to):
+    """Row counts of every kind of tile, without a count on the device, with and without a bias."""
+    gh.say(f"linear M={M} N={N} K={K} to={to}")
+    case = linear_case(M, N, K, 1)
+    if to == "8":
+        case = case[:4] + (None,)
+    y, ys = run_linear(*case, False, to, M, None)
+    check_linear(y, ys, *case, False, to, M)
+
+
+@pytest.mark.parametrize("M", [5, 200])
+def test_scaled_linear_bad_blocks(M):
+    """A NaN block of a row makes that row NaN, one of the weights its 128 columns; the rest is as without it."""
+    case = linear_case(M, 400, 400)
+    a, sa, w, sw, bias = (x.copy() for x in case)
+    a[3, 128:256], sa[3, 1] = 0x7f, 255
+    w[128:256, 384:], sw[1, 3] = 0x7f, 255
+    y, _ = run_linear(a, sa, w, sw, bias, False, "f32", M, None)
+    clean, _ = run_linear(*case, False, "f32", M, None)
+    bad = np.zeros((M, 400), bool)
+    bad[3], bad[:, 128:256] = True, True
+    assert np.array_equal(torch.isnan(y).numpy(), bad)
+    assert np.array_equal(y.numpy()[~bad], clean.numpy()[~bad])
+
+
+def test_scaled_linear_zero_rows_and_extreme_scales():
+    """A row of zeros gives the bias; scales far apart in one row add up as their values do."""
+    a, sa, w, sw, bias = linear_case(20, 128, 512)
+    a[4], sa[4, :4] = 0, 1
+    sa[5, :4] = [97, 127, 140, 60]
+    y, _ = run_linear(a, sa, w, sw, bias, False, "f32", 20, None)
+    assert np.array_equal(y.numpy()[4], bias)
+    check_linear(y, None, a, sa, w, sw, bias, False, "f32", 20)
+
+
+# ------------------------------------------------------------------ streams, graphs, refusals
+
+def test_on_another_stream_and_in_a_graph():
+    """norm -> product -> rotary positions -> codes on a side stream, then recorded and replayed, with eager work
+    between the replays: the bits of the current stream's run each time."""
+    rows, tokens, D, H, dh = 70, 90, 256, 4, 64
+    rng = np.random.default_rng(3)
+    w16 = bf16(0.05 * rng.standard_normal((3 * D, D))).cuda()
+    w, sw = codes(3 * D, D, 128)
+    fdl.fd_quant_blocks(w16, 128, w, sw)
+    h0 = dev(rng.standard_normal((rows, D)).astype(np.float32))
+    y = bf16(rng.standard_normal((rows, D))).cuda()
+    mod = dev((0.1 * rng.standard_normal((1, 3 * D))).astype(np.float32))
+    pos = dev(rng.integers(0, 50, (tokens, 2)).astype(np.int32))
+    idx = dev(np.sort(rng.permutation(tokens)[:rows]).astype(np.int32))
+    cu, m = dev(np.array([0, 60], np.int32)), count(60)
+
+    def state():
+        q, s = codes(rows, D)
+        oq, os_ = codes(rows, D)
+        z = lambda *n: torch.zeros(n, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+        return dict(h=h0.clone(), q=q, s=s, qkv=z(rows, 3 * D), rq=z(rows, D), k=z(tokens, D), v=z(tokens, D), oq=oq, os=os_)
+
+    def chain(t, stream=None):
+        fdl.fd_rms_quant(t["h"], t["q"], t["s"], cu, m, y=y, gate=mod[:, 2 * D:], shift=mod[:, :D], mod_scale=mod[:, D:2 * D], stream=stream)
+        fdl.fd_scaled_linear(t["q"], t["s"], w, sw, t["qkv"], m=m, stream=stream)
+        fdl.fd_rope_axes(t["qkv"], pos, idx, m, t["rq"], t["k"], t["v"], heads=H, kv_heads=H, head_dim=dh, dims=[32, 32], stream=stream)
+        fdl.fd_quant_blocks(t["rq"], 1, t["oq"], t["os"], m=m, stream=stream)
+
+    want = state()
+    chain(want)
+    side, t = torch.cuda.Stream(), state()
+    torch.cuda.synchronize()
+    chain(t, side)
+    torch.cuda.synchronize()
+    for k in want:
+        assert torch.equal(t[k], want[k]), k
+    t = state()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        chain(t)
+    for _ in range(3):
+        t["h"].copy_(h0)
+        _ = (torch.randn(1 << 14, device="cuda") * 2).sum().item()
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in want:
+            assert torch.equal(t[k], want[k]), k
+
+
+def test_bindings_refuse():
+    """Sizes, types and strides that do not fit raise on the host."""
+    q, s = codes(8, 128)
+    h, m, cu = torch.zeros(8, 128, device="cuda"), count(8), dev(np.array([0, 8], np.int32))
+    x = torch.zeros(8, 128, dtype=torch.bfloat16, device="cuda")
+    mod = torch.zeros(1, 128, device="cuda")
+    bad = [
+        lambda: fdl.fd_quant_blocks(x.float(), 1, q, s), lambda: fdl.fd_quant_blocks(x, 1, q[:7], s), lambda: fdl.fd_quant_blocks(x, 1, q, s[:7]),
+        lambda: fdl.fd_quant_blocks(x, 2, q, s), lambda: fdl.fd_quant_blocks(x.t(), 1, q, s), lambda: fdl.fd_quant_blocks(x, 128, q, s, m=m),
+        lambda: fdl.fd_rms_quant(h, q, s[:, :3], cu, m), lambda: fdl.fd_rms_quant(h, q, s, cu, m, gate=mod), lambda: fdl.fd_rms_quant(h, q, s, cu, m, y=h),
+        lambda: fdl.fd_rms_quant(h, q, s, cu, m, shift=mod, mod_scale=torch.zeros(1, 256, device="cuda")[:, :128]),
+        lambda: fdl.fd_rms_quant(h, q, s, cu, m, shift=torch.zeros(1, 256, device="cuda")[:, ::2]),
+        lambda: fdl.fd_rms_quant(h, q, s, cu, m, shift=torch.zeros(2, 128, device="cuda")), lambda: fdl.fd_rms_quant(h.half(), q, s, cu, m),
+        lambda: fdl.fd_rope_axes(x, torch.zeros(8, 2, dtype=torch.int32, device="cuda"), None, m, x, x, x, 1, 1, 64, dims=[64]),
+        lambda: fdl.fd_rope_axes(x, torch.zeros(8, 1, dtype=torch.int32, device="cuda"), None, m, x, x, x, 1, 1, 64, dims=[64]),
+        lambda: fdl.fd_scaled_linear(q, s, q, s, h[:, :7].contiguous()), lambda: fdl.fd_scaled_linear(q, s, q[:, :64].contiguous(), s, h),
+        lambda: fdl.fd_scaled_linear(q, s, q, s, q), lambda: fdl.fd_scaled_linear(q, s[:7], q, s, h), lambda: fdl.fd_scaled_linear(q, s, q, s, h, bias=x),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(fdl.FlashDiffError):
+            call()
+            pytest.fail(f"call {i} was accepted")

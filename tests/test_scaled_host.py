@@ -1,0 +1,129 @@
+"""CPU tests of the 8-bit entry points: refusals before any launch, the scale stride, and the 64-bit
+reference against torch's e4m3 conversion."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import scaled as ref
+from paper_2607_12121_amd import flashdiff as fdl
+from tests.test_abi import no_gpu
+
+P = 0x1000
+
+
+def test_reference_codes_equal_torch():
+    """Every e4m3 byte decodes as torch's, and a dense set of values, ties among them, rounds as torch's."""
+    t = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).double().numpy()
+    np.testing.assert_array_equal(ref.CODES, t)
+    fine = ref.CODES[np.isfinite(ref.CODES)]
+    mids = (np.sort(fine)[1:] + np.sort(fine)[:-1]) / 2
+    v = np.concatenate([fine, mids, mids * (1 + 1e-6), mids * (1 - 1e-6), np.linspace(-448, 448, 4001)]).astype(np.float32)
+    got = ref.encode(v)
+    want = torch.from_numpy(v).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+    np.testing.assert_array_equal(got, want)
+
+
+@pytest.mark.parametrize("top,power", [(448.0, 0), (449.0, 1), (224.0, -1), (224.5, 0), (1.75, -8), (1.76, -7), (0.0, -126),
+                                       (2.0 ** -140, -126), (3.0e38, 120), (np.inf, 128), (np.nan, 128)])
+def test_reference_scale(top, power):
+    assert ref.scale_bytes(np.array([top]))[0] == power + 127
+
+
+def test_reference_rope_is_a_rotation():
+    """Norms of pairs are kept, and equal shifts of q's and k's position leave their product."""
+    rng = np.random.default_rng(0)
+    x, z = rng.standard_normal((2, 5, 3, 64))
+    pos = rng.integers(0, 1000, (5, 2))
+    for halves in (False, True):
+        kw = dict(dims=[24, 30], theta=[1e4, 100.0], step=[1.0, 0.5], halves=halves)
+        r = ref.rope(x, pos, **kw)
+        np.testing.assert_allclose(np.sum(r * r, -1), np.sum(x * x, -1), rtol=1e-12)
+        np.testing.assert_array_equal(r[..., 54:], x[..., 54:])
+        s = np.sum(r * ref.rope(z, pos + 7, **kw), -1)
+        np.testing.assert_allclose(s, np.sum(ref.rope(x, pos + 40, **kw) * ref.rope(z, pos + 47, **kw), -1), rtol=0, atol=1e-10)
+
+
+def test_scale_stride():
+    for cols in (-1, 0, 1, 16, 128, 129, 512, 513, 1536, 6144):
+        assert fdl.fd_scale_stride(cols) == (ref.stride(cols) if cols > 0 else 0)
+
+
+@no_gpu
+@pytest.mark.parametrize("change,status", [
+    (dict(rows=0), 1), (dict(cols=0), 1), (dict(cols=24), 3), (dict(block=64), 1), (dict(x=None), 1), (dict(q=None), 1),
+    (dict(scale=None), 1), (dict(x=P + 8), 1), (dict(q=P + 4), 1), (dict(block=128, m=P), 1)])
+def test_quant_blocks_refuses(change, status):
+    a = dict(rows=4, cols=64, block=1, x=P, m=P, q=P, scale=P)
+    a.update(change)
+    st = fdl.lib().fd_quant_blocks(a["rows"], a["cols"], a["block"], a["x"], a["m"], a["q"], a["scale"], None)
+    assert st == status, fdl.lib().fd_last_error()
+
+
+@no_gpu
+@pytest.mark.parametrize("change,status", [
+    (dict(rows=0), 1), (dict(D=72), 3), (dict(D=12304), 3), (dict(B=0), 1), (dict(h=None), 1), (dict(m=None), 1), (dict(q=None), 1),
+    (dict(q_scale=None), 1), (dict(B=2, cu_q=None), 1), (dict(y=None), 1), (dict(eps=-1.0), 1), (dict(eps=float("nan")), 1),
+    (dict(stride=-4), 1), (dict(stride=6), 1), (dict(h=P + 4), 1), (dict(y=P + 8), 1), (dict(gate=P + 4), 1), (dict(weight=P + 4), 1),
+    (dict(shift=P + 4), 1), (dict(scale=P + 4), 1), (dict(q=P + 8), 1)])
+def test_rms_quant_refuses(change, status):
+    a = dict(rows=4, D=64, B=1, h=P, y=P, gate=P, weight=P, shift=P, scale=P, stride=192, eps=1e-6, cu_q=P, m=P, q=P, q_scale=P)
+    a.update(change)
+    assert fdl.lib().fd_rms_quant(*a.values(), None) == status, fdl.lib().fd_last_error()
+
+
+@no_gpu
+@pytest.mark.parametrize("change,status", [
+    (dict(rows=0), 1), (dict(rows=9), 1), (dict(rope=None), 1), (dict(hq=0), 1), (dict(hk=0), 1), (dict(hq=5000), 3), (dict(dh=32), 3),
+    (dict(coord=None), 1), (dict(qkv=None), 1), (dict(m=None), 1), (dict(q=None), 1), (dict(k=None), 1), (dict(v=None), 1),
+    (dict(qkv=P + 8), 1), (dict(q=P + 8), 1), (dict(k=P + 8), 1), (dict(v=P + 8), 1)])
+def test_rope_axes_refuses(change, status):
+    a = dict(rows=4, tokens=8, rope=ctypes.byref(fdl.rope_axes([64])), hq=2, hk=1, dh=64, coord=P, qkv=P, idx=P, m=P, q=P, k=P, v=P)
+    a.update(change)
+    assert fdl.lib().fd_rope_axes(*a.values(), None) == status, fdl.lib().fd_last_error()
+
+
+@no_gpu
+@pytest.mark.parametrize("field,value", [("n_axes", 0), ("n_axes", 5), ("pairing", 2), ("dim", (3, 0, 0, 0)), ("dim", (0, 0, 0, 0)),
+                                         ("dim", (66, 0, 0, 0)), ("dim", (-2, 0, 0, 0)), ("theta", (0.0,) * 4), ("theta", (float("nan"),) * 4),
+                                         ("theta", (float("inf"),) * 4), ("step", (float("inf"),) * 4)])
+def test_rope_descriptor_refused(field, value):
+    r = fdl.rope_axes([64])
+    if isinstance(value, tuple):
+        for i, v in enumerate(value):
+            getattr(r, field)[i] = v
+    else:
+        setattr(r, field, value)
+    assert fdl.lib().fd_rope_axes(4, 8, ctypes.byref(r), 2, 1, 64, *([P] * 7), None) == 1
+    two = fdl.rope_axes([40, 26])   # together more than the head
+    assert fdl.lib().fd_rope_axes(4, 8, ctypes.byref(two), 2, 1, 64, *([P] * 7), None) == 1
+
+
+def test_rope_binding_refuses():
+    for kw in (dict(dims=[]), dict(dims=[2] * 5), dict(dims=[8, 8], theta=[1e4]), dict(dims=[8], step=[1.0, 2.0])):
+        with pytest.raises(fdl.FlashDiffError):
+            fdl.rope_axes(**kw)
+
+
+@no_gpu
+@pytest.mark.parametrize("change,status", [
+    (dict(rows=0), 1), (dict(n=0), 1), (dict(k=0), 1), (dict(n=40), 3), (dict(k=72), 3), (dict(a=None), 1), (dict(sa=None), 1), (dict(w=None), 1),
+    (dict(sw=None), 1), (dict(yb=None), 1), (dict(yf=P), 1), (dict(yq=P, ys=P), 1), (dict(ys=P), 1), (dict(yb=None, yq=P), 1),
+    (dict(gelu=2), 1), (dict(a=P + 8), 1), (dict(w=P + 8), 1), (dict(sa=P + 2), 1), (dict(sw=P + 2), 1), (dict(bias=P + 4), 1), (dict(yb=P + 8), 1),
+    (dict(yb=None, yf=P + 8), 1), (dict(yb=None, yq=P + 8, ys=P), 1), (dict(n=1 << 17, k=1 << 14), 3)])
+def test_scaled_linear_refuses(change, status):
+    a = dict(rows=4, n=64, k=64, a=P, sa=P, w=P, sw=P, bias=P, gelu=0, m=P, yb=P, yf=None, yq=None, ys=None)
+    a.update(change)
+    assert fdl.lib().fd_scaled_linear(*a.values(), None) == status, fdl.lib().fd_last_error()
+
+
+def test_bindings_refuse_host_tensors():
+    x, q = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(4, 64, dtype=torch.float8_e4m3fn)
+    s, h = torch.zeros(4, 4, dtype=torch.uint8), torch.zeros(4, 64)
+    i = torch.zeros(2, dtype=torch.int32)
+    for call in (lambda: fdl.fd_quant_blocks(x, 1, q, s), lambda: fdl.fd_rms_quant(h, q, s, i, i),
+                 lambda: fdl.fd_rope_axes(x, i.view(1, 2), None, i, x, x, x, 1, 1, 16, dims=[8, 8]),
+                 lambda: fdl.fd_scaled_linear(q, s, q, s, h)):
+        with pytest.raises(fdl.FlashDiffError):
+            call()
