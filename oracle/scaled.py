@@ -48,7 +48,7 @@ def block_tops(x: np.ndarray, block_rows: int) -> np.ndarray:
     r, c = x.shape
     p = np.zeros((-(-r // block_rows) * block_rows, -(-c // 128) * 128))
     p[:r, :c] = np.abs(x)
-    p = p.reshape(p.shape[0] // block_rows, block_rows, -1, 128)
+    p = p.reshape(p.shape[0] // block_rows, block_rows, p.shape[1] // 128, 128)
     return np.max(p, axis=(1, 3))                      # NaN propagates
 
 
