@@ -624,8 +624,8 @@ fd_status fd_scaled_linear(int32_t n_rows, int32_t n_out, int32_t n_in, const ui
   FD_REQUIRE(aligned(a, 16) && aligned(w, 16) && aligned(a_scale, 4) && aligned(w_scale, 4) && aligned(bias, 16) &&
                  aligned(y_bf, 16) && aligned(y_fp, 16) && aligned(y_q, 16),
              "misaligned buffer");
-  if (static_cast<long long>(n_out) * n_in > fdh::kMaxGemmBytes)
-    return fdh::set_error("weights of 2 GiB or more (%d x %d given)", n_out, n_in), FD_E_UNSUPPORTED;
+  if (n_out > (1 << 20) || n_in > (1 << 20) || static_cast<long long>(n_out) * n_in > fdh::kMaxGemmBytes)
+    return fdh::set_error("more than 2^20 columns, or weights of 2 GiB or more (%d x %d given)", n_out, n_in), FD_E_UNSUPPORTED;
   fdh::ScaledArgs g{};
   g.n_rows = n_rows; g.N = n_out; g.K = n_in; g.m = m; g.a = a; g.a_scale = a_scale; g.w = w; g.w_scale = w_scale;
   g.bias = bias; g.gelu = gelu; g.y_bf16 = y_bf; g.y_f32 = y_fp; g.y_q = y_q; g.y_scale = y_scale;

@@ -36,6 +36,9 @@ struct Mma8 {
   static FD_DEVICE f32x4_t mma(const frag& w, const frag& a, f32x4_t c, uint32_t sw, uint32_t sa) {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, c, 0, 0, 0, static_cast<int>(sw), 0, static_cast<int>(sa));
   }
+  static FD_DEVICE f32x16_t mma(const frag& w, const frag& a, f32x16_t c, uint32_t sw, uint32_t sa) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, a, c, 0, 0, 0, static_cast<int>(sw), 0, static_cast<int>(sa));
+  }
 };
 struct MmaExact {
   struct frag { bf16x8_t p[4]; };   // piece p: the lane's values 8 p .. 8 p + 7 (the same ones of both operands)
@@ -54,6 +57,11 @@ struct MmaExact {
   static FD_DEVICE f32x4_t mma(const frag& w, const frag& a, f32x4_t c, uint32_t, uint32_t) {
 #pragma unroll
     for (int p = 0; p < 4; ++p) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.p[p], a.p[p], c, 0, 0, 0);
+    return c;
+  }
+  static FD_DEVICE f32x16_t mma(const frag& w, const frag& a, f32x16_t c, uint32_t, uint32_t) {
+#pragma unroll
+    for (int p = 0; p < 4; ++p) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w.p[p], a.p[p], c, 0, 0, 0);
     return c;
   }
 };
@@ -184,150 +192,296 @@ __global__ __launch_bounds__(kFewWaves * 64) void scaled_few_kernel(fdh::ScaledA
 
 // ---------------------------------------------------------------- tiles
 
-// A workgroup of four waves, one per SIMD, with a tile of 16 FM WM rows x 128 WN columns: a wave owns
-// FM x 8 fragments (its accumulators fill up to 256 accumulation registers).
-template <int FM_, int WM_, int WN_, int STAGES_>
+// A workgroup of WM x WN waves with a tile of 32 FI WM rows x 128 WN columns, K-steps of one block; a
+// wave owns FI x 4 blocks of 32 x 32.  Tiles stream from memory into a ring of LDS stages
+// (buffer_load ... lds); in LDS a tile row is eight 16-byte chunks, chunk c of row r at c ^ swz(r), so
+// that the 16 lanes that read a fragment together meet 16 different 16-byte bank groups.
+template <int FI_, int WM_, int WN_, int STAGES_>
 struct Tile {
-  static constexpr int FM = FM_, WM = WM_, WN = WN_, STAGES = STAGES_;
-  static constexpr int BM = 16 * FM * WM, BN = 128 * WN, WAVES = 4;
+  static constexpr int FI = FI_, WM = WM_, WN = WN_, STAGES = STAGES_;
+  static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
+  static constexpr int BM = 32 * FI * WM, BN = 128 * WN;
   static constexpr int LOADS_A = BM / 8 / WAVES, LOADS = (BM + BN) / 8 / WAVES;   // 8 rows of 128 bytes per wave-load
-  static constexpr int ISSUED = LOADS + 2;                                        // and two of scales
-  static constexpr int SIDE = (BM + BN) * 8;                                      // chunk where the scales begin
-  static constexpr int CHUNKS = SIDE + 2 * WAVES * 16;                            // 16-byte chunks per stage
-  static_assert(WM * WN == WAVES && BM % 32 == 0, "four waves, whole wave-loads");
+  static constexpr int ISSUED = LOADS + 1;                                        // and one of scales or bias
+  static constexpr int SIDE = (BM + BN) * 8;                                      // chunk where a stage's scales begin
+  static constexpr int CHUNKS = SIDE + BM / 4 + 16;                               // row scales, then 256 bytes of column scales
+  static constexpr int BIAS = STAGES * CHUNKS;                                    // four slots of the columns' bias
+  static constexpr int TOTAL = BIAS + 4 * 64;
+  static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && BM % 64 == 0 && BM / 64 + 2 <= WAVES && BN <= 256, "whole wave-loads");
+  static FD_DEVICE int swz_a(int r) { return (r >> 1) & 7; }
+  static FD_DEVICE int swz_w(int r) { return ((r >> 1) & 3) | ((r >> 6) & 1) << 2; }
 };
 
 typedef __attribute__((address_space(3))) void* lds_ptr_t;
 
-FD_DEVICE i32x4_t buffer_of(const void* base) {
+FD_DEVICE i32x4_t buffer_of(const void* base, uint32_t bytes = 0x7fffffffu) {
   const uint64_t p = reinterpret_cast<uint64_t>(base);
-  return i32x4_t{static_cast<int>(static_cast<uint32_t>(p)), static_cast<int>(static_cast<uint32_t>(p >> 32) & 0xffffu), 0x7fffffff, 0x00020000};
+  return i32x4_t{static_cast<int>(static_cast<uint32_t>(p)), static_cast<int>(static_cast<uint32_t>(p >> 32) & 0xffffu), static_cast<int>(bytes), 0x00020000};
 }
-// 16 (4) bytes per lane from buffer offset voff + soff into LDS at lds + 16 (4) * lane; offsets past
-// 2 GiB read zeros.  In assembly so that the compiler does not wait for it before unrelated LDS reads.
+constexpr uint32_t kNowhere = 0x80000000u;   // an offset past every buffer: loads read zeros, stores are dropped
+// 16 (4) bytes per lane from buffer offset voff + soff into LDS at lds + 16 (4) * lane.  In assembly so
+// that the compiler does not wait for it before unrelated LDS reads.
 FD_DEVICE void dma16(uint32_t lds, uint32_t voff, i32x4_t rsrc, uint32_t soff) {
   asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(lds), "v"(voff), "s"(rsrc), "s"(soff));
 }
 FD_DEVICE void dma4(uint32_t lds, uint32_t voff, i32x4_t rsrc, uint32_t soff) {
   asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, %3 offen lds" : : "s"(lds), "v"(voff), "s"(rsrc), "s"(soff));
 }
+// This wave's LDS reads are done and at most N of its vector memory operations are in flight; then the barrier.
 template <int N>
-FD_DEVICE void wait_vm_barrier() {
-  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(N) : "memory");
+FD_DEVICE void wait_barrier() {
+  static_assert(N < 64, "the counter's range");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory");
 }
 
+// A lane's 64 columns of one row to memory; every store issues whatever the row (kStores of them), rows and
+// columns outside go nowhere.  x: the row's values with bias; at: byte offset of the row's first column over
+// the element size from the base of `y`.
+template <int KIND>
+struct Row64 {
+  static constexpr int STORES = KIND == kToCodes ? 5 : KIND == kToBf16 ? 8 : 16;
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  static FD_DEVICE void put(const u32x4& v, __amdgpu_buffer_rsrc_t y, bool ok, uint32_t off) {
+    __builtin_amdgcn_raw_buffer_store_b128(v, y, ok ? off : kNowhere, 0, 0);
+  }
+  static FD_DEVICE void store(float (&v)[64], bool gelu, bool row_ok, int cols, uint32_t row_off, int half, __amdgpu_buffer_rsrc_t y,
+                              __amdgpu_buffer_rsrc_t scale, uint32_t scale_off) {
+    if (gelu) {
+#pragma unroll
+      for (int e = 0; e < 64; ++e) v[e] = fd::gelu_tanh_fast(v[e]);
+    }
+    if constexpr (KIND == kToCodes) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int e = 0; e < 64; ++e) top = (e & ~15) < cols ? max(top, fd::mag_bits(v[e])) : top;
+      top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 32, fd::kWave)));
+      const uint32_t s = fd::scale_byte(top);
+      const float inv = fd::scale_inverse(s);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float* x = v + 16 * c + 4 * i;
+          w[i] = fd::pack_codes(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+        }
+        put(w, y, row_ok && 16 * c < cols, row_off + 16 * c);
+      }
+      __builtin_amdgcn_raw_buffer_store_b8(static_cast<uint8_t>(s), scale, row_ok && half == 0 && cols > 0 ? scale_off : kNowhere, 0, 0);
+    } else if constexpr (KIND == kToBf16) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const float* x = v + 8 * c;
+        put(u32x4{fd::pack_bf2(x[0], x[1]), fd::pack_bf2(x[2], x[3]), fd::pack_bf2(x[4], x[5]), fd::pack_bf2(x[6], x[7])}, y,
+            row_ok && 8 * c < cols, row_off + 16 * c);
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < 16; ++c) {
+        const float* x = v + 4 * c;
+        put(u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])}, y, row_ok && 4 * c < cols,
+            row_off + 16 * c);
+      }
+    }
+  }
+};
+
+// The K-steps of all of a workgroup's tiles are one sequence: the loads run STAGES steps ahead of the
+// products, into the next tile too, and a tile's results leave while the next one's first stages land.
+//
+// A step's eight sub-steps s = (half of K, column fragment) each read one weight fragment two sub-steps
+// ahead.  After sub-step 5 the wave has read all of its stage; the barrier there frees the stage for the
+// load STAGES steps on and publishes the next stage, whose first fragments are read behind sub-steps 6
+// and 7, so that no sub-step waits for LDS or for the barrier with nothing to compute.
 template <class T, int KIND, class Mma>
 FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
-  constexpr int FM = T::FM, STAGES = T::STAGES;
-  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, lg = lane >> 4;
+  constexpr int FI = T::FI, STAGES = T::STAGES;
+  constexpr int kSize = KIND == kToCodes ? 1 : KIND == kToBf16 ? 2 : 4;
+  constexpr int kStores = FI * Row64<KIND>::STORES;
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / T::WN, wn = wave % T::WN;
   const int K = g.K, nk = (K + kScaleBlock - 1) / kScaleBlock, ld = fd::scale_stride(K);
   const int tiles_m = (M + T::BM - 1) / T::BM, tiles_n = (g.N + T::BN - 1) / T::BN, tiles = tiles_m * tiles_n;
   const int per_xcd = (tiles + 7) / 8;
   const uint32_t ring_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr_t)ring));
 
-  for (int u = blockIdx.x; u < per_xcd * 8; u += gridDim.x) {
-    // consecutive tiles on one XCD (a workgroup runs on XCD blockIdx.x % 8), in groups of 8 row tiles x
-    // every column tile, so that the tiles an XCD runs at once share operand rows in its L2
+  // Tile of turn u of this workgroup: consecutive tiles on one XCD (a workgroup runs on XCD
+  // blockIdx.x % 8), in groups of 8 row tiles x every column tile, row tile fastest, so that the tiles
+  // an XCD runs at once share operand rows in its L2.
+  auto tile_at = [&](int u, int& m0, int& n0) -> bool {
     const int tile = (u % 8) * per_xcd + u / 8;
-    if (tile >= tiles) break;
+    if (u >= per_xcd * 8 || tile >= tiles) return false;
     const int grp = tile / (8 * tiles_n), in = tile - grp * 8 * tiles_n, gm = min(8, tiles_m - 8 * grp);
-    const int m0 = (8 * grp + in % gm) * T::BM, n0 = in / gm * T::BN;
+    m0 = (8 * grp + in % gm) * T::BM;
+    n0 = in / gm * T::BN;
+    return true;
+  };
 
-    const i32x4_t ra = buffer_of(g.a + static_cast<size_t>(m0) * K), rw = buffer_of(g.w + static_cast<size_t>(n0) * K);
-    const i32x4_t rsa = buffer_of(g.a_scale + static_cast<size_t>(m0) * ld);
-    const i32x4_t rsw = buffer_of(g.w_scale + static_cast<size_t>(n0 / kScaleBlock) * ld);
-    // this lane's row and chunk of each wave-load; rows past M (N) re-read the last one
-    auto chunk_of = [&](int q) {
-      const bool a = q < T::LOADS_A;
-      const int r = (wave + 4 * (a ? q : q - T::LOADS_A)) * 8 + (lane >> 3);
-      return (lane & 7) ^ (a ? (r >> 1) & 7 : ((r >> 1) & 1) | ((r >> 5) & 3) << 1);
-    };
-    uint32_t off[T::LOADS];
+  // ---- the loads: a cursor over (tile, K-block)
+  int lu = blockIdx.x, lk = 0, lturn = 0, lm0, ln0;
+  if (!tile_at(lu, lm0, ln0)) return;
+  int m0 = lm0, n0 = ln0;   // the products' tile
+  i32x4_t ra, rw, rside;
+  uint32_t off[T::LOADS], off_side;
+  auto row_of = [&](int q) { return (wave + T::WAVES * (q < T::LOADS_A ? q : q - T::LOADS_A)) * 8 + (lane >> 3); };
+  auto chunk_of = [&](int q) { return (lane & 7) ^ (q < T::LOADS_A ? T::swz_a(row_of(q)) : T::swz_w(row_of(q))); };
+  auto aim = [&] {   // the cursor's tile: bases, and this lane's row and chunk of each load (rows past the end re-read the last)
+    ra = buffer_of(g.a + static_cast<size_t>(lm0) * K);
+    rw = buffer_of(g.w + static_cast<size_t>(ln0) * K);
 #pragma unroll
-    for (int q = 0; q < T::LOADS; ++q) {
-      const bool a = q < T::LOADS_A;
-      const int r = (wave + 4 * (a ? q : q - T::LOADS_A)) * 8 + (lane >> 3);
-      off[q] = static_cast<uint32_t>(min(r, (a ? M - m0 : g.N - n0) - 1)) * static_cast<uint32_t>(K) + 16 * chunk_of(q);
+    for (int q = 0; q < T::LOADS; ++q)
+      off[q] = static_cast<uint32_t>(min(row_of(q), (q < T::LOADS_A ? M - lm0 : g.N - ln0) - 1)) * static_cast<uint32_t>(K) + 16 * chunk_of(q);
+    if (wave < T::BM / 64) {
+      rside = buffer_of(g.a_scale + static_cast<size_t>(lm0) * ld);
+      off_side = static_cast<uint32_t>(min(64 * wave + lane, M - lm0 - 1)) * static_cast<uint32_t>(ld);
+    } else if (wave == T::BM / 64) {
+      rside = buffer_of(g.bias, g.bias ? 4u * g.N : 0u);   // no bias: zeros
+      off_side = 4u * ln0 + 16u * lane;
+    } else {
+      rside = buffer_of(g.w_scale + static_cast<size_t>(ln0 / kScaleBlock) * ld);
+      off_side = static_cast<uint32_t>(min(lane % T::WN, (g.N - ln0 - 1) / kScaleBlock) * ld);
     }
-    const uint32_t off_sa = static_cast<uint32_t>(min((64 * wave + lane) % T::BM, M - m0 - 1) * ld);
-    const uint32_t off_sw = static_cast<uint32_t>(min(lane % T::WN, (g.N - n0 - 1) / kScaleBlock) * ld);
-    auto issue = [&](int kb, int slot) {
-      const uint32_t at = ring_at + static_cast<uint32_t>(slot * T::CHUNKS * 16), k = static_cast<uint32_t>(kb * kScaleBlock);
-      auto load = [&](int q, uint32_t v) {
-        const uint32_t blk = q < T::LOADS_A ? wave + 4 * q : T::BM / 8 + wave + 4 * (q - T::LOADS_A);
-        dma16(at + blk * 1024, v, q < T::LOADS_A ? ra : rw, k);
-      };
-      if (kb * kScaleBlock + kScaleBlock <= K) {
+  };
+  auto issue = [&](int slot) {   // the cursor's stage into a slot, and the cursor to the next; at the end it stays
+    const uint32_t at = ring_at + static_cast<uint32_t>(slot * T::CHUNKS * 16), k = static_cast<uint32_t>(lk * kScaleBlock);
+    auto load = [&](int q, uint32_t v) {
+      const uint32_t blk = q < T::LOADS_A ? wave + T::WAVES * q : T::BM / 8 + wave + T::WAVES * (q - T::LOADS_A);
+      dma16(at + blk * 1024, v, q < T::LOADS_A ? ra : rw, k);
+    };
+    if (static_cast<int>(k) + kScaleBlock <= K) {
 #pragma unroll
-        for (int q = 0; q < T::LOADS; ++q) load(q, off[q]);
-      } else {   // the last, shorter K-block: chunks past K read zeros
-        const int left = (K - kb * kScaleBlock) / 16;
+      for (int q = 0; q < T::LOADS; ++q) load(q, off[q]);
+    } else {   // the last, shorter K-block: chunks past K read zeros
+      const int left = (K - static_cast<int>(k)) / 16;
 #pragma unroll
-        for (int q = 0; q < T::LOADS; ++q) load(q, chunk_of(q) < left ? off[q] : 0x80000000u);
+      for (int q = 0; q < T::LOADS; ++q) load(q, chunk_of(q) < left ? off[q] : kNowhere);
+    }
+    if (wave == T::BM / 64) dma16(ring_at + T::BIAS * 16 + (lturn & 3) * 1024, off_side, rside, 0);
+    else dma4(at + T::SIDE * 16 + min(wave, T::BM / 64) * 256, off_side, rside, static_cast<uint32_t>(lk & ~3));
+    if (++lk == nk) {
+      int m, n;
+      if (tile_at(lu + gridDim.x, m, n)) {
+        lu += gridDim.x; lm0 = m; ln0 = n; lk = 0; ++lturn;
+        aim();
+      } else {
+        lk = nk - 1;
       }
-      const uint32_t kb4 = static_cast<uint32_t>(kb & ~3);
-      dma4(at + T::SIDE * 16 + wave * 256, off_sa, rsa, kb4);
-      dma4(at + T::SIDE * 16 + 1024 + wave * 256, off_sw, rsw, kb4);
-    };
-    auto frag_at = [&](const uint4* sm, int row, int swz) {
-      const uint4 lo = sm[row * 8 + ((2 * lg) ^ swz)], hi = sm[row * 8 + ((2 * lg + 1) ^ swz)];
-      return i32x8_t{static_cast<int>(lo.x), static_cast<int>(lo.y), static_cast<int>(lo.z), static_cast<int>(lo.w),
-                     static_cast<int>(hi.x), static_cast<int>(hi.y), static_cast<int>(hi.z), static_cast<int>(hi.w)};
-    };
+    }
+  };
 
-    f32x4_t acc[FM][8] = {};
+  // ---- the products
+  const int arow = 32 * FI * wm + l32;
+  const int wrow = 128 * wn + 64 * ((l32 >> 2) & 1) + 4 * (l32 >> 3) + (l32 & 3);   // of fragment 0: lanes' columns run over 64
+  auto read = [&](const uint4* sm, int row, int swz, int kh) {
+    const int c = 4 * kh + 2 * half;
+    const uint4 lo = sm[row * 8 + (c ^ swz)], hi = sm[row * 8 + ((c + 1) ^ swz)];
+    return i32x8_t{static_cast<int>(lo.x), static_cast<int>(lo.y), static_cast<int>(lo.z), static_cast<int>(lo.w),
+                   static_cast<int>(hi.x), static_cast<int>(hi.y), static_cast<int>(hi.z), static_cast<int>(hi.w)};
+  };
+  i32x8_t a[2][FI], w[3];
+  uint32_t sa[FI], sw, sa_next[FI], sw_next;
+  auto read_a = [&](const uint4* sm, int kh) {
 #pragma unroll
-    for (int p = 0; p < STAGES - 1; ++p) issue(min(p, nk - 1), p);
+    for (int i = 0; i < FI; ++i) a[kh][i] = read(sm, arow + 32 * i, T::swz_a(arow + 32 * i), kh);
+  };
+  auto read_w = [&](const uint4* sm, int s, i32x8_t& to) {
+    const int r = wrow + 16 * (s & 3);
+    to = read(sm + T::BM * 8, r, T::swz_w(r), s >> 2);
+  };
+  auto read_scales = [&](const uint4* sm, int kb) {
+    const uint32_t* side = reinterpret_cast<const uint32_t*>(sm + T::SIDE);
+#pragma unroll
+    for (int i = 0; i < FI; ++i) sa_next[i] = side[arow + 32 * i] >> (8 * (kb & 3));
+    sw_next = side[T::BM + wn] >> (8 * (kb & 3));
+  };
+
+  aim();
+#pragma unroll
+  for (int p = 0; p < STAGES; ++p) issue(p);
+  wait_barrier<(STAGES - 1) * T::ISSUED>();
+  read_a(ring, 0);
+  read_w(ring, 0, w[0]);
+  read_w(ring, 1, w[1]);
+  read_scales(ring, 0);
+
+  int slot = 0, turn = 0;
+  bool stored = false;   // the previous tile's stores were issued after the last stage
+  for (int u = blockIdx.x;;) {
+    f32x16_t acc[FI][4] = {};
     for (int kb = 0; kb < nk; ++kb) {
-      wait_vm_barrier<(STAGES - 2) * T::ISSUED>();
-      issue(min(kb + STAGES - 1, nk - 1), (kb + STAGES - 1) % STAGES);
-      const uint4* sm = ring + (kb % STAGES) * T::CHUNKS;
-      const uint32_t* side = reinterpret_cast<const uint32_t*>(sm + T::SIDE);
-      const int sh = 8 * (kb & 3);
-      const uint32_t sw = side[256 + 64 * wave + wn] >> sh;
-      typename Mma::frag wf[8];
+      const uint4* sm = ring + slot * T::CHUNKS;
+      const int next = slot + 1 == STAGES ? 0 : slot + 1;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int r = 128 * wn + 32 * (l16 >> 2) + 4 * j + (l16 & 3);
-        wf[j] = Mma::make(frag_at(sm + T::BM * 8, r, ((r >> 1) & 1) | ((r >> 5) & 3) << 1), sw);
+      for (int i = 0; i < FI; ++i) sa[i] = sa_next[i];
+      sw = sw_next;
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        if (s == 0) read_a(sm, 1);
+        if (s < 6) read_w(sm, s + 2, w[(s + 2) % 3]);
+        if (s == 6) {
+          if (kb == 0 && stored) wait_barrier<(STAGES - 2) * T::ISSUED + kStores>();
+          else wait_barrier<(STAGES - 2) * T::ISSUED>();
+          issue(slot);
+          const uint4* sn = ring + next * T::CHUNKS;
+          read_a(sn, 0);
+          read_w(sn, 0, w[2]);   // w[6 % 3] and w[7 % 3] are in use
+          read_scales(sn, kb + 1 == nk ? 0 : kb + 1);
+        }
+        const typename Mma::frag wf = Mma::make(w[s % 3], sw);
+#pragma unroll
+        for (int i = 0; i < FI; ++i) acc[i][s & 3] = Mma::mma(wf, Mma::make(a[s >> 2][i], sa[i]), acc[i][s & 3], sw, sa[i]);
+        __builtin_amdgcn_sched_barrier(0);
       }
+      slot = next;
+      w[0] = w[2];
+      read_w(ring + slot * T::CHUNKS, 1, w[1]);
+    }
+    // the tile's results: lane (l32, half) holds row l32 of each 32 and columns 64 half .. + 63
+    {
+      const float* bias = reinterpret_cast<const float*>(ring + T::BIAS + (turn & 3) * 64) + 128 * wn + 64 * half;
+      const int col = n0 + 128 * wn + 64 * half;
+      void* base;
+      if constexpr (KIND == kToCodes) base = g.y_q;
+      else if constexpr (KIND == kToBf16) base = g.y_bf16;
+      else base = g.y_f32;
+      const auto y = __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t*>(base) + (static_cast<size_t>(m0) * g.N + n0) * kSize, 0, 0x7fffffff, 0x00020000);
+      const int lds_y = fd::scale_stride(g.N);
+      const auto ys = __builtin_amdgcn_make_buffer_rsrc(g.y_scale + static_cast<size_t>(m0) * lds_y, 0, 0x7fffffff, 0x00020000);
 #pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        const int r = 16 * FM * wm + 16 * i + l16;
-        const uint32_t sa = side[r] >> sh;
-        const typename Mma::frag af = Mma::make(frag_at(sm, r, (r >> 1) & 7), sa);
+      for (int i = 0; i < FI; ++i) {
+        const int r = arow + 32 * i;
+        float v[64];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[i][j] = Mma::mma(wf[j], af, acc[i][j], sw, sa);
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const float4 b = *reinterpret_cast<const float4*>(bias + 16 * j + e);
+            v[16 * j + e] = acc[i][j][e] + b.x; v[16 * j + e + 1] = acc[i][j][e + 1] + b.y;
+            v[16 * j + e + 2] = acc[i][j][e + 2] + b.z; v[16 * j + e + 3] = acc[i][j][e + 3] + b.w;
+          }
+        __builtin_amdgcn_sched_barrier(0);   // a row at a time: the registers hold one set of 64 bias values
+        Row64<KIND>::store(v, g.gelu, m0 + r < M, g.N - col, static_cast<uint32_t>(r * g.N + col - n0) * kSize, half, y, ys,
+                           static_cast<uint32_t>(r * lds_y + col / kScaleBlock));
       }
     }
-    // the last stages' repeats may still be landing: drained before the ring is used again
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const int row = m0 + 16 * FM * wm + 16 * i + l16;
-      store_row<KIND, 8>(g, row < M, row, n0 + 128 * wn + 32 * lg, acc[i]);
-    }
+    stored = true;
+    ++turn;
+    u += gridDim.x;
+    if (!tile_at(u, m0, n0)) break;
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the repeats of the last stage
 }
 
-using TileLarge = Tile<8, 2, 2, 2>;   // 256 x 256
-using TileMid = Tile<4, 2, 2, 3>;     // 128 x 256
-using TileSmall = Tile<2, 4, 1, 4>;   // 128 x 128
-constexpr int kRing = TileMid::STAGES * TileMid::CHUNKS;
-static_assert(kRing >= TileLarge::STAGES * TileLarge::CHUNKS && kRing >= TileSmall::STAGES * TileSmall::CHUNKS && kRing * 16 <= 160 * 1024, "one ring for all");
+using TileLarge = Tile<2, 4, 2, 2>;   // 256 x 256
+using TileMid = Tile<1, 4, 2, 3>;     // 128 x 256
+using TileSmall = Tile<1, 4, 1, 2>;   // 128 x 128, two workgroups per CU
 
-template <int KIND, class Mma>
-__global__ __launch_bounds__(256, 1) void scaled_tile_kernel(fdh::ScaledArgs g, int shape) {
-  __shared__ uint4 ring[kRing];
+template <int KIND, class Mma, class T, int PER_CU>
+__global__ __launch_bounds__(T::THREADS, PER_CU * T::WAVES / 4) void scaled_tile_kernel(fdh::ScaledArgs g) {
+  __shared__ uint4 ring[T::TOTAL];
+  static_assert(T::TOTAL * 16 * PER_CU <= 160 * 1024, "the LDS of a CU");
   const int M = g.m ? min(*g.m, g.n_rows) : g.n_rows;
-  if (M <= 0) return;
-  switch (shape) {
-    case 0: scaled_tiles<TileLarge, KIND, Mma>(g, M, ring); break;
-    case 1: scaled_tiles<TileMid, KIND, Mma>(g, M, ring); break;
-    default: scaled_tiles<TileSmall, KIND, Mma>(g, M, ring); break;
-  }
+  if (M > 0) scaled_tiles<T, KIND, Mma>(g, M, ring);
 }
 
 }  // namespace
@@ -346,8 +500,10 @@ hipError_t launch_scaled_linear(const ScaledArgs& g, hipStream_t s) {
       return;
     }
     const char* e = getenv("FD_SHAPE");
-    const int shape = e ? atoi(e) : 0;
-    scaled_tile_kernel<KIND, Mma><<<num_cus() / 8 * 8, 256, 0, s>>>(g, shape);
+    const int shape = e ? atoi(e) : 0, cus = num_cus() / 8 * 8;
+    if (shape == 0) scaled_tile_kernel<KIND, Mma, TileLarge, 1><<<cus, TileLarge::THREADS, 0, s>>>(g);
+    else if (shape == 1) scaled_tile_kernel<KIND, Mma, TileMid, 1><<<cus, TileMid::THREADS, 0, s>>>(g);
+    else scaled_tile_kernel<KIND, Mma, TileSmall, 2><<<2 * cus, TileSmall::THREADS, 0, s>>>(g);
   };
   if (g.y_q) run(std::integral_constant<int, kToCodes>{}, Mma8{});
   else if (g.y_bf16) run(std::integral_constant<int, kToBf16>{}, Mma8{});
