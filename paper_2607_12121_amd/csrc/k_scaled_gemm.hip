@@ -201,13 +201,12 @@ struct Tile {
   static constexpr int FI = FI_, WM = WM_, WN = WN_, STAGES = STAGES_;
   static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
   static constexpr int BM = 32 * FI * WM, BN = 128 * WN;
-  static constexpr int LOADS_A = BM / 8 / WAVES, LOADS = (BM + BN) / 8 / WAVES;   // 8 rows of 128 bytes per wave-load
-  static constexpr int ISSUED = LOADS + 1;                                        // and one of scales or bias
+  static constexpr int LOADS_A = BM / 8 / WAVES, LOADS_W = BN / 8 / WAVES;        // 8 rows of 128 bytes per wave-load
+  static constexpr int ISSUED = LOADS_A + LOADS_W + 1;                            // and one of scales or bias
   static constexpr int SIDE = (BM + BN) * 8;                                      // chunk where a stage's scales begin
   static constexpr int CHUNKS = SIDE + BM / 4 + 16;                               // row scales, then 256 bytes of column scales
-  static constexpr int BIAS = STAGES * CHUNKS;                                    // four slots of the columns' bias
-  static constexpr int TOTAL = BIAS + 4 * 64;
-  static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && BM % 64 == 0 && BM / 64 + 2 <= WAVES && BN <= 256, "whole wave-loads");
+  static constexpr int TOTAL = STAGES * CHUNKS;
+  static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && BM % 64 == 0 && BM / 64 < WAVES, "whole wave-loads");
   static FD_DEVICE int swz_a(int r) { return (r >> 1) & 7; }
   static FD_DEVICE int swz_w(int r) { return ((r >> 1) & 3) | ((r >> 6) & 1) << 2; }
 };
@@ -227,16 +226,32 @@ FD_DEVICE void dma16(uint32_t lds, uint32_t voff, i32x4_t rsrc, uint32_t soff) {
 FD_DEVICE void dma4(uint32_t lds, uint32_t voff, i32x4_t rsrc, uint32_t soff) {
   asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, %3 offen lds" : : "s"(lds), "v"(voff), "s"(rsrc), "s"(soff));
 }
-// This wave's LDS reads are done and at most N of its vector memory operations are in flight; then the barrier.
-template <int N>
-FD_DEVICE void wait_barrier() {
-  static_assert(N < 64, "the counter's range");
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory");
+FD_DEVICE f32x16_t scalar_load16(const float* p) {
+  f32x16_t v;
+  asm volatile("s_load_dwordx16 %0, %1, 0x0\n\ts_waitcnt lgkmcnt(0)" : "=s"(v) : "s"(p));
+  return v;
+}
+// This wave's LDS reads are done; then the barrier.
+FD_DEVICE void wait_reads_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
+// ... and at most N of its vector memory operations are in flight (N + MORE where `more`).  One block of assembly:
+// a branch around the wait would end the basic block, across which the compiler moves the products.
+template <int N, int MORE>
+FD_DEVICE void wait_barrier(int more) {
+  static_assert(N + MORE < 64, "the counter's range");
+  asm volatile(
+      "s_waitcnt vmcnt(%1) lgkmcnt(0)\n\t"
+      "s_cmp_lg_u32 %0, 0\n\t"
+      "s_cbranch_scc1 .Lfd_wait_%=\n\t"
+      "s_waitcnt vmcnt(%2)\n"
+      ".Lfd_wait_%=:\n\t"
+      "s_barrier"
+      :
+      : "s"(more), "n"(N + MORE), "n"(N)
+      : "memory", "scc");
 }
 
-// A lane's 64 columns of one row to memory; every store issues whatever the row (kStores of them), rows and
-// columns outside go nowhere.  x: the row's values with bias; at: byte offset of the row's first column over
-// the element size from the base of `y`.
+// A lane's 64 columns of one row to memory (cols of them lie inside N).  Every store issues whatever the row,
+// rows and columns outside go nowhere: the waits count the stores.
 template <int KIND>
 struct Row64 {
   static constexpr int STORES = KIND == kToCodes ? 5 : KIND == kToBf16 ? 8 : 16;
@@ -244,43 +259,46 @@ struct Row64 {
   static FD_DEVICE void put(const u32x4& v, __amdgpu_buffer_rsrc_t y, bool ok, uint32_t off) {
     __builtin_amdgcn_raw_buffer_store_b128(v, y, ok ? off : kNowhere, 0, 0);
   }
-  static FD_DEVICE void store(float (&v)[64], bool gelu, bool row_ok, int cols, uint32_t row_off, int half, __amdgpu_buffer_rsrc_t y,
+  static FD_DEVICE void store(f32x16_t (&v)[4], bool gelu, bool row_ok, int cols, uint32_t row_off, int half, __amdgpu_buffer_rsrc_t y,
                               __amdgpu_buffer_rsrc_t scale, uint32_t scale_off) {
     if (gelu) {
 #pragma unroll
-      for (int e = 0; e < 64; ++e) v[e] = fd::gelu_tanh_fast(v[e]);
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[j][e] = fd::gelu_tanh_fast(v[j][e]);
     }
     if constexpr (KIND == kToCodes) {
       uint32_t top = 0;
 #pragma unroll
-      for (int e = 0; e < 64; ++e) top = (e & ~15) < cols ? max(top, fd::mag_bits(v[e])) : top;
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = 16 * j < cols ? max(top, fd::mag_bits(v[j][e])) : top;
       top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 32, fd::kWave)));
       const uint32_t s = fd::scale_byte(top);
       const float inv = fd::scale_inverse(s);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
+      for (int j = 0; j < 4; ++j) {
         u32x4 w;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float* x = v + 16 * c + 4 * i;
-          w[i] = fd::pack_codes(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
-        }
-        put(w, y, row_ok && 16 * c < cols, row_off + 16 * c);
+        for (int i = 0; i < 4; ++i) w[i] = fd::pack_codes(v[j][4 * i] * inv, v[j][4 * i + 1] * inv, v[j][4 * i + 2] * inv, v[j][4 * i + 3] * inv);
+        put(w, y, row_ok && 16 * j < cols, row_off + 16 * j);
       }
       __builtin_amdgcn_raw_buffer_store_b8(static_cast<uint8_t>(s), scale, row_ok && half == 0 && cols > 0 ? scale_off : kNowhere, 0, 0);
     } else if constexpr (KIND == kToBf16) {
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
-        const float* x = v + 8 * c;
-        put(u32x4{fd::pack_bf2(x[0], x[1]), fd::pack_bf2(x[2], x[3]), fd::pack_bf2(x[4], x[5]), fd::pack_bf2(x[6], x[7])}, y,
-            row_ok && 8 * c < cols, row_off + 16 * c);
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = fd::pack_bf2(v[c >> 1][8 * (c & 1) + 2 * i], v[c >> 1][8 * (c & 1) + 2 * i + 1]);
+        put(w, y, row_ok && 8 * c < cols, row_off + 16 * c);
       }
     } else {
 #pragma unroll
       for (int c = 0; c < 16; ++c) {
-        const float* x = v + 4 * c;
-        put(u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])}, y, row_ok && 4 * c < cols,
-            row_off + 16 * c);
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[c >> 2][4 * (c & 3) + i]);
+        put(w, y, row_ok && 4 * c < cols, row_off + 16 * c);
       }
     }
   }
@@ -290,9 +308,12 @@ struct Row64 {
 // products, into the next tile too, and a tile's results leave while the next one's first stages land.
 //
 // A step's eight sub-steps s = (half of K, column fragment) each read one weight fragment two sub-steps
-// ahead.  After sub-step 5 the wave has read all of its stage; the barrier there frees the stage for the
-// load STAGES steps on and publishes the next stage, whose first fragments are read behind sub-steps 6
-// and 7, so that no sub-step waits for LDS or for the barrier with nothing to compute.
+// ahead.  After sub-step 1 the wave has read its rows, after sub-step 5 its columns; a barrier there frees
+// that part of the stage for the load STAGES steps on, which goes out a few instructions at a time behind
+// products.  The second barrier also publishes the next stage, whose first fragments are read behind
+// sub-steps 6 and 7, so that no sub-step waits for LDS or for the barrier with nothing to compute.  A step
+// is one basic block: across branches the compiler gathers the products at the end.  K has at least STAGES
+// blocks.
 template <class T, int KIND, class Mma>
 FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
   constexpr int FI = T::FI, STAGES = T::STAGES;
@@ -317,76 +338,60 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
     return true;
   };
 
-  // ---- the loads: a cursor over (tile, K-block)
-  int lu = blockIdx.x, lk = 0, lturn = 0, lm0, ln0;
-  if (!tile_at(lu, lm0, ln0)) return;
-  int m0 = lm0, n0 = ln0;   // the products' tile
+  // ---- the loads: of K-block lk of the tile at (lm0, ln0)
+  int u = blockIdx.x, lk = 0, lm0, ln0;
+  if (!tile_at(u, lm0, ln0)) return;
   i32x4_t ra, rw, rside;
-  uint32_t off[T::LOADS], off_side;
-  auto row_of = [&](int q) { return (wave + T::WAVES * (q < T::LOADS_A ? q : q - T::LOADS_A)) * 8 + (lane >> 3); };
-  auto chunk_of = [&](int q) { return (lane & 7) ^ (q < T::LOADS_A ? T::swz_a(row_of(q)) : T::swz_w(row_of(q))); };
-  auto aim = [&] {   // the cursor's tile: bases, and this lane's row and chunk of each load (rows past the end re-read the last)
+  uint32_t off_a[T::LOADS_A], off_w[T::LOADS_W], off_side;
+  auto row_of = [&](int q) { return (wave + T::WAVES * q) * 8 + (lane >> 3); };
+  auto chunk_a = [&](int q) { return (lane & 7) ^ T::swz_a(row_of(q)); };
+  auto chunk_w = [&](int q) { return (lane & 7) ^ T::swz_w(row_of(q)); };
+  auto aim = [&] {   // the tile's bases, and this lane's row and chunk of each load (rows past the end re-read the last)
     ra = buffer_of(g.a + static_cast<size_t>(lm0) * K);
     rw = buffer_of(g.w + static_cast<size_t>(ln0) * K);
 #pragma unroll
-    for (int q = 0; q < T::LOADS; ++q)
-      off[q] = static_cast<uint32_t>(min(row_of(q), (q < T::LOADS_A ? M - lm0 : g.N - ln0) - 1)) * static_cast<uint32_t>(K) + 16 * chunk_of(q);
+    for (int q = 0; q < T::LOADS_A; ++q) off_a[q] = static_cast<uint32_t>(min(row_of(q), M - lm0 - 1)) * static_cast<uint32_t>(K) + 16 * chunk_a(q);
+#pragma unroll
+    for (int q = 0; q < T::LOADS_W; ++q) off_w[q] = static_cast<uint32_t>(min(row_of(q), g.N - ln0 - 1)) * static_cast<uint32_t>(K) + 16 * chunk_w(q);
     if (wave < T::BM / 64) {
       rside = buffer_of(g.a_scale + static_cast<size_t>(lm0) * ld);
       off_side = static_cast<uint32_t>(min(64 * wave + lane, M - lm0 - 1)) * static_cast<uint32_t>(ld);
-    } else if (wave == T::BM / 64) {
-      rside = buffer_of(g.bias, g.bias ? 4u * g.N : 0u);   // no bias: zeros
-      off_side = 4u * ln0 + 16u * lane;
     } else {
       rside = buffer_of(g.w_scale + static_cast<size_t>(ln0 / kScaleBlock) * ld);
       off_side = static_cast<uint32_t>(min(lane % T::WN, (g.N - ln0 - 1) / kScaleBlock) * ld);
     }
   };
-  auto issue = [&](int slot) {   // the cursor's stage into a slot, and the cursor to the next; at the end it stays
-    const uint32_t at = ring_at + static_cast<uint32_t>(slot * T::CHUNKS * 16), k = static_cast<uint32_t>(lk * kScaleBlock);
-    auto load = [&](int q, uint32_t v) {
-      const uint32_t blk = q < T::LOADS_A ? wave + T::WAVES * q : T::BM / 8 + wave + T::WAVES * (q - T::LOADS_A);
-      dma16(at + blk * 1024, v, q < T::LOADS_A ? ra : rw, k);
-    };
-    if (static_cast<int>(k) + kScaleBlock <= K) {
-#pragma unroll
-      for (int q = 0; q < T::LOADS; ++q) load(q, off[q]);
-    } else {   // the last, shorter K-block: chunks past K read zeros
-      const int left = (K - static_cast<int>(k)) / 16;
-#pragma unroll
-      for (int q = 0; q < T::LOADS; ++q) load(q, chunk_of(q) < left ? off[q] : kNowhere);
-    }
-    if (wave == T::BM / 64) dma16(ring_at + T::BIAS * 16 + (lturn & 3) * 1024, off_side, rside, 0);
-    else dma4(at + T::SIDE * 16 + min(wave, T::BM / 64) * 256, off_side, rside, static_cast<uint32_t>(lk & ~3));
-    if (++lk == nk) {
-      int m, n;
-      if (tile_at(lu + gridDim.x, m, n)) {
-        lu += gridDim.x; lm0 = m; ln0 = n; lk = 0; ++lturn;
-        aim();
-      } else {
-        lk = nk - 1;
-      }
-    }
+  // Load q of the rows and of the columns into a slot, and the scales.  The chunks past K of a last,
+  // shorter K-block read zeros.
+  auto issue_a = [&](int slot, int q) {
+    const uint32_t at = ring_at + static_cast<uint32_t>(slot * T::CHUNKS * 16 + wave * 1024);
+    dma16(at + T::WAVES * q * 1024, lk * kScaleBlock + 16 * chunk_a(q) < K ? off_a[q] : kNowhere, ra, static_cast<uint32_t>(lk * kScaleBlock));
+  };
+  auto issue_w = [&](int slot, int q) {
+    const uint32_t at = ring_at + static_cast<uint32_t>(slot * T::CHUNKS * 16 + T::BM * 128 + wave * 1024);
+    dma16(at + T::WAVES * q * 1024, lk * kScaleBlock + 16 * chunk_w(q) < K ? off_w[q] : kNowhere, rw, static_cast<uint32_t>(lk * kScaleBlock));
+  };
+  auto issue_scales = [&](int slot) {
+    dma4(ring_at + static_cast<uint32_t>(slot * T::CHUNKS * 16 + T::SIDE * 16 + min(wave, T::BM / 64) * 256), off_side, rside, static_cast<uint32_t>(lk & ~3));
   };
 
   // ---- the products
   const int arow = 32 * FI * wm + l32;
-  const int wrow = 128 * wn + 64 * ((l32 >> 2) & 1) + 4 * (l32 >> 3) + (l32 & 3);   // of fragment 0: lanes' columns run over 64
+  const int wrow = 128 * wn + 64 * ((l32 >> 2) & 1) + 4 * (l32 >> 3) + (l32 & 3);   // of fragment 0: a lane's columns run over 64
   auto read = [&](const uint4* sm, int row, int swz, int kh) {
     const int c = 4 * kh + 2 * half;
     const uint4 lo = sm[row * 8 + (c ^ swz)], hi = sm[row * 8 + ((c + 1) ^ swz)];
     return i32x8_t{static_cast<int>(lo.x), static_cast<int>(lo.y), static_cast<int>(lo.z), static_cast<int>(lo.w),
                    static_cast<int>(hi.x), static_cast<int>(hi.y), static_cast<int>(hi.z), static_cast<int>(hi.w)};
   };
-  i32x8_t a[2][FI], w[3];
+  i32x8_t a[2][FI], w[4];
   uint32_t sa[FI], sw, sa_next[FI], sw_next;
   auto read_a = [&](const uint4* sm, int kh) {
 #pragma unroll
-    for (int i = 0; i < FI; ++i) a[kh][i] = read(sm, arow + 32 * i, T::swz_a(arow + 32 * i), kh);
+    for (int i = 0; i < FI; ++i) a[kh][i] = read(sm, arow + 32 * i, T::swz_a(arow), kh);   // 32 i leaves the swizzle
   };
-  auto read_w = [&](const uint4* sm, int s, i32x8_t& to) {
-    const int r = wrow + 16 * (s & 3);
-    to = read(sm + T::BM * 8, r, T::swz_w(r), s >> 2);
+  auto read_w = [&](const uint4* sm, int s) {
+    w[s & 3] = read(sm + T::BM * 8, wrow + 16 * (s & 3), T::swz_w(wrow), s >> 2);   // so does 16 j
   };
   auto read_scales = [&](const uint4* sm, int kb) {
     const uint32_t* side = reinterpret_cast<const uint32_t*>(sm + T::SIDE);
@@ -397,77 +402,103 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
 
   aim();
 #pragma unroll
-  for (int p = 0; p < STAGES; ++p) issue(p);
-  wait_barrier<(STAGES - 1) * T::ISSUED>();
+  for (int p = 0; p < STAGES; ++p) {
+#pragma unroll
+    for (int q = 0; q < T::LOADS_A; ++q) issue_a(p, q);
+#pragma unroll
+    for (int q = 0; q < T::LOADS_W; ++q) issue_w(p, q);
+    issue_scales(p);
+    ++lk;
+  }
+  wait_barrier<(STAGES - 1) * T::ISSUED, 0>(0);
   read_a(ring, 0);
-  read_w(ring, 0, w[0]);
-  read_w(ring, 1, w[1]);
+  read_w(ring, 0);
+  read_w(ring, 1);
   read_scales(ring, 0);
 
-  int slot = 0, turn = 0;
-  bool stored = false;   // the previous tile's stores were issued after the last stage
-  for (int u = blockIdx.x;;) {
+  int slot = 0;
+  int stored = 0;   // in a tile's first step: the previous tile's stores were issued after the last stage's loads
+  for (;;) {
+    const int m0 = lm0, n0 = ln0;
     f32x16_t acc[FI][4] = {};
-    for (int kb = 0; kb < nk; ++kb) {
-      const uint4* sm = ring + slot * T::CHUNKS;
-      const int next = slot + 1 == STAGES ? 0 : slot + 1;
-#pragma unroll
-      for (int i = 0; i < FI; ++i) sa[i] = sa_next[i];
-      sw = sw_next;
-#pragma unroll
-      for (int s = 0; s < 8; ++s) {
-        if (s == 0) read_a(sm, 1);
-        if (s < 6) read_w(sm, s + 2, w[(s + 2) % 3]);
-        if (s == 6) {
-          if (kb == 0 && stored) wait_barrier<(STAGES - 2) * T::ISSUED + kStores>();
-          else wait_barrier<(STAGES - 2) * T::ISSUED>();
-          issue(slot);
-          const uint4* sn = ring + next * T::CHUNKS;
-          read_a(sn, 0);
-          read_w(sn, 0, w[2]);   // w[6 % 3] and w[7 % 3] are in use
-          read_scales(sn, kb + 1 == nk ? 0 : kb + 1);
-        }
-        const typename Mma::frag wf = Mma::make(w[s % 3], sw);
-#pragma unroll
-        for (int i = 0; i < FI; ++i) acc[i][s & 3] = Mma::mma(wf, Mma::make(a[s >> 2][i], sa[i]), acc[i][s & 3], sw, sa[i]);
-        __builtin_amdgcn_sched_barrier(0);
+    bool more = false;
+    int kb = 0;
+    // the steps that load this tile, then the last STAGES, which load the next one (or this one's end again)
+    for (int part = 0; part < 2; ++part) {
+      if (part == 1) {
+        more = tile_at(u + gridDim.x, lm0, ln0);
+        lk = more ? 0 : nk - STAGES;
+        if (more) aim();
       }
-      slot = next;
-      w[0] = w[2];
-      read_w(ring + slot * T::CHUNKS, 1, w[1]);
-    }
-    // the tile's results: lane (l32, half) holds row l32 of each 32 and columns 64 half .. + 63
-    {
-      const float* bias = reinterpret_cast<const float*>(ring + T::BIAS + (turn & 3) * 64) + 128 * wn + 64 * half;
-      const int col = n0 + 128 * wn + 64 * half;
-      void* base;
-      if constexpr (KIND == kToCodes) base = g.y_q;
-      else if constexpr (KIND == kToBf16) base = g.y_bf16;
-      else base = g.y_f32;
-      const auto y = __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t*>(base) + (static_cast<size_t>(m0) * g.N + n0) * kSize, 0, 0x7fffffff, 0x00020000);
-      const int lds_y = fd::scale_stride(g.N);
-      const auto ys = __builtin_amdgcn_make_buffer_rsrc(g.y_scale + static_cast<size_t>(m0) * lds_y, 0, 0x7fffffff, 0x00020000);
+      for (const int end = part == 0 ? nk - STAGES : nk; kb < end; ++kb, ++lk) {
+        const int next = slot + 1 == STAGES ? 0 : slot + 1;
+        const uint4 *sm = ring + slot * T::CHUNKS, *sn = ring + next * T::CHUNKS;
 #pragma unroll
-      for (int i = 0; i < FI; ++i) {
-        const int r = arow + 32 * i;
-        float v[64];
+        for (int i = 0; i < FI; ++i) sa[i] = sa_next[i];
+        sw = sw_next;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int e = 0; e < 16; e += 4) {
-            const float4 b = *reinterpret_cast<const float4*>(bias + 16 * j + e);
-            v[16 * j + e] = acc[i][j][e] + b.x; v[16 * j + e + 1] = acc[i][j][e + 1] + b.y;
-            v[16 * j + e + 2] = acc[i][j][e + 2] + b.z; v[16 * j + e + 3] = acc[i][j][e + 3] + b.w;
+        for (int s = 0; s < 8; ++s) {
+          if (s == 2) wait_reads_barrier();
+          if (s == 6) wait_barrier<(STAGES - 2) * T::ISSUED + T::LOADS_A, kStores>(stored);
+          if (s == 0) read_a(sm, 1);
+          if (s < 6) read_w(sm, s + 2);
+          if (s == 6) {
+            read_a(sn, 0);
+            read_w(sn, 0);
+            read_scales(sn, kb + 1 == nk ? 0 : kb + 1);
           }
-        __builtin_amdgcn_sched_barrier(0);   // a row at a time: the registers hold one set of 64 bias values
-        Row64<KIND>::store(v, g.gelu, m0 + r < M, g.N - col, static_cast<uint32_t>(r * g.N + col - n0) * kSize, half, y, ys,
-                           static_cast<uint32_t>(r * lds_y + col / kScaleBlock));
+          if (s == 7) read_w(sn, 1);
+          const typename Mma::frag wf = Mma::make(w[s & 3], sw);
+#pragma unroll
+          for (int i = 0; i < FI; ++i) acc[i][s & 3] = Mma::mma(wf, Mma::make(a[s >> 2][i], sa[i]), acc[i][s & 3], sw, sa[i]);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int q = 0; q < T::LOADS_A; ++q)
+            if (s == 2 + q * 4 / T::LOADS_A) issue_a(slot, q);
+#pragma unroll
+          for (int q = 0; q < T::LOADS_W; ++q)
+            if (s == 6 + q * 2 / T::LOADS_W) issue_w(slot, q);
+          if (s == 7) issue_scales(slot);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        slot = next;
+        stored = 0;
       }
     }
-    stored = true;
-    ++turn;
+
+    // the tile's results: lane (l32, half) holds row l32 of each 32 and columns 64 half .. + 63
+    stored = 1;
+    const int col = n0 + 128 * wn + 64 * half;
+    void* base;
+    if constexpr (KIND == kToCodes) base = g.y_q;
+    else if constexpr (KIND == kToBf16) base = g.y_bf16;
+    else base = g.y_f32;
+    const auto y = __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t*>(base) + (static_cast<size_t>(m0) * g.N + n0) * kSize, 0, 0x7fffffff, 0x00020000);
+    const int lds_y = fd::scale_stride(g.N);
+    const auto ys = __builtin_amdgcn_make_buffer_rsrc(g.y_scale + static_cast<size_t>(m0) * lds_y, 0, 0x7fffffff, 0x00020000);
+    if (g.bias) {
+      // the columns' bias through the scalar cache, 16 at a time and half, so that no vector load waits behind the stages' loads
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x16_t b0 = scalar_load16(g.bias + min(__builtin_amdgcn_readfirstlane(n0) + 128 * wn + 16 * j, g.N - 16));
+        const f32x16_t b1 = scalar_load16(g.bias + min(__builtin_amdgcn_readfirstlane(n0) + 128 * wn + 64 + 16 * j, g.N - 16));
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float b = half ? b1[e] : b0[e];
+#pragma unroll
+          for (int i = 0; i < FI; ++i) acc[i][j][e] += b;
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < FI; ++i) {
+      const int r = arow + 32 * i;
+      Row64<KIND>::store(acc[i], g.gelu, m0 + r < M, g.N - col, static_cast<uint32_t>(r * g.N + col - n0) * kSize, half, y, ys,
+                         static_cast<uint32_t>(r * lds_y + col / kScaleBlock));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (!more) break;
     u += gridDim.x;
-    if (!tile_at(u, m0, n0)) break;
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the repeats of the last stage
 }
@@ -492,11 +523,11 @@ hipError_t launch_scaled_linear(const ScaledArgs& g, hipStream_t s) {
   auto run = [&](auto kind, auto mma) {
     constexpr int KIND = decltype(kind)::value;
     using Mma = decltype(mma);
-    if (g.n_rows <= 64) {
+    if (g.n_rows <= 64 || g.K <= 2 * kScaleBlock) {   // the tiles' loads run up to three blocks ahead
       constexpr int NF = KIND == kToCodes ? 8 : 1;
       const int gx = (g.N + 16 * NF - 1) / (16 * NF);
       if (g.n_rows <= 16) scaled_few_kernel<KIND, Mma, 1, NF><<<dim3(gx, 1), kFewWaves * 64, 0, s>>>(g);
-      else scaled_few_kernel<KIND, Mma, 2, NF><<<dim3(gx, (g.n_rows + 31) / 32), kFewWaves * 64, 0, s>>>(g);
+      else scaled_few_kernel<KIND, Mma, 2, NF><<<dim3(gx, min((g.n_rows + 31) / 32, 4096)), kFewWaves * 64, 0, s>>>(g);
       return;
     }
     const char* e = getenv("FD_SHAPE");
