@@ -3,11 +3,6 @@
 // on v_mfma_scale_f32_16x16x128_f8f6f4, whose K is one block: the scale bytes are operands of the
 // instruction and the sum is kept in fp32 accumulators.
 //
-// The weight fragment is the first operand, so an accumulator holds the transposed block: lane l a
-// row of Y (l & 15) and four columns per fragment.  The 16 weight rows of fragment j of a wave's 128
-// columns are 32 (x >> 2) + 4 j + (x & 3), x < 16: the eight fragments then give lane l the 32
-// consecutive columns 32 (l >> 4) .. + 31, which leave in 16-byte stores, and four lanes hold the
-// 128 columns that share an output scale.
 #include <stdlib.h>
 
 #include <type_traits>
@@ -36,8 +31,8 @@ struct Mma8 {
   static FD_DEVICE f32x4_t mma(const frag& w, const frag& a, f32x4_t c, uint32_t sw, uint32_t sa) {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, c, 0, 0, 0, static_cast<int>(sw), 0, static_cast<int>(sa));
   }
-  static FD_DEVICE f32x16_t mma(const frag& w, const frag& a, f32x16_t c, uint32_t sw, uint32_t sa) {
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, a, c, 0, 0, 0, static_cast<int>(sw), 0, static_cast<int>(sa));
+  static FD_DEVICE f32x16_t mma(const frag& a, const frag& w, f32x16_t c, uint32_t sa, uint32_t sw) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, w, c, 0, 0, 0, static_cast<int>(sa), 0, static_cast<int>(sw));
   }
 };
 struct MmaExact {
@@ -59,13 +54,18 @@ struct MmaExact {
     for (int p = 0; p < 4; ++p) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.p[p], a.p[p], c, 0, 0, 0);
     return c;
   }
-  static FD_DEVICE f32x16_t mma(const frag& w, const frag& a, f32x16_t c, uint32_t, uint32_t) {
+  static FD_DEVICE f32x16_t mma(const frag& a, const frag& w, f32x16_t c, uint32_t, uint32_t) {
 #pragma unroll
-    for (int p = 0; p < 4; ++p) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w.p[p], a.p[p], c, 0, 0, 0);
+    for (int p = 0; p < 4; ++p) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.p[p], w.p[p], c, 0, 0, 0);
     return c;
   }
 };
 
+// The few-row kernel's blocks are 16 x 16 with the weight fragment as the first operand, so that an accumulator
+// holds the transposed block: lane l a row (l & 15) and four columns.  The 16 weight rows of fragment j of a
+// wave's 16 NF columns are 4 NF (x >> 2) + 4 j + (x & 3), x < 16: together the NF fragments give a lane 4 NF
+// consecutive columns, 4 NF (l >> 4) on.
+//
 // One row's 4 NF columns from col on (col a multiple of 4 NF; N is a multiple of 16, so each 16 lie
 // inside or outside).  Every lane of the wave runs it; codes need the whole block (NF = 8).
 template <int KIND, int NF>
@@ -205,10 +205,13 @@ struct Tile {
   static constexpr int ISSUED = LOADS_A + LOADS_W + 1;                            // and one of scales or bias
   static constexpr int SIDE = (BM + BN) * 8;                                      // chunk where a stage's scales begin
   static constexpr int CHUNKS = SIDE + BM / 4 + 16;                               // row scales, then 256 bytes of column scales
-  static constexpr int TOTAL = STAGES * CHUNKS;
-  static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && BM % 64 == 0 && BM / 64 < WAVES, "whole wave-loads");
-  static FD_DEVICE int swz_a(int r) { return (r >> 1) & 7; }
-  static FD_DEVICE int swz_w(int r) { return ((r >> 1) & 3) | ((r >> 6) & 1) << 2; }
+  static constexpr int BIAS = STAGES * CHUNKS;                                    // four slots of the columns' bias
+  static constexpr int TOTAL = BIAS + 4 * BN / 4;
+  static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && BM % 64 == 0 && BM / 64 < WAVES && BN <= 64 * WAVES, "whole wave-loads");
+  static FD_DEVICE int swz(int r) { return (r >> 1) & 7; }
+  // Column of LDS row p: fragment j of 128 columns holds every fourth, from j on, so that a lane of the product
+  // has four consecutive columns in its four fragments.
+  static FD_DEVICE int column(int p) { return (p & ~127) + 4 * (p & 31) + ((p >> 5) & 3); }
 };
 
 typedef __attribute__((address_space(3))) void* lds_ptr_t;
@@ -225,11 +228,6 @@ FD_DEVICE void dma16(uint32_t lds, uint32_t voff, i32x4_t rsrc, uint32_t soff) {
 }
 FD_DEVICE void dma4(uint32_t lds, uint32_t voff, i32x4_t rsrc, uint32_t soff) {
   asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, %3 offen lds" : : "s"(lds), "v"(voff), "s"(rsrc), "s"(soff));
-}
-FD_DEVICE f32x16_t scalar_load16(const float* p) {
-  f32x16_t v;
-  asm volatile("s_load_dwordx16 %0, %1, 0x0\n\ts_waitcnt lgkmcnt(0)" : "=s"(v) : "s"(p));
-  return v;
 }
 // This wave's LDS reads are done; then the barrier.
 FD_DEVICE void wait_reads_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
@@ -250,55 +248,71 @@ FD_DEVICE void wait_barrier(int more) {
       : "memory", "scc");
 }
 
-// A lane's 64 columns of one row to memory (cols of them lie inside N).  Every store issues whatever the row,
-// rows and columns outside go nowhere: the waits count the stores.
+// 32 rows x 128 columns to memory: acc[j][r] is row 8 (r >> 2) + 4 half + (r & 3) and column 4 l32 + j, so that
+// 32 lanes store one row's 128 columns side by side (with rows spread over the lanes, 16 bytes of 64 rows a store,
+// the L2 took 19 us for the 32 MB of a round of tiles).  Every store issues whatever the row, rows and columns
+// outside go nowhere: the waits count the stores.  rows: how many rows from the first on lie inside; off: byte
+// offset of the first row's columns of this lane; pitch: bytes of a row.
 template <int KIND>
-struct Row64 {
-  static constexpr int STORES = KIND == kToCodes ? 5 : KIND == kToBf16 ? 8 : 16;
+struct Rows32 {
+  static constexpr int STORES = KIND == kToCodes ? 17 : 16;
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-  static FD_DEVICE void put(const u32x4& v, __amdgpu_buffer_rsrc_t y, bool ok, uint32_t off) {
-    __builtin_amdgcn_raw_buffer_store_b128(v, y, ok ? off : kNowhere, 0, 0);
+
+  // The largest of each of 16 rows over the 32 lanes of a half, row r's in the lanes with l32 % 16 == r: at each
+  // level a lane hands its partner (mirrored within 16, 8, 4, 2) the half of the rows that the partner keeps.
+  template <int CTRL>
+  static FD_DEVICE uint32_t level(uint32_t low, uint32_t high, bool up) {
+    const uint32_t give = up ? low : high, keep = up ? high : low;
+    return max(keep, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(give), CTRL, 0xf, 0xf, true)));
   }
-  static FD_DEVICE void store(f32x16_t (&v)[4], bool gelu, bool row_ok, int cols, uint32_t row_off, int half, __amdgpu_buffer_rsrc_t y,
-                              __amdgpu_buffer_rsrc_t scale, uint32_t scale_off) {
+  static FD_DEVICE uint32_t row_tops(uint32_t (&t)[16], int l32) {
+#pragma unroll
+    for (int r = 0; r < 8; ++r) t[r] = level<0x140>(t[r], t[r + 8], l32 & 8);   // row_mirror
+#pragma unroll
+    for (int r = 0; r < 4; ++r) t[r] = level<0x141>(t[r], t[r + 4], l32 & 4);   // row_half_mirror
+#pragma unroll
+    for (int r = 0; r < 2; ++r) t[r] = level<0x1b>(t[r], t[r + 2], l32 & 2);    // quad_perm 3 2 1 0
+    const uint32_t top = level<0xb1>(t[0], t[1], l32 & 1);                      // quad_perm 1 0 3 2
+    return max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 16, fd::kWave)));
+  }
+  template <int R>
+  static FD_DEVICE void put_codes(const f32x16_t (&v)[4], float inv, __amdgpu_buffer_rsrc_t y, bool col_ok, int half, int rows,
+                                  uint32_t off, uint32_t pitch) {
+    const float x = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(inv), 0x150 + R, 0xf, 0xf, true));   // row_newbcast
+    const uint32_t w = fd::pack_codes(v[0][R] * x, v[1][R] * x, v[2][R] * x, v[3][R] * x);
+    constexpr int row = 8 * (R >> 2) + (R & 3);
+    __builtin_amdgcn_raw_buffer_store_b32(w, y, col_ok && row + 4 * half < rows ? off : kNowhere, row * pitch, 0);
+    if constexpr (R < 15) put_codes<R + 1>(v, inv, y, col_ok, half, rows, off, pitch);
+  }
+  static FD_DEVICE void store(f32x16_t (&v)[4], const float4 bias, bool gelu, __amdgpu_buffer_rsrc_t y, bool col_ok, int l32, int half,
+                              int rows, uint32_t off, uint32_t pitch, __amdgpu_buffer_rsrc_t scale, uint32_t scale_off, uint32_t scale_pitch) {
+    v[0] += bias.x; v[1] += bias.y; v[2] += bias.z; v[3] += bias.w;
     if (gelu) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v[j][e] = fd::gelu_tanh_fast(v[j][e]);
+        for (int r = 0; r < 16; ++r) v[j][r] = fd::gelu_tanh_fast(v[j][r]);
     }
     if constexpr (KIND == kToCodes) {
-      uint32_t top = 0;
+      uint32_t t[16];
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) top = 16 * j < cols ? max(top, fd::mag_bits(v[j][e])) : top;
-      top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 32, fd::kWave)));
-      const uint32_t s = fd::scale_byte(top);
-      const float inv = fd::scale_inverse(s);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        u32x4 w;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = fd::pack_codes(v[j][4 * i] * inv, v[j][4 * i + 1] * inv, v[j][4 * i + 2] * inv, v[j][4 * i + 3] * inv);
-        put(w, y, row_ok && 16 * j < cols, row_off + 16 * j);
-      }
-      __builtin_amdgcn_raw_buffer_store_b8(static_cast<uint8_t>(s), scale, row_ok && half == 0 && cols > 0 ? scale_off : kNowhere, 0, 0);
-    } else if constexpr (KIND == kToBf16) {
-#pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        u32x4 w;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = fd::pack_bf2(v[c >> 1][8 * (c & 1) + 2 * i], v[c >> 1][8 * (c & 1) + 2 * i + 1]);
-        put(w, y, row_ok && 8 * c < cols, row_off + 16 * c);
-      }
+      for (int r = 0; r < 16; ++r)
+        t[r] = col_ok ? max(max(fd::mag_bits(v[0][r]), fd::mag_bits(v[1][r])), max(fd::mag_bits(v[2][r]), fd::mag_bits(v[3][r]))) : 0u;
+      const uint32_t s = fd::scale_byte(row_tops(t, l32));
+      const int row = 8 * ((l32 >> 2) & 3) + 4 * half + (l32 & 3);
+      __builtin_amdgcn_raw_buffer_store_b8(static_cast<uint8_t>(s), scale, l32 < 16 && row < rows ? scale_off + row * scale_pitch : kNowhere, 0, 0);
+      put_codes<0>(v, fd::scale_inverse(s), y, col_ok, half, rows, off, pitch);
     } else {
 #pragma unroll
-      for (int c = 0; c < 16; ++c) {
-        u32x4 w;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[c >> 2][4 * (c & 3) + i]);
-        put(w, y, row_ok && 4 * c < cols, row_off + 16 * c);
+      for (int r = 0; r < 16; ++r) {
+        const int row = 8 * (r >> 2) + (r & 3);
+        const uint32_t to = col_ok && row + 4 * half < rows ? off : kNowhere;
+        if constexpr (KIND == kToBf16)
+          __builtin_amdgcn_raw_buffer_store_b64(u32x2{fd::pack_bf2(v[0][r], v[1][r]), fd::pack_bf2(v[2][r], v[3][r])}, y, to, row * pitch, 0);
+        else
+          __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(v[0][r]), __float_as_uint(v[1][r]), __float_as_uint(v[2][r]), __float_as_uint(v[3][r])},
+                                                 y, to, row * pitch, 0);
       }
     }
   }
@@ -318,7 +332,7 @@ template <class T, int KIND, class Mma>
 FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
   constexpr int FI = T::FI, STAGES = T::STAGES;
   constexpr int kSize = KIND == kToCodes ? 1 : KIND == kToBf16 ? 2 : 4;
-  constexpr int kStores = FI * Row64<KIND>::STORES;
+  constexpr int kStores = FI * Rows32<KIND>::STORES;
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / T::WN, wn = wave % T::WN;
   const int K = g.K, nk = (K + kScaleBlock - 1) / kScaleBlock, ld = fd::scale_stride(K);
@@ -342,17 +356,17 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
   int u = blockIdx.x, lk = 0, lm0, ln0;
   if (!tile_at(u, lm0, ln0)) return;
   i32x4_t ra, rw, rside;
+  int turn = 3;
   uint32_t off_a[T::LOADS_A], off_w[T::LOADS_W], off_side;
   auto row_of = [&](int q) { return (wave + T::WAVES * q) * 8 + (lane >> 3); };
-  auto chunk_a = [&](int q) { return (lane & 7) ^ T::swz_a(row_of(q)); };
-  auto chunk_w = [&](int q) { return (lane & 7) ^ T::swz_w(row_of(q)); };
+  auto chunk_of = [&](int q) { return (lane & 7) ^ T::swz(row_of(q)); };
   auto aim = [&] {   // the tile's bases, and this lane's row and chunk of each load (rows past the end re-read the last)
     ra = buffer_of(g.a + static_cast<size_t>(lm0) * K);
     rw = buffer_of(g.w + static_cast<size_t>(ln0) * K);
 #pragma unroll
-    for (int q = 0; q < T::LOADS_A; ++q) off_a[q] = static_cast<uint32_t>(min(row_of(q), M - lm0 - 1)) * static_cast<uint32_t>(K) + 16 * chunk_a(q);
+    for (int q = 0; q < T::LOADS_A; ++q) off_a[q] = static_cast<uint32_t>(min(row_of(q), M - lm0 - 1)) * static_cast<uint32_t>(K) + 16 * chunk_of(q);
 #pragma unroll
-    for (int q = 0; q < T::LOADS_W; ++q) off_w[q] = static_cast<uint32_t>(min(row_of(q), g.N - ln0 - 1)) * static_cast<uint32_t>(K) + 16 * chunk_w(q);
+    for (int q = 0; q < T::LOADS_W; ++q) off_w[q] = static_cast<uint32_t>(min(T::column(row_of(q)), g.N - ln0 - 1)) * static_cast<uint32_t>(K) + 16 * chunk_of(q);
     if (wave < T::BM / 64) {
       rside = buffer_of(g.a_scale + static_cast<size_t>(lm0) * ld);
       off_side = static_cast<uint32_t>(min(64 * wave + lane, M - lm0 - 1)) * static_cast<uint32_t>(ld);
@@ -360,16 +374,22 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
       rside = buffer_of(g.w_scale + static_cast<size_t>(ln0 / kScaleBlock) * ld);
       off_side = static_cast<uint32_t>(min(lane % T::WN, (g.N - ln0 - 1) / kScaleBlock) * ld);
     }
+    // the columns' bias (zeros without one), ahead of the tile's first stage.  The tile before this one has
+    // yet to read its own, and with STAGES blocks no barrier has passed since the one before that did: four slots.
+    turn = (turn + 1) & 3;
+    const int c = 64 * (wave % (T::BN / 64));
+    dma4(ring_at + static_cast<uint32_t>(T::BIAS * 16 + turn * T::BN * 4 + c * 4), static_cast<uint32_t>(ln0 + c + lane) * 4,
+         buffer_of(g.bias, g.bias ? 4u * g.N : 0u), 0);
   };
   // Load q of the rows and of the columns into a slot, and the scales.  The chunks past K of a last,
   // shorter K-block read zeros.
   auto issue_a = [&](int slot, int q) {
     const uint32_t at = ring_at + static_cast<uint32_t>(slot * T::CHUNKS * 16 + wave * 1024);
-    dma16(at + T::WAVES * q * 1024, lk * kScaleBlock + 16 * chunk_a(q) < K ? off_a[q] : kNowhere, ra, static_cast<uint32_t>(lk * kScaleBlock));
+    dma16(at + T::WAVES * q * 1024, lk * kScaleBlock + 16 * chunk_of(q) < K ? off_a[q] : kNowhere, ra, static_cast<uint32_t>(lk * kScaleBlock));
   };
   auto issue_w = [&](int slot, int q) {
     const uint32_t at = ring_at + static_cast<uint32_t>(slot * T::CHUNKS * 16 + T::BM * 128 + wave * 1024);
-    dma16(at + T::WAVES * q * 1024, lk * kScaleBlock + 16 * chunk_w(q) < K ? off_w[q] : kNowhere, rw, static_cast<uint32_t>(lk * kScaleBlock));
+    dma16(at + T::WAVES * q * 1024, lk * kScaleBlock + 16 * chunk_of(q) < K ? off_w[q] : kNowhere, rw, static_cast<uint32_t>(lk * kScaleBlock));
   };
   auto issue_scales = [&](int slot) {
     dma4(ring_at + static_cast<uint32_t>(slot * T::CHUNKS * 16 + T::SIDE * 16 + min(wave, T::BM / 64) * 256), off_side, rside, static_cast<uint32_t>(lk & ~3));
@@ -377,7 +397,7 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
 
   // ---- the products
   const int arow = 32 * FI * wm + l32;
-  const int wrow = 128 * wn + 64 * ((l32 >> 2) & 1) + 4 * (l32 >> 3) + (l32 & 3);   // of fragment 0: a lane's columns run over 64
+  const int wrow = 128 * wn + l32;
   auto read = [&](const uint4* sm, int row, int swz, int kh) {
     const int c = 4 * kh + 2 * half;
     const uint4 lo = sm[row * 8 + (c ^ swz)], hi = sm[row * 8 + ((c + 1) ^ swz)];
@@ -388,10 +408,10 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
   uint32_t sa[FI], sw, sa_next[FI], sw_next;
   auto read_a = [&](const uint4* sm, int kh) {
 #pragma unroll
-    for (int i = 0; i < FI; ++i) a[kh][i] = read(sm, arow + 32 * i, T::swz_a(arow), kh);   // 32 i leaves the swizzle
+    for (int i = 0; i < FI; ++i) a[kh][i] = read(sm, arow + 32 * i, T::swz(arow), kh);   // 32 i leaves the swizzle
   };
   auto read_w = [&](const uint4* sm, int s) {
-    w[s & 3] = read(sm + T::BM * 8, wrow + 16 * (s & 3), T::swz_w(wrow), s >> 2);   // so does 16 j
+    w[s & 3] = read(sm + T::BM * 8, wrow + 32 * (s & 3), T::swz(wrow), s >> 2);
   };
   auto read_scales = [&](const uint4* sm, int kb) {
     const uint32_t* side = reinterpret_cast<const uint32_t*>(sm + T::SIDE);
@@ -450,7 +470,7 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
           if (s == 7) read_w(sn, 1);
           const typename Mma::frag wf = Mma::make(w[s & 3], sw);
 #pragma unroll
-          for (int i = 0; i < FI; ++i) acc[i][s & 3] = Mma::mma(wf, Mma::make(a[s >> 2][i], sa[i]), acc[i][s & 3], sw, sa[i]);
+          for (int i = 0; i < FI; ++i) acc[i][s & 3] = Mma::mma(Mma::make(a[s >> 2][i], sa[i]), wf, acc[i][s & 3], sa[i], sw);
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int q = 0; q < T::LOADS_A; ++q)
@@ -466,36 +486,24 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
       }
     }
 
-    // the tile's results: lane (l32, half) holds row l32 of each 32 and columns 64 half .. + 63
     stored = 1;
-    const int col = n0 + 128 * wn + 64 * half;
+    const int col = 128 * wn + 4 * l32;   // this lane's first column of the tile
+    const bool col_ok = n0 + col < g.N;
+    const float4 bias = reinterpret_cast<const float4*>(ring + T::BIAS + (turn - (more ? 1 : 0) & 3) * (T::BN / 4))[col / 4];
     void* base;
     if constexpr (KIND == kToCodes) base = g.y_q;
     else if constexpr (KIND == kToBf16) base = g.y_bf16;
     else base = g.y_f32;
-    const auto y = __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t*>(base) + (static_cast<size_t>(m0) * g.N + n0) * kSize, 0, 0x7fffffff, 0x00020000);
-    const int lds_y = fd::scale_stride(g.N);
-    const auto ys = __builtin_amdgcn_make_buffer_rsrc(g.y_scale + static_cast<size_t>(m0) * lds_y, 0, 0x7fffffff, 0x00020000);
-    if (g.bias) {
-      // the columns' bias through the scalar cache, 16 at a time and half, so that no vector load waits behind the stages' loads
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const f32x16_t b0 = scalar_load16(g.bias + min(__builtin_amdgcn_readfirstlane(n0) + 128 * wn + 16 * j, g.N - 16));
-        const f32x16_t b1 = scalar_load16(g.bias + min(__builtin_amdgcn_readfirstlane(n0) + 128 * wn + 64 + 16 * j, g.N - 16));
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float b = half ? b1[e] : b0[e];
-#pragma unroll
-          for (int i = 0; i < FI; ++i) acc[i][j][e] += b;
-        }
-      }
-    }
+    const int row0 = 32 * FI * wm, lds_y = fd::scale_stride(g.N);
+    const auto y = __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t*>(base) + (static_cast<size_t>(m0 + row0) * g.N + n0) * kSize, 0, 0x7fffffff, 0x00020000);
+    const auto ys = __builtin_amdgcn_make_buffer_rsrc(g.y_scale + static_cast<size_t>(m0 + row0) * lds_y + n0 / kScaleBlock + wn, 0, 0x7fffffff, 0x00020000);
 #pragma unroll
     for (int i = 0; i < FI; ++i) {
-      const int r = arow + 32 * i;
-      Row64<KIND>::store(acc[i], g.gelu, m0 + r < M, g.N - col, static_cast<uint32_t>(r * g.N + col - n0) * kSize, half, y, ys,
-                         static_cast<uint32_t>(r * lds_y + col / kScaleBlock));
-      __builtin_amdgcn_sched_barrier(0);
+      const bool block_ok = n0 + 128 * wn < g.N;   // else no column of this wave
+      Rows32<KIND>::store(acc[i], bias, g.gelu, y, col_ok, l32, half, block_ok ? M - m0 - row0 - 32 * i : 0,
+                          static_cast<uint32_t>((32 * i + 4 * half) * g.N + col) * kSize, static_cast<uint32_t>(g.N) * kSize, ys,
+                          static_cast<uint32_t>(32 * i * lds_y), static_cast<uint32_t>(lds_y));
+      __builtin_amdgcn_sched_barrier(0);   // 32 rows at a time: fewer registers
     }
     if (!more) break;
     u += gridDim.x;
