@@ -55,6 +55,13 @@ FD_DEVICE uint32_t quant_lane8(const float (&v)[8], uint2& codes) {
   return s;
 }
 
+// GELU, tanh form: z / (1 + 2^-t), t = 2 sqrt(2 / pi) log2(e) (z + 0.044715 z^3), in seven instructions with the
+// hardware's exponent and reciprocal (an ulp each).
+FD_DEVICE float gelu(float z) {
+  const float t = z * fmaf(z * z, -0.10294324f, -2.3022082f);
+  return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t));
+}
+
 FD_DEVICE void unpack_bf8(const uint4 x, float (&v)[8]) {
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll

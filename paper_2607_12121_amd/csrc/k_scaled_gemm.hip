@@ -3,11 +3,10 @@
 // on v_mfma_scale_f32_16x16x128_f8f6f4, whose K is one block: the scale bytes are operands of the
 // instruction and the sum is kept in fp32 accumulators.
 //
-#include <stdlib.h>
-
 #include <type_traits>
 
 #include "fd_scaled.h"
+#include "fd_scaled_rules.h"
 
 namespace {
 
@@ -86,7 +85,7 @@ FD_DEVICE void store_row(const fdh::ScaledArgs& g, bool row_ok, int row, int col
   }
   if (g.gelu) {
 #pragma unroll
-    for (int e = 0; e < 4 * NF; ++e) v[e] = fd::gelu_tanh_fast(v[e]);
+    for (int e = 0; e < 4 * NF; ++e) v[e] = fd::gelu(v[e]);
   }
   const size_t at = static_cast<size_t>(row) * g.N + col;
   if constexpr (KIND == kToCodes) {
@@ -127,63 +126,80 @@ FD_DEVICE void store_row(const fdh::ScaledArgs& g, bool row_ok, int row, int col
   }
 }
 
-// 32 bytes at p + k of a row of K bytes, zeros past its end (K is a multiple of 16).
+// 32 bytes at p + k of a row of K bytes, zeros past its end (K is a multiple of 16).  The loads go to the row's last
+// 16 bytes there, so that none waits for a branch.
 FD_DEVICE i32x8_t load32(const uint8_t* p, int k, int K) {
-  const uint4 z = make_uint4(0, 0, 0, 0);
-  const uint4 lo = k < K ? *reinterpret_cast<const uint4*>(p + k) : z, hi = k + 16 < K ? *reinterpret_cast<const uint4*>(p + k + 16) : z;
+  uint4 lo = *reinterpret_cast<const uint4*>(p + min(k, K - 16)), hi = *reinterpret_cast<const uint4*>(p + min(k + 16, K - 16));
+  if (k >= K) lo = make_uint4(0, 0, 0, 0);
+  if (k + 16 >= K) hi = make_uint4(0, 0, 0, 0);
   return i32x8_t{static_cast<int>(lo.x), static_cast<int>(lo.y), static_cast<int>(lo.z), static_cast<int>(lo.w),
                  static_cast<int>(hi.x), static_cast<int>(hi.y), static_cast<int>(hi.z), static_cast<int>(hi.w)};
 }
 
 // ---------------------------------------------------------------- few rows
 
-// Up to FM * 16 rows: the weights are read once and are all there is to read.  A workgroup takes the
-// rows' FM fragments and 16 NF columns, its waves the K-blocks in turn, operands straight from memory
-// into registers; the waves' sums meet in LDS.
+// Up to 64 rows: the weights are read once and are nearly all there is to read, so what counts is how many of their
+// bytes are on the way.  A workgroup takes the rows' FM fragments and 16 NF columns, its waves the K-blocks in turn,
+// operands straight from memory into registers, DEEP blocks at a time; the waves' sums meet in LDS.
 constexpr int kFewWaves = 8;
 
-template <int KIND, class Mma, int FM, int NF>
+template <int KIND, class Mma, int FM, int NF, int DEEP>
 __global__ __launch_bounds__(kFewWaves * 64) void scaled_few_kernel(fdh::ScaledArgs g) {
-  __shared__ f32x4_t part[kFewWaves][FM * NF][64];
+  __shared__ f32x4_t part[kFewWaves][FM][NF][64];
   const int M = g.m ? min(*g.m, g.n_rows) : g.n_rows;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, lg = lane >> 4;
-  const int nk = (g.K + kScaleBlock - 1) / kScaleBlock, ld = fd::scale_stride(g.K);
+  const int K = g.K, nk = (K + kScaleBlock - 1) / kScaleBlock, ld = fd::scale_stride(K);
   const int n0 = blockIdx.x * 16 * NF;
   const uint8_t* sw = g.w_scale + static_cast<size_t>(n0 / kScaleBlock) * ld;
   const uint8_t* w[NF];
 #pragma unroll
   for (int j = 0; j < NF; ++j)
-    w[j] = g.w + static_cast<size_t>(min(n0 + 4 * NF * (l16 >> 2) + 4 * j + (l16 & 3), g.N - 1)) * g.K;
+    w[j] = g.w + static_cast<size_t>(min(n0 + 4 * NF * (l16 >> 2) + 4 * j + (l16 & 3), g.N - 1)) * K;
   for (int m0 = blockIdx.y * 16 * FM; m0 < M; m0 += gridDim.y * 16 * FM) {
     f32x4_t acc[FM][NF] = {};
-    for (int kb = wave; kb < nk; kb += kFewWaves) {
-      const int k = kb * kScaleBlock + 32 * lg;
-      typename Mma::frag wf[NF];
+    for (int kb = wave; kb < nk; kb += kFewWaves * DEEP) {
+      i32x8_t wf[DEEP][NF], af[DEEP][FM];
+      uint32_t s_w[DEEP], s_a[DEEP][FM];
 #pragma unroll
-      for (int j = 0; j < NF; ++j) wf[j] = Mma::make(load32(w[j], k, g.K), sw[kb]);
+      for (int d = 0; d < DEEP; ++d) {   // blocks past the last: zeros
+        const int b = kb + d * kFewWaves, k = b < nk ? b * kScaleBlock + 32 * lg : K, c = min(b, nk - 1);
 #pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        const size_t r = min(m0 + 16 * i + l16, M - 1);
-        const uint32_t sa = g.a_scale[r * ld + kb];
-        const typename Mma::frag af = Mma::make(load32(g.a + r * g.K, k, g.K), sa);
+        for (int j = 0; j < NF; ++j) wf[d][j] = load32(w[j], k, K);
+        s_w[d] = sw[c];
 #pragma unroll
-        for (int j = 0; j < NF; ++j) acc[i][j] = Mma::mma(wf[j], af, acc[i][j], sw[kb], sa);
+        for (int i = 0; i < FM; ++i) {
+          const size_t row = min(m0 + 16 * i + l16, M - 1);
+          af[d][i] = load32(g.a + row * K, k, K);
+          s_a[d][i] = g.a_scale[row * ld + c];
+        }
+      }
+#pragma unroll
+      for (int d = 0; d < DEEP; ++d) {
+        typename Mma::frag wd[NF];
+#pragma unroll
+        for (int j = 0; j < NF; ++j) wd[j] = Mma::make(wf[d][j], s_w[d]);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+          const typename Mma::frag ad = Mma::make(af[d][i], s_a[d][i]);
+#pragma unroll
+          for (int j = 0; j < NF; ++j) acc[i][j] = Mma::mma(wd[j], ad, acc[i][j], s_w[d], s_a[d][i]);
+        }
       }
     }
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
-      for (int j = 0; j < NF; ++j) part[wave][i * NF + j][lane] = acc[i][j];
+      for (int j = 0; j < NF; ++j) part[wave][i][j][lane] = acc[i][j];
     __syncthreads();
-    for (int i = wave; i < FM; i += kFewWaves) {   // a wave per 16 rows adds the waves' sums in order
+    if (wave < FM) {   // a wave per 16 rows adds the waves' sums in order
       f32x4_t sum[NF];
 #pragma unroll
       for (int j = 0; j < NF; ++j) {
-        sum[j] = part[0][i * NF + j][lane];
+        sum[j] = part[0][wave][j][lane];
 #pragma unroll
-        for (int p = 1; p < kFewWaves; ++p) sum[j] += part[p][i * NF + j][lane];
+        for (int p = 1; p < kFewWaves; ++p) sum[j] += part[p][wave][j][lane];
       }
-      const int row = m0 + 16 * i + l16;
+      const int row = m0 + 16 * wave + l16;
       store_row<KIND, NF>(g, row < M, row, n0 + 4 * NF * lg, sum);
     }
     __syncthreads();
@@ -292,7 +308,7 @@ struct Rows32 {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) v[j][r] = fd::gelu_tanh_fast(v[j][r]);
+        for (int r = 0; r < 16; ++r) v[j][r] = fd::gelu(v[j][r]);
     }
     if constexpr (KIND == kToCodes) {
       uint32_t t[16];
@@ -511,16 +527,17 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the repeats of the last stage
 }
 
-using TileLarge = Tile<2, 4, 2, 2>;   // 256 x 256
-using TileMid = Tile<1, 4, 2, 3>;     // 128 x 256
-using TileSmall = Tile<1, 4, 1, 2>;   // 128 x 128, two workgroups per CU
+using TileLarge = Tile<2, 4, 2, 2>;   // 256 x 256, one workgroup per CU
+using TileSmall = Tile<1, 4, 1, 2>;   // 128 x 128, two
 
+// Where both kernels are launched (cus > 0), the one that the row count does not call for ends at once.
 template <int KIND, class Mma, class T, int PER_CU>
-__global__ __launch_bounds__(T::THREADS, PER_CU * T::WAVES / 4) void scaled_tile_kernel(fdh::ScaledArgs g) {
+__global__ __launch_bounds__(T::THREADS, PER_CU * T::WAVES / 4) void scaled_tile_kernel(fdh::ScaledArgs g, int cus) {
   __shared__ uint4 ring[T::TOTAL];
-  static_assert(T::TOTAL * 16 * PER_CU <= 160 * 1024, "the LDS of a CU");
+  static_assert(T::TOTAL * 16 * PER_CU <= 160 * 1024 && T::STAGES <= fd::kTileBlocks, "the LDS of a CU");
   const int M = g.m ? min(*g.m, g.n_rows) : g.n_rows;
-  if (M > 0) scaled_tiles<T, KIND, Mma>(g, M, ring);
+  if (M <= 0 || (cus > 0 && fd::scaled_large(M, g.N, g.K, KIND == kToCodes, cus) != (PER_CU == 1))) return;
+  scaled_tiles<T, KIND, Mma>(g, M, ring);
 }
 
 }  // namespace
@@ -531,18 +548,25 @@ hipError_t launch_scaled_linear(const ScaledArgs& g, hipStream_t s) {
   auto run = [&](auto kind, auto mma) {
     constexpr int KIND = decltype(kind)::value;
     using Mma = decltype(mma);
-    if (g.n_rows <= 64 || g.K <= 2 * kScaleBlock) {   // the tiles' loads run up to three blocks ahead
-      constexpr int NF = KIND == kToCodes ? 8 : 1;
-      const int gx = (g.N + 16 * NF - 1) / (16 * NF);
-      if (g.n_rows <= 16) scaled_few_kernel<KIND, Mma, 1, NF><<<dim3(gx, 1), kFewWaves * 64, 0, s>>>(g);
-      else scaled_few_kernel<KIND, Mma, 2, NF><<<dim3(gx, min((g.n_rows + 31) / 32, 4096)), kFewWaves * 64, 0, s>>>(g);
+    constexpr bool codes = KIND == kToCodes;
+    if (g.n_rows <= fd::scaled_few_rows(codes) || g.K <= (fd::kTileBlocks - 1) * kScaleBlock) {
+      auto few = [&](auto fm, auto nf, auto deep) {
+        constexpr int FM = decltype(fm)::value, NF = decltype(nf)::value;
+        const int gx = (g.N + 16 * NF - 1) / (16 * NF), gy = (g.n_rows + 16 * FM - 1) / (16 * FM);
+        scaled_few_kernel<KIND, Mma, FM, NF, decltype(deep)::value><<<dim3(gx, gy < 4096 ? gy : 4096), kFewWaves * 64, 0, s>>>(g);
+      };
+      using std::integral_constant;
+      if constexpr (codes) few(integral_constant<int, 1>{}, integral_constant<int, 8>{}, integral_constant<int, 2>{});
+      else if (g.n_rows <= 16) few(integral_constant<int, 1>{}, integral_constant<int, 1>{}, integral_constant<int, 6>{});
+      else few(integral_constant<int, 4>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{});
       return;
     }
-    const char* e = getenv("FD_SHAPE");
-    const int shape = e ? atoi(e) : 0, cus = num_cus() / 8 * 8;
-    if (shape == 0) scaled_tile_kernel<KIND, Mma, TileLarge, 1><<<cus, TileLarge::THREADS, 0, s>>>(g);
-    else if (shape == 1) scaled_tile_kernel<KIND, Mma, TileMid, 1><<<cus, TileMid::THREADS, 0, s>>>(g);
-    else scaled_tile_kernel<KIND, Mma, TileSmall, 2><<<2 * cus, TileSmall::THREADS, 0, s>>>(g);
+    const int cus = num_cus() / 8 * 8;   // the tile order counts on whole rounds of the 8 XCDs
+    const bool both = g.m && fd::scaled_both(g.n_rows, g.N, g.K, codes, cus), large = !g.m && fd::scaled_large(g.n_rows, g.N, g.K, codes, cus);
+    const long long tiles = static_cast<long long>((g.n_rows + 127) / 128) * ((g.N + 127) / 128);
+    const int grid = static_cast<int>(tiles < 2 * cus ? (tiles + 7) / 8 * 8 : 2 * cus);
+    if (!large) scaled_tile_kernel<KIND, Mma, TileSmall, 2><<<grid, TileSmall::THREADS, 0, s>>>(g, both ? cus : 0);
+    if (both || large) scaled_tile_kernel<KIND, Mma, TileLarge, 1><<<cus, TileLarge::THREADS, 0, s>>>(g, both ? cus : 0);
   };
   if (g.y_q) run(std::integral_constant<int, kToCodes>{}, Mma8{});
   else if (g.y_bf16) run(std::integral_constant<int, kToBf16>{}, Mma8{});

@@ -408,7 +408,7 @@ def partition(saliency: torch.Tensor, req_tok_off, req_reg_off, stream=None) -> 
 
 def fd_scale_stride(cols: int) -> int:
     """Bytes of a row of block scales: ceil(cols / 128) rounded up to a multiple of 4."""
-    return int(lib().fd_scale_stride(cols))
+    return lib().fd_scale_stride(cols)
 
 
 def _rows(name: str, t: torch.Tensor) -> Sequence[int]:
@@ -417,12 +417,38 @@ def _rows(name: str, t: torch.Tensor) -> Sequence[int]:
     return t.shape
 
 
-def _same_device(**tensors: Optional[torch.Tensor]) -> None:
-    """Every tensor of a call on the current device, whose stream the call runs on."""
-    cur = torch.cuda.current_device()
-    for name, t in tensors.items():
-        if t is not None and t.device.index != cur:
-            raise FlashDiffError(f"{name} is on {t.device}, the current device is {cur}")
+_KIND = {k: frozenset(v) for k, v in _DT.items() if v is not None}
+
+
+def _pointers(stream: Optional[torch.cuda.Stream], *args) -> list:
+    """Checks (name, tensor, kind, elements) tuples as _need does, and that every tensor and the stream are on
+    the current device, the one the call runs on; returns the tensors' addresses and the stream's handle.  One
+    pass of cheap tests, as these calls take microseconds on the GPU; what fails is named by the slow path.
+    An element count below 0 marks an optional tensor of minus that many elements."""
+    cur = None
+    out = []
+    for name, t, kind, n in args:
+        if t is None:
+            if n >= 0:
+                raise FlashDiffError(f"{name} is required")
+            out.append(None)
+            continue
+        if cur is None:
+            if not t.is_cuda:
+                _need(name, t, kind, abs(n))
+            cur = torch.cuda.current_device()
+        if t.get_device() != cur or t.dtype not in _KIND[kind] or t.numel() < abs(n) or not t.is_contiguous():
+            _need(name, t, kind, abs(n))
+            if t.get_device() != cur:
+                raise FlashDiffError(f"{name} is on {t.device}, the current device is {cur}")
+            _ptr(t)
+        out.append(t.data_ptr())
+    if stream is None:
+        stream = torch.cuda.current_stream()
+    elif stream.device.index != cur:
+        raise FlashDiffError(f"the stream is on {stream.device}, the current device is {cur}")
+    out.append(stream.cuda_stream)
+    return out
 
 
 def fd_quant_blocks(x, block_rows: int, q, scale, m=None, stream=None) -> None:
@@ -430,13 +456,9 @@ def fd_quant_blocks(x, block_rows: int, q, scale, m=None, stream=None) -> None:
     [ceil(rows / block_rows), fd_scale_stride(cols)]; block_rows 1 (activations, `m` of
     the rows when given) or 128 (weights)."""
     rows, cols = _rows("x", x)
-    _need("x", x, "b16", rows * cols)
-    _need("q", q, "code", rows * cols)
-    _need("scale", scale, "scale", -(-rows // max(block_rows, 1)) * fd_scale_stride(cols))
-    _need("m", m, "i32", 1, optional=True)
-    _same_device(x=x, q=q, scale=scale, m=m)
-    _check("fd_quant_blocks", lib().fd_quant_blocks(rows, cols, block_rows, _ptr(x), _ptr(m), _ptr(q), _ptr(scale),
-                                                    _stream(stream)))
+    p = _pointers(stream, ("x", x, "b16", rows * cols), ("m", m, "i32", -1), ("q", q, "code", rows * cols),
+                  ("scale", scale, "scale", -(-rows // max(block_rows, 1)) * fd_scale_stride(cols)))
+    _check("fd_quant_blocks", lib().fd_quant_blocks(rows, cols, block_rows, *p))
 
 
 def fd_rms_quant(h, q, scale, cu_q, m, y=None, gate=None, weight=None, shift=None, mod_scale=None, eps: float = 1e-6,
@@ -445,28 +467,24 @@ def fd_rms_quant(h, q, scale, cu_q, m, y=None, gate=None, weight=None, shift=Non
     [rows, D] and scale bytes [rows, fd_scale_stride(D)].  gate, shift and mod_scale: fp32 [requests, D],
     which may be column ranges of one modulation tensor (equal row strides)."""
     rows, D = _rows("h", h)
-    B = int(cu_q.numel()) - 1
-    _need("h", h, "f32", rows * D)
-    _need("y", y, "b16", rows * D, optional=True)
-    _need("weight", weight, "f32", D, optional=True)
-    _need("cu_q", cu_q, "i32", 2)
-    _need("m", m, "i32", 1)
-    _need("q", q, "code", rows * D)
-    _need("scale", scale, "scale", rows * fd_scale_stride(D))
-    stride = None
+    B = cu_q.numel() - 1
+    stride, mod = None, []
     for n_, t_ in (("gate", gate), ("shift", shift), ("mod_scale", mod_scale)):
         if t_ is None:
+            mod.append(None)
             continue
         _need(n_, t_, "f32", B * D)
-        if tuple(_rows(n_, t_)) != (B, D) or t_.stride(1) != 1:
-            raise FlashDiffError(f"{n_} must be [{B}, {D}] with contiguous rows")
+        if tuple(t_.shape) != (B, D) or t_.stride(1) != 1 or t_.device != h.device:
+            raise FlashDiffError(f"{n_} must be [{B}, {D}] with contiguous rows, on {h.device}")
         if stride is not None and t_.stride(0) != stride:
             raise FlashDiffError("gate, shift and mod_scale must have the same row stride")
         stride = t_.stride(0)
-    _same_device(h=h, y=y, gate=gate, weight=weight, shift=shift, mod_scale=mod_scale, cu_q=cu_q, m=m, q=q, scale=scale)
-    at = [None if t is None else t.data_ptr() for t in (gate, shift, mod_scale)]
-    _check("fd_rms_quant", lib().fd_rms_quant(rows, D, B, _ptr(h), _ptr(y), at[0], _ptr(weight), at[1], at[2], stride or 0,
-                                              eps, _ptr(cu_q), _ptr(m), _ptr(q), _ptr(scale), _stream(stream)))
+        mod.append(t_.data_ptr())
+    n = rows * D
+    h_, y_, w_, cu_, m_, q_, s_, st = _pointers(
+        stream, ("h", h, "f32", n), ("y", y, "b16", -n), ("weight", weight, "f32", -D), ("cu_q", cu_q, "i32", 2), ("m", m, "i32", 1),
+        ("q", q, "code", n), ("scale", scale, "scale", rows * fd_scale_stride(D)))
+    _check("fd_rms_quant", lib().fd_rms_quant(rows, D, B, h_, y_, mod[0], w_, mod[1], mod[2], stride or 0, eps, cu_, m_, q_, s_, st))
 
 
 def rope_axes(dims: Sequence[int], theta=10000.0, step=1.0, halves: bool = False) -> FdRope:
@@ -489,17 +507,13 @@ def fd_rope_axes(qkv, coord, idx, m, q, k_cache, v_cache, heads: int, kv_heads: 
     coord [tokens, axes]; q to [rows, heads head_dim], k and v to the caches' rows idx.  The axes
     are given by dims, theta, step and halves, or by a descriptor from rope_axes."""
     r = rope if rope is not None else rope_axes(dims, theta, step, halves)
-    rows, tokens = _rows("qkv", qkv)[0], _rows("coord", coord)[0]
-    _need("qkv", qkv, "b16", rows * (heads + 2 * kv_heads) * head_dim, exact=True)
-    _need("coord", coord, "i32", tokens * r.n_axes, exact=True)
-    _need("idx", idx, "i32", rows, optional=True)
-    _need("m", m, "i32", 1)
-    _need("q", q, "b16", rows * heads * head_dim)
-    _need("k_cache", k_cache, "b16", tokens * kv_heads * head_dim)
-    _need("v_cache", v_cache, "b16", tokens * kv_heads * head_dim)
-    _same_device(qkv=qkv, coord=coord, idx=idx, m=m, q=q, k_cache=k_cache, v_cache=v_cache)
-    _check("fd_rope_axes", lib().fd_rope_axes(rows, tokens, ctypes.byref(r), heads, kv_heads, head_dim, _ptr(coord), _ptr(qkv),
-                                              _ptr(idx), _ptr(m), _ptr(q), _ptr(k_cache), _ptr(v_cache), _stream(stream)))
+    (rows, cols), (tokens, axes) = _rows("qkv", qkv), _rows("coord", coord)
+    if cols != (heads + 2 * kv_heads) * head_dim or axes != r.n_axes:
+        raise FlashDiffError(f"qkv has {cols} columns and coord {axes} axes, needs {(heads + 2 * kv_heads) * head_dim} and {r.n_axes}")
+    kv = tokens * kv_heads * head_dim
+    p = _pointers(stream, ("coord", coord, "i32", tokens * axes), ("qkv", qkv, "b16", rows * cols), ("idx", idx, "i32", -rows),
+                  ("m", m, "i32", 1), ("q", q, "b16", rows * heads * head_dim), ("k_cache", k_cache, "b16", kv), ("v_cache", v_cache, "b16", kv))
+    _check("fd_rope_axes", lib().fd_rope_axes(rows, tokens, ctypes.byref(r), heads, kv_heads, head_dim, *p))
 
 
 def fd_scaled_linear(a, a_scale, w, w_scale, y, y_scale=None, bias=None, gelu: bool = False, m=None, stream=None) -> None:
@@ -508,21 +522,15 @@ def fd_scaled_linear(a, a_scale, w, w_scale, y, y_scale=None, bias=None, gelu: b
     (rows, k), (n, kw) = _rows("a", a), _rows("w", w)
     if k != kw:
         raise FlashDiffError(f"a has {k} columns, w {kw}")
-    codes = y.dtype in _DT["code"]
-    _need("a", a, "code", rows * k)
-    _need("a_scale", a_scale, "scale", rows * fd_scale_stride(k))
-    _need("w", w, "code", n * k)
-    _need("w_scale", w_scale, "scale", -(-n // 128) * fd_scale_stride(k))
-    _need("bias", bias, "f32", n, optional=True)
-    _need("m", m, "i32", 1, optional=True)
-    _need("y", y, "code" if codes else "f32" if y.dtype == torch.float32 else "b16", rows * n)
-    _need("y_scale", y_scale, "scale", rows * fd_scale_stride(n), optional=not codes)
-    _same_device(a=a, a_scale=a_scale, w=w, w_scale=w_scale, y=y, y_scale=y_scale, bias=bias, m=m)
-    out = _ptr(y)
-    _check("fd_scaled_linear", lib().fd_scaled_linear(
-        rows, n, k, _ptr(a), _ptr(a_scale), _ptr(w), _ptr(w_scale), _ptr(bias), int(gelu), _ptr(m),
-        None if codes or y.dtype == torch.float32 else out, out if y.dtype == torch.float32 else None, out if codes else None,
-        _ptr(y_scale) if codes else None, _stream(stream)))
+    codes, wide, ld = y.dtype in _KIND["code"], y.dtype == torch.float32, fd_scale_stride(k)
+    *ptrs, y_, ys_, st = _pointers(
+        stream, ("a", a, "code", rows * k), ("a_scale", a_scale, "scale", rows * ld), ("w", w, "code", n * k),
+        ("w_scale", w_scale, "scale", -(-n // 128) * ld), ("bias", bias, "f32", -n), ("m", m, "i32", -1),
+        ("y", y, "code" if codes else "f32" if wide else "b16", rows * n),
+        ("y_scale", y_scale if codes else None, "scale", rows * fd_scale_stride(n) if codes else -1))
+    a_, as_, w_, ws_, b_, m_ = ptrs
+    _check("fd_scaled_linear", lib().fd_scaled_linear(rows, n, k, a_, as_, w_, ws_, b_, int(gelu), m_, None if codes or wide else y_,
+                                                      y_ if wide else None, y_ if codes else None, ys_, st))
 
 
 def fd_timer_arm(kernel: str, capacity: int) -> None:

@@ -1,14 +1,18 @@
 """CPU tests of the 8-bit entry points: refusals before any launch, the scale stride, and the 64-bit
 reference against torch's e4m3 conversion."""
 import ctypes
+import os
+import subprocess
 
 import numpy as np
 import pytest
 import torch
 
 from oracle import scaled as ref
+from paper_2607_12121_amd import build
 from paper_2607_12121_amd import flashdiff as fdl
 from tests.test_abi import no_gpu
+from tests.test_isa_hazards import _hazards
 
 P = 0x1000
 
@@ -127,3 +131,35 @@ def test_bindings_refuse_host_tensors():
                  lambda: fdl.fd_scaled_linear(q, s, q, s, h)):
         with pytest.raises(fdl.FlashDiffError):
             call()
+
+
+def test_product_rules(tmp_path):
+    """The kernels of measured shapes, and that a call which launches both tile kernels can meet either row count."""
+    src = tmp_path / "r.cpp"
+    src.write_text('''
+#include <cstdio>
+#include "fd_scaled_rules.h"
+int main(int, char**) {
+  int n, N, K, c;
+  while (std::scanf("%d %d %d %d", &n, &N, &K, &c) == 4)
+    std::printf("%d %d %d\\n", fd::scaled_few_rows(c), (int)fd::scaled_large(n, N, K, c, 256), (int)fd::scaled_both(n, N, K, c, 256));
+}
+''')
+    exe = tmp_path / "r"
+    subprocess.run(["g++", "-std=c++17", f"-I{build.CSRC}", str(src), "-o", str(exe)], check=True)
+    cases = [((9828, 1536, 6144, 0), (64, 1, 1)), ((5000, 1536, 6144, 0), (64, 0, 0)), ((9828, 6144, 1536, 1), (16, 0, 0)),
+             ((32760, 1536, 6144, 0), (64, 1, 1)), ((9828, 1536, 1536, 0), (64, 1, 0)), ((1664, 1536, 6144, 0), (64, 0, 0)),
+             ((14280, 4096, 1024, 1), (16, 0, 0)), ((1, 64, 64, 0), (64, 0, 0)), ((1 << 30, 16, 16, 0), (64, 1, 1))]
+    out = subprocess.run([str(exe)], input="\n".join(" ".join(map(str, c)) for c, _ in cases), capture_output=True, text=True, check=True).stdout
+    for line, (case, want) in zip(out.splitlines(), cases):
+        assert tuple(map(int, line.split())) == want, case
+
+
+def test_no_vector_memory_read_of_a_fresh_scalar(tmp_path):
+    """The product's loads in inline assembly, searched as those of the bf16 products are."""
+    out = tmp_path / "k.s"
+    subprocess.run([build.hipcc(), *[f for f in build.HIPCC_FLAGS if f != "-Wall"], "--cuda-device-only", "-S",
+                    os.path.join(build.CSRC, "k_scaled_gemm.hip"), "-o", str(out)], check=True, capture_output=True)
+    seen, bad = _hazards(out.read_text().splitlines())
+    assert seen > 300
+    assert not bad, bad[:3]
