@@ -388,7 +388,7 @@ fd_status fd_quant_blocks(int32_t n_rows, int32_t cols, int32_t block_rows, cons
  * with b the row's request:
  *   h[i] += gate_b * y[i]                                    (only with y)
  *   a    = h[i] / sqrt(mean(h[i]^2) + eps) * weight * (1 + scale_b) + shift_b
- *   q, q_scale = a in codes, one scale per 128 columns
+ *   q, q_scale = a in codes, one scale per 128 columns; both null: only h's update
  * in fp32, a rounded once.  The squares are formed in fp32: rows whose magnitudes
  * exceed 2^63 overflow to a norm of zero.
  *   h      device fp32 [n_rows][D], 16-byte aligned, updated in place
@@ -455,6 +455,39 @@ fd_status fd_rope_axes(int32_t n_rows, int32_t n_tokens, const fd_rope* rope, in
 fd_status fd_scaled_linear(int32_t n_rows, int32_t n_out, int32_t n_in, const uint8_t* a, const uint8_t* a_scale,
                            const uint8_t* w, const uint8_t* w_scale, const float* bias, int32_t gelu, const int32_t* m,
                            uint16_t* y_bf, float* y_fp, uint8_t* y_q, uint8_t* y_scale, fd_stream_t stream);
+
+/* One DiT block's parameters in 8 bits (device).  w_* e4m3 [out][in] with s_* 128 x 128 scales
+ * (fd_quant_blocks, block_rows 128), b_* and norm_* fp32. */
+typedef struct fd_scaled_weights {
+  const uint8_t* w_qkv; const uint8_t* s_qkv; const float* b_qkv;   /* [3D][D]: q | k | v */
+  const uint8_t* w_o;   const uint8_t* s_o;   const float* b_o;     /* [D][D]             */
+  const uint8_t* w_1;   const uint8_t* s_1;   const float* b_1;     /* [F][D]             */
+  const uint8_t* w_2;   const uint8_t* s_2;   const float* b_2;     /* [D][F]             */
+  const float* norm_1;  const float* norm_2;  /* [D] weights of the two norms, or null (1) */
+  const float* mod;     /* [B][6D]: shift1|scale1|gate1|shift2|scale2|gate2, from fd_adaln */
+} fd_scaled_weights;
+
+/*
+ * One adaLN DiT block on the active rows with RMS norms, rotary positions and
+ * 8-bit products (fd_block_forward's place in a step for models of that form;
+ * Sec. 4 Backend), each step by the entry point above of its kind:
+ *   a = codes(RMS(h) * norm_1 * (1 + scale1) + shift1)            RMS: eps 1e-6
+ *   q | k | v = a W_qkv^T + b_qkv (bf16), turned; k, v to the caches' rows idx[i]
+ *   o = attention of q over every token of the request, as in fd_block_forward
+ *   h += gate1 * bf16(codes(o) W_o^T + b_o)
+ *   a = codes(RMS(h) * norm_2 * (1 + scale2) + shift2)
+ *   h += gate2 * bf16(codes(GELU_tanh(a W_1^T + b_1)) W_2^T + b_2)
+ *   rope   rotary descriptor, or null (q and k are not turned)
+ *   coord  device int32 [N][n_axes], read with rope only
+ *   ws     device scratch of fd_scaled_block_ws_size bytes, 256-byte aligned;
+ *          fd_region_importance reads it as it reads fd_block_forward's
+ * Other arguments, limits and errors as fd_block_forward.
+ */
+size_t fd_scaled_block_ws_size(const fd_plan* plan, const fd_dims* dims);
+fd_status fd_scaled_block_forward(const fd_plan* plan, const fd_dims* dims, const fd_scaled_weights* w,
+                                  const fd_rope* rope, const int32_t* coord, float* h, const int32_t* idx,
+                                  const int32_t* cu_q, const int32_t* m, uint16_t* k_cache, uint16_t* v_cache, void* ws,
+                                  size_t ws_bytes, fd_stream_t stream);
 
 /* ---------------------------------------------------------------- timing
  * Kernel timer for measurement: while armed for `kernel`, every launch of that

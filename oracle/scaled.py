@@ -103,3 +103,4 @@ def rope(x, pos, dims, theta, step, halves):
 
 def gelu(z):
     return 0.5 * z * (1.0 + np.tanh(np.sqrt(2.0 / np.pi) * (z + 0.044715 * z ** 3)))
+

@@ -65,6 +65,36 @@ BlockWs carve_block_ws(const fd_plan* p, const fd_dims* d, void* base) {
   return w;
 }
 
+// The 8-bit block's workspace: the block's own (fd_region_importance finds its queries and normalisers where
+// fd_block_forward leaves them), then the rows in 8 bits and the fused projection.  The MLP's hidden codes and
+// scales take the place of its bf16 rows, a branch's output that of the norm's.
+struct ScaledWs {
+  BlockWs block;
+  uint8_t *a, *sa, *g, *sg;
+  uint16_t* qkv;
+  size_t bytes;
+};
+
+ScaledWs carve_scaled_ws(const fd_plan* p, const fd_dims* d, void* base) {
+  const size_t n = static_cast<size_t>(p->n_tokens);
+  ScaledWs w;
+  w.block = carve_block_ws(p, d, base);
+  size_t off = w.block.bytes;
+  const uintptr_t b0 = reinterpret_cast<uintptr_t>(base);
+  auto take = [&](size_t bytes) {
+    const uintptr_t ptr = b0 + off;
+    off += align_up(bytes);
+    return reinterpret_cast<void*>(ptr);
+  };
+  w.a = static_cast<uint8_t*>(take(n * d->D));
+  w.sa = static_cast<uint8_t*>(take(n * fd::scale_stride(d->D)));
+  w.qkv = static_cast<uint16_t*>(take(n * 3 * d->D * 2));
+  w.sg = static_cast<uint8_t*>(take(n * fd::scale_stride(d->F)));
+  w.g = reinterpret_cast<uint8_t*>(w.block.g);
+  w.bytes = off;
+  return w;
+}
+
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 fd_status check_plan(const fd_plan* p) {
@@ -133,6 +163,20 @@ fd_status rope_turns(const fd_rope* r, int dh, fdh::RopeArgs* g) {
     for (int j = 0; j < d / 2; ++j)
       g->turns[g->pairs++] = r->step[a] * pow(r->theta[a], -2.0 * j / d) / 6.283185307179586;
   }
+  return FD_OK;
+}
+
+// What the attention of a block takes.
+fd_status check_attention(const fd_plan* plan, const fd_dims* dims) {
+  if (plan->n_requests > fdh::kMaxAttnRequests)
+    return fdh::set_error("the block supports at most %d requests per call (%d given)", fdh::kMaxAttnRequests,
+                          plan->n_requests),
+           FD_E_UNSUPPORTED;
+  // it addresses a request's key and value rows with 32-bit offsets
+  if (static_cast<long long>(plan->max_request_tokens) * dims->D * 2 >= (1LL << 32))
+    return fdh::set_error("the block supports at most 4 GiB of keys per request (%d tokens x %d given)",
+                          plan->max_request_tokens, dims->D),
+           FD_E_UNSUPPORTED;
   return FD_OK;
 }
 
@@ -403,19 +447,11 @@ fd_status fd_block_forward(const fd_plan* plan, const fd_dims* dims, const fd_bl
                  (w->mod ? aligned(w->mod, 16) : aligned(w->w_ada, 16)) && aligned(h, 16) && aligned(k_cache, 16) &&
                  aligned(v_cache, 16) && aligned(ws, kAlign),
              "misaligned buffer");
-  if (plan->n_requests > fdh::kMaxAttnRequests)
-    return fdh::set_error("the block supports at most %d requests per call (%d given)", fdh::kMaxAttnRequests,
-                          plan->n_requests),
-           FD_E_UNSUPPORTED;
+  FD_TRY(check_attention(plan, dims));
   // the tile loads address the weights of one product with 31-bit offsets
   const long long widest = dims->F > 3LL * dims->D ? dims->F : 3LL * dims->D;
   if (2 * widest * dims->D > fdh::kMaxGemmBytes)
     return fdh::set_error("the block supports weights below 2 GiB per product (%lld x %d given)", widest, dims->D),
-           FD_E_UNSUPPORTED;
-  // the attention addresses a request's key and value rows with 32-bit offsets
-  if (static_cast<long long>(plan->max_request_tokens) * dims->D * 2 >= (1LL << 32))
-    return fdh::set_error("the block supports at most 4 GiB of keys per request (%d tokens x %d given)",
-                          plan->max_request_tokens, dims->D),
            FD_E_UNSUPPORTED;
   const BlockWs bw = carve_block_ws(plan, dims, ws);
   if (ws_bytes < bw.bytes) return fdh::set_error("block workspace too small (%zu < %zu)", ws_bytes, bw.bytes), FD_E_SHAPE;
@@ -580,7 +616,8 @@ fd_status fd_rms_quant(int32_t n_rows, int32_t D, int32_t n_requests, float* h, 
   FD_REQUIRE(n_rows >= 1 && D >= 1 && n_requests >= 1, "sizes must be positive");
   FD_TRY(check_cols(D));
   if (D > 12288) return fdh::set_error("D > 12288 unsupported"), FD_E_UNSUPPORTED;
-  FD_REQUIRE(h && m && q && q_scale && (cu_q || n_requests == 1), "null pointer");
+  FD_REQUIRE(h && m && (cu_q || n_requests == 1), "null pointer");
+  FD_REQUIRE(!q == !q_scale && (q || y), "neither codes with scales nor a branch to add");
   FD_REQUIRE(y || !gate, "a gate without a branch");
   FD_REQUIRE(eps >= 0.f, "eps must be >= 0");
   FD_REQUIRE(mod_stride >= 0 && mod_stride % 4 == 0, "mod_stride = %d, not a multiple of 4", mod_stride);
@@ -631,6 +668,73 @@ fd_status fd_scaled_linear(int32_t n_rows, int32_t n_out, int32_t n_in, const ui
   g.bias = bias; g.gelu = gelu; g.y_bf16 = y_bf; g.y_f32 = y_fp; g.y_q = y_q; g.y_scale = y_scale;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   FD_LAUNCH(FD_K_LINEAR, s, fdh::launch_scaled_linear(g, s));
+  return FD_OK;
+}
+
+size_t fd_scaled_block_ws_size(const fd_plan* plan, const fd_dims* dims) {
+  if (!plan || !dims) return 0;
+  return carve_scaled_ws(plan, dims, nullptr).bytes;
+}
+
+fd_status fd_scaled_block_forward(const fd_plan* plan, const fd_dims* dims, const fd_scaled_weights* w, const fd_rope* rope,
+                                  const int32_t* coord, float* h, const int32_t* idx, const int32_t* cu_q, const int32_t* m,
+                                  uint16_t* k_cache, uint16_t* v_cache, void* ws, size_t ws_bytes, fd_stream_t stream) {
+  FD_TRY(check_plan(plan));
+  FD_TRY(check_dims(dims));
+  FD_REQUIRE(w && h && idx && cu_q && m && k_cache && v_cache && ws, "null pointer");
+  FD_REQUIRE(w->w_qkv && w->s_qkv && w->b_qkv && w->w_o && w->s_o && w->b_o && w->w_1 && w->s_1 && w->b_1 && w->w_2 && w->s_2 &&
+                 w->b_2 && w->mod,
+             "null weight pointer");
+  FD_REQUIRE(!rope || coord, "rotary positions without coordinates");
+  FD_REQUIRE(aligned(h, 16) && aligned(k_cache, 16) && aligned(v_cache, 16) && aligned(ws, kAlign) && aligned(w->mod, 16),
+             "misaligned buffer");
+  FD_TRY(check_attention(plan, dims));
+  const int D = dims->D, F = dims->F, B = plan->n_requests, N = plan->n_tokens;
+  const long long widest = F > 3LL * D ? F : 3LL * D;
+  if (widest > (1 << 20) || widest * D > fdh::kMaxGemmBytes)
+    return fdh::set_error("the block supports weights below 2 GiB per product (%lld x %d given)", widest, D), FD_E_UNSUPPORTED;
+  fdh::RopeArgs r{};
+  if (rope) FD_TRY(rope_turns(rope, dims->dh, &r));
+  const ScaledWs s8 = carve_scaled_ws(plan, dims, ws);
+  const BlockWs& bw = s8.block;
+  if (ws_bytes < s8.bytes) return fdh::set_error("block workspace too small (%zu < %zu)", ws_bytes, s8.bytes), FD_E_SHAPE;
+  // every argument of the steps below is checked: nothing has been enqueued when one is refused
+  for (const void* p : {static_cast<const void*>(w->w_qkv), static_cast<const void*>(w->w_o), static_cast<const void*>(w->w_1),
+                        static_cast<const void*>(w->w_2), static_cast<const void*>(w->b_qkv), static_cast<const void*>(w->b_o),
+                        static_cast<const void*>(w->b_1), static_cast<const void*>(w->b_2), static_cast<const void*>(w->norm_1),
+                        static_cast<const void*>(w->norm_2)})
+    FD_REQUIRE(aligned(p, 16), "misaligned buffer");
+  for (const uint8_t* p : {w->s_qkv, w->s_o, w->s_1, w->s_2}) FD_REQUIRE(aligned(p, 4), "misaligned buffer");
+
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  const float* mod = w->mod;
+  uint16_t* y = bw.a;   // a branch's output
+  fdh::RmsArgs n{};
+  n.n_rows = N; n.D = D; n.n_req = B; n.mod_stride = 6 * D; n.cu_q = cu_q; n.m = m; n.eps = 1e-6f; n.h = h;
+  n.weight = w->norm_1; n.shift = mod; n.scale = mod + D; n.q = s8.a; n.q_scale = s8.sa;
+  FD_LAUNCH(FD_K_RMS, s, fdh::launch_rms_quant(n, s));
+  fdh::ScaledArgs g{};
+  g.n_rows = N; g.m = m;
+  g.N = 3 * D; g.K = D; g.a = s8.a; g.a_scale = s8.sa; g.w = w->w_qkv; g.w_scale = w->s_qkv; g.bias = w->b_qkv; g.y_bf16 = s8.qkv;
+  FD_LAUNCH(FD_K_LINEAR, s, fdh::launch_scaled_linear(g, s));
+  r.n_rows = N; r.hq = dims->H; r.hk = dims->H; r.dh = dims->dh; r.m = m; r.idx = idx; r.coord = coord;
+  r.qkv = s8.qkv; r.q = bw.q; r.k = k_cache; r.v = v_cache;
+  FD_LAUNCH(FD_K_ROPE, s, fdh::launch_rope(r, rope && rope->pairing == FD_ROPE_HALVES, s));
+  FD_LAUNCH(FD_K_ATTN, s,
+            fdh::launch_attention(bw.q, k_cache, v_cache, bw.o, D, dims->H, dims->dh, cu_q, plan->req_tok_off, B, N,
+                                  plan->max_request_tokens, bw.partial, bw.lse, s));
+  FD_LAUNCH(FD_K_QUANT, s, fdh::launch_quant_blocks(bw.o, N, D, 1, m, s8.a, s8.sa, s));
+  g.N = D; g.w = w->w_o; g.w_scale = w->s_o; g.bias = w->b_o; g.y_bf16 = y;
+  FD_LAUNCH(FD_K_LINEAR, s, fdh::launch_scaled_linear(g, s));
+  n.y = y; n.gate = mod + 2 * D; n.weight = w->norm_2; n.shift = mod + 3 * D; n.scale = mod + 4 * D;
+  FD_LAUNCH(FD_K_RMS, s, fdh::launch_rms_quant(n, s));
+  g.N = F; g.w = w->w_1; g.w_scale = w->s_1; g.bias = w->b_1; g.gelu = 1; g.y_bf16 = nullptr; g.y_q = s8.g; g.y_scale = s8.sg;
+  FD_LAUNCH(FD_K_LINEAR, s, fdh::launch_scaled_linear(g, s));
+  g.N = D; g.K = F; g.a = s8.g; g.a_scale = s8.sg; g.w = w->w_2; g.w_scale = w->s_2; g.bias = w->b_2; g.gelu = 0;
+  g.y_bf16 = y; g.y_q = nullptr; g.y_scale = nullptr;
+  FD_LAUNCH(FD_K_LINEAR, s, fdh::launch_scaled_linear(g, s));
+  n.gate = mod + 5 * D; n.q = nullptr; n.q_scale = nullptr;
+  FD_LAUNCH(FD_K_RMS, s, fdh::launch_rms_quant(n, s));
   return FD_OK;
 }
 

@@ -114,6 +114,7 @@ __global__ __launch_bounds__(256) void rms_quant_kernel(fdh::RmsArgs g) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum += v[j][e] * v[j][e];
   }
+  if (!g.q) return;   // the residual alone
   sum = fd::wave_sum(sum);
   if constexpr (WAVES > 1) {
     if ((threadIdx.x & 63) == 0) part[wave] = sum;

@@ -59,6 +59,11 @@ class FdRope(ctypes.Structure):
                 ("step", ctypes.c_double * 4)]
 
 
+class FdScaledWeights(ctypes.Structure):
+    _fields_ = [(n, _p) for n in ("w_qkv", "s_qkv", "b_qkv", "w_o", "s_o", "b_o", "w_1", "s_1", "b_1", "w_2", "s_2", "b_2",
+                                  "norm_1", "norm_2", "mod")]
+
+
 class FlashDiffError(RuntimeError):
     pass
 
@@ -102,6 +107,9 @@ def lib() -> ctypes.CDLL:
         "fd_rms_quant": ([_i32, _i32, _i32, _p, _p, _p, _p, _p, _p, _i32, ctypes.c_float, _p, _p, _p, _p, _p], _i32),
         "fd_rope_axes": ([_i32, _i32, P(FdRope), _i32, _i32, _i32, _p, _p, _p, _p, _p, _p, _p, _p], _i32),
         "fd_scaled_linear": ([_i32, _i32, _i32, _p, _p, _p, _p, _p, _i32, _p, _p, _p, _p, _p, _p], _i32),
+        "fd_scaled_block_ws_size": ([P(FdPlan), P(FdDims)], ctypes.c_size_t),
+        "fd_scaled_block_forward": ([P(FdPlan), P(FdDims), P(FdScaledWeights), P(FdRope), _p, _p, _p, _p, _p, _p, _p, _p,
+                                     ctypes.c_size_t, _p], _i32),
         "fd_timer_arm": ([_i32, _i32], _i32),
         "fd_timer_read": ([_p, _i32], _i32),
         "fd_timer_disarm": ([], None),
@@ -120,7 +128,7 @@ def exported_symbols() -> Sequence[str]:
             "fd_select", "fd_gather", "fd_embed", "fd_adaln", "fd_block_ws_size", "fd_block_forward", "fd_final",
             "fd_scatter_update", "fd_importance_ws_size", "fd_region_importance", "fd_partition_ws_size",
             "fd_partition", "fd_scale_stride", "fd_quant_blocks", "fd_rms_quant", "fd_rope_axes", "fd_scaled_linear",
-            "fd_timer_arm", "fd_timer_read", "fd_timer_disarm")
+            "fd_scaled_block_ws_size", "fd_scaled_block_forward", "fd_timer_arm", "fd_timer_read", "fd_timer_disarm")
 
 
 def _check(name: str, status: int) -> None:
@@ -464,7 +472,7 @@ def fd_quant_blocks(x, block_rows: int, q, scale, m=None, stream=None) -> None:
 def fd_rms_quant(h, q, scale, cu_q, m, y=None, gate=None, weight=None, shift=None, mod_scale=None, eps: float = 1e-6,
                  stream=None) -> None:
     """h [rows, D] fp32 += gate * y (with y), then its RMS norm times weight, modulated, as codes q
-    [rows, D] and scale bytes [rows, fd_scale_stride(D)].  gate, shift and mod_scale: fp32 [requests, D],
+    [rows, D] and scale bytes [rows, fd_scale_stride(D)]; q and scale None: h's update alone.  gate, shift and mod_scale: fp32 [requests, D],
     which may be column ranges of one modulation tensor (equal row strides)."""
     rows, D = _rows("h", h)
     B = cu_q.numel() - 1
@@ -483,7 +491,7 @@ def fd_rms_quant(h, q, scale, cu_q, m, y=None, gate=None, weight=None, shift=Non
     n = rows * D
     h_, y_, w_, cu_, m_, q_, s_, st = _pointers(
         stream, ("h", h, "f32", n), ("y", y, "b16", -n), ("weight", weight, "f32", -D), ("cu_q", cu_q, "i32", 2), ("m", m, "i32", 1),
-        ("q", q, "code", n), ("scale", scale, "scale", rows * fd_scale_stride(D)))
+        ("q", q, "code", n if scale is not None else -n), ("scale", scale, "scale", rows * fd_scale_stride(D) * (1 if q is not None else -1)))
     _check("fd_rms_quant", lib().fd_rms_quant(rows, D, B, h_, y_, mod[0], w_, mod[1], mod[2], stride or 0, eps, cu_, m_, q_, s_, st))
 
 
@@ -533,6 +541,51 @@ def fd_scaled_linear(a, a_scale, w, w_scale, y, y_scale=None, bias=None, gelu: b
                                                       y_ if wide else None, y_ if codes else None, ys_, st))
 
 
+_SCALED = ("w_qkv", "w_o", "w_1", "w_2")
+
+
+def scaled_params(params: Dict[str, torch.Tensor]) -> Dict[str, torch.Tensor]:
+    """The block parameters of a model for 8-bit products, laid out once: every bf16 weight stack
+    [L, out, in] as codes with 128 x 128 scales (s_* for w_*), the rest as it is.  norm_1 and norm_2
+    ([L, D] fp32), where the model has them, are the weights of its RMS norms."""
+    out = {k: v for k, v in params.items() if k not in _SCALED}
+    for k in _SCALED:
+        w = params[k]
+        L, n, c = w.shape
+        q = torch.empty((L, n, c), dtype=torch.float8_e4m3fn, device=w.device)
+        s = torch.zeros((L, -(-n // 128), fd_scale_stride(c)), dtype=torch.uint8, device=w.device)
+        for l in range(L):
+            fd_quant_blocks(w[l], 128, q[l], s[l])
+        out[k], out["s" + k[1:]] = q, s
+    return out
+
+
+def scaled_weights(params: Dict[str, torch.Tensor], l: int, mod: torch.Tensor) -> FdScaledWeights:
+    """Weights of block l of scaled_params' tensors; mod: the block's [B, 6D] fp32 from fd_adaln."""
+    names = ("w_qkv", "s_qkv", "b_qkv", "w_o", "s_o", "b_o", "w_1", "s_1", "b_1", "w_2", "s_2", "b_2")
+    norms = [_ptr(params[n][l]) if n in params else None for n in ("norm_1", "norm_2")]
+    return FdScaledWeights(*[_ptr(params[n][l]) for n in names], *norms, _ptr(mod))
+
+
+def fd_scaled_block_ws_size(plan: Plan, d: FdDims) -> int:
+    return int(lib().fd_scaled_block_ws_size(ctypes.byref(plan.c), ctypes.byref(d)))
+
+
+def fd_scaled_block_forward(plan: Plan, d: FdDims, w: FdScaledWeights, rope: Optional[FdRope], coord, h, idx, cu_q, m, k_cache,
+                            v_cache, ws, stream=None) -> None:
+    """fd_block_forward with RMS norms, rotary positions (rope from rope_axes and coord [tokens, axes], or
+    both None) and 8-bit products; ws of fd_scaled_block_ws_size bytes."""
+    N, B = plan.n_tokens, plan.n_requests
+    p = _pointers(stream, ("h", h, "f32", N * d.D), ("idx", idx, "i32", N), ("cu_q", cu_q, "i32", B + 1), ("m", m, "i32", 1),
+                  ("k_cache", k_cache, "b16", N * d.D), ("v_cache", v_cache, "b16", N * d.D),
+                  ("coord", coord, "i32", -1 if rope is None else N * rope.n_axes))
+    _need("ws", ws, "bytes", fd_scaled_block_ws_size(plan, d))
+    h_, idx_, cu_, m_, k_, v_, c_, st = p
+    _check("fd_scaled_block_forward", lib().fd_scaled_block_forward(
+        ctypes.byref(plan.c), ctypes.byref(d), ctypes.byref(w), None if rope is None else ctypes.byref(rope), c_, h_, idx_, cu_, m_,
+        k_, v_, _ptr(ws), ws.numel() * ws.element_size(), st))
+
+
 def fd_timer_arm(kernel: str, capacity: int) -> None:
     _check("fd_timer_arm", lib().fd_timer_arm(KERNELS[kernel], capacity))
 
@@ -559,11 +612,18 @@ class SparseStep:
     fd_scatter_update on the current stream.  With the importance signal the
     gate thresholds `delta` (carried from the previous step) instead of the
     region score, and fd_region_importance runs after the chosen block.
+
+    With `scaled` (scaled_params of the model) the blocks are fd_scaled_block_forward's: RMS norms
+    and 8-bit products, and rotary positions where `rope` (rope_axes) and `coord` (int32
+    [N, axes], the tokens' positions) are given.
     """
 
     def __init__(self, plan: Plan, d: FdDims, params: Dict[str, torch.Tensor], n_layers: int,
                  k_cache: Optional[torch.Tensor] = None, v_cache: Optional[torch.Tensor] = None,
-                 device: str = "cuda"):
+                 device: str = "cuda", scaled: Optional[Dict[str, torch.Tensor]] = None, rope: Optional[FdRope] = None,
+                 coord: Optional[torch.Tensor] = None):
+        if scaled is None and (rope is not None or coord is not None):
+            raise FlashDiffError("rotary positions belong to the 8-bit blocks: give `scaled` too")
         self.plan, self.d, self.params, self.L = plan, d, params, n_layers
         N, R, B, C, D = plan.n_tokens, plan.n_regions, plan.n_requests, d.C, d.D
         dev = torch.device(device)
@@ -584,9 +644,14 @@ class SparseStep:
         self.v = torch.zeros((N, C), dtype=torch.float32, device=dev)
         self.vcache = torch.zeros((N, C), dtype=torch.float32, device=dev)
         self.ws_score = torch.empty(max(fd_region_score_ws_size(plan, C), 256), dtype=torch.uint8, device=dev)
-        self.ws_block = torch.empty(fd_block_ws_size(plan, d), dtype=torch.uint8, device=dev)
+        ws_block = fd_block_ws_size(plan, d) if scaled is None else fd_scaled_block_ws_size(plan, d)
+        self.ws_block = torch.empty(ws_block, dtype=torch.uint8, device=dev)
         self.mod = torch.zeros((n_layers, B, 6 * D), dtype=torch.float32, device=dev)
-        self.block_w = [block_weights(params, l, self.mod[l]) for l in range(n_layers)]
+        self.scaled, self.rope, self.coord = scaled, rope, coord
+        if scaled is None:
+            self.block_w = [block_weights(params, l, self.mod[l]) for l in range(n_layers)]
+        else:
+            self.block_w = [scaled_weights(scaled, l, self.mod[l]) for l in range(n_layers)]
         self.final_w = final_weights(params)
         self.r_bar = torch.zeros(R, dtype=torch.float64, device=dev)
         self.delta = torch.zeros(R, dtype=torch.float64, device=dev)
@@ -625,8 +690,12 @@ class SparseStep:
         fd_adaln(d, self.L, 6 * d.D, p.n_requests, self.params["w_ada"], self.params["b_ada"], cond, self.mod,
                  stream)
         for l in range(self.L):
-            fd_block_forward(p, d, self.block_w[l], cond, self.h, self.idx, self.cu_q, self.m, self.k_cache[l],
-                             self.v_cache[l], self.ws_block, stream)
+            if self.scaled is None:
+                fd_block_forward(p, d, self.block_w[l], cond, self.h, self.idx, self.cu_q, self.m, self.k_cache[l],
+                                 self.v_cache[l], self.ws_block, stream)
+            else:
+                fd_scaled_block_forward(p, d, self.block_w[l], self.rope, self.coord, self.h, self.idx, self.cu_q, self.m,
+                                        self.k_cache[l], self.v_cache[l], self.ws_block, stream)
             if importance_block == l:
                 fd_region_importance(p, d, self.ws_block, self.k_cache[l], self.idx, self.m, self.active, self.r_bar,
                                      self.delta, self.importance, self.ws_imp, stream)

@@ -163,3 +163,36 @@ def test_no_vector_memory_read_of_a_fresh_scalar(tmp_path):
     seen, bad = _hazards(out.read_text().splitlines())
     assert seen > 300
     assert not bad, bad[:3]
+
+
+@no_gpu
+def test_scaled_block_refuses():
+    lib = fdl.lib()
+    plan, d = fdl.FdPlan(16, 4, 1, 4, 16, *([P] * 6)), fdl.FdDims(16, 128, 2, 64, 256)
+    need = lib.fd_scaled_block_ws_size(ctypes.byref(plan), ctypes.byref(d))
+    assert need > lib.fd_block_ws_size(ctypes.byref(plan), ctypes.byref(d)) > 0
+    assert lib.fd_scaled_block_ws_size(None, None) == 0
+    ok = dict(plan=plan, dims=d, w=[P] * 15, rope=None, coord=None, h=P, idx=P, cu=P, m=P, k=P, v=P, ws=P, n=need)
+
+    def call(**change):
+        a = dict(ok, **change)
+        w = a["w"] and fdl.FdScaledWeights(*a["w"])
+        return lib.fd_scaled_block_forward(ctypes.byref(a["plan"]), ctypes.byref(a["dims"]), ctypes.byref(w) if w else None,
+                                           ctypes.byref(a["rope"]) if a["rope"] else None, a["coord"], *(a[x] for x in ("h", "idx", "cu", "m", "k", "v", "ws", "n")), None)
+
+    for x in ("w", "h", "idx", "cu", "m", "k", "v", "ws"):
+        assert call(**{x: None}) == 1, x
+    for i in range(15):
+        w = [P] * 15
+        w[i] = None
+        assert i in (12, 13) or call(w=w) == 1          # the norms' weights may be absent
+        w[i] = P + 2
+        assert call(w=w) == 1, i
+    assert call(n=need - 1) == 2 and b"workspace" in lib.fd_last_error()
+    assert call(rope=fdl.rope_axes([64])) == 1          # no coordinates
+    assert call(rope=fdl.rope_axes([66]), coord=P) == 1
+    assert call(dims=fdl.FdDims(16, 96, 2, 48, 256)) == 3 and call(dims=fdl.FdDims(16, 128, 4, 64, 256)) == 2
+    assert call(plan=fdl.FdPlan(2050, 1025, 1025, 2, 2, *([P] * 6))) == 3
+    assert call(dims=fdl.FdDims(64, 4096, 32, 128, 1 << 19)) == 3   # 2 GiB of MLP weights
+    for x in ("h", "k", "v", "ws"):
+        assert call(**{x: P + 8}) == 1
