@@ -557,6 +557,7 @@ hipError_t launch_scaled_linear(const ScaledArgs& g, hipStream_t s) {
       };
       using std::integral_constant;
       if constexpr (codes) few(integral_constant<int, 1>{}, integral_constant<int, 8>{}, integral_constant<int, 2>{});
+      else if (g.n_rows <= 16 && g.K <= 2 * kFewWaves * kScaleBlock) few(integral_constant<int, 1>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{});
       else if (g.n_rows <= 16) few(integral_constant<int, 1>{}, integral_constant<int, 1>{}, integral_constant<int, 6>{});
       else few(integral_constant<int, 4>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{});
       return;

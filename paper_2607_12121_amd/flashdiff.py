@@ -428,6 +428,11 @@ def _rows(name: str, t: torch.Tensor) -> Sequence[int]:
 _KIND = {k: frozenset(v) for k, v in _DT.items() if v is not None}
 
 
+# The handle of a device's current stream: without the stream object that torch.cuda.current_stream builds (2.7 us) where
+# this torch has that.
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
 def _pointers(stream: Optional[torch.cuda.Stream], *args) -> list:
     """Checks (name, tensor, kind, elements) tuples as _need does, and that every tensor and the stream are on
     the current device, the one the call runs on; returns the tensors' addresses and the stream's handle.  One
@@ -452,10 +457,11 @@ def _pointers(stream: Optional[torch.cuda.Stream], *args) -> list:
             _ptr(t)
         out.append(t.data_ptr())
     if stream is None:
-        stream = torch.cuda.current_stream()
+        out.append(_current_stream(cur))
     elif stream.device.index != cur:
         raise FlashDiffError(f"the stream is on {stream.device}, the current device is {cur}")
-    out.append(stream.cuda_stream)
+    else:
+        out.append(stream.cuda_stream)
     return out
 
 
@@ -476,23 +482,19 @@ def fd_rms_quant(h, q, scale, cu_q, m, y=None, gate=None, weight=None, shift=Non
     which may be column ranges of one modulation tensor (equal row strides)."""
     rows, D = _rows("h", h)
     B = cu_q.numel() - 1
-    stride, mod = None, []
-    for n_, t_ in (("gate", gate), ("shift", shift), ("mod_scale", mod_scale)):
-        if t_ is None:
-            mod.append(None)
-            continue
-        _need(n_, t_, "f32", B * D)
-        if tuple(t_.shape) != (B, D) or t_.stride(1) != 1 or t_.device != h.device:
-            raise FlashDiffError(f"{n_} must be [{B}, {D}] with contiguous rows, on {h.device}")
-        if stride is not None and t_.stride(0) != stride:
-            raise FlashDiffError("gate, shift and mod_scale must have the same row stride")
-        stride = t_.stride(0)
-        mod.append(t_.data_ptr())
+    stride, mod = 0, [None, None, None]
+    given = [(i, t) for i, t in enumerate((gate, shift, mod_scale)) if t is not None]
+    if given:
+        stride, dev = given[0][1].stride(0), h.get_device()
+        for i, t in given:
+            if t.shape != (B, D) or t.stride() != (stride, 1) or t.dtype != torch.float32 or t.get_device() != dev:
+                raise FlashDiffError(f"gate, shift and mod_scale must be fp32 [{B}, {D}] with contiguous rows of one stride, on {h.device}")
+            mod[i] = t.data_ptr()
     n = rows * D
     h_, y_, w_, cu_, m_, q_, s_, st = _pointers(
         stream, ("h", h, "f32", n), ("y", y, "b16", -n), ("weight", weight, "f32", -D), ("cu_q", cu_q, "i32", 2), ("m", m, "i32", 1),
         ("q", q, "code", n if scale is not None else -n), ("scale", scale, "scale", rows * fd_scale_stride(D) * (1 if q is not None else -1)))
-    _check("fd_rms_quant", lib().fd_rms_quant(rows, D, B, h_, y_, mod[0], w_, mod[1], mod[2], stride or 0, eps, cu_, m_, q_, s_, st))
+    _check("fd_rms_quant", lib().fd_rms_quant(rows, D, B, h_, y_, mod[0], w_, mod[1], mod[2], stride, eps, cu_, m_, q_, s_, st))
 
 
 def rope_axes(dims: Sequence[int], theta=10000.0, step=1.0, halves: bool = False) -> FdRope:
