@@ -394,8 +394,8 @@ fd_status fd_quant_blocks(int32_t n_rows, int32_t cols, int32_t block_rows, cons
  *   h      device fp32 [n_rows][D], 16-byte aligned, updated in place
  *   y      device bf16 [n_rows][D] or null (a branch's output)
  *   gate, scale, shift  device fp32, request b's at + b * mod_stride, or null
- *          (gate 1, scale 0, shift 0); 16-byte aligned, mod_stride % 4 == 0 (may be
- *          0: the same for every request)
+ *          (gate 1, scale 0, shift 0); gate is read only with y; 16-byte aligned,
+ *          mod_stride % 4 == 0 (may be 0: the same for every request)
  *   weight device fp32 [D] or null (1)
  *   cu_q   device int32 [n_requests + 1], m device int32 [1], from fd_select; cu_q is
  *          not read (may be null) with one request

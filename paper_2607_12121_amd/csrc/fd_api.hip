@@ -618,7 +618,6 @@ fd_status fd_rms_quant(int32_t n_rows, int32_t D, int32_t n_requests, float* h, 
   if (D > 12288) return fdh::set_error("D > 12288 unsupported"), FD_E_UNSUPPORTED;
   FD_REQUIRE(h && m && (cu_q || n_requests == 1), "null pointer");
   FD_REQUIRE(!q == !q_scale && (q || y), "neither codes with scales nor a branch to add");
-  FD_REQUIRE(y || !gate, "a gate without a branch");
   FD_REQUIRE(eps >= 0.f, "eps must be >= 0");
   FD_REQUIRE(mod_stride >= 0 && mod_stride % 4 == 0, "mod_stride = %d, not a multiple of 4", mod_stride);
   FD_REQUIRE(aligned(h, 16) && aligned(y, 16) && aligned(gate, 16) && aligned(weight, 16) && aligned(shift, 16) &&

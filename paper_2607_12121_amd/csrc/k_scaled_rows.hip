@@ -103,7 +103,7 @@ __global__ __launch_bounds__(256) void rms_quant_kernel(fdh::RmsArgs g) {
         bias[j][e] = 0.f;
       }
       if (c >= D) continue;
-      if (g.gate) load8(g.gate + mod + c, gate[j]);
+      if (g.y && g.gate) load8(g.gate + mod + c, gate[j]);
       if (!g.q) continue;
       if (g.scale) {
         load8(g.scale + mod + c, gain[j]);

@@ -129,7 +129,7 @@ def run_rms(h, y, mod, weight, cu, m, parts, eps=1e-6):
     return d_h.cpu().numpy(), q.cpu().numpy(), s.cpu().numpy()
 
 
-@pytest.mark.parametrize("parts", ["", "y", "yg", "w", "m", "ygwm"])
+@pytest.mark.parametrize("parts", ["", "y", "yg", "g", "w", "m", "ygwm"])
 @pytest.mark.parametrize("rows,D,B,m", [(1, 16, 1, 1), (5, 64, 1, 3), (9, 1088, 4, 9), (33, 1536, 7, 30), (6, 2048, 2, 6),
                                         (5, 2064, 3, 4), (3, 6160, 2, 3), (2, 12288, 1, 2), (4, 128, 3, 0)])
 def test_rms_quant(rows, D, B, m, parts):
@@ -141,7 +141,7 @@ def test_rms_quant(rows, D, B, m, parts):
     of_row = np.repeat(np.arange(B), np.diff(cu))
     pick = lambda i, on: mod[of_row, i * D:(i + 1) * D].astype(np.float64) if on in parts else None  # noqa: E731
     y64 = None if y is None else y.double().numpy()[:m]
-    gate, shift, scale = pick(2, "g"), pick(0, "m"), pick(1, "m")
+    gate, shift, scale = pick(2, "g"), pick(0, "m"), pick(1, "m")   # a gate without a branch is not read
     wh, wa = ref.rms(h[:m], y64, gate, None if weight is None else weight.astype(np.float64), shift, scale, 1e-6)
     add = 0.0 if y64 is None else np.abs(y64) * (1.0 if gate is None else np.abs(gate))
     assert np.all(np.abs(gh_[:m] - wh) <= 2 * U32 * (np.abs(wh) + add))
@@ -371,7 +371,7 @@ def test_bindings_refuse():
     bad = [
         lambda: fdl.fd_quant_blocks(x.float(), 1, q, s), lambda: fdl.fd_quant_blocks(x, 1, q[:7], s), lambda: fdl.fd_quant_blocks(x, 1, q, s[:7]),
         lambda: fdl.fd_quant_blocks(x, 2, q, s), lambda: fdl.fd_quant_blocks(x.t(), 1, q, s), lambda: fdl.fd_quant_blocks(x, 128, q, s, m=m),
-        lambda: fdl.fd_rms_quant(h, q, s[:, :3], cu, m), lambda: fdl.fd_rms_quant(h, q, s, cu, m, gate=mod), lambda: fdl.fd_rms_quant(h, q, s, cu, m, y=h),
+        lambda: fdl.fd_rms_quant(h, q, s[:, :3], cu, m), lambda: fdl.fd_rms_quant(h, q, s, cu, m, gate=mod[:, :64]), lambda: fdl.fd_rms_quant(h, q, s, cu, m, y=h),
         lambda: fdl.fd_rms_quant(h, q, s, cu, m, shift=mod, mod_scale=torch.zeros(1, 256, device="cuda")[:, :128]),
         lambda: fdl.fd_rms_quant(h, q, s, cu, m, shift=torch.zeros(1, 256, device="cuda")[:, ::2]),
         lambda: fdl.fd_rms_quant(h, q, s, cu, m, shift=torch.zeros(2, 128, device="cuda")), lambda: fdl.fd_rms_quant(h.half(), q, s, cu, m),

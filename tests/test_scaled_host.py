@@ -68,7 +68,7 @@ def test_quant_blocks_refuses(change, status):
 @no_gpu
 @pytest.mark.parametrize("change,status", [
     (dict(rows=0), 1), (dict(D=72), 3), (dict(D=12304), 3), (dict(B=0), 1), (dict(h=None), 1), (dict(m=None), 1), (dict(q=None), 1),
-    (dict(q_scale=None), 1), (dict(B=2, cu_q=None), 1), (dict(y=None), 1), (dict(eps=-1.0), 1), (dict(eps=float("nan")), 1),
+    (dict(q_scale=None), 1), (dict(B=2, cu_q=None), 1), (dict(y=None, q=None, q_scale=None), 1), (dict(eps=-1.0), 1), (dict(eps=float("nan")), 1),
     (dict(stride=-4), 1), (dict(stride=6), 1), (dict(h=P + 4), 1), (dict(y=P + 8), 1), (dict(gate=P + 4), 1), (dict(weight=P + 4), 1),
     (dict(shift=P + 4), 1), (dict(scale=P + 4), 1), (dict(q=P + 8), 1)])
 def test_rms_quant_refuses(change, status):
@@ -149,7 +149,7 @@ int main(int, char**) {
     subprocess.run(["g++", "-std=c++17", f"-I{build.CSRC}", str(src), "-o", str(exe)], check=True)
     cases = [((9828, 1536, 6144, 0), (64, 1, 1)), ((5000, 1536, 6144, 0), (64, 0, 0)), ((9828, 6144, 1536, 1), (16, 0, 0)),
              ((32760, 1536, 6144, 0), (64, 1, 1)), ((9828, 1536, 1536, 0), (64, 1, 0)), ((1664, 1536, 6144, 0), (64, 0, 0)),
-             ((14280, 4096, 1024, 1), (16, 0, 0)), ((1, 64, 64, 0), (64, 0, 0)), ((1 << 30, 16, 16, 0), (64, 1, 1))]
+             ((14280, 4096, 1024, 1), (16, 0, 0)), ((1, 64, 64, 0), (64, 0, 0)), ((1 << 30, 16, 16, 0), (64, 1, 1)), ((9828, 4608, 1536, 0), (64, 1, 0)), ((4096, 6144, 1536, 0), (64, 0, 0))]
     out = subprocess.run([str(exe)], input="\n".join(" ".join(map(str, c)) for c, _ in cases), capture_output=True, text=True, check=True).stdout
     for line, (case, want) in zip(out.splitlines(), cases):
         assert tuple(map(int, line.split())) == want, case
