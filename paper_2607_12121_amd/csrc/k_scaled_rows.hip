@@ -1,5 +1,7 @@
 // Rows to 8-bit codes with block scales: bf16 rows and weights as they are, and the residual
 // stream through its RMS norm.
+#include <type_traits>
+
 #include "fd_scaled.h"
 
 namespace {
@@ -75,12 +77,15 @@ __global__ __launch_bounds__(256) void quant_weights_kernel(const uint16_t* __re
 // one block.  Sums in fp32.  Bound by HBM: 4 bytes of h read and 4 written, 2 of y, 1 of codes per
 // value.  The gate, the weight and the modulation are 16 bytes per value again, from the L2, where each row
 // reads its own: so a row's waves take a run of rows and keep them in registers while the request stays.
-// 8937 x 1536 rows of 8 requests 35.7 us (4.2 TB/s; 41.7 with a row each, the branch's addition alone 23.3),
-// 32760 rows 119 (4.6 TB/s).
+// 8937 x 1536 rows of 8 requests 32.8 us (4.6 TB/s; with a row per wave and no runs 41.7, with runs of a wave
+// each 36), 32760 rows 117 (4.7 TB/s), the branch's addition alone 22 and 104.
+template <int WAVES>
+constexpr int rms_threads() { return WAVES == 1 ? 256 : 64 * WAVES; }   // four rows of a wave each, or one row
+
 template <int VEC, int WAVES>
-__global__ __launch_bounds__(256) void rms_quant_kernel(fdh::RmsArgs g) {
-  constexpr int TEAMS = 4 / WAVES, LANES = 64 * WAVES;
-  __shared__ float part[2][4];
+__global__ __launch_bounds__(rms_threads<WAVES>()) void rms_quant_kernel(fdh::RmsArgs g) {
+  constexpr int TEAMS = WAVES == 1 ? 4 : 1, LANES = 64 * WAVES;
+  __shared__ float part[2][WAVES];
   const int wave = threadIdx.x >> 6, t = threadIdx.x % LANES;
   const int D = g.D, M = min(*g.m, g.n_rows), ld = fd::scale_stride(D);
   const int team = blockIdx.x * TEAMS + (WAVES == 1 ? wave : 0), teams = gridDim.x * TEAMS;
@@ -168,7 +173,8 @@ __global__ __launch_bounds__(256) void rms_quant_kernel(fdh::RmsArgs g) {
       float* p = part[row & 1];   // two sets: a wave may be a row ahead of one that has yet to read
       if ((threadIdx.x & 63) == 0) p[wave] = sum;
       __syncthreads();
-      sum = (p[0] + p[1]) + (p[2] + p[3]);
+      if constexpr (WAVES == 2) sum = p[0] + p[1];
+      else sum = (p[0] + p[1]) + (p[2] + p[3]);
     }
     const float r = 1.0f / sqrtf(sum / static_cast<float>(D) + g.eps);
 #pragma unroll
@@ -204,25 +210,25 @@ hipError_t launch_quant_blocks(const uint16_t* x, int n_rows, int cols, int bloc
 }
 
 hipError_t launch_rms_quant(const RmsArgs& g, hipStream_t s) {
-  // One wave per row up to 2048 columns (32 floats of the row per lane), four above.  As many workgroups as are
-  // resident (192 registers at 1536 columns: two waves per SIMD), so that every run is as long: with twice as many
-  // 8937 x 1536 rows took 38.6 us; held to 168 registers, three waves per SIMD, 44.5, in scratch.
-  const int cap = 2 * num_cus();
-  const int grid = (g.n_rows + 3) / 4 < cap ? (g.n_rows + 3) / 4 : cap, wide = g.n_rows < cap ? g.n_rows : cap;
-  if (g.D <= 2048) {
-    switch ((g.D + 511) / 512) {
-      case 1: rms_quant_kernel<1, 1><<<grid, 256, 0, s>>>(g); break;
-      case 2: rms_quant_kernel<2, 1><<<grid, 256, 0, s>>>(g); break;
-      case 3: rms_quant_kernel<3, 1><<<grid, 256, 0, s>>>(g); break;
-      default: rms_quant_kernel<4, 1><<<grid, 256, 0, s>>>(g);
-    }
-  } else {
-    switch ((g.D + 2047) / 2048) {
-      case 2: rms_quant_kernel<2, 4><<<wide, 256, 0, s>>>(g); break;
-      case 3: rms_quant_kernel<3, 4><<<wide, 256, 0, s>>>(g); break;
-      case 4: rms_quant_kernel<4, 4><<<wide, 256, 0, s>>>(g); break;
-      default: rms_quant_kernel<6, 4><<<wide, 256, 0, s>>>(g);
-    }
+  // 512 columns a wave, so that a lane holds eight of every operand and 16 to 20 waves fit a CU; from 2048
+  // columns on four waves hold more each.  As many workgroups as are resident at 1024 to 2048 columns: runs of
+  // about the same length, whose factors are read once.
+  const int cap = 4 * num_cus();
+  auto run = [&](auto vec, auto waves) {
+    constexpr int VEC = decltype(vec)::value, WAVES = decltype(waves)::value;
+    const int most = WAVES == 2 ? 2 * cap : cap, rows = WAVES == 1 ? (g.n_rows + 3) / 4 : g.n_rows;
+    rms_quant_kernel<VEC, WAVES><<<rows < most ? rows : most, rms_threads<WAVES>(), 0, s>>>(g);
+  };
+  using std::integral_constant;
+  const integral_constant<int, 4> four;
+  if (g.D <= 512) run(integral_constant<int, 1>{}, integral_constant<int, 1>{});
+  else if (g.D <= 1024) run(integral_constant<int, 1>{}, integral_constant<int, 2>{});
+  else switch ((g.D + 2047) / 2048) {
+    case 1: run(integral_constant<int, 1>{}, four); break;
+    case 2: run(integral_constant<int, 2>{}, four); break;
+    case 3: run(integral_constant<int, 3>{}, four); break;
+    case 4: run(integral_constant<int, 4>{}, four); break;
+    default: run(integral_constant<int, 6>{}, four);
   }
   return hipGetLastError();
 }
