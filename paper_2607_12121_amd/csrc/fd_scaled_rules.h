@@ -6,18 +6,36 @@
 
 namespace fd {
 
-// Row capacities up to which the few-row kernel runs (a larger capacity with few rows at work runs the tiles): 16
-// with results in 8 bits, whose blocks want 128 columns of a workgroup, 64 otherwise.  64 x 1536 x 6144: 26 us in
-// tiles, whose 12 workgroups walk 48 K-blocks each.
-FD_RULE int scaled_few_rows(bool codes) { return codes ? 16 : 64; }
-// The tiles' loads run two K-blocks ahead; fewer blocks than three run the few-row kernel at any size.
+// Row capacities up to which the few-row kernel runs (a larger capacity with few rows at work runs the tiles).  Results
+// in 8 bits, whose blocks want 128 columns of a workgroup, leave too few workgroups for it and run the tiles from one
+// row on: 1 x 6144 x 1536 with GELU 11.9 us, in tiles 10.2.  Otherwise 64: 32 x 1536 x 6144 12.0 us, in tiles 20.5;
+// 64 rows of it 19.2 and 20.7.
+FD_RULE int scaled_few_rows(bool codes) { return codes ? 0 : 64; }
+// Its workgroups take 16 columns, or 32 where those of 16 would not each have a CU: every workgroup reads all of the
+// rows.  16 columns and 32, us: 16 x 1536 x 6144 8.9 and 11.4, 16 x 4608 x 6144 14.9 and 11.4, 64 x 4608 x 1536 10.2
+// and 7.4.
+FD_RULE bool scaled_few_wide(int N, int cus) { return (N + 15) / 16 > cus; }
+// The tiles' loads run two or more K-blocks ahead; fewer blocks than three run the few-row kernel at any size.
 constexpr int kTileBlocks = 3;
+
+// Tiles of few workgroups, which a CU has one of: nothing runs beside it while it waits, and what bounds it is the
+// number of K-blocks that it walks.  So the smallest tile whose workgroups each have a CU, and more stages of loads in
+// flight (three, four) than the two of the tiles that run in pairs.  Microseconds to bf16 in tiles of 64 rows / 128
+// rows, four stages / 128 rows, two stages, two a CU: 512 x 1536 x 6144 (96 tiles of 64) 20.7 / 26.0 / 35.5;
+// 1312 x 1024 x 4096 (168) 15.5 / 19.0 / 24.2; 1664 x 1536 x 6144 (156 of 128) 32.5 / 26.7 / 36.0; 512 x 4608 x 1536
+// (144) 10.5 / 10.7 / 11.6; 1664 x 4608 x 1536 (468) 18.5 / 17.7 / 14.7.
+enum ScaledTile { kTile64, kTileDeep, kTile128 };
+FD_RULE ScaledTile scaled_tile(int M, int N, int K, int cus) {
+  const long long columns = (N + 127) / 128;
+  if ((M + 63) / 64 * columns <= cus) return kTile64;
+  return (M + 127) / 128 * columns <= cus && K > 3 * 128 ? kTileDeep : kTile128;
+}
 
 // 256 x 256 tiles, one workgroup per CU, instead of 128 x 128, two: half the LDS and L2 traffic per flop, but nothing
 // to run while results leave.  Worth it where its rounds are full.  To bf16, 128 and 256 tiles: 9828 x 1536 x 6144 (234
-// large tiles on 256 CUs) 98 and 80 us, 5000 rows of it (120 tiles) 48 and 61; 9828 x 4608 x 1536 75 and 73.  Results
+// large tiles on 256 CUs) 96 and 76 us, 5000 rows of it (120 tiles) 48 and 56; 9828 x 4608 x 1536 72 and 68.  Results
 // in 8 bits cost more per tile (their block maxima), so short sums stay with the small tiles: 9828 x 6144 x 1536 with
-// GELU 110 and 115, 14280 x 4096 x 1024 68 and 73.
+// GELU 107 and 110.
 FD_RULE bool scaled_large(int M, int N, int K, bool codes, int cus) {
   const long long tiles = static_cast<long long>((M + 255) / 256) * ((N + 255) / 256);
   const long long rounds = (tiles + cus - 1) / cus;

@@ -68,21 +68,13 @@ struct MmaExact {
 // One row's 4 NF columns from col on (col a multiple of 4 NF; N is a multiple of 16, so each 16 lie
 // inside or outside).  Every lane of the wave runs it; codes need the whole block (NF = 8).
 template <int KIND, int NF>
-FD_DEVICE void store_row(const fdh::ScaledArgs& g, bool row_ok, int row, int col, const f32x4_t (&acc)[NF]) {
+FD_DEVICE void store_row(const fdh::ScaledArgs& g, bool row_ok, int row, int col, const f32x4_t (&acc)[NF], const float4 (&bias)[NF]) {
   static_assert(KIND != kToCodes || NF == 8, "four lanes hold a block's columns");
   float v[4 * NF];
 #pragma unroll
   for (int j = 0; j < NF; ++j)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[4 * j + r] = acc[j][r];
-#pragma unroll
-  for (int j = 0; j < NF; ++j) {
-    const int c = col + 4 * j;
-    if (g.bias && c < g.N) {
-      const float4 b = *reinterpret_cast<const float4*>(g.bias + c);
-      v[4 * j] += b.x; v[4 * j + 1] += b.y; v[4 * j + 2] += b.z; v[4 * j + 3] += b.w;
-    }
-  }
+    for (int r = 0; r < 4; ++r) v[4 * j + r] = acc[j][r] + (r == 0 ? bias[j].x : r == 1 ? bias[j].y : r == 2 ? bias[j].z : bias[j].w);
   if (g.gelu) {
 #pragma unroll
     for (int e = 0; e < 4 * NF; ++e) v[e] = fd::gelu(v[e]);
@@ -126,28 +118,31 @@ FD_DEVICE void store_row(const fdh::ScaledArgs& g, bool row_ok, int row, int col
   }
 }
 
-// 32 bytes at p + k of a row of K bytes, zeros past its end (K is a multiple of 16).  The loads go to the row's last
-// 16 bytes there, so that none waits for a branch.
-FD_DEVICE i32x8_t load32(const uint8_t* p, int k, int K) {
-  uint4 lo = *reinterpret_cast<const uint4*>(p + min(k, K - 16)), hi = *reinterpret_cast<const uint4*>(p + min(k + 16, K - 16));
-  if (k >= K) lo = make_uint4(0, 0, 0, 0);
-  if (k + 16 >= K) hi = make_uint4(0, 0, 0, 0);
+// 32 bytes at p + k of a row of K bytes, K a multiple of 16; past its end the last 16 bytes again, for inside() to clear.
+struct Piece { uint4 lo, hi; };
+FD_DEVICE Piece load32(const uint8_t* p, int k, int K) {
+  return {*reinterpret_cast<const uint4*>(p + min(k, K - 16)), *reinterpret_cast<const uint4*>(p + min(k + 16, K - 16))};
+}
+FD_DEVICE i32x8_t inside(const Piece& x, int k, int K) {
+  const uint4 none = make_uint4(0, 0, 0, 0), lo = k < K ? x.lo : none, hi = k + 16 < K ? x.hi : none;
   return i32x8_t{static_cast<int>(lo.x), static_cast<int>(lo.y), static_cast<int>(lo.z), static_cast<int>(lo.w),
                  static_cast<int>(hi.x), static_cast<int>(hi.y), static_cast<int>(hi.z), static_cast<int>(hi.w)};
 }
 
 // ---------------------------------------------------------------- few rows
 
-// Up to 64 rows: the weights are read once and are nearly all there is to read, so what counts is how many of their
-// bytes are on the way.  A workgroup takes the rows' FM fragments and 16 NF columns, its waves the K-blocks in turn,
-// operands straight from memory into registers, DEEP blocks at a time; the waves' sums meet in LDS.
+// Up to 64 rows: the weights are read once, so what counts is how many of their bytes are on the way.  A workgroup
+// takes the rows' FM fragments and 16 NF columns, its waves the K-blocks in turn, operands straight from memory into
+// registers, up to DEEP blocks at a time; the waves' sums meet in LDS.  DEEP is about what 128 registers hold, so that a
+// CU takes two workgroups: with six blocks and one workgroup, 16 x 4608 x 4096 12.6 us, with three 11.6.  Past its last
+// block a wave loads nothing (loads of nothing, cleared afterwards: 17.1 us).
 constexpr int kFewWaves = 8;
 
 template <int KIND, class Mma, int FM, int NF, int DEEP>
 __global__ __launch_bounds__(kFewWaves * 64) void scaled_few_kernel(fdh::ScaledArgs g) {
   __shared__ f32x4_t part[kFewWaves][FM][NF][64];
   const int M = g.m ? min(*g.m, g.n_rows) : g.n_rows;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, lg = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, lg = lane >> 4;
   const int K = g.K, nk = (K + kScaleBlock - 1) / kScaleBlock, ld = fd::scale_stride(K);
   const int n0 = blockIdx.x * 16 * NF;
   const uint8_t* sw = g.w_scale + static_cast<size_t>(n0 / kScaleBlock) * ld;
@@ -155,32 +150,38 @@ __global__ __launch_bounds__(kFewWaves * 64) void scaled_few_kernel(fdh::ScaledA
 #pragma unroll
   for (int j = 0; j < NF; ++j)
     w[j] = g.w + static_cast<size_t>(min(n0 + 4 * NF * (l16 >> 2) + 4 * j + (l16 & 3), g.N - 1)) * K;
+  float4 bias[NF];
+#pragma unroll
+  for (int j = 0; j < NF; ++j) bias[j] = g.bias ? *reinterpret_cast<const float4*>(g.bias + min(n0 + 4 * NF * lg + 4 * j, g.N - 4)) : make_float4(0, 0, 0, 0);
   for (int m0 = blockIdx.y * 16 * FM; m0 < M; m0 += gridDim.y * 16 * FM) {
     f32x4_t acc[FM][NF] = {};
     for (int kb = wave; kb < nk; kb += kFewWaves * DEEP) {
-      i32x8_t wf[DEEP][NF], af[DEEP][FM];
+      Piece wf[DEEP][NF], af[DEEP][FM];
       uint32_t s_w[DEEP], s_a[DEEP][FM];
 #pragma unroll
-      for (int d = 0; d < DEEP; ++d) {   // blocks past the last: zeros
-        const int b = kb + d * kFewWaves, k = b < nk ? b * kScaleBlock + 32 * lg : K, c = min(b, nk - 1);
+      for (int d = 0; d < DEEP; ++d) {
+        const int b = kb + d * kFewWaves, k = b * kScaleBlock + 32 * lg;
+        if (b >= nk) break;
 #pragma unroll
         for (int j = 0; j < NF; ++j) wf[d][j] = load32(w[j], k, K);
-        s_w[d] = sw[c];
+        s_w[d] = sw[b];
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
           const size_t row = min(m0 + 16 * i + l16, M - 1);
           af[d][i] = load32(g.a + row * K, k, K);
-          s_a[d][i] = g.a_scale[row * ld + c];
+          s_a[d][i] = g.a_scale[row * ld + b];
         }
       }
 #pragma unroll
       for (int d = 0; d < DEEP; ++d) {
+        const int b = kb + d * kFewWaves, k = b * kScaleBlock + 32 * lg;
+        if (b >= nk) break;
         typename Mma::frag wd[NF];
 #pragma unroll
-        for (int j = 0; j < NF; ++j) wd[j] = Mma::make(wf[d][j], s_w[d]);
+        for (int j = 0; j < NF; ++j) wd[j] = Mma::make(inside(wf[d][j], k, K), s_w[d]);
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-          const typename Mma::frag ad = Mma::make(af[d][i], s_a[d][i]);
+          const typename Mma::frag ad = Mma::make(inside(af[d][i], k, K), s_a[d][i]);
 #pragma unroll
           for (int j = 0; j < NF; ++j) acc[i][j] = Mma::mma(wd[j], ad, acc[i][j], s_w[d], s_a[d][i]);
         }
@@ -200,7 +201,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void scaled_few_kernel(fdh::ScaledA
         for (int p = 1; p < kFewWaves; ++p) sum[j] += part[p][wave][j][lane];
       }
       const int row = m0 + 16 * wave + l16;
-      store_row<KIND, NF>(g, row < M, row, n0 + 4 * NF * lg, sum);
+      store_row<KIND, NF>(g, row < M, row, n0 + 4 * NF * lg, sum, bias);
     }
     __syncthreads();
   }
@@ -218,12 +219,13 @@ struct Tile {
   static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
   static constexpr int BM = 32 * FI * WM, BN = 128 * WN;
   static constexpr int LOADS_A = BM / 8 / WAVES, LOADS_W = BN / 8 / WAVES;        // 8 rows of 128 bytes per wave-load
+  static constexpr int SCALE_WAVES = (BM + 63) / 64;                              // waves that load row scales; the others column scales
   static constexpr int ISSUED = LOADS_A + LOADS_W + 1;                            // and one of scales or bias
   static constexpr int SIDE = (BM + BN) * 8;                                      // chunk where a stage's scales begin
-  static constexpr int CHUNKS = SIDE + BM / 4 + 16;                               // row scales, then 256 bytes of column scales
+  static constexpr int CHUNKS = SIDE + SCALE_WAVES * 16 + 16;                     // row scales, then 256 bytes of column scales
   static constexpr int BIAS = STAGES * CHUNKS;                                    // four slots of the columns' bias
   static constexpr int TOTAL = BIAS + 4 * BN / 4;
-  static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && BM % 64 == 0 && BM / 64 < WAVES && BN <= 64 * WAVES, "whole wave-loads");
+  static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && WAVES % 2 == 0 && SCALE_WAVES < WAVES && BN <= 64 * WAVES, "whole wave-loads");
   static FD_DEVICE int swz(int r) { return (r >> 1) & 7; }
   // Column of LDS row p: fragment j of 128 columns holds every fourth, from j on, so that a lane of the product
   // has four consecutive columns in its four fragments.
@@ -240,13 +242,14 @@ constexpr uint32_t kNowhere = 0x80000000u;   // an offset past every buffer: loa
 // Cache policy of wide results: non-temporal, so that they leave the L2 to the operands (9828 x 4608 x 1536 to bf16
 // 77.4 -> 74.8 us, x 1536 x 6144 84.3 -> 79.7; codes, a quarter to a half of the bytes, the same either way).
 constexpr int kStream = 2;
-// 16 (4) bytes per lane from buffer offset voff + soff into LDS at lds + 16 (4) * lane.  In assembly so
-// that the compiler does not wait for it before unrelated LDS reads.
+// 16 (4) bytes per lane from buffer offset voff + soff into LDS at lds + MORE + 16 (4) * lane.  In assembly so that
+// the compiler does not wait for it before unrelated LDS reads.  A load to LDS takes M0 one wait state after its write.
+template <int MORE>
 FD_DEVICE void dma16(uint32_t lds, uint32_t voff, i32x4_t rsrc, uint32_t soff) {
-  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(lds), "v"(voff), "s"(rsrc), "s"(soff));
+  asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(lds), "v"(voff), "s"(rsrc), "s"(soff), "n"(MORE) : "scc");
 }
 FD_DEVICE void dma4(uint32_t lds, uint32_t voff, i32x4_t rsrc, uint32_t soff) {
-  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, %3 offen lds" : : "s"(lds), "v"(voff), "s"(rsrc), "s"(soff));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" : : "s"(lds), "v"(voff), "s"(rsrc), "s"(soff));
 }
 // This wave's LDS reads are done; then the barrier.
 FD_DEVICE void wait_reads_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
@@ -340,13 +343,14 @@ struct Rows32 {
 // The K-steps of all of a workgroup's tiles are one sequence: the loads run STAGES steps ahead of the
 // products, into the next tile too, and a tile's results leave while the next one's first stages land.
 //
-// A step's eight sub-steps s = (half of K, column fragment) each read one weight fragment two sub-steps
-// ahead.  After sub-step 1 the wave has read its rows, after sub-step 5 its columns; a barrier there frees
-// that part of the stage for the load STAGES steps on, which goes out a few instructions at a time behind
-// products.  The second barrier also publishes the next stage, whose first fragments are read behind
-// sub-steps 6 and 7, so that no sub-step waits for LDS or for the barrier with nothing to compute.  A step
-// is one basic block: across branches the compiler gathers the products at the end.  K has at least STAGES
-// blocks.
+// A step's eight sub-steps are s = (half of K, column fragment).  Waves of 32 rows (FI = 1) hold a whole step's
+// operands in registers: sub-steps 0 and 1 read what is left of the stage, the barrier before sub-step 4 frees it and
+// publishes the next one, whose first half sub-steps 4 and 5 read.  Waves of 64 rows have registers for half of that:
+// each sub-step reads one weight fragment two ahead, a barrier after sub-step 1 frees the rows and one after
+// sub-step 5 the columns, the latter also publishing the next stage.  The load STAGES steps on goes out behind the
+// barriers a few instructions at a time between products, so that no sub-step waits with nothing to compute.  A step
+// is one basic block: across branches the compiler gathers the products at the end.  A wave alone on its SIMD is
+// bound by the number of instructions it issues, some 100 a step of 8 products.  K has at least STAGES blocks.
 template <class T, int KIND, class Mma>
 FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
   constexpr int FI = T::FI, STAGES = T::STAGES;
@@ -378,15 +382,15 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
   int turn = 3;
   uint32_t off_a[T::LOADS_A], off_w[T::LOADS_W], off_side;
   auto row_of = [&](int q) { return (wave + T::WAVES * q) * 8 + (lane >> 3); };
-  auto chunk_of = [&](int q) { return (lane & 7) ^ T::swz(row_of(q)); };
+  const int chunk = (lane & 7) ^ T::swz(row_of(0));   // of every load's row: 8 WAVES q leaves the swizzle
   auto aim = [&] {   // the tile's bases, and this lane's row and chunk of each load (rows past the end re-read the last)
     ra = buffer_of(g.a + static_cast<size_t>(lm0) * K);
     rw = buffer_of(g.w + static_cast<size_t>(ln0) * K);
 #pragma unroll
-    for (int q = 0; q < T::LOADS_A; ++q) off_a[q] = static_cast<uint32_t>(min(row_of(q), M - lm0 - 1)) * static_cast<uint32_t>(K) + 16 * chunk_of(q);
+    for (int q = 0; q < T::LOADS_A; ++q) off_a[q] = static_cast<uint32_t>(min(row_of(q), M - lm0 - 1)) * static_cast<uint32_t>(K) + 16 * chunk;
 #pragma unroll
-    for (int q = 0; q < T::LOADS_W; ++q) off_w[q] = static_cast<uint32_t>(min(T::column(row_of(q)), g.N - ln0 - 1)) * static_cast<uint32_t>(K) + 16 * chunk_of(q);
-    if (wave < T::BM / 64) {
+    for (int q = 0; q < T::LOADS_W; ++q) off_w[q] = static_cast<uint32_t>(min(T::column(row_of(q)), g.N - ln0 - 1)) * static_cast<uint32_t>(K) + 16 * chunk;
+    if (wave < T::SCALE_WAVES) {
       rside = buffer_of(g.a_scale + static_cast<size_t>(lm0) * ld);
       off_side = static_cast<uint32_t>(min(64 * wave + lane, M - lm0 - 1)) * static_cast<uint32_t>(ld);
     } else {
@@ -400,62 +404,86 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
     dma4(ring_at + static_cast<uint32_t>(T::BIAS * 16 + turn * T::BN * 4 + c * 4), static_cast<uint32_t>(ln0 + c + lane) * 4,
          buffer_of(g.bias, g.bias ? 4u * g.N : 0u), 0);
   };
-  // Load q of the rows and of the columns into a slot, and the scales.  The chunks past K of a last,
-  // shorter K-block read zeros.
-  auto issue_a = [&](int slot, int q) {
-    const uint32_t at = ring_at + static_cast<uint32_t>(slot * T::CHUNKS * 16 + wave * 1024);
-    dma16(at + T::WAVES * q * 1024, lk * kScaleBlock + 16 * chunk_of(q) < K ? off_a[q] : kNowhere, ra, static_cast<uint32_t>(lk * kScaleBlock));
+  // The chunks past K of a last, shorter K-block read zeros: called before that block's loads.  The next tile's aim
+  // sets the offsets anew.
+  auto last_block = [&] {
+    const bool inside = (nk - 1) * kScaleBlock + 16 * chunk < K;
+#pragma unroll
+    for (int q = 0; q < T::LOADS_A; ++q) off_a[q] = inside ? off_a[q] : kNowhere;
+#pragma unroll
+    for (int q = 0; q < T::LOADS_W; ++q) off_w[q] = inside ? off_w[q] : kNowhere;
   };
-  auto issue_w = [&](int slot, int q) {
-    const uint32_t at = ring_at + static_cast<uint32_t>(slot * T::CHUNKS * 16 + T::BM * 128 + wave * 1024);
-    dma16(at + T::WAVES * q * 1024, lk * kScaleBlock + 16 * chunk_of(q) < K ? off_w[q] : kNowhere, rw, static_cast<uint32_t>(lk * kScaleBlock));
+  // Loads `from` to `to` of the rows (q < LOADS_A) and of the columns (the rest) into a slot, and the scales.
+  constexpr int kSlot = T::CHUNKS * 16;
+  const uint32_t wave_at = ring_at + wave * 1024;
+  auto issue = [&](uint32_t slot_at, auto from, auto to) {
+    constexpr int FROM = decltype(from)::value, TO = decltype(to)::value;
+    auto go = [&](auto self, auto i) {
+      constexpr int q = decltype(i)::value;
+      if constexpr (q < TO) {
+        // tile rows are 128 bytes, the columns' follow the rows', and WAVES loads of 1024 bytes lie between q and q + 1
+        if constexpr (q < T::LOADS_A) dma16<T::WAVES * q * 1024>(wave_at + slot_at, off_a[q], ra, static_cast<uint32_t>(lk * kScaleBlock));
+        else dma16<T::WAVES * q * 1024>(wave_at + slot_at, off_w[q - T::LOADS_A], rw, static_cast<uint32_t>(lk * kScaleBlock));
+        self(self, std::integral_constant<int, q + 1>{});
+      }
+    };
+    go(go, std::integral_constant<int, FROM>{});
   };
-  auto issue_scales = [&](int slot) {
-    dma4(ring_at + static_cast<uint32_t>(slot * T::CHUNKS * 16 + T::SIDE * 16 + min(wave, T::BM / 64) * 256), off_side, rside, static_cast<uint32_t>(lk & ~3));
+  auto issue_scales = [&](uint32_t slot_at) {
+    dma4(ring_at + slot_at + static_cast<uint32_t>(T::SIDE * 16 + min(wave, T::SCALE_WAVES) * 256), off_side, rside, static_cast<uint32_t>(lk & ~3));
   };
 
   // ---- the products
   const int arow = 32 * FI * wm + l32;
   const int wrow = 128 * wn + l32;
-  auto read = [&](const uint4* sm, int row, int swz, int kh) {
-    const int c = 4 * kh + 2 * half;
-    const uint4 lo = sm[row * 8 + (c ^ swz)], hi = sm[row * 8 + ((c + 1) ^ swz)];
+  // byte offsets in a stage of this lane's two chunks of a half K-block, of its first row and its first column (32 rows on: 4096 bytes)
+  uint32_t at_a[2][2], at_w[2][2];
+#pragma unroll
+  for (int kh = 0; kh < 2; ++kh)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      at_a[kh][c] = arow * 128 + ((4 * kh + 2 * half + c) ^ T::swz(arow)) * 16;
+      at_w[kh][c] = (T::BM + wrow) * 128 + ((4 * kh + 2 * half + c) ^ T::swz(wrow)) * 16;
+    }
+  const char* lds = reinterpret_cast<const char*>(ring);
+  auto read = [&](const char* lo_at, const char* hi_at) {
+    const uint4 lo = *reinterpret_cast<const uint4*>(lo_at), hi = *reinterpret_cast<const uint4*>(hi_at);
     return i32x8_t{static_cast<int>(lo.x), static_cast<int>(lo.y), static_cast<int>(lo.z), static_cast<int>(lo.w),
                    static_cast<int>(hi.x), static_cast<int>(hi.y), static_cast<int>(hi.z), static_cast<int>(hi.w)};
   };
-  i32x8_t a[2][FI], w[4];
-  uint32_t sa[FI], sw, sa_next[FI], sw_next;
-  auto read_a = [&](const uint4* sm, int kh) {
+  constexpr int RING = FI == 1 ? 8 : 4;   // weight fragments in registers
+  i32x8_t a[2][FI], w[RING];
+  uint32_t sa[FI], sw, sa_next[FI], sw_next;   // a step's scale bytes, and the next one's words as they come from LDS
+  auto read_a = [&](uint32_t slot_at, int kh) {
 #pragma unroll
-    for (int i = 0; i < FI; ++i) a[kh][i] = read(sm, arow + 32 * i, T::swz(arow), kh);   // 32 i leaves the swizzle
+    for (int i = 0; i < FI; ++i) a[kh][i] = read(lds + (slot_at + at_a[kh][0]) + 4096 * i, lds + (slot_at + at_a[kh][1]) + 4096 * i);
   };
-  auto read_w = [&](const uint4* sm, int s) {
-    w[s & 3] = read(sm + T::BM * 8, wrow + 32 * (s & 3), T::swz(wrow), s >> 2);
+  auto read_w = [&](uint32_t slot_at, int s) {
+    const int kh = s >> 2, j = s & 3;
+    w[s % RING] = read(lds + (slot_at + at_w[kh][0]) + 4096 * j, lds + (slot_at + at_w[kh][1]) + 4096 * j);
   };
-  auto read_scales = [&](const uint4* sm, int kb) {
-    const uint32_t* side = reinterpret_cast<const uint32_t*>(sm + T::SIDE);
+  auto read_scales = [&](uint32_t slot_at) {
+    const uint32_t* side = reinterpret_cast<const uint32_t*>(lds + slot_at + T::SIDE * 16);
 #pragma unroll
-    for (int i = 0; i < FI; ++i) sa_next[i] = side[arow + 32 * i] >> (8 * (kb & 3));
-    sw_next = side[T::BM + wn] >> (8 * (kb & 3));
+    for (int i = 0; i < FI; ++i) sa_next[i] = side[arow + 32 * i];
+    sw_next = side[64 * T::SCALE_WAVES + wn];
   };
 
   aim();
 #pragma unroll
   for (int p = 0; p < STAGES; ++p) {
-#pragma unroll
-    for (int q = 0; q < T::LOADS_A; ++q) issue_a(p, q);
-#pragma unroll
-    for (int q = 0; q < T::LOADS_W; ++q) issue_w(p, q);
-    issue_scales(p);
+    if (lk == nk - 1) last_block();
+    issue(p * kSlot, std::integral_constant<int, 0>{}, std::integral_constant<int, T::LOADS_A + T::LOADS_W>{});
+    issue_scales(p * kSlot);
     ++lk;
   }
   wait_barrier<(STAGES - 1) * T::ISSUED, 0>(0);
-  read_a(ring, 0);
-  read_w(ring, 0);
-  read_w(ring, 1);
-  read_scales(ring, 0);
+  read_a(0, 0);
+#pragma unroll
+  for (int s = 0; s < RING / 2; ++s) read_w(0, s);
+  read_scales(0);
 
-  int slot = 0;
+  uint32_t slot = 0;   // byte offset of the step's stage
   int stored = 0;   // in a tile's first step: the previous tile's stores were issued after the last stage's loads
   for (;;) {
     const int m0 = lm0, n0 = ln0;
@@ -470,34 +498,50 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
         if (more) aim();
       }
       for (const int end = part == 0 ? nk - STAGES : nk; kb < end; ++kb, ++lk) {
-        const int next = slot + 1 == STAGES ? 0 : slot + 1;
-        const uint4 *sm = ring + slot * T::CHUNKS, *sn = ring + next * T::CHUNKS;
+        if (lk == nk - 1) last_block();
+        const uint32_t next = slot == (STAGES - 1) * kSlot ? 0 : slot + kSlot;
 #pragma unroll
-        for (int i = 0; i < FI; ++i) sa[i] = sa_next[i];
-        sw = sw_next;
+        for (int i = 0; i < FI; ++i) sa[i] = sa_next[i] >> (8 * (kb & 3));
+        sw = sw_next >> (8 * (kb & 3));
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
-          if (s == 2) wait_reads_barrier();
-          if (s == 6) wait_barrier<(STAGES - 2) * T::ISSUED + T::LOADS_A, kStores>(stored);
-          if (s == 0) read_a(sm, 1);
-          if (s < 6) read_w(sm, s + 2);
-          if (s == 6) {
-            read_a(sn, 0);
-            read_w(sn, 0);
-            read_scales(sn, kb + 1 == nk ? 0 : kb + 1);
+          if constexpr (FI == 1) {
+            if (s == 4) wait_barrier<(STAGES - 2) * T::ISSUED, kStores>(stored);
+            if (s == 0) read_a(slot, 1);
+            if (s < 2) read_w(slot, 2 * s + 4), read_w(slot, 2 * s + 5);
+            if (s == 4) {
+              read_a(next, 0);
+              read_scales(next);
+            }
+            if (s == 4 || s == 5) read_w(next, 2 * s - 8), read_w(next, 2 * s - 7);
+          } else {
+            if (s == 2) wait_reads_barrier();
+            if (s == 6) wait_barrier<(STAGES - 2) * T::ISSUED + T::LOADS_A, kStores>(stored);
+            if (s == 0) read_a(slot, 1);
+            if (s < 6) read_w(slot, s + 2);
+            if (s == 6) {
+              read_a(next, 0);
+              read_w(next, 0);
+              read_scales(next);
+            }
+            if (s == 7) read_w(next, 1);
           }
-          if (s == 7) read_w(sn, 1);
-          const typename Mma::frag wf = Mma::make(w[s & 3], sw);
+          const typename Mma::frag wf = Mma::make(w[s % RING], sw);
 #pragma unroll
           for (int i = 0; i < FI; ++i) acc[i][s & 3] = Mma::mma(Mma::make(a[s >> 2][i], sa[i]), wf, acc[i][s & 3], sa[i], sw);
           __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int q = 0; q < T::LOADS_A; ++q)
-            if (s == 2 + q * 4 / T::LOADS_A) issue_a(slot, q);
-#pragma unroll
-          for (int q = 0; q < T::LOADS_W; ++q)
-            if (s == 6 + q * 2 / T::LOADS_W) issue_w(slot, q);
-          if (s == 7) issue_scales(slot);
+          if constexpr (FI == 1) {
+            if (s == 4) issue(slot, std::integral_constant<int, 0>{}, std::integral_constant<int, T::LOADS_A / 2>{});
+            if (s == 5) issue(slot, std::integral_constant<int, T::LOADS_A / 2>{}, std::integral_constant<int, T::LOADS_A>{});
+          } else {
+            if (s == 2) issue(slot, std::integral_constant<int, 0>{}, std::integral_constant<int, T::LOADS_A / 2>{});
+            if (s == 4) issue(slot, std::integral_constant<int, T::LOADS_A / 2>{}, std::integral_constant<int, T::LOADS_A>{});
+          }
+          if (s == 6) issue(slot, std::integral_constant<int, T::LOADS_A>{}, std::integral_constant<int, T::LOADS_A + T::LOADS_W / 2>{});
+          if (s == 7) {
+            issue(slot, std::integral_constant<int, T::LOADS_A + T::LOADS_W / 2>{}, std::integral_constant<int, T::LOADS_A + T::LOADS_W>{});
+            issue_scales(slot);
+          }
           __builtin_amdgcn_sched_barrier(0);
         }
         slot = next;
@@ -530,16 +574,18 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the repeats of the last stage
 }
 
-using TileLarge = Tile<2, 4, 2, 2>;   // 256 x 256, one workgroup per CU
-using TileSmall = Tile<1, 4, 1, 2>;   // 128 x 128, two
+using Tile64 = Tile<1, 2, 1, 3>;      // 64 x 128, two workgroups per CU
+using Tile128 = Tile<1, 4, 1, 2>;     // 128 x 128, two
+using TileDeep = Tile<1, 4, 1, 4>;    // 128 x 128, one
+using TileLarge = Tile<2, 4, 2, 2>;   // 256 x 256, one
 
 // Where both kernels are launched (cus > 0), the one that the row count does not call for ends at once.
 template <int KIND, class Mma, class T, int PER_CU>
-__global__ __launch_bounds__(T::THREADS, PER_CU * T::WAVES / 4) void scaled_tile_kernel(fdh::ScaledArgs g, int cus) {
+__global__ __launch_bounds__(T::THREADS, (PER_CU * T::WAVES + 3) / 4) void scaled_tile_kernel(fdh::ScaledArgs g, int cus) {
   __shared__ uint4 ring[T::TOTAL];
-  static_assert(T::TOTAL * 16 * PER_CU <= 160 * 1024 && T::STAGES <= fd::kTileBlocks, "the LDS of a CU");
+  static_assert(T::TOTAL * 16 * PER_CU <= 160 * 1024, "the LDS of a CU");
   const int M = g.m ? min(*g.m, g.n_rows) : g.n_rows;
-  if (M <= 0 || (cus > 0 && fd::scaled_large(M, g.N, g.K, KIND == kToCodes, cus) != (PER_CU == 1))) return;
+  if (M <= 0 || (cus > 0 && fd::scaled_large(M, g.N, g.K, KIND == kToCodes, cus) != (T::BM == TileLarge::BM))) return;
   scaled_tiles<T, KIND, Mma>(g, M, ring);
 }
 
@@ -558,19 +604,38 @@ hipError_t launch_scaled_linear(const ScaledArgs& g, hipStream_t s) {
         const int gx = (g.N + 16 * NF - 1) / (16 * NF), gy = (g.n_rows + 16 * FM - 1) / (16 * FM);
         scaled_few_kernel<KIND, Mma, FM, NF, decltype(deep)::value><<<dim3(gx, gy < 4096 ? gy : 4096), kFewWaves * 64, 0, s>>>(g);
       };
-      using std::integral_constant;
-      if constexpr (codes) few(integral_constant<int, 1>{}, integral_constant<int, 8>{}, integral_constant<int, 2>{});
-      else if (g.n_rows <= 16 && g.K <= 2 * kFewWaves * kScaleBlock) few(integral_constant<int, 1>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{});
-      else if (g.n_rows <= 16) few(integral_constant<int, 1>{}, integral_constant<int, 1>{}, integral_constant<int, 6>{});
-      else few(integral_constant<int, 4>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{});
+      const std::integral_constant<int, 1> one{};
+      const std::integral_constant<int, 2> two{};
+      const std::integral_constant<int, 3> three{};
+      const std::integral_constant<int, 4> four{};
+      if constexpr (codes) few(one, std::integral_constant<int, 8>{}, one);
+      else if (fd::scaled_few_wide(g.N, num_cus())) {
+        if (g.n_rows <= 16) few(one, two, two);
+        else if (g.n_rows <= 32) few(two, two, two);
+        else few(four, two, one);
+      } else {
+        if (g.n_rows <= 16) few(one, one, three);
+        else if (g.n_rows <= 32) few(two, one, two);
+        else few(four, one, one);
+      }
       return;
     }
     const int cus = num_cus() / 8 * 8;   // the tile order counts on whole rounds of the 8 XCDs
     const bool both = g.m && fd::scaled_both(g.n_rows, g.N, g.K, codes, cus), large = !g.m && fd::scaled_large(g.n_rows, g.N, g.K, codes, cus);
-    const long long tiles = static_cast<long long>((g.n_rows + 127) / 128) * ((g.N + 127) / 128);
-    const int grid = static_cast<int>(tiles < 2 * cus ? (tiles + 7) / 8 * 8 : 2 * cus);
-    if (!large) scaled_tile_kernel<KIND, Mma, TileSmall, 2><<<grid, TileSmall::THREADS, 0, s>>>(g, both ? cus : 0);
-    if (both || large) scaled_tile_kernel<KIND, Mma, TileLarge, 1><<<cus, TileLarge::THREADS, 0, s>>>(g, both ? cus : 0);
+    auto tiles = [&](auto tile, auto per_cu, int check) {
+      using T = decltype(tile);
+      constexpr int PER_CU = decltype(per_cu)::value;
+      const long long all = static_cast<long long>((g.n_rows + T::BM - 1) / T::BM) * ((g.N + T::BN - 1) / T::BN), most = PER_CU * cus;
+      scaled_tile_kernel<KIND, Mma, T, PER_CU><<<static_cast<int>(all < most ? (all + 7) / 8 * 8 : most), T::THREADS, 0, s>>>(g, check);
+    };
+    using std::integral_constant;
+    const fd::ScaledTile small = fd::scaled_tile(g.n_rows, g.N, g.K, cus);
+    if (both || !large) {
+      if (small == fd::kTile64) tiles(Tile64{}, integral_constant<int, 2>{}, 0);
+      else if (small == fd::kTileDeep) tiles(TileDeep{}, integral_constant<int, 1>{}, 0);
+      else tiles(Tile128{}, integral_constant<int, 2>{}, both ? cus : 0);
+    }
+    if (both || large) tiles(TileLarge{}, integral_constant<int, 1>{}, both ? cus : 0);
   };
   if (g.y_q) run(std::integral_constant<int, kToCodes>{}, Mma8{});
   else if (g.y_bf16) run(std::integral_constant<int, kToBf16>{}, Mma8{});

@@ -287,6 +287,27 @@ def test_scaled_linear_sizes(M, N, K, to):
     check_linear(y, ys, *case, False, to, M)
 
 
+@pytest.mark.parametrize("M,N,K,m", [(700, 1040, 272, 700), (700, 1040, 1168, 65), (1600, 1552, 400, 1600), (1600, 1552, 512, 129), (1590, 1552, 1072, None),
+                                     (2500, 2064, 272, 2400)])
+@pytest.mark.parametrize("to,gelu", [("bf16", True), ("f32", False), ("8", True)])
+def test_scaled_linear_tiles(M, N, K, m, to, gelu):
+    """Tiles of 64 rows, of 128 with four stages and with two: as few K-blocks as their stages, and more."""
+    gh.say(f"linear M={M} N={N} K={K} m={m} to={to} gelu={gelu}")
+    a, sa, w, sw, bias = linear_case(M, N, K, 2)
+    y, ys = run_linear(a, sa, w, sw, bias, gelu, to, M, m)
+    check_linear(y, ys, a, sa, w, sw, bias, gelu, to, M if m is None else m)
+
+
+@pytest.mark.parametrize("M,N,K,rows", [(5, 4112, 400, 9), (20, 4128, 1088, 32), (50, 4112, 1296, 64), (33, 1040, 1168, 40), (300, 4112, 240, 310)])
+@pytest.mark.parametrize("to,gelu", [("bf16", True), ("f32", False), ("8", False)])
+def test_scaled_linear_few_rows(M, N, K, rows, to, gelu):
+    """Workgroups of 32 columns, last ones of 16, and K-blocks that leave some of the waves without one."""
+    gh.say(f"linear M={M} N={N} K={K} rows={rows} to={to} gelu={gelu}")
+    case = linear_case(M, N, K, 3)
+    y, ys = run_linear(*case, gelu, to, rows, M)
+    check_linear(y, ys, *case, gelu, to, M)
+
+
 @pytest.mark.parametrize("M", [5, 200])
 def test_scaled_linear_bad_blocks(M):
     """A NaN block of a row makes that row NaN, one of the weights its 128 columns; the rest is as without it."""
