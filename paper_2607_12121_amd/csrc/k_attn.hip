@@ -72,7 +72,7 @@ FD_DEVICE int32x4_t settled(int32x4_t r) {
 // 16 bytes per lane from buffer offset voff + soff (soff wave-uniform) into LDS at
 // lds_addr + 16 * lane.
 FD_DEVICE void lds_dma16(uint32_t lds_addr, uint32_t voff, int32x4_t rsrc, uint32_t soff) {
-  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                :
                : "s"(lds_addr), "v"(voff), "s"(rsrc), "s"(soff));
 }
