@@ -8,8 +8,8 @@ namespace fd {
 
 // Row capacities up to which the few-row kernel runs (a larger capacity with few rows at work runs the tiles).  Results
 // in 8 bits, whose blocks want 128 columns of a workgroup, leave too few workgroups for it and run the tiles from one
-// row on: 1 x 6144 x 1536 with GELU 11.9 us, in tiles 10.2.  Otherwise 64: 32 x 1536 x 6144 12.0 us, in tiles 20.5;
-// 64 rows of it 19.2 and 20.7.
+// row on: 1 x 6144 x 1536 with GELU 11.9 us, in tiles 10.3.  Otherwise 64: 32 x 1536 x 6144 12.0 us, in tiles 21.2;
+// 64 rows of it 19.2 and 21.3.
 FD_RULE int scaled_few_rows(bool codes) { return codes ? 0 : 64; }
 // Its workgroups take 16 columns, or 32 where those of 16 would not each have a CU: every workgroup reads all of the
 // rows.  16 columns and 32, us: 16 x 1536 x 6144 8.9 and 11.4, 16 x 4608 x 6144 14.9 and 11.4, 64 x 4608 x 1536 10.2
@@ -18,18 +18,11 @@ FD_RULE bool scaled_few_wide(int N, int cus) { return (N + 15) / 16 > cus; }
 // The tiles' loads run two or more K-blocks ahead; fewer blocks than three run the few-row kernel at any size.
 constexpr int kTileBlocks = 3;
 
-// Tiles of few workgroups, which a CU has one of: nothing runs beside it while it waits, and what bounds it is the
-// number of K-blocks that it walks.  So the smallest tile whose workgroups each have a CU, and more stages of loads in
-// flight (three, four) than the two of the tiles that run in pairs.  Microseconds to bf16 in tiles of 64 rows / 128
-// rows, four stages / 128 rows, two stages, two a CU: 512 x 1536 x 6144 (96 tiles of 64) 20.7 / 26.0 / 35.5;
-// 1312 x 1024 x 4096 (168) 15.5 / 19.0 / 24.2; 1664 x 1536 x 6144 (156 of 128) 32.5 / 26.7 / 36.0; 512 x 4608 x 1536
-// (144) 10.5 / 10.7 / 11.6; 1664 x 4608 x 1536 (468) 18.5 / 17.7 / 14.7.
-enum ScaledTile { kTile64, kTileDeep, kTile128 };
-FD_RULE ScaledTile scaled_tile(int M, int N, int K, int cus) {
-  const long long columns = (N + 127) / 128;
-  if ((M + 63) / 64 * columns <= cus) return kTile64;
-  return (M + 127) / 128 * columns <= cus && K > 3 * 128 ? kTileDeep : kTile128;
-}
+// 64 x 128 tiles with three stages of loads instead of 128 x 128 with two, where each has a CU: nothing runs beside a
+// workgroup that is alone while it waits, and what bounds it is the K-blocks that it walks.  To bf16, us: 512 x 1536 x
+// 6144 (96 tiles of 64 rows) 21.9 and 26.9, 1312 x 1024 x 4096 (168) 16.1 and 20.0; 512 x 4608 x 1536 (288) 10.4 and
+// 9.9, 1664 x 1536 x 6144 (312) 32.0 and 28.2.
+FD_RULE bool scaled_small(int M, int N, int cus) { return static_cast<long long>((M + 63) / 64) * ((N + 127) / 128) <= cus; }
 
 // 256 x 256 tiles, one workgroup per CU, instead of 128 x 128, two: half the LDS and L2 traffic per flop, but nothing
 // to run while results leave.  Worth it where its rounds are full.  To bf16, 128 and 256 tiles: 9828 x 1536 x 6144 (234

@@ -343,14 +343,14 @@ struct Rows32 {
 // The K-steps of all of a workgroup's tiles are one sequence: the loads run STAGES steps ahead of the
 // products, into the next tile too, and a tile's results leave while the next one's first stages land.
 //
-// A step's eight sub-steps are s = (half of K, column fragment).  Waves of 32 rows (FI = 1) hold a whole step's
-// operands in registers: sub-steps 0 and 1 read what is left of the stage, the barrier before sub-step 4 frees it and
-// publishes the next one, whose first half sub-steps 4 and 5 read.  Waves of 64 rows have registers for half of that:
-// each sub-step reads one weight fragment two ahead, a barrier after sub-step 1 frees the rows and one after
-// sub-step 5 the columns, the latter also publishing the next stage.  The load STAGES steps on goes out behind the
-// barriers a few instructions at a time between products, so that no sub-step waits with nothing to compute.  A step
-// is one basic block: across branches the compiler gathers the products at the end.  A wave alone on its SIMD is
-// bound by the number of instructions it issues, some 100 a step of 8 products.  K has at least STAGES blocks.
+// A step's eight sub-steps s = (half of K, column fragment) each read one weight fragment two sub-steps
+// ahead.  After sub-step 1 the wave has read its rows, after sub-step 5 its columns; a barrier there frees
+// that part of the stage for the load STAGES steps on, which goes out a few instructions at a time behind
+// products.  The second barrier also publishes the next stage, whose first fragments are read behind
+// sub-steps 6 and 7, so that no sub-step waits for LDS or for the barrier with nothing to compute.  (One barrier
+// in the middle of a step, with its operands in registers: the loads have 5 sub-steps to land instead of 7 and 10,
+// 1664 x 1536 x 6144 in 128 x 128 tiles 36.4 us against 28.2.)  A step is one basic block: across branches the
+// compiler gathers the products at the end.  K has at least STAGES blocks.
 template <class T, int KIND, class Mma>
 FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
   constexpr int FI = T::FI, STAGES = T::STAGES;
@@ -451,8 +451,7 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
     return i32x8_t{static_cast<int>(lo.x), static_cast<int>(lo.y), static_cast<int>(lo.z), static_cast<int>(lo.w),
                    static_cast<int>(hi.x), static_cast<int>(hi.y), static_cast<int>(hi.z), static_cast<int>(hi.w)};
   };
-  constexpr int RING = FI == 1 ? 8 : 4;   // weight fragments in registers
-  i32x8_t a[2][FI], w[RING];
+  i32x8_t a[2][FI], w[4];
   uint32_t sa[FI], sw, sa_next[FI], sw_next;   // a step's scale bytes, and the next one's words as they come from LDS
   auto read_a = [&](uint32_t slot_at, int kh) {
 #pragma unroll
@@ -460,7 +459,7 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
   };
   auto read_w = [&](uint32_t slot_at, int s) {
     const int kh = s >> 2, j = s & 3;
-    w[s % RING] = read(lds + (slot_at + at_w[kh][0]) + 4096 * j, lds + (slot_at + at_w[kh][1]) + 4096 * j);
+    w[s & 3] = read(lds + (slot_at + at_w[kh][0]) + 4096 * j, lds + (slot_at + at_w[kh][1]) + 4096 * j);
   };
   auto read_scales = [&](uint32_t slot_at) {
     const uint32_t* side = reinterpret_cast<const uint32_t*>(lds + slot_at + T::SIDE * 16);
@@ -479,8 +478,8 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
   }
   wait_barrier<(STAGES - 1) * T::ISSUED, 0>(0);
   read_a(0, 0);
-#pragma unroll
-  for (int s = 0; s < RING / 2; ++s) read_w(0, s);
+  read_w(0, 0);
+  read_w(0, 1);
   read_scales(0);
 
   uint32_t slot = 0;   // byte offset of the step's stage
@@ -505,38 +504,22 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
         sw = sw_next >> (8 * (kb & 3));
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
-          if constexpr (FI == 1) {
-            if (s == 4) wait_barrier<(STAGES - 2) * T::ISSUED, kStores>(stored);
-            if (s == 0) read_a(slot, 1);
-            if (s < 2) read_w(slot, 2 * s + 4), read_w(slot, 2 * s + 5);
-            if (s == 4) {
-              read_a(next, 0);
-              read_scales(next);
-            }
-            if (s == 4 || s == 5) read_w(next, 2 * s - 8), read_w(next, 2 * s - 7);
-          } else {
-            if (s == 2) wait_reads_barrier();
-            if (s == 6) wait_barrier<(STAGES - 2) * T::ISSUED + T::LOADS_A, kStores>(stored);
-            if (s == 0) read_a(slot, 1);
-            if (s < 6) read_w(slot, s + 2);
-            if (s == 6) {
-              read_a(next, 0);
-              read_w(next, 0);
-              read_scales(next);
-            }
-            if (s == 7) read_w(next, 1);
+          if (s == 2) wait_reads_barrier();
+          if (s == 6) wait_barrier<(STAGES - 2) * T::ISSUED + T::LOADS_A, kStores>(stored);
+          if (s == 0) read_a(slot, 1);
+          if (s < 6) read_w(slot, s + 2);
+          if (s == 6) {
+            read_a(next, 0);
+            read_w(next, 0);
+            read_scales(next);
           }
-          const typename Mma::frag wf = Mma::make(w[s % RING], sw);
+          if (s == 7) read_w(next, 1);
+          const typename Mma::frag wf = Mma::make(w[s & 3], sw);
 #pragma unroll
           for (int i = 0; i < FI; ++i) acc[i][s & 3] = Mma::mma(Mma::make(a[s >> 2][i], sa[i]), wf, acc[i][s & 3], sa[i], sw);
           __builtin_amdgcn_sched_barrier(0);
-          if constexpr (FI == 1) {
-            if (s == 4) issue(slot, std::integral_constant<int, 0>{}, std::integral_constant<int, T::LOADS_A / 2>{});
-            if (s == 5) issue(slot, std::integral_constant<int, T::LOADS_A / 2>{}, std::integral_constant<int, T::LOADS_A>{});
-          } else {
-            if (s == 2) issue(slot, std::integral_constant<int, 0>{}, std::integral_constant<int, T::LOADS_A / 2>{});
-            if (s == 4) issue(slot, std::integral_constant<int, T::LOADS_A / 2>{}, std::integral_constant<int, T::LOADS_A>{});
-          }
+          if (s == 2) issue(slot, std::integral_constant<int, 0>{}, std::integral_constant<int, T::LOADS_A / 2>{});
+          if (s == 4) issue(slot, std::integral_constant<int, T::LOADS_A / 2>{}, std::integral_constant<int, T::LOADS_A>{});
           if (s == 6) issue(slot, std::integral_constant<int, T::LOADS_A>{}, std::integral_constant<int, T::LOADS_A + T::LOADS_W / 2>{});
           if (s == 7) {
             issue(slot, std::integral_constant<int, T::LOADS_A + T::LOADS_W / 2>{}, std::integral_constant<int, T::LOADS_A + T::LOADS_W>{});
@@ -576,14 +559,13 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
 
 using Tile64 = Tile<1, 2, 1, 3>;      // 64 x 128, two workgroups per CU
 using Tile128 = Tile<1, 4, 1, 2>;     // 128 x 128, two
-using TileDeep = Tile<1, 4, 1, 4>;    // 128 x 128, one
 using TileLarge = Tile<2, 4, 2, 2>;   // 256 x 256, one
 
 // Where both kernels are launched (cus > 0), the one that the row count does not call for ends at once.
 template <int KIND, class Mma, class T, int PER_CU>
 __global__ __launch_bounds__(T::THREADS, (PER_CU * T::WAVES + 3) / 4) void scaled_tile_kernel(fdh::ScaledArgs g, int cus) {
   __shared__ uint4 ring[T::TOTAL];
-  static_assert(T::TOTAL * 16 * PER_CU <= 160 * 1024, "the LDS of a CU");
+  static_assert(T::TOTAL * 16 * PER_CU <= 160 * 1024 && T::STAGES <= fd::kTileBlocks, "the LDS of a CU");
   const int M = g.m ? min(*g.m, g.n_rows) : g.n_rows;
   if (M <= 0 || (cus > 0 && fd::scaled_large(M, g.N, g.K, KIND == kToCodes, cus) != (T::BM == TileLarge::BM))) return;
   scaled_tiles<T, KIND, Mma>(g, M, ring);
@@ -629,12 +611,8 @@ hipError_t launch_scaled_linear(const ScaledArgs& g, hipStream_t s) {
       scaled_tile_kernel<KIND, Mma, T, PER_CU><<<static_cast<int>(all < most ? (all + 7) / 8 * 8 : most), T::THREADS, 0, s>>>(g, check);
     };
     using std::integral_constant;
-    const fd::ScaledTile small = fd::scaled_tile(g.n_rows, g.N, g.K, cus);
-    if (both || !large) {
-      if (small == fd::kTile64) tiles(Tile64{}, integral_constant<int, 2>{}, 0);
-      else if (small == fd::kTileDeep) tiles(TileDeep{}, integral_constant<int, 1>{}, 0);
-      else tiles(Tile128{}, integral_constant<int, 2>{}, both ? cus : 0);
-    }
+    if (fd::scaled_small(g.n_rows, g.N, cus)) return tiles(Tile64{}, integral_constant<int, 2>{}, 0);
+    if (both || !large) tiles(Tile128{}, integral_constant<int, 2>{}, both ? cus : 0);
     if (both || large) tiles(TileLarge{}, integral_constant<int, 1>{}, both ? cus : 0);
   };
   if (g.y_q) run(std::integral_constant<int, kToCodes>{}, Mma8{});

@@ -291,7 +291,7 @@ def test_scaled_linear_sizes(M, N, K, to):
                                      (2500, 2064, 272, 2400)])
 @pytest.mark.parametrize("to,gelu", [("bf16", True), ("f32", False), ("8", True)])
 def test_scaled_linear_tiles(M, N, K, m, to, gelu):
-    """Tiles of 64 rows, of 128 with four stages and with two: as few K-blocks as their stages, and more."""
+    """Tiles of 64 rows and of 128, one of them or several a workgroup: as few K-blocks as their stages, and more."""
     gh.say(f"linear M={M} N={N} K={K} m={m} to={to} gelu={gelu}")
     a, sa, w, sw, bias = linear_case(M, N, K, 2)
     y, ys = run_linear(a, sa, w, sw, bias, gelu, to, M, m)

@@ -142,16 +142,16 @@ def test_product_rules(tmp_path):
 int main(int, char**) {
   int n, N, K, c;
   while (std::scanf("%d %d %d %d", &n, &N, &K, &c) == 4)
-    std::printf("%d %d %d %d %d\\n", fd::scaled_few_rows(c), (int)fd::scaled_large(n, N, K, c, 256), (int)fd::scaled_both(n, N, K, c, 256), (int)fd::scaled_tile(n, N, K, 256), (int)fd::scaled_few_wide(N, 256));
+    std::printf("%d %d %d %d %d\\n", fd::scaled_few_rows(c), (int)fd::scaled_large(n, N, K, c, 256), (int)fd::scaled_both(n, N, K, c, 256), (int)fd::scaled_small(n, N, 256), (int)fd::scaled_few_wide(N, 256));
 }
 ''')
     exe = tmp_path / "r"
     subprocess.run(["g++", "-std=c++17", f"-I{build.CSRC}", str(src), "-o", str(exe)], check=True)
-    d64, deep, d128 = 0, 1, 2
+    d64, d128 = 1, 0
     cases = [((9828, 1536, 6144, 0), (64, 1, 1, d128)), ((5000, 1536, 6144, 0), (64, 0, 0, d128)), ((9828, 6144, 1536, 1), (0, 0, 0, d128)),
-             ((32760, 1536, 6144, 0), (64, 1, 1, d128)), ((9828, 1536, 1536, 0), (64, 1, 0, d128)), ((1664, 1536, 6144, 0), (64, 0, 0, deep)),
+             ((32760, 1536, 6144, 0), (64, 1, 1, d128)), ((9828, 1536, 1536, 0), (64, 1, 0, d128)), ((1664, 1536, 6144, 0), (64, 0, 0, d128)),
              ((14280, 4096, 1024, 1), (0, 0, 0, d128)), ((1, 64, 64, 0), (64, 0, 0, d64)), ((1 << 30, 16, 16, 0), (64, 1, 1, d128)), ((9828, 4608, 1536, 0), (64, 1, 0, d128)),
-             ((4096, 6144, 1536, 0), (64, 0, 0, d128)), ((1312, 1024, 4096, 0), (64, 0, 0, d64)), ((1664, 1536, 400, 0), (64, 0, 0, deep)), ((1664, 1536, 384, 0), (64, 0, 0, d128))]
+             ((4096, 6144, 1536, 0), (64, 0, 0, d128)), ((1312, 1024, 4096, 0), (64, 0, 0, d64)), ((1366, 1536, 400, 0), (64, 0, 0, d128)), ((1344, 1536, 384, 0), (64, 0, 0, d64))]
     out = subprocess.run([str(exe)], input="\n".join(" ".join(map(str, c)) for c, _ in cases), capture_output=True, text=True, check=True).stdout
     for line, (case, want) in zip(out.splitlines(), cases):
         assert tuple(map(int, line.split())) == want + (int(case[1] > 4096),), case
