@@ -366,9 +366,10 @@ fd_status fd_scatter_update(const fd_plan* plan, int32_t C, float* x, const floa
  * most 448, and codes are rounded to nearest even, so a value is off by at most
  * 2^-4 of itself or 2^-10 of its scale.  A block that holds an infinity or a NaN has s = 255 and
  * NaN in every code.  Scale bytes are [rows or row blocks][fd_scale_stride(cols)]:
- * byte kb of a row belongs to columns 128 kb ..; the padding is neither read nor
- * written.  Row counts `m` are device int32 [1], at most n_rows (the capacity);
- * outputs past them are untouched.  Column counts are multiples of 16.
+ * byte kb of a row belongs to columns 128 kb ..; the padding is not written and its
+ * values are not used.  Row counts `m` are device int32 [1], at most n_rows (the capacity,
+ * up to 2^30); outputs past them are untouched.  Column counts are multiples of 16.
+ * Outputs overlap neither inputs nor each other.
  */
 int32_t fd_scale_stride(int32_t cols); /* ceil(cols / 128) rounded up to a multiple of 4; 0 for cols < 1 */
 
@@ -390,7 +391,7 @@ fd_status fd_quant_blocks(int32_t n_rows, int32_t cols, int32_t block_rows, cons
  *   a    = h[i] / sqrt(mean(h[i]^2) + eps) * weight * (1 + scale_b) + shift_b
  *   q, q_scale = a in codes, one scale per 128 columns; both null: only h's update
  * in fp32, a rounded once.  The squares are formed in fp32: rows whose magnitudes
- * exceed 2^63 overflow to a norm of zero.
+ * exceed 2^63 overflow to a norm of zero, and with eps 0 rows below 2^-75 divide by zero.
  *   h      device fp32 [n_rows][D], 16-byte aligned, updated in place
  *   y      device bf16 [n_rows][D] or null (a branch's output)
  *   gate, scale, shift  device fp32, request b's at + b * mod_stride, or null
@@ -417,7 +418,7 @@ typedef struct fd_rope {
   int32_t pairing;     /* FD_ROPE_INTERLEAVED or FD_ROPE_HALVES       */
   int32_t dim[4];      /* even, >= 2; their sum is at most the head dim */
   double theta[4];     /* > 0                                         */
-  double step[4];      /* finite; 1 for unscaled positions            */
+  double step[4];      /* finite; 1 for unscaled positions; a pair turns at most 2^20 times per position */
 } fd_rope;
 
 /*
@@ -432,8 +433,7 @@ typedef struct fd_rope {
  *          or null (row i is token i)
  *   q      device bf16 [n_rows][heads dh] (output)
  *   k_cache, v_cache  device bf16 [n_tokens][kv_heads dh]; rows of other tokens untouched
- * All 16-byte aligned but coord, idx and m; the outputs must not overlap qkv or
- * each other.
+ * All 16-byte aligned but coord, idx and m.
  */
 fd_status fd_rope_axes(int32_t n_rows, int32_t n_tokens, const fd_rope* rope, int32_t heads, int32_t kv_heads, int32_t dh,
                        const int32_t* coord, const uint16_t* qkv, const int32_t* idx, const int32_t* m, uint16_t* q,
@@ -449,8 +449,11 @@ fd_status fd_rope_axes(int32_t n_rows, int32_t n_tokens, const fd_rope* rope, in
  *   m           device int32 [1] or null (all n_rows)
  *   one output, 16-byte aligned: y_bf [n_rows][n_out] bf16, y_fp fp32, or y_q and
  *   y_scale (codes and row scales)
- * n_in and n_out are multiples of 16; weights below 2 GiB.  Codes, bias and outputs
- * 16-byte, scales 4-byte aligned; the output must not overlap the inputs.
+ * n_in and n_out are multiples of 16, at most 2^20; weights below 2 GiB.  Codes, bias and
+ * outputs 16-byte, scales 4-byte aligned.  Sums to bf16 and codes are off by up to 2^-10
+ * of the sum of the products' magnitudes (with random operands by some 1.5e-5 of their own
+ * size) before they are rounded, those to fp32 by fp32's roundings, with values below
+ * 2^-126 taken as zeros.
  */
 fd_status fd_scaled_linear(int32_t n_rows, int32_t n_out, int32_t n_in, const uint8_t* a, const uint8_t* a_scale,
                            const uint8_t* w, const uint8_t* w_scale, const float* bias, int32_t gelu, const int32_t* m,

@@ -146,6 +146,12 @@ fd_status check_cols(int cols) {
   return FD_OK;
 }
 
+// Row counts: a kernel's 32-bit row numbers run past the last by at most a launch's rows.
+fd_status check_rows(int rows) {
+  if (rows > (1 << 30)) return fdh::set_error("%d rows, more than 2^30", rows), FD_E_UNSUPPORTED;
+  return FD_OK;
+}
+
 // Checks a rotary descriptor and fills the kernel's sections and the turns of its pairs.
 fd_status rope_turns(const fd_rope* r, int dh, fdh::RopeArgs* g) {
   FD_REQUIRE(r, "rope is null");
@@ -160,8 +166,11 @@ fd_status rope_turns(const fd_rope* r, int dh, fdh::RopeArgs* g) {
     FD_REQUIRE(d >= 2 && d % 2 == 0 && d <= dh - 2 * g->pairs, "axis %d: %d values of a head of %d", a, d, dh);
     FD_REQUIRE(r->theta[a] > 0 && isfinite(r->theta[a]) && isfinite(r->step[a]), "axis %d: theta or step", a);
     g->dim[a] = d;
-    for (int j = 0; j < d / 2; ++j)
-      g->turns[g->pairs++] = r->step[a] * pow(r->theta[a], -2.0 * j / d) / 6.283185307179586;
+    for (int j = 0; j < d / 2; ++j) {
+      const double turns = r->step[a] * pow(r->theta[a], -2.0 * j / d) / 6.283185307179586;
+      FD_REQUIRE(fabs(turns) <= 1 << 20, "axis %d: %g turns per position", a, turns);
+      g->turns[g->pairs++] = turns;
+    }
   }
   return FD_OK;
 }
@@ -601,6 +610,7 @@ fd_status fd_quant_blocks(int32_t n_rows, int32_t cols, int32_t block_rows, cons
                           uint8_t* q, uint8_t* scale, fd_stream_t stream) {
   FD_REQUIRE(n_rows >= 1 && cols >= 1, "sizes must be positive");
   FD_REQUIRE(block_rows == 1 || block_rows == fd::kScaleBlock, "block_rows = %d, not 1 or 128", block_rows);
+  FD_TRY(check_rows(n_rows));
   FD_TRY(check_cols(cols));
   FD_REQUIRE(x && q && scale, "null pointer");
   FD_REQUIRE(!m || block_rows == 1, "a row count with 128-row blocks");
@@ -614,6 +624,7 @@ fd_status fd_rms_quant(int32_t n_rows, int32_t D, int32_t n_requests, float* h, 
                        const float* weight, const float* shift, const float* scale, int32_t mod_stride, float eps,
                        const int32_t* cu_q, const int32_t* m, uint8_t* q, uint8_t* q_scale, fd_stream_t stream) {
   FD_REQUIRE(n_rows >= 1 && D >= 1 && n_requests >= 1, "sizes must be positive");
+  FD_TRY(check_rows(n_rows));
   FD_TRY(check_cols(D));
   if (D > 12288) return fdh::set_error("D > 12288 unsupported"), FD_E_UNSUPPORTED;
   FD_REQUIRE(h && m && (cu_q || n_requests == 1), "null pointer");
@@ -635,6 +646,7 @@ fd_status fd_rope_axes(int32_t n_rows, int32_t n_tokens, const fd_rope* rope, in
                        const int32_t* coord, const uint16_t* qkv, const int32_t* idx, const int32_t* m, uint16_t* q,
                        uint16_t* k_cache, uint16_t* v_cache, fd_stream_t stream) {
   FD_REQUIRE(n_rows >= 1 && n_rows <= n_tokens, "%d rows of %d tokens", n_rows, n_tokens);
+  FD_TRY(check_rows(n_rows));
   FD_REQUIRE(heads >= 1 && kv_heads >= 1, "heads must be positive");
   FD_REQUIRE(coord && qkv && m && q && k_cache && v_cache, "null pointer");
   FD_REQUIRE(aligned(qkv, 16) && aligned(q, 16) && aligned(k_cache, 16) && aligned(v_cache, 16), "misaligned buffer");
@@ -652,6 +664,7 @@ fd_status fd_scaled_linear(int32_t n_rows, int32_t n_out, int32_t n_in, const ui
                            const uint8_t* w, const uint8_t* w_scale, const float* bias, int32_t gelu, const int32_t* m,
                            uint16_t* y_bf, float* y_fp, uint8_t* y_q, uint8_t* y_scale, fd_stream_t stream) {
   FD_REQUIRE(n_rows >= 1 && n_out >= 1 && n_in >= 1, "sizes must be positive");
+  FD_TRY(check_rows(n_rows));
   FD_TRY(check_cols(n_in));
   FD_TRY(check_cols(n_out));
   FD_REQUIRE(a && a_scale && w && w_scale, "null pointer");

@@ -7,7 +7,7 @@
 // One wave per row.  The angle is the same for every head, so lane p < dh / 2 forms the cosine and
 // sine of pair p once per row, from the angle in turns: pos * (step theta^.. / 2 pi) in fp64, whose
 // nearest integer is taken off before the rest, at most half a turn, is rounded to fp32 (an error of
-// 2^-26 of a turn at any position; in fp32 a position of 10^5 would be off by 2^-8 of a turn).  Each
+// 2^-26 of a turn for positions up to 10^8; in fp32 a position of 10^5 would be off by 2^-8 of a turn).  Each
 // lane then takes 8 consecutive values of a head at a time; 64 lanes are a whole number of heads, so
 // a lane meets the same place in every head and keeps its cosines and sines in registers.
 #include "fd_scaled.h"

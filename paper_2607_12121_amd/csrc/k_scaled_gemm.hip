@@ -22,7 +22,7 @@ enum { kToBf16, kToF32, kToCodes };
 //   largest of them (measured: 1 + 2^-14 gives 1 within such a group, and is exact across groups and
 //   with the accumulator), which leaves random operands' sums off by 1.5e-5 of their size.
 //   Outputs of 8 (bf16) or 4 (e4m3) bits of mantissa round by 100 times that at least.
-// - exact: the codes times their scales as bf16 (exact) through v_mfma_f32_16x16x32_bf16, half the
+// - exact: the codes times their scales as bf16 (exact from 2^-126 on) through v_mfma_f32_16x16x32_bf16, half the
 //   rate, whose sums are fp32's.  fp32 outputs take this one.
 struct Mma8 {
   typedef i32x8_t frag;

@@ -420,8 +420,8 @@ def fd_scale_stride(cols: int) -> int:
 
 
 def _rows(name: str, t: torch.Tensor) -> Sequence[int]:
-    if t.dim() != 2:
-        raise FlashDiffError(f"{name} must have two dimensions, got {tuple(t.shape)}")
+    if t.dim() != 2 or max(t.shape) > 1 << 30:
+        raise FlashDiffError(f"{name} must have two dimensions of at most 2^30, got {tuple(t.shape)}")
     return t.shape
 
 
@@ -478,21 +478,22 @@ def fd_quant_blocks(x, block_rows: int, q, scale, m=None, stream=None) -> None:
 def fd_rms_quant(h, q, scale, cu_q, m, y=None, gate=None, weight=None, shift=None, mod_scale=None, eps: float = 1e-6,
                  stream=None) -> None:
     """h [rows, D] fp32 += gate * y (with y), then its RMS norm times weight, modulated, as codes q
-    [rows, D] and scale bytes [rows, fd_scale_stride(D)]; q and scale None: h's update alone.  gate, shift and mod_scale: fp32 [requests, D],
-    which may be column ranges of one modulation tensor (equal row strides)."""
+    [rows, D] and scale bytes [rows, fd_scale_stride(D)]; q and scale None: h's update alone.  cu_q None: one
+    request.  gate, shift and mod_scale: fp32 [requests, D], which may be column ranges of one modulation tensor
+    (equal row strides)."""
     rows, D = _rows("h", h)
-    B = cu_q.numel() - 1
+    B = 1 if cu_q is None else cu_q.numel() - 1
     stride, mod = 0, [None, None, None]
     given = [(i, t) for i, t in enumerate((gate, shift, mod_scale)) if t is not None]
     if given:
         stride, dev = given[0][1].stride(0), h.get_device()
         for i, t in given:
-            if t.shape != (B, D) or t.stride() != (stride, 1) or t.dtype != torch.float32 or t.get_device() != dev:
+            if t.shape != (B, D) or t.stride() != (stride, 1) or stride > 1 << 30 or t.dtype != torch.float32 or t.get_device() != dev:
                 raise FlashDiffError(f"gate, shift and mod_scale must be fp32 [{B}, {D}] with contiguous rows of one stride, on {h.device}")
             mod[i] = t.data_ptr()
     n = rows * D
     h_, y_, w_, cu_, m_, q_, s_, st = _pointers(
-        stream, ("h", h, "f32", n), ("y", y, "b16", -n), ("weight", weight, "f32", -D), ("cu_q", cu_q, "i32", 2), ("m", m, "i32", 1),
+        stream, ("h", h, "f32", n), ("y", y, "b16", -n), ("weight", weight, "f32", -D), ("cu_q", cu_q, "i32", -2 if B == 1 else 2), ("m", m, "i32", 1),
         ("q", q, "code", n if scale is not None else -n), ("scale", scale, "scale", rows * fd_scale_stride(D) * (1 if q is not None else -1)))
     _check("fd_rms_quant", lib().fd_rms_quant(rows, D, B, h_, y_, mod[0], w_, mod[1], mod[2], stride, eps, cu_, m_, q_, s_, st))
 
@@ -582,6 +583,8 @@ def fd_scaled_block_forward(plan: Plan, d: FdDims, w: FdScaledWeights, rope: Opt
                   ("k_cache", k_cache, "b16", N * d.D), ("v_cache", v_cache, "b16", N * d.D),
                   ("coord", coord, "i32", -1 if rope is None else N * rope.n_axes))
     _need("ws", ws, "bytes", fd_scaled_block_ws_size(plan, d))
+    if ws.device != h.device:
+        raise FlashDiffError(f"ws is on {ws.device}, h on {h.device}")
     h_, idx_, cu_, m_, k_, v_, c_, st = p
     _check("fd_scaled_block_forward", lib().fd_scaled_block_forward(
         ctypes.byref(plan.c), ctypes.byref(d), ctypes.byref(w), None if rope is None else ctypes.byref(rope), c_, h_, idx_, cu_, m_,

@@ -156,6 +156,19 @@ def test_rms_quant(rows, D, B, m, parts):
     assert np.all(q[m:] == 0x55) and np.all(s[m:] == 0x55)
 
 
+def test_rms_quant_without_request_offsets():
+    """One request without cu_q: the bits of the call with it."""
+    rng = np.random.default_rng(8)
+    h, y = dev(rng.standard_normal((7, 144)).astype(np.float32)), bf16(rng.standard_normal((7, 144))).cuda()
+    mod = dev(rng.standard_normal((1, 432)).astype(np.float32))
+    out = []
+    for cu in (None, dev(np.array([0, 7], np.int32))):
+        x, (q, s) = h.clone(), codes(7, 144)
+        fdl.fd_rms_quant(x, q, s, cu, count(7), y=y, gate=mod[:, :144], shift=mod[:, 144:288], mod_scale=mod[:, 288:])
+        out.append((x.cpu(), q.cpu().view(torch.uint8), s.cpu()))
+    assert all(torch.equal(a, b) for a, b in zip(*out))
+
+
 def test_rms_quant_zero_and_bad_rows():
     """A row of zeros (eps 0: 0 * inf is NaN, as the formula says; eps > 0: codes of zero), rows with an infinity
     or a NaN: those rows alone are NaN."""

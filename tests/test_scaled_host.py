@@ -104,6 +104,30 @@ def test_rope_descriptor_refused(field, value):
     assert fdl.lib().fd_rope_axes(4, 8, ctypes.byref(two), 2, 1, 64, *([P] * 7), None) == 1
 
 
+@no_gpu
+def test_sizes_beyond_32_bits_refused():
+    """Rows whose numbers would pass 32 bits, and angles with no fraction left."""
+    lib, n = fdl.lib(), (1 << 30) + 1
+    assert lib.fd_quant_blocks(n, 64, 1, P, P, P, P, None) == 3
+    assert lib.fd_rms_quant(n, 64, 1, P, None, None, None, None, None, 0, 1e-6, None, P, P, P, None) == 3
+    assert lib.fd_rope_axes(n, n, ctypes.byref(fdl.rope_axes([64])), 2, 1, 64, *([P] * 7), None) == 3
+    assert lib.fd_scaled_linear(n, 64, 64, P, P, P, P, None, 0, P, P, None, None, None, None) == 3
+    for kw in (dict(step=7e6), dict(step=-7e6), dict(step=1e300, theta=1e-300), dict(theta=1e-8)):
+        assert lib.fd_rope_axes(4, 8, ctypes.byref(fdl.rope_axes([64], **kw)), 2, 1, 64, *([P] * 7), None) == 1, kw
+
+
+def test_bindings_refuse_wide_shapes():
+    """Shapes whose sizes a 32-bit argument would cut; expanded, so that they hold one element."""
+    one = torch.zeros(1, 1, dtype=torch.float8_e4m3fn)
+    big, s = one.expand((1 << 32) + 4, 16), torch.zeros(4, 4, dtype=torch.uint8)
+    i, h = torch.zeros(1, dtype=torch.int32), torch.zeros(1, 1)
+    for call in (lambda: fdl.fd_quant_blocks(big, 1, big, s), lambda: fdl.fd_rms_quant(h.expand((1 << 32) + 4, 16), None, None, None, i),
+                 lambda: fdl.fd_rope_axes(big, i.view(1, 1), None, i, h, h, h, 1, 1, 16, dims=[16]),
+                 lambda: fdl.fd_scaled_linear(big, s, one, s, h)):
+        with pytest.raises(fdl.FlashDiffError, match="at most 2"):
+            call()
+
+
 def test_rope_binding_refuses():
     for kw in (dict(dims=[]), dict(dims=[2] * 5), dict(dims=[8, 8], theta=[1e4]), dict(dims=[8], step=[1.0, 2.0])):
         with pytest.raises(fdl.FlashDiffError):
