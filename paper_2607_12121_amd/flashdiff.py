@@ -54,9 +54,11 @@ class FdGate(ctypes.Structure):
     _fields_ = [("eta", ctypes.c_double), ("max_skip", _i32)]
 
 
+_Axes, _Reals = _i32 * 4, ctypes.c_double * 4
+
+
 class FdRope(ctypes.Structure):
-    _fields_ = [("n_axes", _i32), ("pairing", _i32), ("dim", _i32 * 4), ("theta", ctypes.c_double * 4),
-                ("step", ctypes.c_double * 4)]
+    _fields_ = [("n_axes", _i32), ("pairing", _i32), ("dim", _Axes), ("theta", _Reals), ("step", _Reals)]
 
 
 class FdScaledWeights(ctypes.Structure):
@@ -419,10 +421,16 @@ def fd_scale_stride(cols: int) -> int:
     return lib().fd_scale_stride(cols)
 
 
+def _stride(cols: int) -> int:
+    """fd_scale_stride without the call into the library (0.2 us)."""
+    return (cols + 511) // 512 * 4
+
+
 def _rows(name: str, t: torch.Tensor) -> Sequence[int]:
-    if t.dim() != 2 or max(t.shape) > 1 << 30:
-        raise FlashDiffError(f"{name} must have two dimensions of at most 2^30, got {tuple(t.shape)}")
-    return t.shape
+    s = t.shape
+    if len(s) != 2 or s[0] > 1 << 30 or s[1] > 1 << 30:
+        raise FlashDiffError(f"{name} must have two dimensions of at most 2^30, got {tuple(s)}")
+    return s
 
 
 _KIND = {k: frozenset(v) for k, v in _DT.items() if v is not None}
@@ -450,7 +458,7 @@ def _pointers(stream: Optional[torch.cuda.Stream], *args) -> list:
             if not t.is_cuda:
                 _need(name, t, kind, abs(n))
             cur = torch.cuda.current_device()
-        if t.get_device() != cur or t.dtype not in _KIND[kind] or t.numel() < abs(n) or not t.is_contiguous():
+        if t.get_device() != cur or t.dtype not in _KIND[kind] or t.numel() < (n if n >= 0 else -n) or not t.is_contiguous():
             _need(name, t, kind, abs(n))
             if t.get_device() != cur:
                 raise FlashDiffError(f"{name} is on {t.device}, the current device is {cur}")
@@ -471,7 +479,7 @@ def fd_quant_blocks(x, block_rows: int, q, scale, m=None, stream=None) -> None:
     the rows when given) or 128 (weights)."""
     rows, cols = _rows("x", x)
     p = _pointers(stream, ("x", x, "b16", rows * cols), ("m", m, "i32", -1), ("q", q, "code", rows * cols),
-                  ("scale", scale, "scale", -(-rows // max(block_rows, 1)) * fd_scale_stride(cols)))
+                  ("scale", scale, "scale", -(-rows // max(block_rows, 1)) * _stride(cols)))
     _check("fd_quant_blocks", lib().fd_quant_blocks(rows, cols, block_rows, *p))
 
 
@@ -494,7 +502,7 @@ def fd_rms_quant(h, q, scale, cu_q, m, y=None, gate=None, weight=None, shift=Non
     n = rows * D
     h_, y_, w_, cu_, m_, q_, s_, st = _pointers(
         stream, ("h", h, "f32", n), ("y", y, "b16", -n), ("weight", weight, "f32", -D), ("cu_q", cu_q, "i32", -2 if B == 1 else 2), ("m", m, "i32", 1),
-        ("q", q, "code", n if scale is not None else -n), ("scale", scale, "scale", rows * fd_scale_stride(D) * (1 if q is not None else -1)))
+        ("q", q, "code", n if scale is not None else -n), ("scale", scale, "scale", rows * _stride(D) * (1 if q is not None else -1)))
     _check("fd_rms_quant", lib().fd_rms_quant(rows, D, B, h_, y_, mod[0], w_, mod[1], mod[2], stride, eps, cu_, m_, q_, s_, st))
 
 
@@ -508,8 +516,7 @@ def rope_axes(dims: Sequence[int], theta=10000.0, step=1.0, halves: bool = False
     if len(th) != n or len(st) != n:
         raise FlashDiffError("dims, theta and step must have one entry per axis")
     pad = (0,) * (4 - n)
-    return FdRope(n, int(bool(halves)), (_i32 * 4)(*dims, *pad), (ctypes.c_double * 4)(*th, *pad),
-                  (ctypes.c_double * 4)(*st, *pad))
+    return FdRope(n, int(bool(halves)), _Axes(*dims, *pad), _Reals(*th, *pad), _Reals(*st, *pad))
 
 
 def fd_rope_axes(qkv, coord, idx, m, q, k_cache, v_cache, heads: int, kv_heads: int, head_dim: int, dims=None, theta=10000.0,
@@ -533,12 +540,13 @@ def fd_scaled_linear(a, a_scale, w, w_scale, y, y_scale=None, bias=None, gelu: b
     (rows, k), (n, kw) = _rows("a", a), _rows("w", w)
     if k != kw:
         raise FlashDiffError(f"a has {k} columns, w {kw}")
-    codes, wide, ld = y.dtype in _KIND["code"], y.dtype == torch.float32, fd_scale_stride(k)
+    dt, ld = y.dtype, _stride(k)
+    codes, wide = dt in _KIND["code"], dt == torch.float32
     *ptrs, y_, ys_, st = _pointers(
         stream, ("a", a, "code", rows * k), ("a_scale", a_scale, "scale", rows * ld), ("w", w, "code", n * k),
         ("w_scale", w_scale, "scale", -(-n // 128) * ld), ("bias", bias, "f32", -n), ("m", m, "i32", -1),
         ("y", y, "code" if codes else "f32" if wide else "b16", rows * n),
-        ("y_scale", y_scale if codes else None, "scale", rows * fd_scale_stride(n) if codes else -1))
+        ("y_scale", y_scale if codes else None, "scale", rows * _stride(n) if codes else -1))
     a_, as_, w_, ws_, b_, m_ = ptrs
     _check("fd_scaled_linear", lib().fd_scaled_linear(rows, n, k, a_, as_, w_, ws_, b_, int(gelu), m_, None if codes or wide else y_,
                                                       y_ if wide else None, y_ if codes else None, ys_, st))
