@@ -6,17 +6,23 @@
 
 namespace fd {
 
-// Row capacities up to which the few-row kernel runs (a larger capacity with few rows at work runs the tiles).  Results
-// in 8 bits, whose blocks want 128 columns of a workgroup, leave too few workgroups for it and run the tiles from one
-// row on: 1 x 6144 x 1536 with GELU 11.9 us, in tiles 10.3.  Otherwise 64: 32 x 1536 x 6144 12.0 us, in tiles 21.2;
-// 64 rows of it 19.2 and 21.3.
-FD_RULE int scaled_few_rows(bool codes) { return codes ? 0 : 64; }
-// Its workgroups take 16 columns, or 32 where those of 16 would not each have a CU: every workgroup reads all of the
-// rows.  16 columns and 32, us: 16 x 1536 x 6144 8.9 and 11.4, 16 x 4608 x 6144 14.9 and 11.4, 64 x 4608 x 1536 10.2
-// and 7.4.
+// bf16 and fp32 results of few rows come from the few-row kernel, whose workgroups take 16, 32 or 64 rows and 16 columns,
+// or 32 where those of 16 would not each have a CU: every workgroup reads all of the rows.  16 columns and 32, us: 16 x
+// 1536 x 6144 8.9 and 11.4, 16 x 4608 x 6144 14.9 and 11.4, 64 x 4608 x 1536 10.2 and 7.4.
 FD_RULE bool scaled_few_wide(int N, int cus) { return (N + 15) / 16 > cus; }
-// The tiles' loads run two or more K-blocks ahead; fewer blocks than three run the few-row kernel at any size.
-constexpr int kTileBlocks = 3;
+FD_RULE int scaled_few_frags(int M) { return M <= 16 ? 1 : M <= 32 ? 2 : 4; }   // of 16 rows
+// Up to 16 rows it is the faster one at every size.  Beyond, a workgroup of f fragments takes 7 + 3 f units of time where
+// the tiles, whose workgroups walk all K-blocks, take 19 (fp32 results, at half the matrix rate, 36), and it runs as long
+// as the rounds of workgroups stay below that.  Few-row kernel and tiles, us: to bf16 1 x 65536 x 4096 51 and 74, 32 x
+// 12288 x 4096 (384 workgroups) 22.5 and 15.6, 32 x 8192 x 4096 (256) 12.5 and 15.4, 64 x 1536 x 6144 (96) 19.2 and
+// 21.3, 128 rows of it (192) 19.2 and 21.1, 200 (384) 34.4 and 21.3, 128 x 640 x 1536 (80) 5.9 and 8.0; to fp32 200 x
+// 1536 x 6144 34.3 and 42.8, 400 rows (672) 50.2 and 43.1.  Codes, whose blocks want 128 columns of a workgroup, would
+// leave it too few of them: 1 x 6144 x 1536 with GELU 11.9, in tiles 10.3.
+FD_RULE bool scaled_few(int M, int N, bool codes, bool exact, int cus) {
+  const int f = scaled_few_frags(M), columns = scaled_few_wide(N, cus) ? 32 : 16;
+  const long long groups = static_cast<long long>((M + 16 * f - 1) / (16 * f)) * ((N + columns - 1) / columns);
+  return !codes && (f == 1 || groups * (7 + 3 * f) <= (exact ? 36LL : 19LL) * cus);
+}
 
 // 64 x 128 tiles with three stages of loads instead of 128 x 128 with two, where each has a CU: nothing runs beside a
 // workgroup that is alone while it waits, and what bounds it is the K-blocks that it walks.  To bf16, us: 512 x 1536 x

@@ -1,8 +1,7 @@
 // The product of 8-bit rows and weights with block scales:
 //   Y[M][N] = act(sum over K-blocks kb of 2^(sa[row][kb] + sw[col / 128][kb] - 254) (A . W^T)_kb + bias)
-// on v_mfma_scale_f32_16x16x128_f8f6f4, whose K is one block: the scale bytes are operands of the
-// instruction and the sum is kept in fp32 accumulators.
-//
+// on v_mfma_scale_f32_16x16x128_f8f6f4 and 32x32x64: a block is one or two steps of the instruction, the scale bytes
+// are its operands and the sum is kept in fp32 accumulators.
 #include <type_traits>
 
 #include "fd_scaled.h"
@@ -18,11 +17,11 @@ typedef int i32x4_t __attribute__((ext_vector_type(4)));
 enum { kToBf16, kToF32, kToCodes };
 
 // Two ways to the sum of one K-block of 128:
-// - 8-bit: v_mfma_scale_f32_16x16x128_f8f6f4.  It adds 8 products at a time on a grid 2^-13 below the
+// - 8-bit: v_mfma_scale_f32_*_f8f6f4.  It adds 8 products at a time on a grid 2^-13 below the
 //   largest of them (measured: 1 + 2^-14 gives 1 within such a group, and is exact across groups and
 //   with the accumulator), which leaves random operands' sums off by 1.5e-5 of their size.
 //   Outputs of 8 (bf16) or 4 (e4m3) bits of mantissa round by 100 times that at least.
-// - exact: the codes times their scales as bf16 (exact from 2^-126 on) through v_mfma_f32_16x16x32_bf16, half the
+// - exact: the codes times their scales as bf16 (exact from 2^-126 on) through v_mfma_f32_*_bf16, half the
 //   rate, whose sums are fp32's.  fp32 outputs take this one.
 struct Mma8 {
   typedef i32x8_t frag;
@@ -66,10 +65,9 @@ struct MmaExact {
 // consecutive columns, 4 NF (l >> 4) on.
 //
 // One row's 4 NF columns from col on (col a multiple of 4 NF; N is a multiple of 16, so each 16 lie
-// inside or outside).  Every lane of the wave runs it; codes need the whole block (NF = 8).
+// inside or outside).
 template <int KIND, int NF>
 FD_DEVICE void store_row(const fdh::ScaledArgs& g, bool row_ok, int row, int col, const f32x4_t (&acc)[NF], const float4 (&bias)[NF]) {
-  static_assert(KIND != kToCodes || NF == 8, "four lanes hold a block's columns");
   float v[4 * NF];
 #pragma unroll
   for (int j = 0; j < NF; ++j)
@@ -80,27 +78,7 @@ FD_DEVICE void store_row(const fdh::ScaledArgs& g, bool row_ok, int row, int col
     for (int e = 0; e < 4 * NF; ++e) v[e] = fd::gelu(v[e]);
   }
   const size_t at = static_cast<size_t>(row) * g.N + col;
-  if constexpr (KIND == kToCodes) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int e = 0; e < 32; ++e) top = (col + (e & 16) < g.N) ? max(top, fd::mag_bits(v[e])) : top;
-    top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 16, fd::kWave)));
-    top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 32, fd::kWave)));
-    const uint32_t s = fd::scale_byte(top);
-    const float inv = fd::scale_inverse(s);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint32_t w[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float* x = v + 16 * h + 4 * i;
-        w[i] = fd::pack_codes(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
-      }
-      if (row_ok && col + 16 * h < g.N) *reinterpret_cast<uint4*>(g.y_q + at + 16 * h) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    if (row_ok && col < g.N && (col & (kScaleBlock - 1)) == 0)
-      g.y_scale[static_cast<size_t>(row) * fd::scale_stride(g.N) + col / kScaleBlock] = static_cast<uint8_t>(s);
-  } else if constexpr (KIND == kToBf16 && NF == 1) {
+  if constexpr (KIND == kToBf16 && NF == 1) {
     if (row_ok && col < g.N) *reinterpret_cast<uint2*>(g.y_bf16 + at) = make_uint2(fd::pack_bf2(v[0], v[1]), fd::pack_bf2(v[2], v[3]));
   } else if constexpr (KIND == kToBf16) {
 #pragma unroll
@@ -131,7 +109,7 @@ FD_DEVICE i32x8_t inside(const Piece& x, int k, int K) {
 
 // ---------------------------------------------------------------- few rows
 
-// Up to 64 rows: the weights are read once, so what counts is how many of their bytes are on the way.  A workgroup
+// Few rows: the weights are read once (by every 64 rows), so what counts is how many of their bytes are on the way.  A workgroup
 // takes the rows' FM fragments and 16 NF columns, its waves the K-blocks in turn, operands straight from memory into
 // registers, up to DEEP blocks at a time; the waves' sums meet in LDS.  DEEP is about what 128 registers hold, so that a
 // CU takes two workgroups: with six blocks and one workgroup, 16 x 4608 x 4096 12.6 us, with three 11.6.  Past its last
@@ -144,7 +122,8 @@ __global__ __launch_bounds__(kFewWaves * 64) void scaled_few_kernel(fdh::ScaledA
   const int M = g.m ? min(*g.m, g.n_rows) : g.n_rows;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, lg = lane >> 4;
   const int K = g.K, nk = (K + kScaleBlock - 1) / kScaleBlock, ld = fd::scale_stride(K);
-  const int n0 = blockIdx.x * 16 * NF;
+  const int n0 = blockIdx.x * 16 * NF, m0 = blockIdx.y * 16 * FM;
+  if (m0 >= M) return;
   const uint8_t* sw = g.w_scale + static_cast<size_t>(n0 / kScaleBlock) * ld;
   const uint8_t* w[NF];
 #pragma unroll
@@ -153,57 +132,54 @@ __global__ __launch_bounds__(kFewWaves * 64) void scaled_few_kernel(fdh::ScaledA
   float4 bias[NF];
 #pragma unroll
   for (int j = 0; j < NF; ++j) bias[j] = g.bias ? *reinterpret_cast<const float4*>(g.bias + min(n0 + 4 * NF * lg + 4 * j, g.N - 4)) : make_float4(0, 0, 0, 0);
-  for (int m0 = blockIdx.y * 16 * FM; m0 < M; m0 += gridDim.y * 16 * FM) {
-    f32x4_t acc[FM][NF] = {};
-    for (int kb = wave; kb < nk; kb += kFewWaves * DEEP) {
-      Piece wf[DEEP][NF], af[DEEP][FM];
-      uint32_t s_w[DEEP], s_a[DEEP][FM];
+  f32x4_t acc[FM][NF] = {};
+  for (int kb = wave; kb < nk; kb += kFewWaves * DEEP) {
+    Piece wf[DEEP][NF], af[DEEP][FM];
+    uint32_t s_w[DEEP], s_a[DEEP][FM];
 #pragma unroll
-      for (int d = 0; d < DEEP; ++d) {
-        const int b = kb + d * kFewWaves, k = b * kScaleBlock + 32 * lg;
-        if (b >= nk) break;
+    for (int d = 0; d < DEEP; ++d) {
+      const int b = kb + d * kFewWaves, k = b * kScaleBlock + 32 * lg;
+      if (b >= nk) break;
 #pragma unroll
-        for (int j = 0; j < NF; ++j) wf[d][j] = load32(w[j], k, K);
-        s_w[d] = sw[b];
+      for (int j = 0; j < NF; ++j) wf[d][j] = load32(w[j], k, K);
+      s_w[d] = sw[b];
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
-          const size_t row = min(m0 + 16 * i + l16, M - 1);
-          af[d][i] = load32(g.a + row * K, k, K);
-          s_a[d][i] = g.a_scale[row * ld + b];
-        }
-      }
-#pragma unroll
-      for (int d = 0; d < DEEP; ++d) {
-        const int b = kb + d * kFewWaves, k = b * kScaleBlock + 32 * lg;
-        if (b >= nk) break;
-        typename Mma::frag wd[NF];
-#pragma unroll
-        for (int j = 0; j < NF; ++j) wd[j] = Mma::make(inside(wf[d][j], k, K), s_w[d]);
-#pragma unroll
-        for (int i = 0; i < FM; ++i) {
-          const typename Mma::frag ad = Mma::make(inside(af[d][i], k, K), s_a[d][i]);
-#pragma unroll
-          for (int j = 0; j < NF; ++j) acc[i][j] = Mma::mma(wd[j], ad, acc[i][j], s_w[d], s_a[d][i]);
-        }
+      for (int i = 0; i < FM; ++i) {
+        const size_t row = min(m0 + 16 * i + l16, M - 1);
+        af[d][i] = load32(g.a + row * K, k, K);
+        s_a[d][i] = g.a_scale[row * ld + b];
       }
     }
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+    for (int d = 0; d < DEEP; ++d) {
+      const int b = kb + d * kFewWaves, k = b * kScaleBlock + 32 * lg;
+      if (b >= nk) break;
+      typename Mma::frag wd[NF];
 #pragma unroll
-      for (int j = 0; j < NF; ++j) part[wave][i][j][lane] = acc[i][j];
-    __syncthreads();
-    if (wave < FM) {   // a wave per 16 rows adds the waves' sums in order
-      f32x4_t sum[NF];
+      for (int j = 0; j < NF; ++j) wd[j] = Mma::make(inside(wf[d][j], k, K), s_w[d]);
 #pragma unroll
-      for (int j = 0; j < NF; ++j) {
-        sum[j] = part[0][wave][j][lane];
+      for (int i = 0; i < FM; ++i) {
+        const typename Mma::frag ad = Mma::make(inside(af[d][i], k, K), s_a[d][i]);
 #pragma unroll
-        for (int p = 1; p < kFewWaves; ++p) sum[j] += part[p][wave][j][lane];
+        for (int j = 0; j < NF; ++j) acc[i][j] = Mma::mma(wd[j], ad, acc[i][j], s_w[d], s_a[d][i]);
       }
-      const int row = m0 + 16 * wave + l16;
-      store_row<KIND, NF>(g, row < M, row, n0 + 4 * NF * lg, sum, bias);
     }
-    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < NF; ++j) part[wave][i][j][lane] = acc[i][j];
+  __syncthreads();
+  if (wave < FM) {   // a wave per 16 rows adds the waves' sums in order
+    f32x4_t sum[NF];
+#pragma unroll
+    for (int j = 0; j < NF; ++j) {
+      sum[j] = part[0][wave][j][lane];
+#pragma unroll
+      for (int p = 1; p < kFewWaves; ++p) sum[j] += part[p][wave][j][lane];
+    }
+    const int row = m0 + 16 * wave + l16;
+    store_row<KIND, NF>(g, row < M, row, n0 + 4 * NF * lg, sum, bias);
   }
 }
 
@@ -350,7 +326,7 @@ struct Rows32 {
 // sub-steps 6 and 7, so that no sub-step waits for LDS or for the barrier with nothing to compute.  (One barrier
 // in the middle of a step, with its operands in registers: the loads have 5 sub-steps to land instead of 7 and 10,
 // 1664 x 1536 x 6144 in 128 x 128 tiles 36.4 us against 28.2.)  A step is one basic block: across branches the
-// compiler gathers the products at the end.  K has at least STAGES blocks.
+// compiler gathers the products at the end.
 template <class T, int KIND, class Mma>
 FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
   constexpr int FI = T::FI, STAGES = T::STAGES;
@@ -358,7 +334,7 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
   constexpr int kStores = FI * Rows32<KIND>::STORES;
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / T::WN, wn = wave % T::WN;
-  const int K = g.K, nk = (K + kScaleBlock - 1) / kScaleBlock, ld = fd::scale_stride(K);
+  const int K = g.K, blocks = (K + kScaleBlock - 1) / kScaleBlock, nk = max(blocks, STAGES), ld = fd::scale_stride(K);
   const int tiles_m = (M + T::BM - 1) / T::BM, tiles_n = (g.N + T::BN - 1) / T::BN, tiles = tiles_m * tiles_n;
   const int per_xcd = (tiles + 7) / 8;
   const uint32_t ring_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr_t)ring));
@@ -404,10 +380,10 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
     dma4(ring_at + static_cast<uint32_t>(T::BIAS * 16 + turn * T::BN * 4 + c * 4), static_cast<uint32_t>(ln0 + c + lane) * 4,
          buffer_of(g.bias, g.bias ? 4u * g.N : 0u), 0);
   };
-  // The chunks past K of a last, shorter K-block read zeros: called before that block's loads.  The next tile's aim
-  // sets the offsets anew.
+  // The chunks past K of a last, shorter K-block read zeros, and all of those that fill a short sum up to STAGES
+  // blocks: called before such a block's loads.  The next tile's aim sets the offsets anew.
   auto last_block = [&] {
-    const bool inside = (nk - 1) * kScaleBlock + 16 * chunk < K;
+    const bool inside = lk * kScaleBlock + 16 * chunk < K;
 #pragma unroll
     for (int q = 0; q < T::LOADS_A; ++q) off_a[q] = inside ? off_a[q] : kNowhere;
 #pragma unroll
@@ -471,7 +447,7 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
   aim();
 #pragma unroll
   for (int p = 0; p < STAGES; ++p) {
-    if (lk == nk - 1) last_block();
+    if (lk >= blocks - 1) last_block();
     issue(p * kSlot, std::integral_constant<int, 0>{}, std::integral_constant<int, T::LOADS_A + T::LOADS_W>{});
     issue_scales(p * kSlot);
     ++lk;
@@ -497,11 +473,12 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
         if (more) aim();
       }
       for (const int end = part == 0 ? nk - STAGES : nk; kb < end; ++kb, ++lk) {
-        if (lk == nk - 1) last_block();
+        if (lk >= blocks - 1) last_block();
         const uint32_t next = slot == (STAGES - 1) * kSlot ? 0 : slot + kSlot;
+        const int shift = 8 * (min(kb, blocks - 1) & 3);   // blocks of zeros take the last one's scales
 #pragma unroll
-        for (int i = 0; i < FI; ++i) sa[i] = sa_next[i] >> (8 * (kb & 3));
-        sw = sw_next >> (8 * (kb & 3));
+        for (int i = 0; i < FI; ++i) sa[i] = sa_next[i] >> shift;
+        sw = sw_next >> shift;
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
           if (s == 2) wait_reads_barrier();
@@ -557,6 +534,10 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the repeats of the last stage
 }
 
+// What bounds them is LDS traffic: a K-step of 128 x 128 reads 80 KB at 128 bytes a clock and is written by loads of 32
+// KB at 64, 1152 clocks beside 512 of matrix instructions; of 256 x 256, 192 and 64 KB, 2560 beside 2048.  9828 x 6144 x
+// 1536 to codes with GELU in 128 x 128 tiles 104 us (1780 TFLOP/s), 9828 x 1536 x 6144 to bf16 in 256 x 256 72 us (2560
+// TFLOP/s; a large fp8 product of the library 2720), 32760 x 1536 x 6144 to fp32 457 us (1350, at half the rate).
 using Tile64 = Tile<1, 2, 1, 3>;      // 64 x 128, two workgroups per CU
 using Tile128 = Tile<1, 4, 1, 2>;     // 128 x 128, two
 using TileLarge = Tile<2, 4, 2, 2>;   // 256 x 256, one
@@ -565,7 +546,7 @@ using TileLarge = Tile<2, 4, 2, 2>;   // 256 x 256, one
 template <int KIND, class Mma, class T, int PER_CU>
 __global__ __launch_bounds__(T::THREADS, (PER_CU * T::WAVES + 3) / 4) void scaled_tile_kernel(fdh::ScaledArgs g, int cus) {
   __shared__ uint4 ring[T::TOTAL];
-  static_assert(T::TOTAL * 16 * PER_CU <= 160 * 1024 && T::STAGES <= fd::kTileBlocks, "the LDS of a CU");
+  static_assert(T::TOTAL * 16 * PER_CU <= 160 * 1024, "the LDS of a CU");
   const int M = g.m ? min(*g.m, g.n_rows) : g.n_rows;
   if (M <= 0 || (cus > 0 && fd::scaled_large(M, g.N, g.K, KIND == kToCodes, cus) != (T::BM == TileLarge::BM))) return;
   scaled_tiles<T, KIND, Mma>(g, M, ring);
@@ -580,27 +561,28 @@ hipError_t launch_scaled_linear(const ScaledArgs& g, hipStream_t s) {
     constexpr int KIND = decltype(kind)::value;
     using Mma = decltype(mma);
     constexpr bool codes = KIND == kToCodes;
-    if (g.n_rows <= fd::scaled_few_rows(codes) || g.K <= (fd::kTileBlocks - 1) * kScaleBlock) {
-      auto few = [&](auto fm, auto nf, auto deep) {
-        constexpr int FM = decltype(fm)::value, NF = decltype(nf)::value;
-        const int gx = (g.N + 16 * NF - 1) / (16 * NF), gy = (g.n_rows + 16 * FM - 1) / (16 * FM);
-        scaled_few_kernel<KIND, Mma, FM, NF, decltype(deep)::value><<<dim3(gx, gy < 4096 ? gy : 4096), kFewWaves * 64, 0, s>>>(g);
-      };
-      const std::integral_constant<int, 1> one{};
-      const std::integral_constant<int, 2> two{};
-      const std::integral_constant<int, 3> three{};
-      const std::integral_constant<int, 4> four{};
-      if constexpr (codes) few(one, std::integral_constant<int, 8>{}, one);
-      else if (fd::scaled_few_wide(g.N, num_cus())) {
-        if (g.n_rows <= 16) few(one, two, two);
-        else if (g.n_rows <= 32) few(two, two, two);
-        else few(four, two, one);
-      } else {
-        if (g.n_rows <= 16) few(one, one, three);
-        else if (g.n_rows <= 32) few(two, one, two);
-        else few(four, one, one);
+    if constexpr (!codes) {
+      if (fd::scaled_few(g.n_rows, g.N, codes, KIND == kToF32, num_cus())) {
+        auto few = [&](auto fm, auto nf, auto deep) {
+          constexpr int FM = decltype(fm)::value, NF = decltype(nf)::value;
+          scaled_few_kernel<KIND, Mma, FM, NF, decltype(deep)::value><<<dim3((g.N + 16 * NF - 1) / (16 * NF), (g.n_rows + 16 * FM - 1) / (16 * FM)), kFewWaves * 64, 0, s>>>(g);
+        };
+        const std::integral_constant<int, 1> one{};
+        const std::integral_constant<int, 2> two{};
+        const std::integral_constant<int, 3> three{};
+        const std::integral_constant<int, 4> four{};
+        const int frags = fd::scaled_few_frags(g.n_rows);
+        if (fd::scaled_few_wide(g.N, num_cus())) {
+          if (frags == 1) few(one, two, two);
+          else if (frags == 2) few(two, two, two);
+          else few(four, two, one);
+        } else {
+          if (frags == 1) few(one, one, three);
+          else if (frags == 2) few(two, one, two);
+          else few(four, one, one);
+        }
+        return;
       }
-      return;
     }
     const int cus = num_cus() / 8 * 8;   // the tile order counts on whole rounds of the 8 XCDs
     const bool both = g.m && fd::scaled_both(g.n_rows, g.N, g.K, codes, cus), large = !g.m && fd::scaled_large(g.n_rows, g.N, g.K, codes, cus);

@@ -311,6 +311,16 @@ def test_scaled_linear_tiles(M, N, K, m, to, gelu):
     check_linear(y, ys, a, sa, w, sw, bias, gelu, to, M if m is None else m)
 
 
+@pytest.mark.parametrize("M,N,K,rows", [(9000, 1040, 16, 9000), (9000, 1040, 144, 9010), (8192, 2048, 128, 8192), (8190, 2048, 240, 8192), (700, 272, 48, 700)])
+@pytest.mark.parametrize("to,gelu", [("bf16", False), ("f32", True), ("8", False)])
+def test_scaled_linear_short_sums(M, N, K, rows, to, gelu):
+    """Sums of one and two K-blocks in every kind of tile, several tiles a workgroup; the scales' padding is NaN."""
+    gh.say(f"linear M={M} N={N} K={K} rows={rows} to={to} gelu={gelu}")
+    case = linear_case(M, N, K, 4)
+    y, ys = run_linear(*case, gelu, to, rows, M)
+    check_linear(y, ys, *case, gelu, to, M)
+
+
 @pytest.mark.parametrize("M,N,K,rows", [(5, 4112, 400, 9), (20, 4128, 1088, 32), (50, 4112, 1296, 64), (33, 1040, 1168, 40), (300, 4112, 240, 310)])
 @pytest.mark.parametrize("to,gelu", [("bf16", True), ("f32", False), ("8", False)])
 def test_scaled_linear_few_rows(M, N, K, rows, to, gelu):

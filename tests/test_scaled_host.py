@@ -166,16 +166,18 @@ def test_product_rules(tmp_path):
 int main(int, char**) {
   int n, N, K, c;
   while (std::scanf("%d %d %d %d", &n, &N, &K, &c) == 4)
-    std::printf("%d %d %d %d %d\\n", fd::scaled_few_rows(c), (int)fd::scaled_large(n, N, K, c, 256), (int)fd::scaled_both(n, N, K, c, 256), (int)fd::scaled_small(n, N, 256), (int)fd::scaled_few_wide(N, 256));
+    std::printf("%d %d %d %d %d\\n", (int)fd::scaled_few(n, N, c, false, 256) + 2 * (int)fd::scaled_few(n, N, c, true, 256), (int)fd::scaled_large(n, N, K, c, 256), (int)fd::scaled_both(n, N, K, c, 256), (int)fd::scaled_small(n, N, 256), (int)fd::scaled_few_wide(N, 256));
 }
 ''')
     exe = tmp_path / "r"
     subprocess.run(["g++", "-std=c++17", f"-I{build.CSRC}", str(src), "-o", str(exe)], check=True)
-    d64, d128 = 1, 0
-    cases = [((9828, 1536, 6144, 0), (64, 1, 1, d128)), ((5000, 1536, 6144, 0), (64, 0, 0, d128)), ((9828, 6144, 1536, 1), (0, 0, 0, d128)),
-             ((32760, 1536, 6144, 0), (64, 1, 1, d128)), ((9828, 1536, 1536, 0), (64, 1, 0, d128)), ((1664, 1536, 6144, 0), (64, 0, 0, d128)),
-             ((14280, 4096, 1024, 1), (0, 0, 0, d128)), ((1, 64, 64, 0), (64, 0, 0, d64)), ((1 << 30, 16, 16, 0), (64, 1, 1, d128)), ((9828, 4608, 1536, 0), (64, 1, 0, d128)),
-             ((4096, 6144, 1536, 0), (64, 0, 0, d128)), ((1312, 1024, 4096, 0), (64, 0, 0, d64)), ((1366, 1536, 400, 0), (64, 0, 0, d128)), ((1344, 1536, 384, 0), (64, 0, 0, d64))]
+    # (M, N, K, codes): few rows (1: to bf16, 2: to fp32), 256-row tiles, both, 64-row tiles
+    cases = [((9828, 1536, 6144, 0), (0, 1, 1, 0)), ((5000, 1536, 6144, 0), (0, 0, 0, 0)), ((9828, 6144, 1536, 1), (0, 0, 0, 0)),
+             ((32760, 1536, 6144, 0), (0, 1, 1, 0)), ((9828, 1536, 1536, 0), (0, 1, 0, 0)), ((1664, 1536, 6144, 0), (0, 0, 0, 0)),
+             ((14280, 4096, 1024, 1), (0, 0, 0, 0)), ((1, 64, 64, 0), (3, 0, 0, 1)), ((1 << 30, 16, 16, 0), (0, 1, 1, 0)), ((9828, 4608, 1536, 0), (0, 1, 0, 0)),
+             ((4096, 6144, 1536, 0), (0, 0, 0, 0)), ((1312, 1024, 4096, 0), (0, 0, 0, 1)), ((1366, 1536, 400, 0), (0, 0, 0, 0)), ((1344, 1536, 384, 0), (0, 0, 0, 1)),
+             ((1, 1 << 20, 1024, 0), (3, 1, 0, 0)), ((1, 6144, 1536, 1), (0, 0, 0, 1)), ((32, 12288, 4096, 0), (2, 0, 0, 1)), ((128, 1536, 6144, 0), (3, 0, 0, 1)),
+             ((200, 1536, 6144, 0), (2, 0, 0, 1)), ((400, 1536, 6144, 0), (0, 0, 0, 1))]
     out = subprocess.run([str(exe)], input="\n".join(" ".join(map(str, c)) for c, _ in cases), capture_output=True, text=True, check=True).stdout
     for line, (case, want) in zip(out.splitlines(), cases):
         assert tuple(map(int, line.split())) == want + (int(case[1] > 4096),), case
