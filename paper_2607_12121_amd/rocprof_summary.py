@@ -200,7 +200,8 @@ def mfma(a) -> str:
         alg.append((label, re.compile(rx), float(fl)))
     out = [f"# {a.title}", "", "commands (run from the repo root on an MI355X):", ""]
     out += [f"    {c}" for c in a.cmd]
-    out += ["", f"one MFMA instruction = {a.flops_per_mfma} flops (v_mfma_f32_32x32x16_bf16, the only MFMA the kernels "
+    name = "v_mfma_scale_f32_32x32x64_f8f6f4" if a.flops_per_mfma == 131072 else "v_mfma_f32_32x32x16_bf16"
+    out += ["", f"one MFMA instruction = {a.flops_per_mfma} flops ({name}, the only MFMA the kernels "
                 f"issue); {a.simds} SIMDs; GRBM_GUI_ACTIVE summed over {a.xcds} XCDs; nominal peak {a.peak_tflops} TFLOP/s",
             "", "| kernel | step | launches | avg us | MFMA instructions | MFMA flops | algorithmic / MFMA flops | "
                 "clock GHz | MFMA busy % of SIMD cycles | % of nominal peak |",
