@@ -11,23 +11,22 @@ namespace fd {
 // 1536 x 6144 8.9 and 11.4, 16 x 4608 x 6144 14.9 and 11.4, 64 x 4608 x 1536 10.2 and 7.4.
 FD_RULE bool scaled_few_wide(int N, int cus) { return (N + 15) / 16 > cus; }
 FD_RULE int scaled_few_frags(int M) { return M <= 16 ? 1 : M <= 32 ? 2 : 4; }   // of 16 rows
-// Up to 16 rows it is the faster one at every size.  Beyond, a workgroup of f fragments takes 7 + 3 f units of time where
-// the tiles, whose workgroups walk all K-blocks, take 19 (fp32 results, at half the matrix rate, 36), and it runs as long
-// as the rounds of workgroups stay below that.  Few-row kernel and tiles, us: to bf16 1 x 65536 x 4096 51 and 74, 32 x
-// 12288 x 4096 (384 workgroups) 22.5 and 15.6, 32 x 8192 x 4096 (256) 12.5 and 15.4, 64 x 1536 x 6144 (96) 19.2 and
-// 21.3, 128 rows of it (192) 19.2 and 21.1, 200 (384) 34.4 and 21.3, 128 x 640 x 1536 (80) 5.9 and 8.0; to fp32 200 x
-// 1536 x 6144 34.3 and 42.8, 400 rows (672) 50.2 and 43.1.  Codes, whose blocks want 128 columns of a workgroup, would
-// leave it too few of them: 1 x 6144 x 1536 with GELU 11.9, in tiles 10.3.
-FD_RULE bool scaled_few(int M, int N, bool codes, bool exact, int cus) {
+// Up to 16 rows it is the faster one at every size: 1 x 65536 x 4096 to bf16 51 us, in tiles 74.  Beyond, where each of
+// its workgroups has a CU; bf16 results of more than 32 rows, whose sums cost the tiles less, up to 26 K-blocks.  Few-row
+// kernel and tiles, us: to bf16 32 x 12288 x 4096 (384 workgroups) 22.5 and 15.6, 32 x 8192 x 4096 (256) 12.5 and 15.4,
+// 128 x 1536 x 1536 (192) 6.3 and 7.0, 128 x 1536 x 2560 9.6 and 10.1, x 4096 15.6 and 13.3; to fp32 128 x 1536 x 6144
+// 19.4 and 29.3, 128 x 4608 x 6144 (288) 40.8 and 29.8.  Codes, whose blocks want 128 columns of a workgroup, would leave
+// it too few of them: 1 x 6144 x 1536 with GELU 11.9, in tiles 10.3.
+FD_RULE bool scaled_few(int M, int N, int K, bool codes, bool exact, int cus) {
   const int f = scaled_few_frags(M), columns = scaled_few_wide(N, cus) ? 32 : 16;
   const long long groups = static_cast<long long>((M + 16 * f - 1) / (16 * f)) * ((N + columns - 1) / columns);
-  return !codes && (f == 1 || groups * (7 + 3 * f) <= (exact ? 36LL : 19LL) * cus);
+  return !codes && (f == 1 || (groups <= cus && (exact || f == 2 || K <= 26 * 128)));
 }
 
 // 64 x 128 tiles with three stages of loads instead of 128 x 128 with two, where each has a CU: nothing runs beside a
 // workgroup that is alone while it waits, and what bounds it is the K-blocks that it walks.  To bf16, us: 512 x 1536 x
-// 6144 (96 tiles of 64 rows) 21.9 and 26.9, 1312 x 1024 x 4096 (168) 16.1 and 20.0; 512 x 4608 x 1536 (288) 10.4 and
-// 9.9, 1664 x 1536 x 6144 (312) 32.0 and 28.2.
+// 6144 (96 tiles of 64 rows) 19.1 and 27.1, 1312 x 1024 x 4096 (168) 14.4 and 20.0; 512 x 4608 x 1536 (288) 11.0 and
+// 10.2, 1664 x 1536 x 6144 (312) 33.6 and 28.7.  In 32 x 128 a wave 21.5 and 16.3; to fp32 42.6 for 30.0.
 FD_RULE bool scaled_small(int M, int N, int cus) { return static_cast<long long>((M + 63) / 64) * ((N + 127) / 128) <= cus; }
 
 // 256 x 256 tiles, one workgroup per CU, instead of 128 x 128, two: half the LDS and L2 traffic per flop, but nothing
@@ -38,13 +37,13 @@ FD_RULE bool scaled_small(int M, int N, int cus) { return static_cast<long long>
 FD_RULE bool scaled_large(int M, int N, int K, bool codes, int cus) {
   const long long tiles = static_cast<long long>((M + 255) / 256) * ((N + 255) / 256);
   const long long rounds = (tiles + cus - 1) / cus;
-  return 10 * tiles >= 9 * rounds * cus && (!codes || K >= 24 * 128);
+  return 10 * tiles >= 9 * rounds * cus && (!codes || K > 22 * 128);
 }
 // Whether a call whose row count only the device knows launches both kernels.  The one that ends at once takes 4 to
 // 5 us, so only where a product at capacity takes some twenty times that; else the small tiles run alone.
 FD_RULE bool scaled_both(int n_max, int N, int K, bool codes, int cus) {
   const long long tiles = static_cast<long long>((n_max + 255) / 256) * ((N + 255) / 256);
-  return 10 * tiles >= 9LL * cus && (!codes || K >= 24 * 128) && 2.0 * n_max * N * K >= 1.45e11;
+  return 10 * tiles >= 9LL * cus && (!codes || K > 22 * 128) && 2.0 * n_max * N * K >= 1.45e11;
 }
 
 }  // namespace fd

@@ -185,15 +185,15 @@ __global__ __launch_bounds__(kFewWaves * 64) void scaled_few_kernel(fdh::ScaledA
 
 // ---------------------------------------------------------------- tiles
 
-// A workgroup of WM x WN waves with a tile of 32 FI WM rows x 128 WN columns, K-steps of one block; a
-// wave owns FI x 4 blocks of 32 x 32.  Tiles stream from memory into a ring of LDS stages
+// A workgroup of WM x WN waves with a tile of 32 FI WM rows x 32 NJ WN columns, K-steps of one block; a
+// wave owns FI x NJ blocks of 32 x 32.  Tiles stream from memory into a ring of LDS stages
 // (buffer_load ... lds); in LDS a tile row is eight 16-byte chunks, chunk c of row r at c ^ swz(r), so
 // that the 16 lanes that read a fragment together meet 16 different 16-byte bank groups.
-template <int FI_, int WM_, int WN_, int STAGES_>
+template <int FI_, int NJ_, int WM_, int WN_, int STAGES_>
 struct Tile {
-  static constexpr int FI = FI_, WM = WM_, WN = WN_, STAGES = STAGES_;
+  static constexpr int FI = FI_, NJ = NJ_, WM = WM_, WN = WN_, STAGES = STAGES_;
   static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
-  static constexpr int BM = 32 * FI * WM, BN = 128 * WN;
+  static constexpr int BM = 32 * FI * WM, BN = 32 * NJ * WN;
   static constexpr int LOADS_A = BM / 8 / WAVES, LOADS_W = BN / 8 / WAVES;        // 8 rows of 128 bytes per wave-load
   static constexpr int SCALE_WAVES = (BM + 63) / 64;                              // waves that load row scales; the others column scales
   static constexpr int ISSUED = LOADS_A + LOADS_W + 1;                            // and one of scales or bias
@@ -201,11 +201,12 @@ struct Tile {
   static constexpr int CHUNKS = SIDE + SCALE_WAVES * 16 + 16;                     // row scales, then 256 bytes of column scales
   static constexpr int BIAS = STAGES * CHUNKS;                                    // four slots of the columns' bias
   static constexpr int TOTAL = BIAS + 4 * BN / 4;
+  static_assert(BN % kScaleBlock == 0 && (NJ == 4 || NJ == 2), "whole blocks of columns");
   static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && WAVES % 2 == 0 && SCALE_WAVES < WAVES && BN <= 64 * WAVES, "whole wave-loads");
   static FD_DEVICE int swz(int r) { return (r >> 1) & 7; }
-  // Column of LDS row p: fragment j of 128 columns holds every fourth, from j on, so that a lane of the product
-  // has four consecutive columns in its four fragments.
-  static FD_DEVICE int column(int p) { return (p & ~127) + 4 * (p & 31) + ((p >> 5) & 3); }
+  // Column of LDS row p: fragment j of a wave's columns holds every NJ-th, from j on, so that a lane of the product
+  // has NJ consecutive columns in its NJ fragments.
+  static FD_DEVICE int column(int p) { return (p & ~(32 * NJ - 1)) + NJ * (p & 31) + ((p >> 5) & (NJ - 1)); }
 };
 
 typedef __attribute__((address_space(3))) void* lds_ptr_t;
@@ -246,13 +247,14 @@ FD_DEVICE void wait_barrier(int more) {
       : "memory", "scc");
 }
 
-// 32 rows x 128 columns to memory: acc[j][r] is row 8 (r >> 2) + 4 half + (r & 3) and column 4 l32 + j, so that
-// 32 lanes store one row's 128 columns side by side (with rows spread over the lanes, 16 bytes of 64 rows a store,
+// 32 rows x 32 NJ columns to memory: acc[j][r] is row 8 (r >> 2) + 4 half + (r & 3) and column NJ l32 + j, so that
+// 32 lanes store one row's columns side by side (with rows spread over the lanes, 16 bytes of 64 rows a store,
 // the L2 took 19 us for the 32 MB of a round of tiles).  Every store issues whatever the row, rows and columns
 // outside go nowhere: the waits count the stores.  rows: how many rows from the first on lie inside; off: byte
 // offset of the first row's columns of this lane; pitch: bytes of a row.
-template <int KIND>
+template <int KIND, int NJ>
 struct Rows32 {
+  static_assert(KIND != kToCodes || NJ == 4, "32 lanes hold a block's columns");
   static constexpr int STORES = KIND == kToCodes ? 17 : 16;
   typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -283,12 +285,13 @@ struct Rows32 {
     __builtin_amdgcn_raw_buffer_store_b32(w, y, col_ok && row + 4 * half < rows ? off : kNowhere, row * pitch, 0);
     if constexpr (R < 15) put_codes<R + 1>(v, inv, y, col_ok, half, rows, off, pitch);
   }
-  static FD_DEVICE void store(f32x16_t (&v)[4], const float4 bias, bool gelu, __amdgpu_buffer_rsrc_t y, bool col_ok, int l32, int half,
+  static FD_DEVICE void store(f32x16_t (&v)[NJ], const float (&bias)[NJ], bool gelu, __amdgpu_buffer_rsrc_t y, bool col_ok, int l32, int half,
                               int rows, uint32_t off, uint32_t pitch, __amdgpu_buffer_rsrc_t scale, uint32_t scale_off, uint32_t scale_pitch) {
-    v[0] += bias.x; v[1] += bias.y; v[2] += bias.z; v[3] += bias.w;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) v[j] += bias[j];
     if (gelu) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int r = 0; r < 16; ++r) v[j][r] = fd::gelu(v[j][r]);
     }
@@ -306,7 +309,11 @@ struct Rows32 {
       for (int r = 0; r < 16; ++r) {
         const int row = 8 * (r >> 2) + (r & 3);
         const uint32_t to = col_ok && row + 4 * half < rows ? off : kNowhere;
-        if constexpr (KIND == kToBf16)
+        if constexpr (KIND == kToBf16 && NJ == 2)
+          __builtin_amdgcn_raw_buffer_store_b32(fd::pack_bf2(v[0][r], v[1][r]), y, to, row * pitch, kStream);
+        else if constexpr (NJ == 2)
+          __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(v[0][r]), __float_as_uint(v[1][r])}, y, to, row * pitch, kStream);
+        else if constexpr (KIND == kToBf16)
           __builtin_amdgcn_raw_buffer_store_b64(u32x2{fd::pack_bf2(v[0][r], v[1][r]), fd::pack_bf2(v[2][r], v[3][r])}, y, to, row * pitch, kStream);
         else
           __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(v[0][r]), __float_as_uint(v[1][r]), __float_as_uint(v[2][r]), __float_as_uint(v[3][r])},
@@ -323,15 +330,16 @@ struct Rows32 {
 // ahead.  After sub-step 1 the wave has read its rows, after sub-step 5 its columns; a barrier there frees
 // that part of the stage for the load STAGES steps on, which goes out a few instructions at a time behind
 // products.  The second barrier also publishes the next stage, whose first fragments are read behind
-// sub-steps 6 and 7, so that no sub-step waits for LDS or for the barrier with nothing to compute.  (One barrier
+// sub-steps 6 and 7, so that no sub-step waits for LDS or for the barrier with nothing to compute.  (Waves of two
+// fragments a half have four sub-steps and the one barrier after sub-step 1, which frees all of the stage.  One barrier
 // in the middle of a step, with its operands in registers: the loads have 5 sub-steps to land instead of 7 and 10,
 // 1664 x 1536 x 6144 in 128 x 128 tiles 36.4 us against 28.2.)  A step is one basic block: across branches the
 // compiler gathers the products at the end.
 template <class T, int KIND, class Mma>
 FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
-  constexpr int FI = T::FI, STAGES = T::STAGES;
+  constexpr int FI = T::FI, NJ = T::NJ, STAGES = T::STAGES, kSubs = 2 * NJ;
   constexpr int kSize = KIND == kToCodes ? 1 : KIND == kToBf16 ? 2 : 4;
-  constexpr int kStores = FI * Rows32<KIND>::STORES;
+  constexpr int kStores = FI * Rows32<KIND, NJ>::STORES;
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / T::WN, wn = wave % T::WN;
   const int K = g.K, blocks = (K + kScaleBlock - 1) / kScaleBlock, nk = max(blocks, STAGES), ld = fd::scale_stride(K);
@@ -371,7 +379,7 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
       off_side = static_cast<uint32_t>(min(64 * wave + lane, M - lm0 - 1)) * static_cast<uint32_t>(ld);
     } else {
       rside = buffer_of(g.w_scale + static_cast<size_t>(ln0 / kScaleBlock) * ld);
-      off_side = static_cast<uint32_t>(min(lane % T::WN, (g.N - ln0 - 1) / kScaleBlock) * ld);
+      off_side = static_cast<uint32_t>(min(lane % (T::BN / kScaleBlock), (g.N - ln0 - 1) / kScaleBlock) * ld);
     }
     // the columns' bias (zeros without one), ahead of the tile's first stage.  The tile before this one has
     // yet to read its own, and with STAGES blocks no barrier has passed since the one before that did: four slots.
@@ -411,7 +419,7 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
 
   // ---- the products
   const int arow = 32 * FI * wm + l32;
-  const int wrow = 128 * wn + l32;
+  const int wrow = 32 * NJ * wn + l32;
   // byte offsets in a stage of this lane's two chunks of a half K-block, of its first row and its first column (32 rows on: 4096 bytes)
   uint32_t at_a[2][2], at_w[2][2];
 #pragma unroll
@@ -434,14 +442,14 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
     for (int i = 0; i < FI; ++i) a[kh][i] = read(lds + (slot_at + at_a[kh][0]) + 4096 * i, lds + (slot_at + at_a[kh][1]) + 4096 * i);
   };
   auto read_w = [&](uint32_t slot_at, int s) {
-    const int kh = s >> 2, j = s & 3;
+    const int kh = s / NJ, j = s % NJ;
     w[s & 3] = read(lds + (slot_at + at_w[kh][0]) + 4096 * j, lds + (slot_at + at_w[kh][1]) + 4096 * j);
   };
   auto read_scales = [&](uint32_t slot_at) {
     const uint32_t* side = reinterpret_cast<const uint32_t*>(lds + slot_at + T::SIDE * 16);
 #pragma unroll
     for (int i = 0; i < FI; ++i) sa_next[i] = side[arow + 32 * i];
-    sw_next = side[64 * T::SCALE_WAVES + wn];
+    sw_next = side[64 * T::SCALE_WAVES + 32 * NJ * wn / kScaleBlock];
   };
 
   aim();
@@ -462,7 +470,7 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
   int stored = 0;   // in a tile's first step: the previous tile's stores were issued after the last stage's loads
   for (;;) {
     const int m0 = lm0, n0 = ln0;
-    f32x16_t acc[FI][4] = {};
+    f32x16_t acc[FI][NJ] = {};
     bool more = false;
     int kb = 0;
     // the steps that load this tile, then the last STAGES, which load the next one (or this one's end again)
@@ -480,25 +488,26 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
         for (int i = 0; i < FI; ++i) sa[i] = sa_next[i] >> shift;
         sw = sw_next >> shift;
 #pragma unroll
-        for (int s = 0; s < 8; ++s) {
-          if (s == 2) wait_reads_barrier();
-          if (s == 6) wait_barrier<(STAGES - 2) * T::ISSUED + T::LOADS_A, kStores>(stored);
+        for (int s = 0; s < kSubs; ++s) {
+          // waves of two fragments have read all of the stage by the barrier after sub-step 1
+          if (NJ == 4 && s == 2) wait_reads_barrier();
+          if (s == kSubs - 2) wait_barrier<(STAGES - 2) * T::ISSUED + (NJ == 4 ? T::LOADS_A : 0), kStores>(stored);
           if (s == 0) read_a(slot, 1);
-          if (s < 6) read_w(slot, s + 2);
-          if (s == 6) {
+          if (s < kSubs - 2) read_w(slot, s + 2);
+          if (s == kSubs - 2) {
             read_a(next, 0);
             read_w(next, 0);
             read_scales(next);
           }
-          if (s == 7) read_w(next, 1);
+          if (s == kSubs - 1) read_w(next, 1);
           const typename Mma::frag wf = Mma::make(w[s & 3], sw);
 #pragma unroll
-          for (int i = 0; i < FI; ++i) acc[i][s & 3] = Mma::mma(Mma::make(a[s >> 2][i], sa[i]), wf, acc[i][s & 3], sa[i], sw);
+          for (int i = 0; i < FI; ++i) acc[i][s % NJ] = Mma::mma(Mma::make(a[s / NJ][i], sa[i]), wf, acc[i][s % NJ], sa[i], sw);
           __builtin_amdgcn_sched_barrier(0);
           if (s == 2) issue(slot, std::integral_constant<int, 0>{}, std::integral_constant<int, T::LOADS_A / 2>{});
-          if (s == 4) issue(slot, std::integral_constant<int, T::LOADS_A / 2>{}, std::integral_constant<int, T::LOADS_A>{});
-          if (s == 6) issue(slot, std::integral_constant<int, T::LOADS_A>{}, std::integral_constant<int, T::LOADS_A + T::LOADS_W / 2>{});
-          if (s == 7) {
+          if (s == (NJ == 4 ? 4 : 2)) issue(slot, std::integral_constant<int, T::LOADS_A / 2>{}, std::integral_constant<int, T::LOADS_A>{});
+          if (s == kSubs - 2) issue(slot, std::integral_constant<int, T::LOADS_A>{}, std::integral_constant<int, T::LOADS_A + T::LOADS_W / 2>{});
+          if (s == kSubs - 1) {
             issue(slot, std::integral_constant<int, T::LOADS_A + T::LOADS_W / 2>{}, std::integral_constant<int, T::LOADS_A + T::LOADS_W>{});
             issue_scales(slot);
           }
@@ -510,20 +519,23 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
     }
 
     stored = 1;
-    const int col = 128 * wn + 4 * l32;   // this lane's first column of the tile
+    const int col = 32 * NJ * wn + NJ * l32;   // this lane's first column of the tile
     const bool col_ok = n0 + col < g.N;
-    const float4 bias = reinterpret_cast<const float4*>(ring + T::BIAS + (turn - (more ? 1 : 0) & 3) * (T::BN / 4))[col / 4];
+    const float* columns = reinterpret_cast<const float*>(ring + T::BIAS + (turn - (more ? 1 : 0) & 3) * (T::BN / 4)) + col;
+    float bias[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) bias[j] = columns[j];
     void* base;
     if constexpr (KIND == kToCodes) base = g.y_q;
     else if constexpr (KIND == kToBf16) base = g.y_bf16;
     else base = g.y_f32;
     const int row0 = 32 * FI * wm, lds_y = fd::scale_stride(g.N);
     const auto y = __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t*>(base) + (static_cast<size_t>(m0 + row0) * g.N + n0) * kSize, 0, 0x7fffffff, 0x00020000);
-    const auto ys = __builtin_amdgcn_make_buffer_rsrc(g.y_scale + static_cast<size_t>(m0 + row0) * lds_y + n0 / kScaleBlock + wn, 0, 0x7fffffff, 0x00020000);
+    const auto ys = __builtin_amdgcn_make_buffer_rsrc(g.y_scale + static_cast<size_t>(m0 + row0) * lds_y + (n0 + 32 * NJ * wn) / kScaleBlock, 0, 0x7fffffff, 0x00020000);
 #pragma unroll
     for (int i = 0; i < FI; ++i) {
-      const bool block_ok = n0 + 128 * wn < g.N;   // else no column of this wave
-      Rows32<KIND>::store(acc[i], bias, g.gelu, y, col_ok, l32, half, block_ok ? M - m0 - row0 - 32 * i : 0,
+      const bool block_ok = n0 + 32 * NJ * wn < g.N;   // else no column of this wave
+      Rows32<KIND, NJ>::store(acc[i], bias, g.gelu, y, col_ok, l32, half, block_ok ? M - m0 - row0 - 32 * i : 0,
                           static_cast<uint32_t>((32 * i + 4 * half) * g.N + col) * kSize, static_cast<uint32_t>(g.N) * kSize, ys,
                           static_cast<uint32_t>(32 * i * lds_y), static_cast<uint32_t>(lds_y));
       __builtin_amdgcn_sched_barrier(0);   // 32 rows at a time: fewer registers
@@ -538,9 +550,10 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
 // KB at 64, 1152 clocks beside 512 of matrix instructions; of 256 x 256, 192 and 64 KB, 2560 beside 2048.  9828 x 6144 x
 // 1536 to codes with GELU in 128 x 128 tiles 104 us (1780 TFLOP/s), 9828 x 1536 x 6144 to bf16 in 256 x 256 72 us (2560
 // TFLOP/s; a large fp8 product of the library 2720), 32760 x 1536 x 6144 to fp32 457 us (1350, at half the rate).
-using Tile64 = Tile<1, 2, 1, 3>;      // 64 x 128, two workgroups per CU
-using Tile128 = Tile<1, 4, 1, 2>;     // 128 x 128, two
-using TileLarge = Tile<2, 4, 2, 2>;   // 256 x 256, one
+using Tile64 = Tile<1, 2, 2, 2, 3>;        // 64 x 128, two workgroups per CU, in 32 x 64 a wave: all four SIMDs of a CU that has one
+using Tile64Codes = Tile<1, 4, 2, 1, 3>;   // 64 x 128 where a wave has to hold a block's 128 columns
+using Tile128 = Tile<1, 4, 4, 1, 2>;       // 128 x 128, two
+using TileLarge = Tile<2, 4, 4, 2, 2>;     // 256 x 256, one
 
 // Where both kernels are launched (cus > 0), the one that the row count does not call for ends at once.
 template <int KIND, class Mma, class T, int PER_CU>
@@ -562,7 +575,7 @@ hipError_t launch_scaled_linear(const ScaledArgs& g, hipStream_t s) {
     using Mma = decltype(mma);
     constexpr bool codes = KIND == kToCodes;
     if constexpr (!codes) {
-      if (fd::scaled_few(g.n_rows, g.N, codes, KIND == kToF32, num_cus())) {
+      if (fd::scaled_few(g.n_rows, g.N, g.K, codes, KIND == kToF32, num_cus())) {
         auto few = [&](auto fm, auto nf, auto deep) {
           constexpr int FM = decltype(fm)::value, NF = decltype(nf)::value;
           scaled_few_kernel<KIND, Mma, FM, NF, decltype(deep)::value><<<dim3((g.N + 16 * NF - 1) / (16 * NF), (g.n_rows + 16 * FM - 1) / (16 * FM)), kFewWaves * 64, 0, s>>>(g);
@@ -593,7 +606,8 @@ hipError_t launch_scaled_linear(const ScaledArgs& g, hipStream_t s) {
       scaled_tile_kernel<KIND, Mma, T, PER_CU><<<static_cast<int>(all < most ? (all + 7) / 8 * 8 : most), T::THREADS, 0, s>>>(g, check);
     };
     using std::integral_constant;
-    if (fd::scaled_small(g.n_rows, g.N, cus)) return tiles(Tile64{}, integral_constant<int, 2>{}, 0);
+    using Small = std::conditional_t<codes, Tile64Codes, Tile64>;
+    if (fd::scaled_small(g.n_rows, g.N, cus)) return tiles(Small{}, integral_constant<int, 2>{}, 0);
     if (both || !large) tiles(Tile128{}, integral_constant<int, 2>{}, both ? cus : 0);
     if (both || large) tiles(TileLarge{}, integral_constant<int, 1>{}, both ? cus : 0);
   };

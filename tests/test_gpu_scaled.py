@@ -311,7 +311,7 @@ def test_scaled_linear_tiles(M, N, K, m, to, gelu):
     check_linear(y, ys, a, sa, w, sw, bias, gelu, to, M if m is None else m)
 
 
-@pytest.mark.parametrize("M,N,K,rows", [(9000, 1040, 16, 9000), (9000, 1040, 144, 9010), (8192, 2048, 128, 8192), (8190, 2048, 240, 8192), (700, 272, 48, 700)])
+@pytest.mark.parametrize("M,N,K,rows", [(9000, 1040, 16, 9000), (9000, 1040, 144, 9010), (8192, 2048, 128, 8192), (8190, 2048, 240, 8192), (700, 272, 48, 700), (700, 1040, 240, 700), (700, 1040, 64, 701)])
 @pytest.mark.parametrize("to,gelu", [("bf16", False), ("f32", True), ("8", False)])
 def test_scaled_linear_short_sums(M, N, K, rows, to, gelu):
     """Sums of one and two K-blocks in every kind of tile, several tiles a workgroup; the scales' padding is NaN."""

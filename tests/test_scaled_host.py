@@ -166,7 +166,7 @@ def test_product_rules(tmp_path):
 int main(int, char**) {
   int n, N, K, c;
   while (std::scanf("%d %d %d %d", &n, &N, &K, &c) == 4)
-    std::printf("%d %d %d %d %d\\n", (int)fd::scaled_few(n, N, c, false, 256) + 2 * (int)fd::scaled_few(n, N, c, true, 256), (int)fd::scaled_large(n, N, K, c, 256), (int)fd::scaled_both(n, N, K, c, 256), (int)fd::scaled_small(n, N, 256), (int)fd::scaled_few_wide(N, 256));
+    std::printf("%d %d %d %d %d\\n", (int)fd::scaled_few(n, N, K, c, false, 256) + 2 * (int)fd::scaled_few(n, N, K, c, true, 256), (int)fd::scaled_large(n, N, K, c, 256), (int)fd::scaled_both(n, N, K, c, 256), (int)fd::scaled_small(n, N, 256), (int)fd::scaled_few_wide(N, 256));
 }
 ''')
     exe = tmp_path / "r"
@@ -176,8 +176,8 @@ int main(int, char**) {
              ((32760, 1536, 6144, 0), (0, 1, 1, 0)), ((9828, 1536, 1536, 0), (0, 1, 0, 0)), ((1664, 1536, 6144, 0), (0, 0, 0, 0)),
              ((14280, 4096, 1024, 1), (0, 0, 0, 0)), ((1, 64, 64, 0), (3, 0, 0, 1)), ((1 << 30, 16, 16, 0), (0, 1, 1, 0)), ((9828, 4608, 1536, 0), (0, 1, 0, 0)),
              ((4096, 6144, 1536, 0), (0, 0, 0, 0)), ((1312, 1024, 4096, 0), (0, 0, 0, 1)), ((1366, 1536, 400, 0), (0, 0, 0, 0)), ((1344, 1536, 384, 0), (0, 0, 0, 1)),
-             ((1, 1 << 20, 1024, 0), (3, 1, 0, 0)), ((1, 6144, 1536, 1), (0, 0, 0, 1)), ((32, 12288, 4096, 0), (2, 0, 0, 1)), ((128, 1536, 6144, 0), (3, 0, 0, 1)),
-             ((200, 1536, 6144, 0), (2, 0, 0, 1)), ((400, 1536, 6144, 0), (0, 0, 0, 1))]
+             ((1, 1 << 20, 1024, 0), (3, 1, 0, 0)), ((1, 6144, 1536, 1), (0, 0, 0, 1)), ((32, 12288, 4096, 0), (0, 0, 0, 1)), ((32, 8192, 4096, 0), (3, 0, 0, 1)), ((64, 6144, 1536, 0), (3, 0, 0, 1)), ((128, 1536, 6144, 0), (2, 0, 0, 1)), ((128, 1536, 1536, 0), (3, 0, 0, 1)), ((128, 4608, 6144, 0), (0, 0, 0, 1)),
+             ((200, 1536, 6144, 0), (0, 0, 0, 1)), ((400, 1536, 6144, 0), (0, 0, 0, 1))]
     out = subprocess.run([str(exe)], input="\n".join(" ".join(map(str, c)) for c, _ in cases), capture_output=True, text=True, check=True).stdout
     for line, (case, want) in zip(out.splitlines(), cases):
         assert tuple(map(int, line.split())) == want + (int(case[1] > 4096),), case
