@@ -331,6 +331,32 @@ def test_scaled_linear_few_rows(M, N, K, rows, to, gelu):
     check_linear(y, ys, *case, gelu, to, M)
 
 
+@pytest.mark.parametrize("m", [9984, 5000, 77, 0])
+def test_scaled_linear_row_count_on_the_device(m):
+    """A capacity at which the row count, known on the device alone, picks between 256- and 128-row tiles: the bits of a call
+    with just those rows where the host picks the same tiles (9984 and 5000), else within the bound of check_linear; rows
+    past them stay."""
+    rows, N, K = 9984, 1536, 6144
+    gh.say(f"linear capacity {rows} N={N} K={K} m={m}")
+    rng = np.random.default_rng(6)
+    a, w = torch.empty((rows, K), dtype=torch.uint8), torch.empty((N, K), dtype=torch.uint8)
+    a.copy_(torch.from_numpy(rng.integers(0, 120, (rows, K), dtype=np.uint8)))
+    w.copy_(torch.from_numpy(rng.integers(0, 120, (N, K), dtype=np.uint8)))
+    w += torch.from_numpy(128 * rng.integers(0, 2, (N, K), dtype=np.uint8))
+    sa, sw = (torch.from_numpy(rng.integers(110, 125, (n, ref.stride(K)), dtype=np.uint8)) for n in (rows, N // 128))
+    ad, sad, wd, swd = a.cuda(), sa.cuda(), w.cuda(), sw.cuda()
+    y = torch.full((rows, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    fdl.fd_scaled_linear(ad, sad, wd, swd, y, m=count(m))
+    assert bool((y[m:] == 7.0).all())
+    if m in (9984, 5000):
+        alone = torch.empty((m, N), dtype=torch.bfloat16, device="cuda")
+        fdl.fd_scaled_linear(ad[:m], sad[:m], wd, swd, alone)
+        assert torch.equal(y[:m], alone)
+    some = np.unique(np.r_[:min(m, 40), max(0, m - 40):m].astype(int))
+    if len(some):
+        check_linear(y[some].cpu(), None, a[some].numpy(), sa[some].numpy(), w.numpy(), sw.numpy(), None, False, "bf16", len(some))
+
+
 @pytest.mark.parametrize("M", [5, 200])
 def test_scaled_linear_bad_blocks(M):
     """A NaN block of a row makes that row NaN, one of the weights its 128 columns; the rest is as without it."""
