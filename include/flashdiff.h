@@ -451,9 +451,11 @@ fd_status fd_rope_axes(int32_t n_rows, int32_t n_tokens, const fd_rope* rope, in
  *   y_scale (codes and row scales)
  * n_in and n_out are multiples of 16, at most 2^20; weights below 2 GiB.  Codes, bias and
  * outputs 16-byte, scales 4-byte aligned.  Sums to bf16 and codes are off by up to 2^-10
- * of the sum of the products' magnitudes (with random operands by some 1.5e-5 of their own
- * size) before they are rounded, those to fp32 by fp32's roundings, with values below
- * 2^-126 taken as zeros.
+ * of the sum of the products' magnitudes (with random operands by some 2e-5 of their own
+ * size) before they are rounded: a bf16 result or a code that near a tie may be the other
+ * neighbour, and a block whose maximum is that near 448 times a power of two may have the
+ * next scale and its codes.  Sums to fp32 are off by fp32's roundings, with values below
+ * 2^-126 taken as zeros; a caller that needs them so takes y_fp.
  */
 fd_status fd_scaled_linear(int32_t n_rows, int32_t n_out, int32_t n_in, const uint8_t* a, const uint8_t* a_scale,
                            const uint8_t* w, const uint8_t* w_scale, const float* bias, int32_t gelu, const int32_t* m,

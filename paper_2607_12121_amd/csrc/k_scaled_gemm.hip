@@ -19,8 +19,10 @@ enum { kToBf16, kToF32, kToCodes };
 // Two ways to the sum of one K-block of 128:
 // - 8-bit: v_mfma_scale_f32_*_f8f6f4.  It adds 8 products at a time on a grid 2^-13 below the
 //   largest of them (measured: 1 + 2^-14 gives 1 within such a group, and is exact across groups and
-//   with the accumulator), which leaves random operands' sums off by 1.5e-5 of their size.
-//   Outputs of 8 (bf16) or 4 (e4m3) bits of mantissa round by 100 times that at least.
+//   with the accumulator; v_mfma_f32_32x32x16_fp8_fp8 is no different), which leaves random operands'
+//   sums off by 2e-5 of their size.  Outputs of 8 (bf16) or 4 (e4m3) bits of mantissa round by 100 times
+//   that at least; one that near a tie, or a block maximum that near a scale's limit, may go the other way.
+//   Codes through the exact way below: 1021 x 4288 x 1088 20.7 us for 14.4, 9828 x 6144 x 1536 183 for 107.
 // - exact: the codes times their scales as bf16 (exact from 2^-126 on) through v_mfma_f32_*_bf16, half the
 //   rate, whose sums are fp32's.  fp32 outputs take this one.
 struct Mma8 {
