@@ -1,0 +1,149 @@
+"""The 8-bit operators where their kernels take another path: products in 256 x 256 tiles with a bias, GELU, 8-bit
+results and short or ragged sums, blocks of NaN and far scale bytes through every kind of result, and norms of more rows than waves, whose requests change inside a run."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import scaled as ref
+from paper_2607_12121_amd import flashdiff as fdl
+from tests import gpu_harness as gh
+from tests.test_gpu_scaled import U32, check_linear, linear_case, rms_case, run_linear, run_rms
+from tests.test_gpu_scaled_precision import check_same_codes
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    fdl.lib()
+
+
+# ------------------------------------------------------------------ product
+
+# (M, N, K): 256 x 256 tiles where the row count is the host's (test_scaled_host.py holds the rule to it).  Short sums, last
+# blocks of 16 and of 112 columns, tiles that rows and columns leave part of, one tile a workgroup and two.
+LARGE_WIDE = [(8192, 2048, 16), (8190, 2032, 240), (8190, 2048, 512), (14999, 2032, 144)]
+LARGE_CODES = [(3500, 4112, 2896), (6800, 4368, 2832)]
+
+
+@pytest.mark.parametrize("M,N,K", LARGE_WIDE)
+@pytest.mark.parametrize("to,gelu", [("bf16", False), ("bf16", True), ("f32", False), ("f32", True)])
+def test_large_tiles(M, N, K, to, gelu):
+    gh.say(f"linear M={M} N={N} K={K} to={to} gelu={gelu}")
+    case = linear_case(M, N, K, 5)
+    y, ys = run_linear(*case, gelu, to, M, None)
+    check_linear(y, ys, *case, gelu, to, M)
+
+
+@pytest.mark.parametrize("M,N,K", LARGE_CODES)
+@pytest.mark.parametrize("gelu", [False, True])
+def test_large_tiles_to_codes(M, N, K, gelu):
+    gh.say(f"linear M={M} N={N} K={K} to codes, gelu={gelu}")
+    case = linear_case(M, N, K, 5)
+    y, ys = run_linear(*case, gelu, "8", M, None)
+    check_linear(y, ys, *case, gelu, "8", M)
+
+
+@pytest.mark.parametrize("m", [6800, 3000, 77, 0])
+def test_codes_with_the_row_count_on_the_device(m):
+    """A capacity at which both tiles of 8-bit results are launched and the row count picks: codes and scale bytes of the
+    call with just those rows where the host picks the same tiles (6800 and 3000), else within the bound of check_linear; rows
+    past them stay."""
+    M, N, K = LARGE_CODES[1]
+    gh.say(f"linear capacity {M} N={N} K={K} to codes, m={m}")
+    a, sa, w, sw, bias = linear_case(M, N, K, 6)
+    y, ys = run_linear(a, sa, w, sw, bias, True, "8", M, m)
+    if m in (6800, 3000):
+        y2, ys2 = run_linear(a[:m], sa[:m], w, sw, bias, True, "8", m, None)
+        assert torch.equal(y[:m], y2) and np.array_equal(ys[:m], ys2)
+    some = np.unique(np.r_[:min(m, 40), max(0, m - 40):m].astype(int))
+    if len(some):
+        check_linear(y[some], ys[some], a[some], sa[some], w, sw, bias, True, "8", len(some))
+    nk = -(-N // 128)
+    assert (y[m:] == 0x55).all() and np.all(ys[m:] == 0x55) and np.all(ys[:, nk:] == 0x55)
+
+
+@pytest.mark.parametrize("to", ["bf16", "8"])
+@pytest.mark.parametrize("M,N,K", [(5, 400, 400), (200, 400, 400), (3000, 1536, 400), (8190, 2048, 400), (3500, 4112, 2896)])
+def test_bad_blocks(M, N, K, to):
+    """A NaN block of a row makes that row NaN, one of the weights its 128 columns, as values and as 8-bit blocks; the rest
+    has the bits that it has without them."""
+    gh.say(f"NaN blocks M={M} N={N} K={K} to={to}")
+    case = linear_case(M, N, K)
+    a, sa, w, sw, bias = (x.copy() for x in case)
+    a[3, 128:256], sa[3, 1] = 0x7f, 255
+    w[128:256, 384:512], sw[1, 3] = 0x7f, 255
+    (y, ys), (clean, cs) = run_linear(a, sa, w, sw, bias, False, to, M, None), run_linear(*case, False, to, M, None)
+    bad = np.zeros((M, N), bool)
+    bad[3], bad[:, 128:256] = True, True
+    if to == "8":
+        y, clean, nk = y.numpy(), clean.numpy(), -(-N // 128)
+        assert np.all((y[bad] & 127) == 127) and np.array_equal(ys[:, :nk] == 255, bad[:, ::128])
+        assert np.array_equal(ys[:, :nk][~bad[:, ::128]], cs[:, :nk][~bad[:, ::128]])
+    else:
+        assert np.array_equal(torch.isnan(y).numpy(), bad)
+        y, clean = y.view(torch.int16).numpy(), clean.view(torch.int16).numpy()
+    assert np.array_equal(y[~bad], clean[~bad])
+
+
+@pytest.mark.parametrize("s", [0, 1, 2, 60, 127, 200, 246, 253, 254])
+@pytest.mark.parametrize("to", ["bf16", "f32", "8"])
+@pytest.mark.parametrize("M", [5, 200])
+def test_every_finite_scale_byte(M, to, s):
+    """Rows' scale bytes from 0 (2^-127, which fd_quant_blocks does not write) to 254, against weights that bring the product
+    back towards ordinary size.  Codes are cut to values that are normal in fp32: 2 or more, or zero, beside the smallest
+    scales, 1 or less beside the largest."""
+    gh.say(f"scale byte {s} M={M} to={to}")
+    a, sa, w, sw, _ = linear_case(M, 144, 256, 9)
+    sa[:, :2], sw[:, :2] = s, np.clip(250 - s, 1, 246)
+    mag = a & 0x7f
+    if s < 3:
+        a = np.where(mag >= 0x40, a, 0).astype(np.uint8)
+    if s > 246:
+        a = ((a & 0x80) | np.minimum(mag, 0x38)).astype(np.uint8)
+    if sw[0, 0] < 20:
+        w = np.where((w & 0x7f) >= 0x40, w, 0).astype(np.uint8)
+    y, ys = run_linear(a, sa, w, sw, None, False, to, M, None)
+    check_linear(y, ys, a, sa, w, sw, None, False, to, M)
+
+
+# ------------------------------------------------------------------ residual and norm
+
+@pytest.mark.parametrize("parts", ["ygwm", "m", "yg"])
+@pytest.mark.parametrize("rows,D,B,m", [
+    (9001, 320, 40, 8999), (5000, 768, 5, 5000), (4099, 1024, 9, 4099), (2100, 1088, 30, 2099), (3200, 1536, 2, 3200), (1500, 2064, 7, 1500),
+    (1300, 6144, 4, 1290), (1100, 8192, 6, 1100), (1100, 12288, 3, 1030),
+    (33, 528, 3, 30), (7, 1024, 2, 7), (5, 4112, 2, 5), (3, 6144, 3, 2)])
+def test_rms_runs(rows, D, B, m, parts):
+    """Runs of several rows a team of one, two and four waves, whose requests begin inside a run, one or more of them empty; and
+    the widths between the forms.  fp32 errors as in test_rms_quant of test_gpu_scaled.py."""
+    gh.say(f"rms {rows}x{D} B={B} m={m} parts={parts!r}")
+    h, y, mod, weight, cu = rms_case(rows, D, B, m, parts, 1)
+    if B > 2:
+        cu[2] = cu[1]   # an empty request between two others
+    got, q, s = run_rms(h, y, mod, weight, cu, m, parts)
+    of_row = np.repeat(np.arange(B), np.diff(cu))
+    pick = lambda i, on: mod[of_row, i * D:(i + 1) * D].astype(np.float64) if on in parts else None  # noqa: E731
+    y64 = None if y is None else y.double().numpy()[:m]
+    gate, shift, scale = pick(2, "g"), pick(0, "m"), pick(1, "m")
+    wh, wa = ref.rms(h[:m], y64, gate, None if weight is None else weight.astype(np.float64), shift, scale, 1e-6)
+    add = 0.0 if y64 is None else np.abs(y64) * (1.0 if gate is None else np.abs(gate))
+    assert np.all(np.abs(got[:m] - wh) <= 2 * U32 * (np.abs(wh) + add))
+    np.testing.assert_array_equal(got[m:], h[m:])
+    base = np.abs(wa - (0 if shift is None else shift))
+    h_err = 2 * U32 * (np.abs(wh) + add) / np.sqrt(np.mean(wh * wh, 1, keepdims=True))
+    w_abs = (1.0 if weight is None else np.abs(weight)) * (1.0 if scale is None else np.abs(1 + scale))
+    err = (28 + 8 + 2) * U32 * base + h_err * w_abs + 2 * U32 * np.abs(wa)
+    check_same_codes(q[:m], s[:m], wa, err, 0.99)
+    assert np.all(q[m:] == 0x55) and np.all(s[m:] == 0x55)
+
+
+def test_residual_alone_in_runs():
+    """h's update without codes, more rows than teams: the bits of the call that writes codes too."""
+    h, y, mod, _, cu = rms_case(5000, 1088, 6, 4990, "yg", 2)
+    want, _, _ = run_rms(h, y, mod, None, cu, 4990, "yg")
+    x, d_mod = torch.from_numpy(h).cuda(), torch.from_numpy(mod).cuda()
+    fdl.fd_rms_quant(x, None, None, torch.from_numpy(cu).cuda(), torch.tensor([4990], dtype=torch.int32, device="cuda"), y=y.cuda(), gate=d_mod[:, 2176:])
+    assert np.array_equal(x.cpu().numpy(), want)

@@ -224,3 +224,29 @@ def test_scaled_block_refuses():
     assert call(dims=fdl.FdDims(64, 4096, 32, 128, 1 << 19)) == 3   # 2 GiB of MLP weights
     for x in ("h", "k", "v", "ws"):
         assert call(**{x: P + 8}) == 1
+
+
+def test_large_tile_cases_run_large_tiles(tmp_path):
+    """The GPU tests of the 256 x 256 tiles have shapes that the rules send there, two tiles a workgroup among them; the
+    one whose row count the device picks by launches both kernels."""
+    from tests.test_gpu_scaled_paths import LARGE_CODES, LARGE_WIDE
+    src = tmp_path / "r.cpp"
+    src.write_text('''
+#include <cstdio>
+#include "fd_scaled_rules.h"
+int main(int, char**) {
+  int n, N, K, c;
+  while (std::scanf("%d %d %d %d", &n, &N, &K, &c) == 4)
+    std::printf("%d %d %d\\n", (int)(fd::scaled_few(n, N, K, c, false, 256) || fd::scaled_small(n, N, 256)), (int)fd::scaled_large(n, N, K, c, 256), (int)fd::scaled_both(n, N, K, c, 256));
+}
+''')
+    exe = tmp_path / "r"
+    subprocess.run(["g++", "-std=c++17", f"-I{build.CSRC}", str(src), "-o", str(exe)], check=True)
+    cases = [(*s, 0) for s in LARGE_WIDE] + [(*s, 1) for s in LARGE_CODES] + [(3000, *LARGE_CODES[1][1:], 1)]
+    out = subprocess.run([str(exe)], input="\n".join(" ".join(map(str, c)) for c in cases), capture_output=True, text=True, check=True).stdout
+    got = [tuple(map(int, line.split())) for line in out.splitlines()]
+    assert all(few_or_small == 0 for few_or_small, _, _ in got)
+    assert [large for _, large, _ in got] == [1] * (len(cases) - 1) + [0]
+    assert got[-2][2] == 1
+    tiles = [-(-M // 256) * -(-N // 256) for M, N, _, _ in cases[:-1]]
+    assert max(tiles[:len(LARGE_WIDE)]) > 256 and max(tiles[len(LARGE_WIDE):]) > 256
