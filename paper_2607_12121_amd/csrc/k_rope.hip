@@ -21,10 +21,10 @@ enum { kInterleaved, kHalvesWide, kHalves };
 // the axis' section; the partner is read again from the row (it is in the L1), 16 bytes at a time
 // where every dim is a multiple of 16 (kHalvesWide), else value by value.
 template <int KIND>
-__global__ __launch_bounds__(256) void rope_kernel(fdh::RopeArgs g) {
+__global__ __launch_bounds__(256) void rope_kernel(fdh::RopeArgs g, int row0) {
   __shared__ float2 turn[4][64];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int row = blockIdx.x * 4 + wave;
+  const int row = row0 + blockIdx.x * 4 + wave;
   if (row >= min(*g.m, g.n_rows)) return;   // no barrier follows: each wave reads its own table
   const int tok = g.idx ? g.idx[row] : row;
   const int dh = g.dh;
@@ -99,13 +99,18 @@ __global__ __launch_bounds__(256) void rope_kernel(fdh::RopeArgs g) {
 namespace fdh {
 
 hipError_t launch_rope(const RopeArgs& g, bool halves, hipStream_t s) {
-  const int grid = (g.n_rows + 3) / 4;
   bool wide = true;
   for (int a = 0; a < g.n_axes; ++a) wide = wide && g.dim[a] % 16 == 0;
-  if (!halves) rope_kernel<kInterleaved><<<grid, 256, 0, s>>>(g);
-  else if (wide) rope_kernel<kHalvesWide><<<grid, 256, 0, s>>>(g);
-  else rope_kernel<kHalves><<<grid, 256, 0, s>>>(g);
-  return hipGetLastError();
+  // a launch has fewer than 2^32 threads, 64 of them a row
+  constexpr int kRows = 1 << 25;
+  for (int row0 = 0; row0 < g.n_rows; row0 += kRows) {
+    const int rows = g.n_rows - row0 < kRows ? g.n_rows - row0 : kRows, grid = (rows + 3) / 4;
+    if (!halves) rope_kernel<kInterleaved><<<grid, 256, 0, s>>>(g, row0);
+    else if (wide) rope_kernel<kHalvesWide><<<grid, 256, 0, s>>>(g, row0);
+    else rope_kernel<kHalves><<<grid, 256, 0, s>>>(g, row0);
+    if (const hipError_t e = hipGetLastError()) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace fdh

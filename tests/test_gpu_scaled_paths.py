@@ -147,3 +147,25 @@ def test_residual_alone_in_runs():
     x, d_mod = torch.from_numpy(h).cuda(), torch.from_numpy(mod).cuda()
     fdl.fd_rms_quant(x, None, None, torch.from_numpy(cu).cuda(), torch.tensor([4990], dtype=torch.int32, device="cuda"), y=y.cuda(), gate=d_mod[:, 2176:])
     assert np.array_equal(x.cpu().numpy(), want)
+
+
+# ------------------------------------------------------------------ rotary positions
+
+def test_rope_of_more_rows_than_a_launch_has():
+    """2^26 + 5 rows of 3 x 16, 64 threads a row: rows at both ends and where one launch meets the next, against the same rows
+    in a call of their own."""
+    rows, dh = (1 << 26) + 5, 16
+    gh.say(f"rope of {rows} rows")
+    pick = torch.cat([torch.arange(a, b) for a, b in ((0, 50), ((1 << 25) - 50, (1 << 25) + 50), ((1 << 26) - 50, rows))]).cuda()
+    x = torch.zeros((rows, 3 * dh), dtype=torch.bfloat16, device="cuda")
+    part = torch.randn((len(pick), 3 * dh), device="cuda").to(torch.bfloat16)
+    x[pick] = part
+    coord = torch.zeros((rows, 1), dtype=torch.int32, device="cuda")
+    coord[pick] = torch.arange(1, len(pick) + 1, dtype=torch.int32, device="cuda")[:, None]
+    m = torch.tensor([rows], dtype=torch.int32, device="cuda")
+    (q, k, v), (q2, k2, v2) = ([torch.zeros((n, dh), dtype=torch.bfloat16, device="cuda") for _ in range(3)] for n in (rows, len(pick)))
+    kw = dict(heads=1, kv_heads=1, head_dim=dh, dims=[16])
+    fdl.fd_rope_axes(x, coord, None, m, q, k, v, **kw)
+    fdl.fd_rope_axes(part, coord[pick].contiguous(), None, m, q2, k2, v2, **kw)
+    assert torch.equal(q[pick], q2) and torch.equal(k[pick], k2) and torch.equal(v[pick], v2)
+    assert not torch.equal(q2, part[:, :dh])
