@@ -486,7 +486,7 @@ typedef struct fd_scaled_weights {
  *   coord  device int32 [N][n_axes], read with rope only
  *   ws     device scratch of fd_scaled_block_ws_size bytes, 256-byte aligned;
  *          fd_region_importance reads it as it reads fd_block_forward's
- * Other arguments, limits and errors as fd_block_forward.
+ * Other arguments, limits and errors as fd_block_forward; at most 2^30 tokens.
  */
 size_t fd_scaled_block_ws_size(const fd_plan* plan, const fd_dims* dims);
 fd_status fd_scaled_block_forward(const fd_plan* plan, const fd_dims* dims, const fd_scaled_weights* w,

@@ -701,6 +701,7 @@ fd_status fd_scaled_block_forward(const fd_plan* plan, const fd_dims* dims, cons
   FD_REQUIRE(aligned(h, 16) && aligned(k_cache, 16) && aligned(v_cache, 16) && aligned(ws, kAlign) && aligned(w->mod, 16),
              "misaligned buffer");
   FD_TRY(check_attention(plan, dims));
+  FD_TRY(check_rows(plan->n_tokens));
   const int D = dims->D, F = dims->F, B = plan->n_requests, N = plan->n_tokens;
   const long long widest = F > 3LL * D ? F : 3LL * D;
   if (widest > (1 << 20) || widest * D > fdh::kMaxGemmBytes)

@@ -250,3 +250,12 @@ int main(int, char**) {
     assert got[-2][2] == 1
     tiles = [-(-M // 256) * -(-N // 256) for M, N, _, _ in cases[:-1]]
     assert max(tiles[:len(LARGE_WIDE)]) > 256 and max(tiles[len(LARGE_WIDE):]) > 256
+
+
+@no_gpu
+def test_scaled_block_refuses_rows_beyond_its_steps():
+    """More tokens than the steps' row numbers hold: refused before the first of them is enqueued."""
+    n = (1 << 30) + 1
+    plan, d, w = fdl.FdPlan(n, 1025, 1024, 1 << 20, 1 << 20, *([P] * 6)), fdl.FdDims(16, 128, 2, 64, 256), fdl.FdScaledWeights(*[P] * 15)
+    st = fdl.lib().fd_scaled_block_forward(ctypes.byref(plan), ctypes.byref(d), ctypes.byref(w), None, None, *([P] * 7), 1 << 62, None)
+    assert st == 3 and b"rows" in fdl.lib().fd_last_error()
