@@ -412,7 +412,9 @@ enum { FD_ROPE_INTERLEAVED = 0, FD_ROPE_HALVES = 1 };
 /* Rotary positions on up to four axes (a video's time, height and width): the head's
  * first dim[0] values turn with the first axis, the next dim[1] with the second, ...;
  * values past the last section are not turned.  Pair j of axis a turns by
- *   pos_a * step[a] * theta[a]^(-2j / dim[a])  radians. */
+ *   pos_a * step[a] * theta[a]^(-2j / dim[a])  radians,
+ * an angle that is off by at most 2^-26 + |pos| (2^-48 + 2^-58 r) of a turn where the pair
+ * turns r times per position (and theta is within 1e-12 .. 1e12). */
 typedef struct fd_rope {
   int32_t n_axes;      /* 1 .. 4                                      */
   int32_t pairing;     /* FD_ROPE_INTERLEAVED or FD_ROPE_HALVES       */

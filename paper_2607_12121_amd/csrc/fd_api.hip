@@ -167,8 +167,12 @@ fd_status rope_turns(const fd_rope* r, int dh, fdh::RopeArgs* g) {
     FD_REQUIRE(r->theta[a] > 0 && isfinite(r->theta[a]) && isfinite(r->step[a]), "axis %d: theta or step", a);
     g->dim[a] = d;
     for (int j = 0; j < d / 2; ++j) {
-      const double turns = r->step[a] * pow(r->theta[a], -2.0 * j / d) / 6.283185307179586;
+      double turns = r->step[a] * pow(r->theta[a], -2.0 * j / d) / 6.283185307179586;
       FD_REQUIRE(fabs(turns) <= 1 << 20, "axis %d: %g turns per position", a, turns);
+      if (fabs(turns) > 0.5) {   // positions are whole numbers: whole turns of each go, and the rest keeps its bits
+        const long double t = r->step[a] * powl(r->theta[a], -2.0L * j / d) / 6.283185307179586476925L;
+        turns = static_cast<double>(t - rintl(t));
+      }
       g->turns[g->pairs++] = turns;
     }
   }

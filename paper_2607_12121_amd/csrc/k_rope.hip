@@ -6,8 +6,10 @@
 //
 // One wave per row.  The angle is the same for every head, so lane p < dh / 2 forms the cosine and
 // sine of pair p once per row, from the angle in turns: pos * (step theta^.. / 2 pi) in fp64, whose
-// nearest integer is taken off before the rest, at most half a turn, is rounded to fp32 (an error of
-// 2^-26 of a turn for positions up to 10^8; in fp32 a position of 10^5 would be off by 2^-8 of a turn).  Each
+// nearest integer is taken off before the rest, at most half a turn, is rounded to fp32 (an error of 2^-26 of a
+// turn, and of |pos| 2^-52 from the product and its factor where theta >= 1 and the step is at most 1; in fp32 a
+// position of 10^5 would be off by 2^-8 of a turn).  Pairs that turn more than half a turn per position come with
+// their whole turns taken off in 64 bits of mantissa: |pos| 2^-58 of their turns per position.  Each
 // lane then takes 8 consecutive values of a head at a time; 64 lanes are a whole number of heads, so
 // a lane meets the same place in every head and keeps its cosines and sines in registers.  9828 rows of 36 heads of
 // 128: 40 us (4.5 TB/s); 1664 rows of 40 heads of 64: 8, a chain of index, position, values and results.

@@ -1,5 +1,7 @@
 """The 8-bit operators where their kernels take another path: products in 256 x 256 tiles with a bias, GELU, 8-bit
 results and short or ragged sums, blocks of NaN and far scale bytes through every kind of result, and norms of more rows than waves, whose requests change inside a run."""
+from decimal import Decimal, localcontext
+
 import numpy as np
 import pytest
 import torch
@@ -169,3 +171,39 @@ def test_rope_of_more_rows_than_a_launch_has():
     fdl.fd_rope_axes(part, coord[pick].contiguous(), None, m, q2, k2, v2, **kw)
     assert torch.equal(q[pick], q2) and torch.equal(k[pick], k2) and torch.equal(v[pick], v2)
     assert not torch.equal(q2, part[:, :dh])
+
+
+def rest_of_turns(pos, dim, theta, step):
+    """pos * step * theta^(-2j / dim) / 2 pi without its whole turns, from 70 digits: [len(pos)][dim / 2], and the turns per
+    position [dim / 2]."""
+    with localcontext() as c:
+        c.prec = 70
+        two_pi = 2 * Decimal("3.1415926535897932384626433832795028841971693993751058209749445923078164")
+        rate = [Decimal(step) * Decimal(theta) ** (Decimal(-2 * j) / Decimal(dim)) / two_pi for j in range(dim // 2)]
+        turns = [[int(p) * r for r in rate] for p in pos]
+        return np.array([[float(t - t.to_integral_value()) for t in row] for row in turns]), np.array([abs(float(r)) for r in rate])
+
+
+@pytest.mark.parametrize("halves", [False, True])
+@pytest.mark.parametrize("theta,step", [(1e4, 1.0), (1e4, 6.5e6), (100.0, -40.0), (0.25, 3.0), (1e4, 1e5)])
+def test_rope_of_far_positions(theta, step, halves):
+    """Positions to the ends of int32 and pairs that turn up to a million times per position, against angles from 70 digits,
+    within the error that the header states: 2^-26 + |pos| (2^-48 + 2^-58 r) of a turn, as radians times the pair's length; cosine,
+    sine and products as in test_rope of test_gpu_scaled.py."""
+    gh.say(f"rope theta={theta} step={step} halves={halves}")
+    pos = np.array([0, 1, -1, 12345, 1_000_003, -99_999_999, 100_000_000, 1_234_567_891, 2 ** 31 - 1, -2 ** 31], np.int64)
+    rows, dh = len(pos), 64
+    x = torch.from_numpy(np.random.default_rng(11).standard_normal((rows, 3 * dh)).astype(np.float32)).to(torch.bfloat16)
+    q, k, v = (torch.zeros((rows, dh), dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    fdl.fd_rope_axes(x.cuda(), torch.from_numpy(pos.astype(np.int32))[:, None].cuda(), None, torch.tensor([rows], dtype=torch.int32, device="cuda"),
+                     q, k, v, heads=1, kv_heads=1, head_dim=dh, dims=[dh], theta=theta, step=step, halves=halves)
+    rest, rate = rest_of_turns(pos, dh, theta, step)
+    c, n = np.cos(2 * np.pi * rest), np.sin(2 * np.pi * rest)
+    err = 2 * np.pi * (2.0 ** -26 + np.abs(pos)[:, None] * (2.0 ** -48 + 2.0 ** -58 * rate))
+    for got, at in ((q, 0), (k, dh)):
+        x64, got = x.double().numpy()[:, at:at + dh], got.double().cpu().numpy()
+        a, b = (slice(0, dh // 2), slice(dh // 2, dh)) if halves else (slice(0, dh, 2), slice(1, dh, 2))
+        u, w = x64[:, a], x64[:, b]
+        for part, want in ((a, u * c - w * n), (b, u * n + w * c)):
+            far = err * np.hypot(u, w) + 2.0 ** -21 * (np.abs(u) + np.abs(w))
+            assert np.all(np.abs(got[:, part] - want) <= 2.0 ** -8 * np.abs(want) + (1 + 2.0 ** -8) * far)
