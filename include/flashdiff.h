@@ -368,7 +368,8 @@ fd_status fd_scatter_update(const fd_plan* plan, int32_t C, float* x, const floa
  * NaN in every code.  Scale bytes are [rows or row blocks][fd_scale_stride(cols)]:
  * byte kb of a row belongs to columns 128 kb ..; the padding is not written and its
  * values are not used.  Row counts `m` are device int32 [1], at most n_rows (the capacity,
- * up to 2^30); outputs past them are untouched.  Column counts are multiples of 16.
+ * up to 2^30); outputs past them are untouched.  Column counts are multiples of 16, at
+ * most 2^30 (fewer where an entry point says so).
  * Outputs overlap neither inputs nor each other.
  */
 int32_t fd_scale_stride(int32_t cols); /* ceil(cols / 128) rounded up to a multiple of 4; 0 for cols < 1 */

@@ -140,8 +140,9 @@ fd_status check_C(int C) {
     if (st_ != FD_OK) return st_;     \
   } while (0)
 
-// Column counts of 8-bit rows: 16-byte aligned rows.
+// Column counts of 8-bit rows: 16-byte aligned rows, and column numbers that run past the last by at most a block.
 fd_status check_cols(int cols) {
+  if (cols > (1 << 30)) return fdh::set_error("%d columns, more than 2^30", cols), FD_E_UNSUPPORTED;
   if (cols % 16) return fdh::set_error("%d columns, not a multiple of 16", cols), FD_E_UNSUPPORTED;
   return FD_OK;
 }

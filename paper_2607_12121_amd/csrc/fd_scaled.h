@@ -15,7 +15,7 @@ constexpr int kScaleBlock = 128;
 
 // Bytes between the scale rows of `cols` columns: a byte per block, padded to whole 4-byte words
 // (the product reads the scales of four blocks with one load).
-__host__ __device__ inline int scale_stride(int cols) { return ((cols + kScaleBlock - 1) / kScaleBlock + 3) & ~3; }
+__host__ __device__ inline int scale_stride(int cols) { return (cols / kScaleBlock + (cols % kScaleBlock != 0) + 3) & ~3; }
 
 // |x| as ordered bits: the integer maximum of these is the largest magnitude, and infinities and
 // NaN come out on top (which a float maximum would drop).

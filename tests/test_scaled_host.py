@@ -259,3 +259,18 @@ def test_scaled_block_refuses_rows_beyond_its_steps():
     plan, d, w = fdl.FdPlan(n, 1025, 1024, 1 << 20, 1 << 20, *([P] * 6)), fdl.FdDims(16, 128, 2, 64, 256), fdl.FdScaledWeights(*[P] * 15)
     st = fdl.lib().fd_scaled_block_forward(ctypes.byref(plan), ctypes.byref(d), ctypes.byref(w), None, None, *([P] * 7), 1 << 62, None)
     assert st == 3 and b"rows" in fdl.lib().fd_last_error()
+
+
+def test_scale_stride_to_the_last_column_count():
+    for cols in ((1 << 30) + 1, 2 ** 31 - 129, 2 ** 31 - 128, 2 ** 31 - 127, 2 ** 31 - 1):
+        assert fdl.fd_scale_stride(cols) == ref.stride(cols)
+
+
+@no_gpu
+def test_columns_beyond_32_bits_refused():
+    lib = fdl.lib()
+    for cols in ((1 << 30) + 16, 2 ** 31 - 128, 2 ** 31 - 16):
+        assert lib.fd_quant_blocks(1, cols, 1, P, None, P, P, None) == 3 and b"columns" in lib.fd_last_error()
+        assert lib.fd_quant_blocks(1, cols, 128, P, None, P, P, None) == 3
+        assert lib.fd_rms_quant(1, cols, 1, P, None, None, None, None, None, 0, 1e-6, None, P, P, P, None) == 3
+        assert lib.fd_scaled_linear(1, 64, cols, P, P, P, P, None, 0, None, P, None, None, None, None) == 3
