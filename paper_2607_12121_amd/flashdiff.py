@@ -637,6 +637,10 @@ class SparseStep:
                  coord: Optional[torch.Tensor] = None):
         if scaled is None and (rope is not None or coord is not None):
             raise FlashDiffError("rotary positions belong to the 8-bit blocks: give `scaled` too")
+        if (rope is None) != (coord is None):
+            raise FlashDiffError("rotary positions need both `rope` and `coord`")
+        if coord is not None and tuple(coord.shape) != (plan.n_tokens, rope.n_axes):
+            raise FlashDiffError(f"coord must be [{plan.n_tokens}, {rope.n_axes}], got {tuple(coord.shape)}")
         self.plan, self.d, self.params, self.L = plan, d, params, n_layers
         N, R, B, C, D = plan.n_tokens, plan.n_regions, plan.n_requests, d.C, d.D
         dev = torch.device(device)

@@ -274,3 +274,13 @@ def test_columns_beyond_32_bits_refused():
         assert lib.fd_quant_blocks(1, cols, 128, P, None, P, P, None) == 3
         assert lib.fd_rms_quant(1, cols, 1, P, None, None, None, None, None, 0, 1e-6, None, P, P, P, None) == 3
         assert lib.fd_scaled_linear(1, 64, cols, P, P, P, P, None, 0, None, P, None, None, None, None) == 3
+
+
+def test_step_refuses_half_of_the_rotary_positions():
+    """A descriptor without positions would fail in the first step, after the gate has moved on; positions without a
+    descriptor would be ignored; positions laid out the other way round would turn by the wrong ones."""
+    plan = fdl.make_plan(np.zeros(6, np.int32), np.array([0, 6]), 1, device="cpu")
+    d, r, pos = fdl.dims(16, 64, 1, 64, 256), fdl.rope_axes([32, 32]), torch.zeros(6, 2, dtype=torch.int32)
+    for rope, coord, why in ((r, None, "both"), (None, pos, "both"), (r, pos.t().contiguous(), "6, 2"), (r, pos[:5], "6, 2"), (r, pos[:, :1], "6, 2")):
+        with pytest.raises(fdl.FlashDiffError, match=why):
+            fdl.SparseStep(plan, d, {}, 1, device="cpu", scaled={}, rope=rope, coord=coord)
