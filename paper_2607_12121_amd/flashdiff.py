@@ -573,9 +573,18 @@ def scaled_params(params: Dict[str, torch.Tensor]) -> Dict[str, torch.Tensor]:
 
 def scaled_weights(params: Dict[str, torch.Tensor], l: int, mod: torch.Tensor) -> FdScaledWeights:
     """Weights of block l of scaled_params' tensors; mod: the block's [B, 6D] fp32 from fd_adaln."""
-    names = ("w_qkv", "s_qkv", "b_qkv", "w_o", "s_o", "b_o", "w_1", "s_1", "b_1", "w_2", "s_2", "b_2")
-    norms = [_ptr(params[n][l]) if n in params else None for n in ("norm_1", "norm_2")]
-    return FdScaledWeights(*[_ptr(params[n][l]) for n in names], *norms, _ptr(mod))
+    D, F = params["w_o"].shape[1], params["w_1"].shape[1]
+    block, kinds = [], []
+    for n, out, cols in (("qkv", 3 * D, D), ("o", D, D), ("1", F, D), ("2", D, F)):
+        block += [params["w_" + n][l], params["s_" + n][l], params["b_" + n][l]]
+        kinds += [("w_" + n, "code", out * cols), ("s_" + n, "scale", -(-out // 128) * _stride(cols)), ("b_" + n, "f32", out)]
+    for n in ("norm_1", "norm_2"):
+        block.append(params[n][l] if n in params else None)
+        kinds.append((n, "f32", D))
+    for t, (name, kind, numel) in zip(block, kinds):
+        _need(name, t, kind, numel, exact=True, optional=kind == "f32" and name.startswith("norm"))
+    _need("mod", mod, "f32", 6 * D)
+    return FdScaledWeights(*[_ptr(t) for t in block], _ptr(mod))
 
 
 def fd_scaled_block_ws_size(plan: Plan, d: FdDims) -> int:

@@ -10,6 +10,7 @@ from oracle import scaled as ref
 from paper_2607_12121_amd import flashdiff as fdl
 from tests import gpu_harness as gh
 from tests.test_gpu_scaled import U32, check_linear, linear_case, rms_case, run_linear, run_rms
+from tests.test_gpu_scaled_block import make
 from tests.test_gpu_scaled_precision import check_same_codes
 
 pytestmark = pytest.mark.gpu
@@ -207,3 +208,20 @@ def test_rope_of_far_positions(theta, step, halves):
         for part, want in ((a, u * c - w * n), (b, u * n + w * c)):
             far = err * np.hypot(u, w) + 2.0 ** -21 * (np.abs(u) + np.abs(w))
             assert np.all(np.abs(got[:, part] - want) <= 2.0 ** -8 * np.abs(want) + (1 + 2.0 ** -8) * far)
+
+
+# ------------------------------------------------------------------ refusals
+
+def test_block_weights_of_another_type_or_size_refused():
+    """The block reads its parameters by address: what does not hold what it reads raises."""
+    case, scaled, _, _ = make("tiny")
+    mod = torch.zeros((case.w.B, 6 * case.w.D), device="cuda")
+    fdl.scaled_weights(scaled, 0, mod)
+    fdl.scaled_weights({k: t for k, t in scaled.items() if not k.startswith("norm")}, 0, mod)
+    change = dict(norm_1=lambda t: t.bfloat16(), norm_2=lambda t: t[:, :-16].contiguous(), b_qkv=lambda t: t.bfloat16(), b_1=lambda t: t[:, :-64].contiguous(),
+                  s_2=lambda t: t[..., :-4].contiguous(), w_1=lambda t: t.to(torch.float32), s_qkv=lambda t: t.cpu(), w_2=lambda t: t[:, :-64].contiguous())
+    for name, f in change.items():
+        with pytest.raises(fdl.FlashDiffError, match=name):
+            fdl.scaled_weights(dict(scaled, **{name: f(scaled[name])}), 0, mod)
+    with pytest.raises(fdl.FlashDiffError, match="mod"):
+        fdl.scaled_weights(scaled, 0, mod[:, :-1].contiguous())
