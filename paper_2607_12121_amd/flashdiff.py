@@ -426,7 +426,9 @@ def _stride(cols: int) -> int:
     return (cols + 511) // 512 * 4
 
 
-def _rows(name: str, t: torch.Tensor) -> Sequence[int]:
+def _rows(name: str, t: Optional[torch.Tensor]) -> Sequence[int]:
+    if t is None:
+        raise FlashDiffError(f"{name} is required")
     s = t.shape
     if len(s) != 2 or s[0] > 1 << 30 or s[1] > 1 << 30:
         raise FlashDiffError(f"{name} must have two dimensions of at most 2^30, got {tuple(s)}")
@@ -524,6 +526,8 @@ def fd_rope_axes(qkv, coord, idx, m, q, k_cache, v_cache, heads: int, kv_heads: 
     """q | k | v rows qkv [rows, (heads + 2 kv_heads) head_dim]: q and k turned by the token's
     coord [tokens, axes]; q to [rows, heads head_dim], k and v to the caches' rows idx.  The axes
     are given by dims, theta, step and halves, or by a descriptor from rope_axes."""
+    if rope is None and dims is None:
+        raise FlashDiffError("the axes are required: dims or rope")
     r = rope if rope is not None else rope_axes(dims, theta, step, halves)
     (rows, cols), (tokens, axes) = _rows("qkv", qkv), _rows("coord", coord)
     if cols != (heads + 2 * kv_heads) * head_dim or axes != r.n_axes:
@@ -540,6 +544,8 @@ def fd_scaled_linear(a, a_scale, w, w_scale, y, y_scale=None, bias=None, gelu: b
     (rows, k), (n, kw) = _rows("a", a), _rows("w", w)
     if k != kw:
         raise FlashDiffError(f"a has {k} columns, w {kw}")
+    if y is None:
+        raise FlashDiffError("y is required")
     dt, ld = y.dtype, _stride(k)
     codes, wide = dt in _KIND["code"], dt == torch.float32
     *ptrs, y_, ys_, st = _pointers(

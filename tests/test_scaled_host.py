@@ -284,3 +284,15 @@ def test_step_refuses_half_of_the_rotary_positions():
     for rope, coord, why in ((r, None, "both"), (None, pos, "both"), (r, pos.t().contiguous(), "6, 2"), (r, pos[:5], "6, 2"), (r, pos[:, :1], "6, 2")):
         with pytest.raises(fdl.FlashDiffError, match=why):
             fdl.SparseStep(plan, d, {}, 1, device="cpu", scaled={}, rope=rope, coord=coord)
+
+
+def test_bindings_name_what_is_absent():
+    q, s, h, i = torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(4, 4, dtype=torch.uint8), torch.zeros(4, 64), torch.zeros(2, dtype=torch.int32)
+    for call, what in ((lambda: fdl.fd_quant_blocks(None, 1, q, s), "x is"), (lambda: fdl.fd_rms_quant(None, q, s, i, i), "h is"),
+                       (lambda: fdl.fd_rope_axes(None, i, None, i, h, h, h, 1, 1, 16, dims=[16]), "qkv is"),
+                       (lambda: fdl.fd_rope_axes(h, None, None, i, h, h, h, 2, 1, 16, dims=[16]), "coord is"),
+                       (lambda: fdl.fd_rope_axes(h, i.view(1, 2), None, i, h, h, h, 2, 1, 16), "axes are"),
+                       (lambda: fdl.fd_scaled_linear(None, s, q, s, h), "a is"), (lambda: fdl.fd_scaled_linear(q, s, None, s, h), "w is"),
+                       (lambda: fdl.fd_scaled_linear(q, s, q, s, None), "y is")):
+        with pytest.raises(fdl.FlashDiffError, match=what):
+            call()
