@@ -391,8 +391,10 @@ fd_status fd_quant_blocks(int32_t n_rows, int32_t cols, int32_t block_rows, cons
  *   h[i] += gate_b * y[i]                                    (only with y)
  *   a    = h[i] / sqrt(mean(h[i]^2) + eps) * weight * (1 + scale_b) + shift_b
  *   q, q_scale = a in codes, one scale per 128 columns; both null: only h's update
- * in fp32, a rounded once.  The squares are formed in fp32: rows whose magnitudes
- * exceed 2^63 overflow to a norm of zero, and with eps 0 rows below 2^-75 divide by zero.
+ * in fp32, a rounded once.  The squares are formed and summed in fp32: rows whose squares
+ * add up to 2^128 or more (magnitudes from 2^64 / sqrt(D) on, 2^57.2 at the widest) have a
+ * norm of zero; with eps 0 rows below 2^-63 lose bits, and those below 2^-75, whose squares
+ * are zeros, divide by zero.
  *   h      device fp32 [n_rows][D], 16-byte aligned, updated in place
  *   y      device bf16 [n_rows][D] or null (a branch's output)
  *   gate, scale, shift  device fp32, request b's at + b * mod_stride, or null

@@ -152,6 +152,19 @@ def test_residual_alone_in_runs():
     assert np.array_equal(x.cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("D", [16, 768, 1536, 12288])
+def test_rms_on_both_sides_of_the_overflow(D):
+    """Rows of one magnitude, 2% below and above 2^64 / sqrt(D): their squares add up to 0.96 and 1.04 times 2^128.  Below, the
+    norm is 1 (within the 38 half steps of test_rms_quant, so its code is 1's), above it is zero, as the header says; an
+    ordinary row between them is as ever."""
+    v = 2.0 ** 64 / np.sqrt(D)
+    sign = np.where(np.arange(D) % 3 == 0, -1.0, 1.0)
+    h = np.stack([0.98 * v * sign, sign, 1.02 * v * sign]).astype(np.float32)
+    _, q, s = run_rms(h, None, np.zeros((1, 3 * D), np.float32), None, np.array([0, 3], np.int32), 3, "")
+    got = ref.values(q, s)
+    assert np.array_equal(got[0], sign) and np.array_equal(got[1], sign) and np.all(got[2] == 0)
+
+
 # ------------------------------------------------------------------ rotary positions
 
 def test_rope_of_more_rows_than_a_launch_has():
