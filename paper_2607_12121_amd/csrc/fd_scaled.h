@@ -56,7 +56,7 @@ FD_DEVICE uint32_t quant_lane8(const float (&v)[8], uint2& codes) {
 }
 
 // GELU, tanh form: z / (1 + 2^-t), t = 2 sqrt(2 / pi) log2(e) (z + 0.044715 z^3), in seven instructions with the
-// hardware's exponent and reciprocal (an ulp each).
+// hardware's exponent and reciprocal (an ulp each); gelu_tanh_fast, whose bits the bf16 products keep, takes two more.
 FD_DEVICE float gelu(float z) {
   const float t = z * fmaf(z * z, -0.10294324f, -2.3022082f);
   return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t));

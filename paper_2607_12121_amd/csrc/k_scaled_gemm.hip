@@ -337,6 +337,10 @@ struct Rows32 {
 // in the middle of a step, with its operands in registers: the loads have 5 sub-steps to land instead of 7 and 10,
 // 1664 x 1536 x 6144 in 128 x 128 tiles 36.4 us against 28.2.)  A step is one basic block: across branches the
 // compiler gathers the products at the end.
+//
+// The 256 x 256 tiles leave the results' offsets no registers: the compiler keeps 10 (bf16), 12 (fp32) and 14 (codes) of
+// them in scratch, and waits for each reload between the stores, which holds the stores before it and the next tile's
+// loads up.  The counted waits only get stricter by it.
 template <class T, int KIND, class Mma>
 FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
   constexpr int FI = T::FI, NJ = T::NJ, STAGES = T::STAGES, kSubs = 2 * NJ;
@@ -548,10 +552,12 @@ FD_DEVICE void scaled_tiles(const fdh::ScaledArgs& g, int M, uint4* ring) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the repeats of the last stage
 }
 
-// What bounds them is LDS traffic: a K-step of 128 x 128 reads 80 KB at 128 bytes a clock and is written by loads of 32
-// KB at 64, 1152 clocks beside 512 of matrix instructions; of 256 x 256, 192 and 64 KB, 2560 beside 2048.  9828 x 6144 x
-// 1536 to codes with GELU in 128 x 128 tiles 104 us (1780 TFLOP/s), 9828 x 1536 x 6144 to bf16 in 256 x 256 72 us (2560
-// TFLOP/s; a large fp8 product of the library 2720), 32760 x 1536 x 6144 to fp32 457 us (1350, at half the rate).
+// A K-step of 128 x 128 loads 32 KB into LDS at 64 bytes a clock of its CU (measured 63), 512 clocks, as long as its matrix
+// instructions take; it reads 80 KB from LDS at 256 (measured 225 with 16 waves), 320.  Of 256 x 256: 64 KB, 1024 beside
+// 2048, and 192 KB, 768.  No pipe is full.  9828 x 6144 x 1536 to codes with GELU in 128 x 128 tiles 104 us (1780 TFLOP/s):
+// matrix instructions 42% of the clocks, vector ones (GELU, maxima, codes) 40%, loads 42%, LDS reads 28% without
+// conflicts.  9828 x 1536 x 6144 to bf16 in 256 x 256 72 us (2560 TFLOP/s; a large fp8 product of the library 2720), 32760 x
+// 1536 x 6144 to fp32 457 us (1350, at half the rate): matrix 70%, vector (the codes to bf16) 39%, loads 17%, reads 14%.
 using Tile64 = Tile<1, 2, 2, 2, 3>;        // 64 x 128, two workgroups per CU, in 32 x 64 a wave: all four SIMDs of a CU that has one
 using Tile64Codes = Tile<1, 4, 2, 1, 3>;   // 64 x 128 where a wave has to hold a block's 128 columns
 using Tile128 = Tile<1, 4, 4, 1, 2>;       // 128 x 128, two
