@@ -654,8 +654,11 @@ class SparseStep:
             raise FlashDiffError("rotary positions belong to the 8-bit blocks: give `scaled` too")
         if (rope is None) != (coord is None):
             raise FlashDiffError("rotary positions need both `rope` and `coord`")
-        if coord is not None and tuple(coord.shape) != (plan.n_tokens, rope.n_axes):
-            raise FlashDiffError(f"coord must be [{plan.n_tokens}, {rope.n_axes}], got {tuple(coord.shape)}")
+        if coord is not None:
+            if tuple(coord.shape) != (plan.n_tokens, rope.n_axes):
+                raise FlashDiffError(f"coord must be [{plan.n_tokens}, {rope.n_axes}], got {tuple(coord.shape)}")
+            _need("coord", coord, "i32", coord.numel())
+            _ptr(coord)
         self.plan, self.d, self.params, self.L = plan, d, params, n_layers
         N, R, B, C, D = plan.n_tokens, plan.n_regions, plan.n_requests, d.C, d.D
         dev = torch.device(device)

@@ -238,3 +238,14 @@ def test_block_weights_of_another_type_or_size_refused():
             fdl.scaled_weights(dict(scaled, **{name: f(scaled[name])}), 0, mod)
     with pytest.raises(fdl.FlashDiffError, match="mod"):
         fdl.scaled_weights(scaled, 0, mod[:, :-1].contiguous())
+
+
+def test_step_refuses_positions_that_its_blocks_would():
+    """Positions of another type, or with strides, raise when the step is made, not in it after the gate has moved on."""
+    case, scaled, rope, pos = make("tiny")
+    r, c = fdl.rope_axes(**rope), torch.from_numpy(pos).cuda()
+    kw = dict(k_cache=case.k_cache.cuda(), v_cache=case.v_cache.cuda(), scaled=scaled, rope=r)
+    fdl.SparseStep(case.plan, case.dims, case.params_gpu, case.w.L, coord=c, **kw)
+    for bad in (c.long(), c.float(), c.t().contiguous().t(), c.cpu()):
+        with pytest.raises(fdl.FlashDiffError):
+            fdl.SparseStep(case.plan, case.dims, case.params_gpu, case.w.L, coord=bad, **kw)

@@ -281,7 +281,7 @@ def test_step_refuses_half_of_the_rotary_positions():
     descriptor would be ignored; positions laid out the other way round would turn by the wrong ones."""
     plan = fdl.make_plan(np.zeros(6, np.int32), np.array([0, 6]), 1, device="cpu")
     d, r, pos = fdl.dims(16, 64, 1, 64, 256), fdl.rope_axes([32, 32]), torch.zeros(6, 2, dtype=torch.int32)
-    for rope, coord, why in ((r, None, "both"), (None, pos, "both"), (r, pos.t().contiguous(), "6, 2"), (r, pos[:5], "6, 2"), (r, pos[:, :1], "6, 2")):
+    for rope, coord, why in ((r, None, "both"), (None, pos, "both"), (r, pos.t().contiguous(), "6, 2"), (r, pos[:5], "6, 2"), (r, pos[:, :1], "6, 2"), (r, pos, "coord must be a device tensor")):
         with pytest.raises(fdl.FlashDiffError, match=why):
             fdl.SparseStep(plan, d, {}, 1, device="cpu", scaled={}, rope=rope, coord=coord)
 
