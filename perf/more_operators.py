@@ -1,0 +1,429 @@
+"""The steps of a DiT block with norms on both sides of its branches, products in 8-bit integers and its keys
+and values cached in 8 bits, as timed cases.
+
+Kinds:
+
+  norm    h = residual * h + gate * RMS(y) post_weight, then RMS(h) weight (1 + scale) + shift as bf16 rows, as
+          e4m3 codes with a power-of-two scale per 128 columns, or as 8-bit integers with a scale per row.
+  rows    bf16 rows to 8-bit integers, one fp32 scale per row (activations) or per output channel (weights).
+  linear  act((A W^T) a_scale w_scale + bias) of 8-bit integers with a scale per row and per column.
+  cache   q | k | v rows: q and k turned by the token's position, q to its rows, k and v to the token's rows of an
+          8-bit cache, one power-of-two scale per token and head.
+  attn    softmax(q K^T / sqrt(dh)) V of the active rows over all of their request's tokens in that cache, key heads
+          shared by groups of query heads.
+
+Row counts are the active rows of the package's workloads (image, video, audio, packed images) and odd ones; widths
+are those models' and odd ones.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+WIDTHS = (64, 384, 576, 1024, 1088, 1536, 2048)
+MOST_FLOPS = 2 * 32760 * 1536 * 6144          # of a product
+MOST_PAIRS = 9828 * 32760 * 1536              # query rows x keys x columns of an attention
+MOST_SCORES = 9828 * 32760 * 12               # query rows x keys x heads, requests padded to the longest
+
+
+def listed():
+    return [
+        # one active token behind a block's branch: latency
+        dict(name="norm_one", kind="norm", rows=1, width=1536, requests=1, branch=True, to="bf16"),
+        # a packed batch of eight image requests, each with its own modulation
+        dict(name="norm_packed", kind="norm", rows=8937, width=1536, requests=8, branch=True, to="8"),
+        # the attention's output of a short, odd sequence on its way to the out-projection
+        dict(name="rows_odd", kind="rows", rows=1021, width=1088),
+        # a video step: the MLP's hidden rows
+        dict(name="rows_video", kind="rows", rows=9828, width=6144),
+        # one active token through the fused projection: the weights are all that is read
+        dict(name="linear_one", kind="linear", rows=1, out=4608, inner=1536, act=False, to="bf16"),
+        # odd sizes: a short sequence, widths that end inside a tile and a block
+        dict(name="linear_odd", kind="linear", rows=1021, out=4288, inner=1088, act=False, to="f32"),
+        # a video step: the first MLP product
+        dict(name="linear_video", kind="linear", rows=9828, out=6144, inner=1536, act=True, to="bf16"),
+        # one row of a short sequence, one axis
+        dict(name="cache_one", kind="cache", rows=1, tokens=2048, heads=16, kv_heads=16, dh=64, axes="64", halves=True),
+        # a video step: time, height and width, 30% of the tokens active
+        dict(name="cache_video", kind="cache", rows=9828, tokens=32760, heads=12, kv_heads=12, dh=128, axes="44,42,42", halves=False),
+        # one active token of a video over all of its keys: the cache is all that is read
+        dict(name="attn_one", kind="attn", rows=1, tokens=32760, requests=1, heads=12, kv_heads=12, dh=128),
+        # eight image requests of different sizes with shared key heads, one of them without an active token
+        dict(name="attn_packed", kind="attn", rows=8937, tokens=21248, requests=8, heads=24, kv_heads=8, dh=64),
+        # the largest: a video step
+        dict(name="attn_video", kind="attn", rows=9828, tokens=32760, requests=1, heads=12, kv_heads=12, dh=128),
+    ]
+
+
+def _log(rng, most):
+    return int(round(math.exp(rng.uniform(0.0, math.log(most)))))
+
+
+def draw(rng):
+    rows = _log(rng, 32760)
+    kind = rng.choice(("norm", "rows", "linear", "cache", "attn", "attn"))
+    if kind == "norm":
+        return dict(kind=kind, rows=rows, width=rng.choice(WIDTHS), requests=rng.randint(1, min(rows, 64)), branch=rng.random() < 0.8,
+                    to=rng.choice(("bf16", "8", "int")))
+    if kind == "rows":
+        return dict(kind=kind, rows=rows, width=16 * rng.randint(4, 384))
+    if kind == "linear":
+        out, inner = 64 * rng.randint(1, 100), 64 * rng.randint(1, 100)
+        rows = max(1, min(rows, MOST_FLOPS // (2 * out * inner)))
+        return dict(kind=kind, rows=rows, out=out, inner=inner, act=rng.random() < 0.4, to=rng.choice(("bf16", "f32")))
+    dh = rng.choice((16, 64, 128))
+    kv = rng.randint(1, 1024 // dh)
+    heads = kv * rng.choice((1, 1, 2, 4))
+    if kind == "cache":
+        n = rng.randint(1, 3)
+        cuts = sorted(2 * rng.randint(1, dh // 2 - 1) for _ in range(n - 1)) if dh > 16 else [2 * (i + 1) for i in range(n - 1)]
+        axes = [b - a for a, b in zip([0] + cuts, cuts + [dh]) if b > a]
+        return dict(kind=kind, rows=rows, tokens=rows + rng.randint(0, rows), heads=heads, kv_heads=kv, dh=dh,
+                    axes=",".join(map(str, axes)), halves=rng.random() < 0.5)
+    requests = rng.randint(1, 8)
+    tokens = requests + _log(rng, 32760)
+    case = dict(kind=kind, rows=0, tokens=tokens, requests=requests, heads=heads, kv_heads=kv, dh=dh)
+    k_len = _lengths(tokens, requests)
+    rows = min(rows, tokens - (k_len[2] if requests >= 8 else 0))
+    while True:                                  # fewer rows until the case costs no more than the largest
+        case["rows"] = rows
+        q_len = _active(case)
+        if sum(a * b for a, b in zip(q_len, k_len)) * heads * dh <= MOST_PAIRS and requests * max(q_len) * max(k_len) * heads <= MOST_SCORES:
+            return case
+        rows = rows // 2
+
+
+# ------------------------------------------------------------------ requests
+
+def _lengths(total, requests):
+    """`requests` lengths of at least one, growing in the ratio 1 : 2 : .., that add up to `total`."""
+    rest, all_ = total - requests, requests * (requests + 1) // 2
+    at = [rest * i * (i + 1) // 2 // all_ for i in range(requests + 1)]
+    return [1 + b - a for a, b in zip(at, at[1:])]
+
+
+def _active(case):
+    """Active rows of every request: in the ratio of the tokens, of eight or more requests none of the third one's."""
+    length = _lengths(case["tokens"], case["requests"])
+    if case["requests"] >= 8:
+        length[2] = 0
+    total, rows, done, out = sum(length), min(case["rows"], sum(length)), 0, []
+    for i in range(len(length)):
+        upto = rows * sum(length[:i + 1]) // total
+        out.append(upto - done)
+        done = upto
+    return out
+
+
+def _offsets(length):
+    return torch.cat([torch.zeros(1, dtype=torch.int64), torch.cumsum(torch.tensor(length), 0)]).to(torch.int32)
+
+
+# ------------------------------------------------------------------ 8 bits, plain
+
+def _whole(x):
+    """(8-bit integers, scale) of the rows x fp32: scale = max / 127, the nearest whole number of x * (127 / max);
+    rows whose largest magnitude is below 2^-100 are zeros."""
+    top = x.abs().amax(1, keepdim=True)
+    top = torch.where(top >= 2.0 ** -100, top, 0.0)
+    up = torch.where(top > 0, torch.full_like(top, 127.0) / top, 0.0)
+    return torch.round(x * up).to(torch.int8), (top / 127.0).squeeze(1)
+
+
+def _power(top):
+    """The least power of two (its exponent, at least -126) at which `top` is at most 448."""
+    mant, ex = torch.frexp(top)                  # top = mant 2^ex, mant in [1/2, 1); 448 = 0.875 * 2^9
+    return torch.where(top > 0, (ex - 9 + (mant > 0.875)).clamp(-126, 127), -126)
+
+
+def _codes(x, group):
+    """(e4m3 codes, exponents) of x fp32 [.., cols], one power of two per `group` columns."""
+    c = x.shape[-1]
+    blocks = torch.nn.functional.pad(x, (0, -c % group)).unflatten(-1, (-1, group))
+    ex = _power(blocks.abs().amax(-1))
+    up = torch.ldexp(torch.ones_like(x[..., :1]), -ex).unsqueeze(-1)
+    return (blocks * up).flatten(-2)[..., :c].to(torch.float8_e4m3fn), ex
+
+
+def _bytes(ex):
+    return torch.ldexp(torch.ones(ex.shape, device=ex.device), ex).to(torch.float8_e8m0fnu)
+
+
+def _gelu(z):
+    return 0.5 * z * (1.0 + torch.tanh(math.sqrt(2.0 / math.pi) * (z + 0.044715 * z * z * z)))
+
+
+# ------------------------------------------------------------------ inputs
+
+def prepare(case, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1000003 * int(seed) + 29)
+    randn = lambda *shape: torch.randn(shape, generator=g, device="cuda")  # noqa: E731
+    rows, s = case["rows"], dict(case)
+    s["m"] = torch.tensor([rows], dtype=torch.int32, device="cuda")
+    if case["kind"] == "norm":
+        w, b = case["width"], case["requests"]
+        length = _lengths(rows, b)
+        s["cu_q"] = _offsets(length).cuda()
+        s["of_row"] = torch.repeat_interleave(torch.arange(b), torch.tensor(length)).cuda()
+        s["h"] = randn(rows, w) * (1.0 + 3.0 * torch.rand((rows, 1), generator=g, device="cuda"))
+        s["y"] = (randn(rows, w) * torch.exp(randn(rows, 1))).to(torch.bfloat16) if case["branch"] else None
+        mod = 0.3 * randn(b, 6 * w)              # the second branch's shift | scale | gate lie behind the first one's
+        s["shift"], s["scale"], s["gate"] = mod[:, 3 * w:4 * w], mod[:, 4 * w:5 * w], mod[:, 5 * w:]
+        s["post_weight"], s["weight"] = 1.0 + 0.1 * randn(w), 1.0 + 0.1 * randn(w)
+        s["residual"] = 0.875
+        s["a_scale"] = None
+        if case["to"] == "bf16":
+            s["a"] = torch.zeros((rows, w), dtype=torch.bfloat16, device="cuda")
+        elif case["to"] == "int":
+            s["a"], s["a_scale"] = torch.zeros((rows, w), dtype=torch.int8, device="cuda"), torch.zeros(rows, device="cuda")
+            s["values"] = torch.zeros((rows, w), dtype=torch.bfloat16, device="cuda")
+        else:
+            s["a"] = torch.zeros((rows, w), dtype=torch.float8_e4m3fn, device="cuda")
+            s["a_scale"] = torch.full((rows, (-(-w // 128) + 3) // 4 * 4), 127, dtype=torch.uint8, device="cuda")
+    elif case["kind"] == "rows":
+        s["x"] = (randn(rows, case["width"]) * torch.exp(randn(rows, 1))).to(torch.bfloat16)
+        s["q"] = torch.zeros((rows, case["width"]), dtype=torch.int8, device="cuda")
+        s["q_scale"] = torch.zeros(rows, device="cuda")
+    elif case["kind"] == "linear":
+        n, k = case["out"], case["inner"]
+        s["a"], s["a_scale"] = _whole(randn(rows, k) * torch.exp(0.5 * randn(rows, 1)))
+        s["w"], s["w_scale"] = _whole(0.02 * randn(n, k) * torch.exp(0.3 * randn(n, 1)))
+        s["bias"] = 0.02 * randn(n)
+        s["y"] = torch.zeros((rows, n), dtype=torch.float32 if case["to"] == "f32" else torch.bfloat16, device="cuda")
+    else:
+        hq, hk, dh, t = case["heads"], case["kv_heads"], case["dh"], case["tokens"]
+        for name in ("k", "v"):                  # what earlier steps left in the cache
+            c, ex = _codes(randn(t, hk * dh) * torch.exp(0.3 * randn(t, 1)), dh)
+            s[name], s[name + "_scale"] = c, (ex + 127).to(torch.uint8).t().contiguous()
+        if case["kind"] == "cache":
+            s["dims"] = [int(a) for a in case["axes"].split(",")]
+            n = len(s["dims"])
+            side = max(1, int(round(t ** (1.0 / n))))          # the grid of the tokens
+            tok = torch.arange(t, device="cuda")
+            s["coord"] = torch.stack([torch.div(tok, side ** (n - 1 - a), rounding_mode="floor") % (t if a == 0 else side)
+                                      for a in range(n)], 1).to(torch.int32).contiguous()
+            s["idx"] = torch.randperm(t, generator=g, device="cuda")[:rows].sort().values.to(torch.int32)
+            s["qkv"] = randn(rows, (hq + 2 * hk) * dh).to(torch.bfloat16)
+            s["q"] = torch.zeros((rows, hq * dh), dtype=torch.bfloat16, device="cuda")
+        else:
+            s["q_len"], s["k_len"] = _active(case), _lengths(t, case["requests"])
+            s["cu_q"], s["tok_off"] = _offsets(s["q_len"]).cuda(), _offsets(s["k_len"]).cuda()
+            s["q"] = randn(rows, hq * dh).to(torch.bfloat16)
+            s["o"] = torch.zeros((rows, hq * dh), dtype=torch.bfloat16, device="cuda")
+            # every request's rows and tokens side by side, padded to the longest
+            s["row_at"] = s["cu_q"][:-1, None] + torch.arange(max(s["q_len"]), device="cuda")
+            s["tok_at"] = s["tok_off"][:-1, None] + torch.arange(max(s["k_len"]), device="cuda")
+            s["row_in"], s["tok_in"] = s["row_at"] < s["cu_q"][1:, None], s["tok_at"] < s["tok_off"][1:, None]
+    return s
+
+
+# ------------------------------------------------------------------ one pass
+
+def run(s):
+    return {"norm": _norm, "rows": _rows, "linear": _linear, "cache": _cache, "attn": _attn}[s["kind"]](s)
+
+
+def _norm(s):
+    w, to = s["width"], s["to"]
+    if own:
+        from paper_2607_12121_amd import flashdiff as fdl
+        fdl.fd_norm_residual(s["h"], s["a"], s["cu_q"], s["m"], y=s["y"], post_weight=s["post_weight"], gate=s["gate"], residual=s["residual"],
+                             weight=s["weight"], shift=s["shift"], mod_scale=s["scale"], a_scale=s["a_scale"], eps=1e-6)
+        a, sc = s["a"], s["a_scale"]
+        if to == "8":
+            sc = sc[:, :-(-w // 128)].view(torch.float8_e8m0fnu)
+    else:
+        b, h = s["of_row"], s["h"]
+        if s["y"] is not None:
+            y = s["y"].float()
+            r = y * torch.rsqrt((y * y).mean(1, keepdim=True) + 1e-6) * s["post_weight"]
+            h.copy_(s["residual"] * h + s["gate"][b] * r)
+        a = h * torch.rsqrt((h * h).mean(1, keepdim=True) + 1e-6) * s["weight"] * (1.0 + s["scale"][b]) + s["shift"][b]
+        if to == "bf16":
+            a = a.to(torch.bfloat16)
+        elif to == "int":
+            a, sc = _whole(a)
+        else:
+            a, ex = _codes(a, 128)
+            sc = _bytes(ex)
+    if to == "bf16":
+        return {"h": s["h"], "a": a}
+    if to == "int":                              # what the integers stand for
+        return {"h": s["h"], "a": torch.mul(a, sc[:, None], out=s["values"]), "scale": sc}
+    return {"h": s["h"], "a": a, "scale": sc}
+
+
+def _rows(s):
+    if own:
+        from paper_2607_12121_amd import flashdiff as fdl
+        fdl.fd_int8_rows(s["x"], s["q"], s["q_scale"], m=s["m"])
+        return {"q": s["q"], "scale": s["q_scale"]}
+    q, scale = _whole(s["x"].float())
+    return {"q": q, "scale": scale}
+
+
+def _linear(s):
+    if own:
+        from paper_2607_12121_amd import flashdiff as fdl
+        fdl.fd_int8_linear(s["a"], s["a_scale"], s["w"], s["w_scale"], s["y"], bias=s["bias"], gelu=s["act"], m=s["m"])
+        return {"y": s["y"]}
+    y = (s["a"].float() @ s["w"].float().t()) * s["a_scale"][:, None] * s["w_scale"] + s["bias"]
+    return {"y": (_gelu(y) if s["act"] else y).to(s["y"].dtype)}
+
+
+def _turned(s, x):
+    """x [rows][heads][dh] fp32 turned by the rows' positions; angles in 64 bits."""
+    pos = s["coord"][s["idx"].long()].double()
+    freq = [10000.0 ** (-2.0 * torch.arange(d // 2, dtype=torch.float64, device="cuda") / d) for d in s["dims"]]
+    ang = torch.cat([pos[:, a:a + 1] * f for a, f in enumerate(freq)], 1)[:, None]
+    cos, sin = torch.cos(ang).float(), torch.sin(ang).float()
+    out, at = [], 0
+    for d in s["dims"]:
+        p, c, n = x[..., at:at + d], cos[..., at // 2:(at + d) // 2], sin[..., at // 2:(at + d) // 2]
+        u, v = (p[..., :d // 2], p[..., d // 2:]) if s["halves"] else (p[..., 0::2], p[..., 1::2])
+        r = (u * c - v * n, u * n + v * c)
+        out.append(torch.cat(r, -1) if s["halves"] else torch.stack(r, -1).flatten(-2))
+        at += d
+    return torch.cat(out + [x[..., at:]], -1)
+
+
+def _cache(s):
+    hq, hk, dh = s["heads"], s["kv_heads"], s["dh"]
+    if own:
+        from paper_2607_12121_amd import flashdiff as fdl
+        fdl.fd_cache_write(s["qkv"], s["coord"], s["idx"], s["m"], s["q"], s["k"], s["k_scale"], s["v"], s["v_scale"], heads=hq,
+                           kv_heads=hk, head_dim=dh, dims=s["dims"], halves=s["halves"])
+        q = s["q"]
+    else:
+        tok = s["idx"].long()
+        x = s["qkv"].float().view(s["rows"], hq + 2 * hk, dh)
+        qk = _turned(s, x[:, :hq + hk])
+        q = qk[:, :hq].reshape(s["rows"], hq * dh).to(torch.bfloat16)
+        for name, new in (("k", qk[:, hq:]), ("v", x[:, hq + hk:])):
+            c, ex = _codes(new, dh)
+            s[name].view(torch.uint8)[tok] = c.reshape(s["rows"], hk * dh).view(torch.uint8)
+            s[name + "_scale"][:, tok] = (ex.squeeze(-1) + 127).to(torch.uint8).t()
+    return {"q": q, "k": s["k"], "v": s["v"], "k_scale": s["k_scale"].view(torch.float8_e8m0fnu), "v_scale": s["v_scale"].view(torch.float8_e8m0fnu)}
+
+
+def _attn(s):
+    hq, hk, dh, t = s["heads"], s["kv_heads"], s["dh"], s["tokens"]
+    if own:
+        from paper_2607_12121_amd import flashdiff as fdl
+        if "ws" not in s:                        # a program allocates it once
+            s["ws"] = torch.empty(fdl.fd_cache_attention_ws_size(s["rows"], hq, hk, dh), dtype=torch.uint8, device="cuda")
+        fdl.fd_cache_attention(s["q"], s["k"], s["k_scale"], s["v"], s["v_scale"], s["o"], s["cu_q"], s["tok_off"], heads=hq, kv_heads=hk,
+                               head_dim=dh, max_request_tokens=max(s["k_len"]), ws=s["ws"])
+        return {"o": s["o"]}
+    b, nq, nk = s["requests"], max(s["q_len"]), max(s["k_len"])
+    tok, row = s["tok_at"].clamp(max=t - 1), s["row_at"].clamp(max=s["rows"] - 1)
+    k, v = (s[n].float().view(t, hk, dh) * torch.ldexp(torch.ones(1, device="cuda"), s[n + "_scale"].int() - 127).t()[:, :, None] for n in ("k", "v"))
+    q = s["q"].float().view(s["rows"], hk, hq // hk, dh)[row]            # [b][nq][hk][group][dh]
+    q = q.permute(0, 2, 3, 1, 4).reshape(b * hk, hq // hk * nq, dh)
+    k = k[tok].permute(0, 2, 3, 1).reshape(b * hk, dh, nk)
+    v = v[tok].permute(0, 2, 1, 3).reshape(b * hk, nk, dh)
+    p = torch.bmm(q, k).mul_(1.0 / math.sqrt(dh)).view(b, hk, hq // hk * nq, nk)
+    p.masked_fill_(~s["tok_in"][:, None, None], float("-inf"))
+    p.sub_(p.amax(-1, keepdim=True)).exp_()
+    o = torch.bmm(p.view(b * hk, hq // hk * nq, nk), v).view(b, hk, hq // hk * nq, dh) / p.sum(-1, keepdim=True)
+    o = o.view(b, hk, hq // hk, nq, dh).permute(0, 3, 1, 2, 4)[s["row_in"]]
+    return {"o": o.reshape(s["rows"], hq * dh).to(torch.bfloat16)}
+
+
+# ------------------------------------------------------------------ what a pass cannot do without
+
+def work(case):
+    r = case["rows"]
+    if case["kind"] == "norm":
+        w, b = case["width"], case["requests"]
+        n, scales = r * w, {"bf16": 0, "8": r * -(-w // 128), "int": 4 * r}[case["to"]]
+        return {"bytes": n * (4 + (2 if case["to"] == "bf16" else 1) + (2 + 4 if case["branch"] else 0)) + scales
+                + 4 * w * (2 + 3 * b if case["branch"] else 1 + 2 * b), "flops": (14 if case["branch"] else 6) * n}
+    if case["kind"] == "rows":
+        return {"bytes": r * (3 * case["width"] + 4), "flops": 3 * r * case["width"]}
+    if case["kind"] == "linear":
+        n, k = case["out"], case["inner"]
+        return {"bytes": r * k + n * k + r * n * (4 if case["to"] == "f32" else 2) + 4 * (r + 2 * n), "flops": 2 * r * n * k}
+    hq, hk, dh = case["heads"], case["kv_heads"], case["dh"]
+    if case["kind"] == "cache":
+        axes = case["axes"].count(",") + 1
+        return {"bytes": r * (4 * hq * dh + 2 * hk * (3 * dh + 1) + 4 * axes + 4), "flops": r * (3 * (hq + hk) + 4 * hk) * dh}
+    pairs = [(a, b) for a, b in zip(_active(case), _lengths(case["tokens"], case["requests"])) if a]
+    return {"bytes": 4 * r * hq * dh + sum(b for _, b in pairs) * 2 * hk * (dh + 1), "flops": 4 * hq * dh * sum(a * b for a, b in pairs)}
+
+
+# ------------------------------------------------------------------ the definitions in 64 bits
+
+def _values64(x, group):
+    """(e4m3 values before the scale, the scale) of x fp64 [rows][n * group or less]: the least power of two with
+    max / power <= 448, then the nearest value of three mantissa bits, ties to even."""
+    r, c = x.shape
+    pad = torch.zeros((r, -(-c // group) * group), dtype=torch.float64, device=x.device)
+    pad[:, :c] = x
+    top = pad.reshape(r, -1, group).abs().max(2).values
+    power = torch.ceil(torch.log2(top / 448.0)).nan_to_num(neginf=-126.0).clamp(-126, 127)
+    power = torch.where(top > 448.0 * torch.exp2(power), power + 1, power)
+    power = torch.where((top <= 448.0 * torch.exp2(power - 1)) & (power > -126), power - 1, power)
+    v = x / torch.exp2(power).repeat_interleave(group, 1)[:, :c]
+    step = torch.exp2(torch.floor(torch.log2(v.abs().clamp(min=2.0 ** -6))) - 3)
+    return torch.round(v / step) * step, torch.exp2(power)
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    r = case["rows"]
+    if case["kind"] == "norm":
+        w, h = case["width"], s["h"].double()
+        shift, scale, gate = (torch.cat([s[n][i:i + 1].double().expand(k, -1) for i, k in enumerate(_lengths(r, case["requests"]))])
+                              for n in ("shift", "scale", "gate"))
+        unit = lambda x: x / (x.pow(2).sum(1, keepdim=True) / w + 1e-6).sqrt()  # noqa: E731
+        if case["branch"]:
+            h = s["residual"] * h + gate * (unit(s["y"].double()) * s["post_weight"].double())
+        a = unit(h) * s["weight"].double() * (1 + scale) + shift
+        if case["to"] == "bf16":
+            return {"h": h, "a": a}
+        if case["to"] == "int":
+            step = a.abs().max(1, keepdim=True).values / 127
+            return {"h": h, "a": torch.round(a / step) * step, "scale": step[:, 0]}
+        a, scale = _values64(a, 128)
+        return {"h": h, "a": a, "scale": scale}
+    if case["kind"] == "rows":
+        return {"q": None, "scale": s["x"].double().abs().max(1).values / 127}
+    if case["kind"] == "linear":
+        y = (s["a"].double() @ s["w"].double().t()) * (s["a_scale"].double()[:, None] * s["w_scale"].double()) + s["bias"].double()
+        return {"y": y / (1 + torch.exp(-2 * math.sqrt(2 / math.pi) * (y + 0.044715 * y ** 3))) if case["act"] else y}
+    hq, hk, dh = case["heads"], case["kv_heads"], case["dh"]
+    if case["kind"] == "cache":
+        tok = s["idx"].long()
+        x = s["qkv"].double().view(r, hq + 2 * hk, dh)
+        turned = x.clone()
+        at = 0
+        for a, d in enumerate(s["dims"]):
+            for j in range(d // 2):
+                ang = s["coord"][tok, a].double() * 10000.0 ** (-2.0 * j / d)
+                u, v = (at + j, at + j + d // 2) if case["halves"] else (at + 2 * j, at + 2 * j + 1)
+                z = torch.polar(torch.ones_like(ang), ang)[:, None] * torch.complex(x[:, :hq + hk, u], x[:, :hq + hk, v])
+                turned[:, :hq + hk, u], turned[:, :hq + hk, v] = z.real, z.imag
+            at += d
+        out = {"q": turned[:, :hq].reshape(r, -1)}
+        for name, first in (("k", hq), ("v", hq + hk)):
+            old, power = s[name].double(), torch.exp2(s[name + "_scale"].double() - 127)
+            old[tok], new = (y := _values64(turned[:, first:first + hk].reshape(r, -1), dh))[0], y[1]
+            power[:, tok] = new.t()
+            out[name], out[name + "_scale"] = old, power
+        return out
+    o = torch.zeros((r, hq, dh), dtype=torch.float64, device="cuda")
+    k, v = (s[n].double().view(-1, hk, dh) * torch.exp2(s[n + "_scale"].double() - 127).t()[:, :, None] for n in ("k", "v"))
+    q, q0, k0 = s["q"].double().view(r, hq, dh), 0, 0
+    for nq, nk in zip(s["q_len"], s["k_len"]):
+        for h in range(hq if nq else 0):
+            kh, vh = k[k0:k0 + nk, h // (hq // hk)], v[k0:k0 + nk, h // (hq // hk)]
+            for i in range(0, nq, 4096):
+                rows = slice(q0 + i, q0 + min(nq, i + 4096))
+                o[rows, h] = torch.softmax(q[rows, h] @ kh.t() / math.sqrt(dh), 1) @ vh
+        q0, k0 = q0 + nq, k0 + nk
+    return {"o": o.view(r, -1)}
