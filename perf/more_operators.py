@@ -260,7 +260,7 @@ def _norm(s):
 def _rows(s):
     if own:
         from paper_2607_12121_amd import flashdiff as fdl
-        fdl.fd_int8_rows(s["x"], s["q"], s["q_scale"], m=s["m"])
+        fdl.fd_int_rows(s["x"], s["q"], s["q_scale"], m=s["m"])
         return {"q": s["q"], "scale": s["q_scale"]}
     q, scale = _whole(s["x"].float())
     return {"q": q, "scale": scale}
@@ -269,7 +269,7 @@ def _rows(s):
 def _linear(s):
     if own:
         from paper_2607_12121_amd import flashdiff as fdl
-        fdl.fd_int8_linear(s["a"], s["a_scale"], s["w"], s["w_scale"], s["y"], bias=s["bias"], gelu=s["act"], m=s["m"])
+        fdl.fd_int_linear(s["a"], s["a_scale"], s["w"], s["w_scale"], s["y"], bias=s["bias"], gelu=s["act"], m=s["m"])
         return {"y": s["y"]}
     y = (s["a"].float() @ s["w"].float().t()) * s["a_scale"][:, None] * s["w_scale"] + s["bias"]
     return {"y": (_gelu(y) if s["act"] else y).to(s["y"].dtype)}
