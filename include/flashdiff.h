@@ -499,6 +499,110 @@ fd_status fd_scaled_block_forward(const fd_plan* plan, const fd_dims* dims, cons
                                   const int32_t* cu_q, const int32_t* m, uint16_t* k_cache, uint16_t* v_cache, void* ws,
                                   size_t ws_bytes, fd_stream_t stream);
 
+/* ---------------------------------------------------------------- 8-bit integers
+ * Rows and weights as 8-bit integers, for checkpoints in that form (a scale per token
+ * of the activations and per output channel of the weights; Sec. 4 Backend runs the
+ * active patches through the backbone's linear layers).  A value is q * scale,
+ *   scale = max / 127,  q = round(x * (127 / max)),  max the row's largest magnitude,
+ * both quotients and the product rounded to fp32, q to the nearest whole number (ties to
+ * even), -127 .. 127: off by at most half the scale (1 + 2^-15).  Rows whose largest magnitude
+ * is below 2^-100 are zeros with scale 0; rows that hold an infinity or a NaN have scale
+ * NaN and zeros.  Column counts are multiples of 16, at most 65536; row counts, `m`,
+ * alignment and overlap as for the 8-bit rows above.
+ */
+
+/*
+ * bf16 rows to integers: activations, or weights [out][in] with the scale of each output channel.
+ *   x      device bf16 [n_rows][cols], 16-byte aligned
+ *   m      device int32 [1] or null (all n_rows)
+ *   q      device int8 [n_rows][cols], 16-byte aligned (output)
+ *   scale  device fp32 [n_rows] (output)
+ */
+fd_status fd_int_rows(int32_t n_rows, int32_t cols, const uint16_t* x, const int32_t* m, int8_t* q, float* scale,
+                       fd_stream_t stream);
+
+/*
+ * A linear layer on integers:
+ *   y[i][j] = act(sum_k a[i][k] w[j][k] * (a_scale[i] * w_scale[j]) + bias[j])  for i < *m,
+ * the sum exact, then in fp32; act GELU (tanh form) or none.  -128 is taken as it is.
+ *   a, a_scale  device int8 [n_rows][n_in], fp32 [n_rows]
+ *   w, w_scale  device int8 [n_out][n_in], fp32 [n_out]
+ *   bias        device fp32 [n_out] or null
+ *   m           device int32 [1] or null (all n_rows)
+ *   one output: y_bf [n_rows][n_out] bf16, or y_fp fp32
+ * n_out at most 2^20, a multiple of 16; weights below 2 GiB.  a, w, w_scale, bias and outputs 16-byte, a_scale
+ * 4-byte aligned.
+ */
+fd_status fd_int_linear(int32_t n_rows, int32_t n_out, int32_t n_in, const int8_t* a, const float* a_scale, const int8_t* w,
+                         const float* w_scale, const float* bias, int32_t gelu, const int32_t* m, uint16_t* y_bf, float* y_fp,
+                         fd_stream_t stream);
+
+/*
+ * The residual stream through the norms behind one branch and before the next (models
+ * that normalise both sides of a branch), for i < *m with b the row's request:
+ *   h[i] = residual * h[i] + gate_b * (y[i] / sqrt(mean(y[i]^2) + eps) * post_weight)   (only with y)
+ *   a    = h[i] / sqrt(mean(h[i]^2) + eps) * weight * (1 + scale_b) + shift_b
+ * in fp32, a rounded once, to one of
+ *   a_bf                 bf16
+ *   a_codes, code_scale  e4m3 codes, one scale byte per 128 columns (fd_quant_blocks' format)
+ *   a_int, row_scale     8-bit integers, one fp32 scale per row (fd_int_rows' format)
+ * or to none (h's update alone, which needs y).
+ *   h      device fp32 [n_rows][D], updated in place with y
+ *   y      device bf16 [n_rows][D] or null (a branch's output)
+ *   residual  factor of the stream, finite (with y)
+ *   gate, scale, shift, mod_stride, cu_q, m, eps  as for fd_rms_quant, whose remarks on the range
+ *          of the squares' sums hold for both norms
+ *   post_weight, weight  device fp32 [D] or null (1)
+ * All 16-byte aligned but cu_q, m and the scales.  D is a multiple of 16, at most 12288.
+ */
+fd_status fd_norm_residual(int32_t n_rows, int32_t D, int32_t n_requests, float* h, const uint16_t* y, float residual,
+                           const float* post_weight, const float* gate, const float* weight, const float* shift,
+                           const float* scale, int32_t mod_stride, float eps, const int32_t* cu_q, const int32_t* m,
+                           uint16_t* a_bf, uint8_t* a_codes, uint8_t* code_scale, int8_t* a_int, float* row_scale,
+                           fd_stream_t stream);
+
+/* ---------------------------------------------------------------- 8-bit cache
+ * The K/V cache of a block in half the bytes (Sec. 4 Backend keeps the keys and values
+ * of every token of every block; the paper does not prescribe their format): keys and values as
+ * e4m3 codes, one scale byte per token and key head.  A value is code * 2^(s - 127) as for the 8-bit
+ * rows, its block the head's dh values; s is 1 .. 247, or 255 for a head that holds an infinity or a NaN.
+ *   k, v              device e4m3 [n_tokens][kv_heads dh], 16-byte aligned
+ *   k_scale, v_scale  device uint8 [kv_heads][n_tokens] (a head's bytes side by side)
+ */
+
+/*
+ * fd_rope_axes to an 8-bit cache: q | k | v rows, q and k turned by the token's position; q to its row in
+ * bf16, k and v to the cache rows of the row's token, each rounded once.
+ *   rope   rotary descriptor, or null: q and k are not turned and coord is not read (may be null)
+ * Other arguments as fd_rope_axes.
+ */
+fd_status fd_cache_write(int32_t n_rows, int32_t n_tokens, const fd_rope* rope, int32_t heads, int32_t kv_heads, int32_t dh,
+                         const int32_t* coord, const uint16_t* qkv, const int32_t* idx, const int32_t* m, uint16_t* q,
+                         uint8_t* k, uint8_t* k_scale, uint8_t* v, uint8_t* v_scale, fd_stream_t stream);
+
+/*
+ * Attention of the active rows over every token of their request in an 8-bit cache:
+ *   o_i = softmax(scale * q_i K_b^T) V_b   per head, head h with the keys of key head h / (heads / kv_heads),
+ * for the rows cu_q[b] <= i < cu_q[b + 1] and the tokens req_tok_off[b] .. req_tok_off[b + 1] - 1 of each
+ * request b.  Products of the values that the codes stand for; scores, softmax and sums in fp32, probabilities
+ * rounded to bf16.  Rows of a request without tokens are zeros; rows past cu_q[n_requests] are untouched.
+ *   n_rows      row capacity, cu_q[n_requests] <= n_rows
+ *   max_request_tokens  the most tokens of a request (as in fd_plan): sizes the launch
+ *   heads       a multiple of kv_heads; dh in {16, 64, 128}
+ *   scale       > 0 and finite (1 / sqrt(dh) in a DiT)
+ *   q           device bf16 [n_rows][heads dh], from fd_cache_write
+ *   cu_q, req_tok_off  device int32 [n_requests + 1], ascending; 1 .. 1024 requests
+ *   o           device bf16 [n_rows][heads dh] (output)
+ *   ws          device scratch of fd_cache_attention_ws_size bytes, 256-byte aligned; not read after the call.
+ *               Calls that overlap (streams, captured graphs) need one each.
+ * q and o 16-byte aligned.  n_rows * heads / kv_heads is at most 2^30.
+ */
+size_t fd_cache_attention_ws_size(int32_t n_rows, int32_t heads, int32_t kv_heads, int32_t dh);
+fd_status fd_cache_attention(int32_t n_rows, int32_t n_tokens, int32_t n_requests, int32_t max_request_tokens, int32_t heads,
+                             int32_t kv_heads, int32_t dh, float scale, const uint16_t* q, const uint8_t* k, const uint8_t* k_scale,
+                             const uint8_t* v, const uint8_t* v_scale, const int32_t* cu_q, const int32_t* req_tok_off,
+                             uint16_t* o, void* ws, size_t ws_bytes, fd_stream_t stream);
+
 /* ---------------------------------------------------------------- timing
  * Kernel timer for measurement: while armed for `kernel`, every launch of that
  * kernel records a pair of HIP events around it on its stream (up to
@@ -513,7 +617,8 @@ enum {
   FD_K_SCORE = 1, FD_K_SELECT, FD_K_GATHER, FD_K_EMBED, FD_K_ADALN, FD_K_LN,
   FD_K_GEMM_QKV, FD_K_ATTN, FD_K_GEMM_O, FD_K_GEMM_MLP1, FD_K_GEMM_MLP2,
   FD_K_FINAL, FD_K_SCATTER, FD_K_IMPORTANCE, FD_K_PARTITION,
-  FD_K_QUANT, FD_K_RMS, FD_K_ROPE, FD_K_LINEAR
+  FD_K_QUANT, FD_K_RMS, FD_K_ROPE, FD_K_LINEAR,
+  FD_K_INT_ROWS, FD_K_INT_LINEAR, FD_K_NORM_RESIDUAL, FD_K_CACHE_WRITE, FD_K_CACHE_ATTN
 };
 fd_status fd_timer_arm(int32_t kernel, int32_t capacity);
 int32_t fd_timer_read(float* ms, int32_t capacity);

@@ -153,6 +153,20 @@ fd_status check_rows(int rows) {
   return FD_OK;
 }
 
+// Rows of 8-bit integers: their products' sums stay below 2^31.
+fd_status check_int_cols(int cols) {
+  if (cols > (1 << 16)) return fdh::set_error("%d columns, more than 65536", cols), FD_E_UNSUPPORTED;
+  return check_cols(cols);
+}
+
+// Heads of an 8-bit cache.
+fd_status check_heads(int heads, int kv_heads, int dh) {
+  FD_REQUIRE(heads >= 1 && kv_heads >= 1, "heads must be positive");
+  if (dh != 16 && dh != 64 && dh != 128) return fdh::set_error("head dim %d not in {16, 64, 128}", dh), FD_E_UNSUPPORTED;
+  if (heads > 4096 || kv_heads > 4096) return fdh::set_error("more than 4096 heads"), FD_E_UNSUPPORTED;
+  return FD_OK;
+}
+
 // Checks a rotary descriptor and fills the kernel's sections and the turns of its pairs.
 fd_status rope_turns(const fd_rope* r, int dh, fdh::RopeArgs* g) {
   FD_REQUIRE(r, "rope is null");
@@ -756,8 +770,121 @@ fd_status fd_scaled_block_forward(const fd_plan* plan, const fd_dims* dims, cons
   return FD_OK;
 }
 
+fd_status fd_int_rows(int32_t n_rows, int32_t cols, const uint16_t* x, const int32_t* m, int8_t* q, float* scale,
+                       fd_stream_t stream) {
+  FD_REQUIRE(n_rows >= 1 && cols >= 1, "sizes must be positive");
+  FD_TRY(check_rows(n_rows));
+  FD_TRY(check_int_cols(cols));
+  FD_REQUIRE(x && q && scale, "null pointer");
+  FD_REQUIRE(aligned(x, 16) && aligned(q, 16) && aligned(scale, 4), "misaligned buffer");
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  FD_LAUNCH(FD_K_INT_ROWS, s, fdh::launch_int_rows(x, n_rows, cols, m, reinterpret_cast<uint8_t*>(q), scale, s));
+  return FD_OK;
+}
+
+fd_status fd_int_linear(int32_t n_rows, int32_t n_out, int32_t n_in, const int8_t* a, const float* a_scale, const int8_t* w,
+                         const float* w_scale, const float* bias, int32_t gelu, const int32_t* m, uint16_t* y_bf, float* y_fp,
+                         fd_stream_t stream) {
+  FD_REQUIRE(n_rows >= 1 && n_out >= 1 && n_in >= 1, "sizes must be positive");
+  FD_TRY(check_rows(n_rows));
+  FD_TRY(check_int_cols(n_in));
+  FD_TRY(check_cols(n_out));
+  FD_REQUIRE(a && a_scale && w && w_scale, "null pointer");
+  FD_REQUIRE((y_bf != nullptr) + (y_fp != nullptr) == 1, "not one output");
+  FD_REQUIRE(gelu == 0 || gelu == 1, "gelu = %d", gelu);
+  FD_REQUIRE(aligned(a, 16) && aligned(w, 16) && aligned(a_scale, 4) && aligned(w_scale, 16) && aligned(bias, 16) && aligned(y_bf, 16) &&
+                 aligned(y_fp, 16),
+             "misaligned buffer");
+  if (n_out > (1 << 20) || static_cast<long long>(n_out) * n_in > fdh::kMaxGemmBytes)
+    return fdh::set_error("more than 2^20 columns, or weights of 2 GiB or more (%d x %d given)", n_out, n_in), FD_E_UNSUPPORTED;
+  fdh::IntLinearArgs g{};
+  g.n_rows = n_rows; g.N = n_out; g.K = n_in; g.m = m; g.a = a; g.a_scale = a_scale; g.w = w; g.w_scale = w_scale;
+  g.bias = bias; g.gelu = gelu; g.y_bf16 = y_bf; g.y_f32 = y_fp;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  FD_LAUNCH(FD_K_INT_LINEAR, s, fdh::launch_int_linear(g, s));
+  return FD_OK;
+}
+
+fd_status fd_norm_residual(int32_t n_rows, int32_t D, int32_t n_requests, float* h, const uint16_t* y, float residual,
+                           const float* post_weight, const float* gate, const float* weight, const float* shift,
+                           const float* scale, int32_t mod_stride, float eps, const int32_t* cu_q, const int32_t* m,
+                           uint16_t* a_bf, uint8_t* a_codes, uint8_t* code_scale, int8_t* a_int, float* row_scale,
+                           fd_stream_t stream) {
+  FD_REQUIRE(n_rows >= 1 && D >= 1 && n_requests >= 1, "sizes must be positive");
+  FD_TRY(check_rows(n_rows));
+  FD_TRY(check_cols(D));
+  if (D > 12288) return fdh::set_error("D > 12288 unsupported"), FD_E_UNSUPPORTED;
+  FD_REQUIRE(h && m && (cu_q || n_requests == 1), "null pointer");
+  FD_REQUIRE(!a_codes == !code_scale && !a_int == !row_scale, "8-bit rows without scales, or scales without rows");
+  const int results = (a_bf != nullptr) + (a_codes != nullptr) + (a_int != nullptr);
+  FD_REQUIRE(results == 1 || (results == 0 && y), "not one result, nor a branch to add");
+  FD_REQUIRE(eps >= 0.f, "eps must be >= 0");
+  FD_REQUIRE(isfinite(residual), "residual must be finite");
+  FD_REQUIRE(mod_stride >= 0 && mod_stride % 4 == 0, "mod_stride = %d, not a multiple of 4", mod_stride);
+  FD_REQUIRE(aligned(h, 16) && aligned(y, 16) && aligned(post_weight, 16) && aligned(gate, 16) && aligned(weight, 16) && aligned(shift, 16) &&
+                 aligned(scale, 16) && aligned(a_bf, 16) && aligned(a_codes, 16) && aligned(a_int, 16) && aligned(row_scale, 4),
+             "misaligned buffer");
+  fdh::ResidualArgs g{};
+  g.n_rows = n_rows; g.D = D; g.n_req = n_requests; g.mod_stride = mod_stride; g.cu_q = cu_q; g.m = m; g.eps = eps; g.residual = residual;
+  g.h = h; g.y = y; g.post_weight = post_weight; g.gate = gate; g.weight = weight; g.shift = shift; g.scale = scale;
+  g.a_bf16 = a_bf; g.a8 = a_codes ? a_codes : reinterpret_cast<uint8_t*>(a_int); g.code_scale = code_scale; g.row_scale = row_scale;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  FD_LAUNCH(FD_K_NORM_RESIDUAL, s, fdh::launch_norm_residual(g, s));
+  return FD_OK;
+}
+
+fd_status fd_cache_write(int32_t n_rows, int32_t n_tokens, const fd_rope* rope, int32_t heads, int32_t kv_heads, int32_t dh,
+                         const int32_t* coord, const uint16_t* qkv, const int32_t* idx, const int32_t* m, uint16_t* q,
+                         uint8_t* k, uint8_t* k_scale, uint8_t* v, uint8_t* v_scale, fd_stream_t stream) {
+  FD_REQUIRE(n_rows >= 1 && n_rows <= n_tokens, "%d rows of %d tokens", n_rows, n_tokens);
+  FD_TRY(check_rows(n_rows));
+  FD_TRY(check_heads(heads, kv_heads, dh));
+  FD_REQUIRE((coord || !rope) && qkv && m && q && k && k_scale && v && v_scale, "null pointer");
+  FD_REQUIRE(aligned(qkv, 16) && aligned(q, 16) && aligned(k, 16) && aligned(v, 16), "misaligned buffer");
+  fdh::RopeArgs g{};
+  if (rope) FD_TRY(rope_turns(rope, dh, &g));
+  g.n_rows = n_rows; g.n_tokens = n_tokens; g.hq = heads; g.hk = kv_heads; g.dh = dh; g.m = m; g.idx = idx; g.coord = coord;
+  g.qkv = qkv; g.q = q; g.k8 = k; g.k_scale = k_scale; g.v8 = v; g.v_scale = v_scale;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  FD_LAUNCH(FD_K_CACHE_WRITE, s, fdh::launch_rope(g, rope && rope->pairing == FD_ROPE_HALVES, s));
+  return FD_OK;
+}
+
+size_t fd_cache_attention_ws_size(int32_t n_rows, int32_t heads, int32_t kv_heads, int32_t dh) {
+  if (n_rows < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads || (dh != 16 && dh != 64 && dh != 128)) return 0;
+  return align_up(fdh::cache_attention_scratch_bytes(n_rows, heads, kv_heads, dh));
+}
+
+fd_status fd_cache_attention(int32_t n_rows, int32_t n_tokens, int32_t n_requests, int32_t max_request_tokens, int32_t heads,
+                             int32_t kv_heads, int32_t dh, float scale, const uint16_t* q, const uint8_t* k, const uint8_t* k_scale,
+                             const uint8_t* v, const uint8_t* v_scale, const int32_t* cu_q, const int32_t* req_tok_off,
+                             uint16_t* o, void* ws, size_t ws_bytes, fd_stream_t stream) {
+  FD_REQUIRE(n_rows >= 1 && n_tokens >= 1 && n_requests >= 1, "sizes must be positive");
+  FD_REQUIRE(max_request_tokens >= 0 && max_request_tokens <= n_tokens, "requests of %d of %d tokens", max_request_tokens, n_tokens);
+  FD_TRY(check_rows(n_rows));
+  FD_TRY(check_rows(n_tokens));
+  FD_TRY(check_heads(heads, kv_heads, dh));
+  FD_REQUIRE(heads % kv_heads == 0, "%d heads of %d key heads", heads, kv_heads);
+  FD_REQUIRE(scale > 0.f && isfinite(scale), "scale must be positive and finite");
+  if (n_requests > fdh::kMaxAttnRequests)
+    return fdh::set_error("at most %d requests per call (%d given)", fdh::kMaxAttnRequests, n_requests), FD_E_UNSUPPORTED;
+  if (static_cast<long long>(n_rows) * (heads / kv_heads) > (1 << 30))
+    return fdh::set_error("more than 2^30 rows of a key head"), FD_E_UNSUPPORTED;
+  FD_REQUIRE(q && k && k_scale && v && v_scale && cu_q && req_tok_off && o && ws, "null pointer");
+  FD_REQUIRE(aligned(q, 16) && aligned(k, 16) && aligned(v, 16) && aligned(o, 16) && aligned(ws, kAlign), "misaligned buffer");
+  const size_t need = fd_cache_attention_ws_size(n_rows, heads, kv_heads, dh);
+  if (ws_bytes < need) return fdh::set_error("attention workspace too small (%zu < %zu)", ws_bytes, need), FD_E_SHAPE;
+  fdh::CacheAttnArgs g{};
+  g.n_rows = n_rows; g.n_tokens = n_tokens; g.n_req = n_requests; g.heads = heads; g.kv_heads = kv_heads; g.dh = dh;
+  g.max_req_tokens = max_request_tokens; g.scale = scale; g.q = q; g.o = o; g.k = k; g.v = v; g.k_scale = k_scale; g.v_scale = v_scale;
+  g.cu_q = cu_q; g.tok_off = req_tok_off; g.partial = static_cast<float*>(ws);
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  FD_LAUNCH(FD_K_CACHE_ATTN, s, fdh::launch_cache_attention(g, s));
+  return FD_OK;
+}
+
 fd_status fd_timer_arm(int32_t kernel, int32_t capacity) {
-  FD_REQUIRE(kernel >= FD_K_SCORE && kernel <= FD_K_LINEAR && capacity >= 1 && capacity <= (1 << 20),
+  FD_REQUIRE(kernel >= FD_K_SCORE && kernel <= FD_K_CACHE_ATTN && capacity >= 1 && capacity <= (1 << 20),
              "bad timer arguments");
   std::lock_guard<std::mutex> lk(g_timer.mu);
   for (hipEvent_t e : g_timer.ev) (void)hipEventDestroy(e);

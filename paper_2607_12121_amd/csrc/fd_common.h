@@ -180,6 +180,9 @@ struct RopeArgs {
   const int32_t* m; const int32_t* idx; const int32_t* coord;
   const uint16_t* qkv;           // [n_rows][(hq + 2 hk) dh]
   uint16_t* q; uint16_t* k; uint16_t* v;
+  // instead of k and v: an 8-bit cache, codes [n_tokens][hk * dh] and scales [hk][n_tokens]
+  int n_tokens;
+  uint8_t* k8; uint8_t* v8; uint8_t* k_scale; uint8_t* v_scale;
   double turns[kMaxRopePairs];   // turns of each pair per unit of its axis' position
 };
 hipError_t launch_rope(const RopeArgs& g, bool halves, hipStream_t s);
@@ -195,6 +198,45 @@ struct ScaledArgs {
   uint8_t* y_q; uint8_t* y_scale;
 };
 hipError_t launch_scaled_linear(const ScaledArgs& g, hipStream_t s);
+
+// Rows of 8-bit integers (fd_int.h) and the norms on both sides of a branch.
+hipError_t launch_int_rows(const uint16_t* x, int n_rows, int cols, const int32_t* m, uint8_t* q, float* scale, hipStream_t s);
+struct ResidualArgs {
+  int n_rows, D, n_req, mod_stride;
+  const int32_t* cu_q; const int32_t* m;
+  float eps, residual;
+  float* h;                      // [n_rows][D], = residual * h + gate * norm(y)
+  const uint16_t* y;             // optional
+  const float* post_weight;      // optional [D], as weight
+  const float* gate;             // optional, [n_req] rows of mod_stride, as shift and scale
+  const float* weight; const float* shift; const float* scale;
+  uint16_t* a_bf16;              // one of the results, or none: bf16, or 8 bits with one of the scales
+  uint8_t* a8; uint8_t* code_scale; float* row_scale;
+};
+hipError_t launch_norm_residual(const ResidualArgs& g, hipStream_t s);
+
+struct IntLinearArgs {
+  int n_rows, N, K;
+  const int32_t* m;                             // optional: all n_rows rows without it
+  const int8_t* a; const float* a_scale;        // [n_rows][K], [n_rows]
+  const int8_t* w; const float* w_scale;        // [N][K], [N]
+  const float* bias;                            // optional
+  int gelu;
+  uint16_t* y_bf16; float* y_f32;               // one of the outputs: [n_rows][N]
+};
+hipError_t launch_int_linear(const IntLinearArgs& g, hipStream_t s);
+
+struct CacheAttnArgs {
+  int n_rows, n_tokens, n_req, heads, kv_heads, dh, max_req_tokens;
+  float scale;
+  const uint16_t* q; uint16_t* o;               // [n_rows][heads * dh]
+  const uint8_t* k; const uint8_t* v;           // [n_tokens][kv_heads * dh] codes
+  const uint8_t* k_scale; const uint8_t* v_scale;   // [kv_heads][n_tokens]
+  const int32_t* cu_q; const int32_t* tok_off;
+  float* partial;
+};
+size_t cache_attention_scratch_bytes(int n_rows, int heads, int kv_heads, int dh);
+hipError_t launch_cache_attention(const CacheAttnArgs& g, hipStream_t s);
 
 // Bytes of KV-split scratch the attention kernel needs for head dim dh.
 size_t attn_scratch_bytes(int dh);

@@ -40,20 +40,24 @@ FD_DEVICE uint32_t pack_codes(float a, float b, float c, float d) {
   return static_cast<uint32_t>(r);
 }
 
-// Eight values of a lane to codes: the 16 lanes that share a block (lane & ~15) agree on its
-// scale byte, which is returned.  Lanes past the row's end pass zeros.
-FD_DEVICE uint32_t quant_lane8(const float (&v)[8], uint2& codes) {
+// Eight values of a lane to codes: the `lanes` lanes (2, 8 or 16, from a multiple of them on) that share a block
+// agree on its scale byte, which is returned.  Lanes past the row's end pass zeros.
+FD_DEVICE uint32_t quant_lanes8(const float (&v)[8], int lanes, uint2& codes) {
   uint32_t top = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) top = max(top, mag_bits(v[e]));
 #pragma unroll
-  for (int o = 8; o > 0; o >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), o, kWave)));
+  for (int o = 8; o > 0; o >>= 1)
+    if (o < lanes) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), o, kWave)));
   const uint32_t s = scale_byte(top);
   const float inv = scale_inverse(s);
   codes.x = pack_codes(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
   codes.y = pack_codes(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
   return s;
 }
+
+// ... of a block of 128 columns
+FD_DEVICE uint32_t quant_lane8(const float (&v)[8], uint2& codes) { return quant_lanes8(v, 16, codes); }
 
 // GELU, tanh form: z / (1 + 2^-t), t = 2 sqrt(2 / pi) log2(e) (z + 0.044715 z^3), in seven instructions with the
 // hardware's exponent and reciprocal (an ulp each); gelu_tanh_fast, whose bits the bf16 products keep, takes two more.

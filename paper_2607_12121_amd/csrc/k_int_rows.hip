@@ -1,0 +1,284 @@
+// Rows of 8-bit integers: bf16 rows as they are, and the residual stream through the norms behind and before a
+// block's branches (which also come as bf16 rows and as codes).
+#include <type_traits>
+
+#include "fd_int.h"
+
+namespace {
+
+// bf16 rows [M][cols] to integers.  WAVES waves hold a row in registers between its maximum and its integers: lane t
+// of the row's 64 * WAVES takes the 8 columns at 8 * (t + 64 * WAVES * j), j < VEC.  Bound by HBM: 3 bytes a value.
+template <int VEC, int WAVES>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void int_rows_kernel(const uint16_t* __restrict__ x, int n_rows, int cols,
+                                                                                const int32_t* __restrict__ m_dev, uint8_t* __restrict__ q,
+                                                                                float* __restrict__ scale) {
+  constexpr int TEAMS = WAVES == 1 ? 4 : 1, LANES = 64 * WAVES;
+  __shared__ uint32_t part[2][WAVES];
+  const int M = m_dev ? min(*m_dev, n_rows) : n_rows;
+  const int wave = threadIdx.x >> 6, t = threadIdx.x % LANES;
+  int odd = 0;
+  for (int row = blockIdx.x * TEAMS + (WAVES == 1 ? wave : 0); row < M; row += gridDim.x * TEAMS, odd ^= 1) {
+    const size_t at = static_cast<size_t>(row) * cols;
+    uint4 x8[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      const int c = 8 * (t + LANES * j);
+      x8[j] = c < cols ? *reinterpret_cast<const uint4*>(x + at + c) : make_uint4(0, 0, 0, 0);
+    }
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      float v[8];
+      fd::unpack_bf8(x8[j], v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, fd::mag_bits(v[e]));
+    }
+    top = fd::wave_top(top);
+    if constexpr (WAVES > 1) {   // two sets: a wave may be a row ahead of one that has yet to read
+      if ((threadIdx.x & 63) == 0) part[odd][wave] = top;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) top = max(top, part[odd][w]);
+    }
+    const fd::IntScale s = fd::int_scale(top);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      const int c = 8 * (t + LANES * j);
+      float v[8];
+      fd::unpack_bf8(x8[j], v);
+      if (c < cols) *reinterpret_cast<uint2*>(q + at + c) = fd::pack_ints(v, s.up);
+    }
+    if (t == 0) scale[row] = s.scale;
+  }
+}
+
+enum { kNone, kBf16, kCodes, kInts };
+
+// For row i of request b, with sums in fp32:
+//   r = y / sqrt(mean(y^2) + eps) * post_weight;  h = residual * h + gate_b * r              (only with y)
+//   a = h / sqrt(mean(h^2) + eps) * weight * (1 + scale_b) + shift_b                         (only with a result)
+// A team of WAVES waves takes a run of rows and keeps a request's factors of a value (gate * post_weight, weight *
+// (1 + scale), shift) in registers while the request stays.  Bound by HBM: 4 bytes of h read and 4 written, 2 of y,
+// 1 or 2 of the result per value.
+template <int VEC, int WAVES, int OUT>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_residual_kernel(fdh::ResidualArgs g) {
+  constexpr int TEAMS = WAVES == 1 ? 4 : 1, LANES = 64 * WAVES;
+  __shared__ float part[2][3][WAVES];
+  const int wave = threadIdx.x >> 6, t = threadIdx.x % LANES;
+  const int D = g.D, M = min(*g.m, g.n_rows), ld = fd::scale_stride(D);
+  const int team = blockIdx.x * TEAMS + (WAVES == 1 ? wave : 0), teams = gridDim.x * TEAMS;
+  const int run = (M + teams - 1) / teams, first = min(static_cast<long long>(team) * run, static_cast<long long>(M)), end = min(first + run, M);
+  if (first >= end) return;   // the whole team together
+  float gain[VEC][8], bias[VEC][8], gate[VEC][8];
+  auto load8 = [&](const float* p, float (&v)[8]) {
+    const float4 lo = *reinterpret_cast<const float4*>(p), hi = *reinterpret_cast<const float4*>(p + 4);
+    v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w;
+    v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
+  };
+  auto request = [&](int b) {
+    const size_t mod = static_cast<size_t>(b) * g.mod_stride;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      const int c = 8 * (t + LANES * j);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        gain[j][e] = gate[j][e] = 1.f;
+        bias[j][e] = 0.f;
+      }
+      if (c >= D) continue;
+      float w[8];
+      if (g.y) {
+        if (g.gate) load8(g.gate + mod + c, gate[j]);
+        if (g.post_weight) {
+          load8(g.post_weight + c, w);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) gate[j][e] *= w[e];
+        }
+      }
+      if constexpr (OUT != kNone) {
+        if (g.scale) {
+          load8(g.scale + mod + c, gain[j]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) gain[j][e] += 1.f;
+        }
+        if (g.weight) {
+          load8(g.weight + c, w);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) gain[j][e] *= w[e];
+        }
+        if (g.shift) load8(g.shift + mod + c, bias[j]);
+      }
+    }
+  };
+  float v[VEC][8];
+  uint4 y[VEC];
+  auto fetch = [&](int row) {   // a row's values, zeros past its end
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      const int c = 8 * (t + LANES * j);
+      y[j] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[j][e] = 0.f;
+      if (c >= D) continue;
+      load8(g.h + static_cast<size_t>(row) * D + c, v[j]);
+      if (g.y) y[j] = *reinterpret_cast<const uint4*>(g.y + static_cast<size_t>(row) * D + c);
+    }
+  };
+  // The sum over the row's lanes, the same in all of them: over a wave, then over the waves' sums in order.  Set `at`
+  // of this row's parity is not written again before every wave has passed the barrier of the row after.
+  auto row_sum = [&](float s, int row, int at) {
+    s = fd::wave_sum(s);
+    if constexpr (WAVES > 1) {
+      float* p = part[row & 1][at];
+      if ((threadIdx.x & 63) == 0) p[wave] = s;
+      __syncthreads();
+      if constexpr (WAVES == 2) s = p[0] + p[1];
+      else s = (p[0] + p[1]) + (p[2] + p[3]);
+    }
+    return s;
+  };
+  int b = g.n_req == 1 ? 0 : fd::row_request(g.cu_q, g.n_req, first);
+  int b_end = g.n_req == 1 ? M : g.cu_q[b + 1];   // rows of the request
+  fetch(first);
+  request(b);
+  for (int row = first; row < end; ++row) {
+    if (row >= b_end && g.n_req > 1) {
+      b = fd::row_request(g.cu_q, g.n_req, row);
+      b_end = g.cu_q[b + 1];
+      request(b);
+    }
+    float a[VEC][8];
+    if (g.y) {
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        float y8[8];
+        fd::unpack_bf8(y[j], y8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += y8[e] * y8[e];
+      }
+      const float r = 1.0f / sqrtf(row_sum(sum, row, 0) / static_cast<float>(D) + g.eps);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const int c = 8 * (t + LANES * j);
+        float y8[8];
+        fd::unpack_bf8(y[j], y8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[j][e] = g.residual * v[j][e] + gate[j][e] * (y8[e] * r);
+        if (c < D) {
+          float* h = g.h + static_cast<size_t>(row) * D + c;
+          *reinterpret_cast<float4*>(h) = make_float4(a[j][0], a[j][1], a[j][2], a[j][3]);
+          *reinterpret_cast<float4*>(h + 4) = make_float4(a[j][4], a[j][5], a[j][6], a[j][7]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[j][e] = v[j][e];
+    }
+    if (row + 1 < end) fetch(row + 1);   // on its way while this row is summed and rounded
+    if constexpr (OUT != kNone) {
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += 8 * (t + LANES * j) < D ? a[j][e] * a[j][e] : 0.f;   // past the end y r may be NaN
+      const float r = 1.0f / sqrtf(row_sum(sum, row, 1) / static_cast<float>(D) + g.eps);
+      uint32_t top = 0;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          a[j][e] = 8 * (t + LANES * j) < D ? a[j][e] * r * gain[j][e] + bias[j][e] : 0.f;   // zeros past the end, whatever r is
+          if constexpr (OUT == kInts) top = max(top, fd::mag_bits(a[j][e]));
+        }
+      fd::IntScale s = {};
+      if constexpr (OUT == kInts) {
+        top = fd::wave_top(top);
+        if constexpr (WAVES > 1) {
+          float* p = part[row & 1][2];
+          if ((threadIdx.x & 63) == 0) p[wave] = __uint_as_float(top);
+          __syncthreads();
+#pragma unroll
+          for (int w = 0; w < WAVES; ++w) top = max(top, __float_as_uint(p[w]));
+        }
+        s = fd::int_scale(top);
+        if (t == 0) g.row_scale[row] = s.scale;
+      }
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const int c = 8 * (t + LANES * j);
+        const size_t at = static_cast<size_t>(row) * D + c;
+        if constexpr (OUT == kCodes) {
+          uint2 codes;
+          const uint32_t sb = fd::quant_lane8(a[j], codes);
+          if (c < D) {
+            *reinterpret_cast<uint2*>(g.a8 + at) = codes;
+            if ((t & 15) == 0) g.code_scale[static_cast<size_t>(row) * ld + c / fd::kScaleBlock] = static_cast<uint8_t>(sb);
+          }
+        } else if constexpr (OUT == kInts) {
+          if (c < D) *reinterpret_cast<uint2*>(g.a8 + at) = fd::pack_ints(a[j], s.up);
+        } else if (c < D) {
+          *reinterpret_cast<uint4*>(g.a_bf16 + at) = make_uint4(fd::pack_bf2(a[j][0], a[j][1]), fd::pack_bf2(a[j][2], a[j][3]),
+                                                                fd::pack_bf2(a[j][4], a[j][5]), fd::pack_bf2(a[j][6], a[j][7]));
+        }
+      }
+    }
+  }
+}
+
+}  // namespace
+
+namespace fdh {
+
+hipError_t launch_int_rows(const uint16_t* x, int n_rows, int cols, const int32_t* m, uint8_t* q, float* scale, hipStream_t s) {
+  using std::integral_constant;
+  const int cap = 16 * num_cus();
+  auto run = [&](auto vec, auto waves) {
+    constexpr int VEC = decltype(vec)::value, WAVES = decltype(waves)::value;
+    const int groups = WAVES == 1 ? (n_rows + 3) / 4 : n_rows;
+    int_rows_kernel<VEC, WAVES><<<groups < cap ? groups : cap, WAVES == 1 ? 256 : 64 * WAVES, 0, s>>>(x, n_rows, cols, m, q, scale);
+  };
+  const integral_constant<int, 1> one{};
+  const integral_constant<int, 2> two{};
+  const integral_constant<int, 4> four{};
+  const integral_constant<int, 16> sixteen{};
+  if (cols <= 512) run(one, one);
+  else if (cols <= 1024) run(two, one);
+  else if (cols <= 2048) run(one, four);
+  else if (cols <= 4096) run(two, four);
+  else if (cols <= 8192) run(four, four);
+  else if (cols <= 32768) run(four, sixteen);
+  else run(integral_constant<int, 8>{}, sixteen);
+  return hipGetLastError();
+}
+
+hipError_t launch_norm_residual(const ResidualArgs& g, hipStream_t s) {
+  using std::integral_constant;
+  const int cap = 4 * num_cus();
+  auto out = [&](auto kind) {
+    auto run = [&](auto vec, auto waves) {
+      constexpr int VEC = decltype(vec)::value, WAVES = decltype(waves)::value, OUT = decltype(kind)::value;
+      const int most = WAVES == 2 ? 2 * cap : cap, rows = WAVES == 1 ? (g.n_rows + 3) / 4 : g.n_rows;
+      norm_residual_kernel<VEC, WAVES, OUT><<<rows < most ? rows : most, WAVES == 1 ? 256 : 64 * WAVES, 0, s>>>(g);
+    };
+    const integral_constant<int, 4> four{};
+    if (g.D <= 512) run(integral_constant<int, 1>{}, integral_constant<int, 1>{});
+    else if (g.D <= 1024) run(integral_constant<int, 1>{}, integral_constant<int, 2>{});
+    else switch ((g.D + 2047) / 2048) {
+      case 1: run(integral_constant<int, 1>{}, four); break;
+      case 2: run(integral_constant<int, 2>{}, four); break;
+      case 3: run(integral_constant<int, 3>{}, four); break;
+      case 4: run(integral_constant<int, 4>{}, four); break;
+      default: run(integral_constant<int, 6>{}, four);
+    }
+  };
+  if (g.a_bf16) out(integral_constant<int, kBf16>{});
+  else if (g.code_scale) out(integral_constant<int, kCodes>{});
+  else if (g.row_scale) out(integral_constant<int, kInts>{});
+  else out(integral_constant<int, kNone>{});
+  return hipGetLastError();
+}
+
+}  // namespace fdh

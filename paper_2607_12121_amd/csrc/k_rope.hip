@@ -22,7 +22,9 @@ enum { kInterleaved, kHalvesWide, kHalves };
 // KIND kInterleaved: pairs (2j, 2j + 1); the lane holds both.  kHalves: pairs (j, j + dim / 2) of
 // the axis' section; the partner is read again from the row (it is in the L1), 16 bytes at a time
 // where every dim is a multiple of 16 (kHalvesWide), else value by value.
-template <int KIND>
+//
+// CODES: k and v go to an 8-bit cache, straight from the fp32 results: the dh / 8 lanes of a head agree on its scale.
+template <int KIND, bool CODES>
 __global__ __launch_bounds__(256) void rope_kernel(fdh::RopeArgs g, int row0) {
   __shared__ float2 turn[4][64];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -75,6 +77,14 @@ __global__ __launch_bounds__(256) void rope_kernel(fdh::RopeArgs g, int row0) {
   uint16_t* q = g.q + static_cast<size_t>(row) * g.hq * dh;
   uint16_t* k = g.k + static_cast<size_t>(tok) * g.hk * dh;
   uint16_t* v = g.v + static_cast<size_t>(tok) * g.hk * dh;
+  // values 8 i .. 8 i + 7 of the token's row of a cache
+  auto put_codes = [&](const float (&o)[8], int i, uint8_t* cache, uint8_t* scale) {
+    const int lanes = dh / 8;   // the lanes of a head run this together: 64 and the heads' first values are multiples of it
+    uint2 codes;
+    const uint32_t s = fd::quant_lanes8(o, lanes, codes);
+    *reinterpret_cast<uint2*>(cache + static_cast<size_t>(tok) * g.hk * dh + 8 * i) = codes;
+    if (i % lanes == 0) scale[static_cast<size_t>(i / lanes) * g.n_tokens + tok] = static_cast<uint8_t>(s);
+  };
   for (int i = lane; i < qk8; i += 64) {
     float x[8], y[8], o[8];
     fd::unpack_bf8(*reinterpret_cast<const uint4*>(src + 8 * i), x);
@@ -89,30 +99,49 @@ __global__ __launch_bounds__(256) void rope_kernel(fdh::RopeArgs g, int row0) {
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] = turned[e] ? x[e] * c[e] + y[e] * n[e] : x[e];
+    if (CODES && i >= q8) {
+      put_codes(o, i - q8, g.k8, g.k_scale);
+      continue;
+    }
     const uint4 out = make_uint4(fd::pack_bf2(o[0], o[1]), fd::pack_bf2(o[2], o[3]), fd::pack_bf2(o[4], o[5]), fd::pack_bf2(o[6], o[7]));
     *reinterpret_cast<uint4*>(i < q8 ? q + 8 * i : k + 8 * (i - q8)) = out;
   }
-  for (int i = lane; i < k8; i += 64)
-    *reinterpret_cast<uint4*>(v + 8 * i) = *reinterpret_cast<const uint4*>(src + 8 * (qk8 + i));
+  for (int i = lane; i < k8; i += 64) {
+    const uint4 x = *reinterpret_cast<const uint4*>(src + 8 * (qk8 + i));
+    if constexpr (CODES) {
+      float o[8];
+      fd::unpack_bf8(x, o);
+      put_codes(o, i, g.v8, g.v_scale);
+    } else {
+      *reinterpret_cast<uint4*>(v + 8 * i) = x;
+    }
+  }
 }
 
 }  // namespace
 
 namespace fdh {
 
-hipError_t launch_rope(const RopeArgs& g, bool halves, hipStream_t s) {
+namespace {
+template <bool CODES>
+hipError_t launch_to(const RopeArgs& g, bool halves, hipStream_t s) {
   bool wide = true;
   for (int a = 0; a < g.n_axes; ++a) wide = wide && g.dim[a] % 16 == 0;
   // a launch has fewer than 2^32 threads, 64 of them a row
   constexpr int kRows = 1 << 25;
   for (int row0 = 0; row0 < g.n_rows; row0 += kRows) {
     const int rows = g.n_rows - row0 < kRows ? g.n_rows - row0 : kRows, grid = (rows + 3) / 4;
-    if (!halves) rope_kernel<kInterleaved><<<grid, 256, 0, s>>>(g, row0);
-    else if (wide) rope_kernel<kHalvesWide><<<grid, 256, 0, s>>>(g, row0);
-    else rope_kernel<kHalves><<<grid, 256, 0, s>>>(g, row0);
+    if (!halves) rope_kernel<kInterleaved, CODES><<<grid, 256, 0, s>>>(g, row0);
+    else if (wide) rope_kernel<kHalvesWide, CODES><<<grid, 256, 0, s>>>(g, row0);
+    else rope_kernel<kHalves, CODES><<<grid, 256, 0, s>>>(g, row0);
     if (const hipError_t e = hipGetLastError()) return e;
   }
   return hipSuccess;
+}
+}  // namespace
+
+hipError_t launch_rope(const RopeArgs& g, bool halves, hipStream_t s) {
+  return g.k8 ? launch_to<true>(g, halves, s) : launch_to<false>(g, halves, s);
 }
 
 }  // namespace fdh

@@ -24,7 +24,8 @@ FD_SKIP_REUSE_DRIFT = 1
 
 KERNELS = {"score": 1, "select": 2, "gather": 3, "embed": 4, "adaln": 5, "ln": 6, "gemm_qkv": 7,
            "attn": 8, "gemm_o": 9, "gemm_mlp1": 10, "gemm_mlp2": 11, "final": 12, "scatter": 13,
-           "importance": 14, "partition": 15, "quant": 16, "rms": 17, "rope": 18, "linear": 19}
+           "importance": 14, "partition": 15, "quant": 16, "rms": 17, "rope": 18, "linear": 19,
+           "int_rows": 20, "int_linear": 21, "norm_residual": 22, "cache_write": 23, "cache_attn": 24}
 
 _p = ctypes.c_void_p
 _i32 = ctypes.c_int32
@@ -112,6 +113,14 @@ def lib() -> ctypes.CDLL:
         "fd_scaled_block_ws_size": ([P(FdPlan), P(FdDims)], ctypes.c_size_t),
         "fd_scaled_block_forward": ([P(FdPlan), P(FdDims), P(FdScaledWeights), P(FdRope), _p, _p, _p, _p, _p, _p, _p, _p,
                                      ctypes.c_size_t, _p], _i32),
+        "fd_int_rows": ([_i32, _i32, _p, _p, _p, _p, _p], _i32),
+        "fd_int_linear": ([_i32, _i32, _i32, _p, _p, _p, _p, _p, _i32, _p, _p, _p, _p], _i32),
+        "fd_norm_residual": ([_i32, _i32, _i32, _p, _p, ctypes.c_float, _p, _p, _p, _p, _p, _i32, ctypes.c_float, _p, _p, _p, _p, _p,
+                              _p, _p, _p], _i32),
+        "fd_cache_write": ([_i32, _i32, P(FdRope), _i32, _i32, _i32, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p], _i32),
+        "fd_cache_attention_ws_size": ([_i32, _i32, _i32, _i32], ctypes.c_size_t),
+        "fd_cache_attention": ([_i32, _i32, _i32, _i32, _i32, _i32, _i32, ctypes.c_float, _p, _p, _p, _p, _p, _p, _p, _p, _p,
+                                ctypes.c_size_t, _p], _i32),
         "fd_timer_arm": ([_i32, _i32], _i32),
         "fd_timer_read": ([_p, _i32], _i32),
         "fd_timer_disarm": ([], None),
@@ -130,7 +139,8 @@ def exported_symbols() -> Sequence[str]:
             "fd_select", "fd_gather", "fd_embed", "fd_adaln", "fd_block_ws_size", "fd_block_forward", "fd_final",
             "fd_scatter_update", "fd_importance_ws_size", "fd_region_importance", "fd_partition_ws_size",
             "fd_partition", "fd_scale_stride", "fd_quant_blocks", "fd_rms_quant", "fd_rope_axes", "fd_scaled_linear",
-            "fd_scaled_block_ws_size", "fd_scaled_block_forward", "fd_timer_arm", "fd_timer_read", "fd_timer_disarm")
+            "fd_scaled_block_ws_size", "fd_scaled_block_forward", "fd_int_rows", "fd_int_linear", "fd_norm_residual",
+            "fd_cache_write", "fd_cache_attention_ws_size", "fd_cache_attention", "fd_timer_arm", "fd_timer_read", "fd_timer_disarm")
 
 
 def _check(name: str, status: int) -> None:
@@ -149,7 +159,7 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 _DT = {"f32": (torch.float32,), "f64": (torch.float64,), "i32": (torch.int32,), "u8": (torch.uint8,),
        "b16": (torch.bfloat16, torch.int16, torch.uint16), "bytes": None,
-       "code": (torch.float8_e4m3fn, torch.uint8), "scale": (torch.uint8, torch.float8_e8m0fnu)}
+       "code": (torch.float8_e4m3fn, torch.uint8), "scale": (torch.uint8, torch.float8_e8m0fnu), "i8": (torch.int8,)}
 
 
 def _need(name: str, t: Optional[torch.Tensor], kind: str, numel: int, exact: bool = False,
@@ -485,6 +495,19 @@ def fd_quant_blocks(x, block_rows: int, q, scale, m=None, stream=None) -> None:
     _check("fd_quant_blocks", lib().fd_quant_blocks(rows, cols, block_rows, *p))
 
 
+def _modulation(h, B: int, D: int, *parts):
+    """(row stride, addresses) of a request's gate, shift and scale: fp32 [B, D] on h's device, or None."""
+    stride, mod = 0, [None] * len(parts)
+    given = [(i, t) for i, t in enumerate(parts) if t is not None]
+    if given:
+        stride, dev = given[0][1].stride(0), h.get_device()
+        for i, t in given:
+            if t.shape != (B, D) or t.stride() != (stride, 1) or stride > 1 << 30 or t.dtype != torch.float32 or t.get_device() != dev:
+                raise FlashDiffError(f"gate, shift and mod_scale must be fp32 [{B}, {D}] with contiguous rows of one stride, on {h.device}")
+            mod[i] = t.data_ptr()
+    return stride, mod
+
+
 def fd_rms_quant(h, q, scale, cu_q, m, y=None, gate=None, weight=None, shift=None, mod_scale=None, eps: float = 1e-6,
                  stream=None) -> None:
     """h [rows, D] fp32 += gate * y (with y), then its RMS norm times weight, modulated, as codes q
@@ -493,14 +516,7 @@ def fd_rms_quant(h, q, scale, cu_q, m, y=None, gate=None, weight=None, shift=Non
     (equal row strides)."""
     rows, D = _rows("h", h)
     B = 1 if cu_q is None else cu_q.numel() - 1
-    stride, mod = 0, [None, None, None]
-    given = [(i, t) for i, t in enumerate((gate, shift, mod_scale)) if t is not None]
-    if given:
-        stride, dev = given[0][1].stride(0), h.get_device()
-        for i, t in given:
-            if t.shape != (B, D) or t.stride() != (stride, 1) or stride > 1 << 30 or t.dtype != torch.float32 or t.get_device() != dev:
-                raise FlashDiffError(f"gate, shift and mod_scale must be fp32 [{B}, {D}] with contiguous rows of one stride, on {h.device}")
-            mod[i] = t.data_ptr()
+    stride, mod = _modulation(h, B, D, gate, shift, mod_scale)
     n = rows * D
     h_, y_, w_, cu_, m_, q_, s_, st = _pointers(
         stream, ("h", h, "f32", n), ("y", y, "b16", -n), ("weight", weight, "f32", -D), ("cu_q", cu_q, "i32", -2 if B == 1 else 2), ("m", m, "i32", 1),
@@ -612,6 +628,113 @@ def fd_scaled_block_forward(plan: Plan, d: FdDims, w: FdScaledWeights, rope: Opt
     _check("fd_scaled_block_forward", lib().fd_scaled_block_forward(
         ctypes.byref(plan.c), ctypes.byref(d), ctypes.byref(w), None if rope is None else ctypes.byref(rope), c_, h_, idx_, cu_, m_,
         k_, v_, _ptr(ws), ws.numel() * ws.element_size(), st))
+
+
+# ------------------------------------------------------------------ 8-bit integers
+
+def fd_int_rows(x, q, scale, m=None, stream=None) -> None:
+    """bf16 x [rows, cols] to int8 q [rows, cols] and fp32 scale [rows]: activations (`m` of the rows when given), or
+    weights with a scale per output channel."""
+    rows, cols = _rows("x", x)
+    p = _pointers(stream, ("x", x, "b16", rows * cols), ("m", m, "i32", -1), ("q", q, "i8", rows * cols), ("scale", scale, "f32", rows))
+    _check("fd_int_rows", lib().fd_int_rows(rows, cols, *p))
+
+
+def fd_int_linear(a, a_scale, w, w_scale, y, bias=None, gelu: bool = False, m=None, stream=None) -> None:
+    """y = act((a w^T) * a_scale * w_scale + bias) of int8 a [rows, n_in] and w [n_out, n_in] with fp32 scales per row
+    and per output channel; y bf16 or fp32."""
+    (rows, k), (n, kw) = _rows("a", a), _rows("w", w)
+    if k != kw:
+        raise FlashDiffError(f"a has {k} columns, w {kw}")
+    if y is None:
+        raise FlashDiffError("y is required")
+    wide = y.dtype == torch.float32
+    a_, as_, w_, ws_, b_, m_, y_, st = _pointers(
+        stream, ("a", a, "i8", rows * k), ("a_scale", a_scale, "f32", rows), ("w", w, "i8", n * k), ("w_scale", w_scale, "f32", n),
+        ("bias", bias, "f32", -n), ("m", m, "i32", -1), ("y", y, "f32" if wide else "b16", rows * n))
+    _check("fd_int_linear", lib().fd_int_linear(rows, n, k, a_, as_, w_, ws_, b_, int(gelu), m_, None if wide else y_, y_ if wide else None, st))
+
+
+def fd_norm_residual(h, a, cu_q, m, y=None, post_weight=None, gate=None, residual: float = 1.0, weight=None, shift=None, mod_scale=None,
+                     a_scale=None, eps: float = 1e-6, stream=None) -> None:
+    """h [rows, D] fp32 = residual * h + gate * RMS(y) post_weight (with y), then a = RMS(h) * weight, modulated.  a's type
+    chooses the result: bf16 rows, e4m3 codes with a_scale bytes [rows, fd_scale_stride(D)], or int8 with a_scale fp32
+    [rows]; None: h's update alone.  cu_q None: one request; gate, shift and mod_scale as for fd_rms_quant."""
+    rows, D = _rows("h", h)
+    B = 1 if cu_q is None else cu_q.numel() - 1
+    stride, mod = _modulation(h, B, D, gate, shift, mod_scale)
+    n, dt = rows * D, None if a is None else a.dtype
+    kind, per = ("i8", rows) if dt == torch.int8 else ("code", rows * _stride(D)) if dt in _KIND["code"] else ("b16", 0)
+    if a_scale is not None and not per:
+        raise FlashDiffError("a_scale belongs to 8-bit rows")
+    h_, y_, p_, w_, cu_, m_, a_, s_, st = _pointers(
+        stream, ("h", h, "f32", n), ("y", y, "b16", -n), ("post_weight", post_weight, "f32", -D), ("weight", weight, "f32", -D),
+        ("cu_q", cu_q, "i32", -2 if B == 1 else 2), ("m", m, "i32", 1), ("a", a, kind, -n),
+        ("a_scale", a_scale, "f32" if kind == "i8" else "scale", per if per else -1))
+    bf, codes, ints = kind == "b16", kind == "code", kind == "i8"
+    _check("fd_norm_residual", lib().fd_norm_residual(
+        rows, D, B, h_, y_, residual, p_, mod[0], w_, mod[1], mod[2], stride, eps, cu_, m_, a_ if bf else None, a_ if codes else None,
+        s_ if codes else None, a_ if ints else None, s_ if ints else None, st))
+
+
+# ------------------------------------------------------------------ 8-bit cache
+
+def _cache(name: str, t, scale, kv_heads: int, head_dim: int) -> int:
+    """Tokens of a cache [tokens, kv_heads * head_dim] with scales [kv_heads, tokens]."""
+    tokens, cols = _rows(name, t)
+    if cols != kv_heads * head_dim:
+        raise FlashDiffError(f"{name} has {cols} columns, needs {kv_heads * head_dim}")
+    if tuple(_rows(name + "_scale", scale)) != (kv_heads, tokens):
+        raise FlashDiffError(f"{name}_scale must be [{kv_heads}, {tokens}], got {tuple(scale.shape)}")
+    return tokens
+
+
+def fd_cache_write(qkv, coord, idx, m, q, k, k_scale, v, v_scale, heads: int, kv_heads: int, head_dim: int, dims=None, theta=10000.0,
+                   step=1.0, halves: bool = False, rope: Optional[FdRope] = None, stream=None) -> None:
+    """fd_rope_axes to an 8-bit cache: k and v e4m3 [tokens, kv_heads head_dim] with scale bytes [kv_heads, tokens].  coord
+    None (with no dims or rope): q and k are not turned."""
+    r = rope if rope is not None else rope_axes(dims, theta, step, halves) if dims is not None else None
+    if (r is None) != (coord is None):
+        raise FlashDiffError("rotary positions need both coord and the axes (dims or rope)")
+    rows, cols = _rows("qkv", qkv)
+    if cols != (heads + 2 * kv_heads) * head_dim:
+        raise FlashDiffError(f"qkv has {cols} columns, needs {(heads + 2 * kv_heads) * head_dim}")
+    tokens = _cache("k", k, k_scale, kv_heads, head_dim)
+    if _cache("v", v, v_scale, kv_heads, head_dim) != tokens:
+        raise FlashDiffError("k and v must have the same tokens")
+    if coord is not None and tuple(coord.shape) != (tokens, r.n_axes):
+        raise FlashDiffError(f"coord must be [{tokens}, {r.n_axes}], got {tuple(coord.shape)}")
+    kv = tokens * kv_heads
+    p = _pointers(stream, ("coord", coord, "i32", -1 if r is None else tokens * r.n_axes), ("qkv", qkv, "b16", rows * cols), ("idx", idx, "i32", -rows),
+                  ("m", m, "i32", 1), ("q", q, "b16", rows * heads * head_dim), ("k", k, "code", kv * head_dim), ("k_scale", k_scale, "scale", kv),
+                  ("v", v, "code", kv * head_dim), ("v_scale", v_scale, "scale", kv))
+    _check("fd_cache_write", lib().fd_cache_write(rows, tokens, None if r is None else ctypes.byref(r), heads, kv_heads, head_dim, *p))
+
+
+def fd_cache_attention_ws_size(n_rows: int, heads: int, kv_heads: int, head_dim: int) -> int:
+    return int(lib().fd_cache_attention_ws_size(n_rows, heads, kv_heads, head_dim))
+
+
+def fd_cache_attention(q, k, k_scale, v, v_scale, o, cu_q, req_tok_off, heads: int, kv_heads: int, head_dim: int, ws,
+                       max_request_tokens: Optional[int] = None, scale: Optional[float] = None, stream=None) -> None:
+    """Attention of q's rows [rows, heads head_dim] (request b's are cu_q[b] .. cu_q[b + 1] - 1) over their request's
+    tokens (req_tok_off) in an 8-bit cache, to o [rows, heads head_dim] bf16; scale None: 1 / sqrt(head_dim).  ws of
+    fd_cache_attention_ws_size bytes, its own for calls that overlap."""
+    rows, cols = _rows("q", q)
+    tokens = _cache("k", k, k_scale, kv_heads, head_dim)
+    if cols != heads * head_dim or _cache("v", v, v_scale, kv_heads, head_dim) != tokens:
+        raise FlashDiffError(f"q has {cols} columns of {heads} heads, or v other tokens than k")
+    if cu_q is None or req_tok_off is None or cu_q.numel() < 2 or cu_q.numel() != req_tok_off.numel():
+        raise FlashDiffError("cu_q and req_tok_off must both have requests + 1 entries")
+    B, kv = cu_q.numel() - 1, tokens * kv_heads
+    if ws is None or not ws.is_cuda or not ws.is_contiguous() or ws.get_device() != q.get_device():
+        raise FlashDiffError("ws must be a contiguous tensor on q's device")
+    q_, k_, ks_, v_, vs_, cu_, to_, o_, st = _pointers(
+        stream, ("q", q, "b16", rows * cols), ("k", k, "code", kv * head_dim), ("k_scale", k_scale, "scale", kv), ("v", v, "code", kv * head_dim),
+        ("v_scale", v_scale, "scale", kv), ("cu_q", cu_q, "i32", B + 1), ("req_tok_off", req_tok_off, "i32", B + 1), ("o", o, "b16", rows * cols))
+    _check("fd_cache_attention", lib().fd_cache_attention(
+        rows, tokens, B, tokens if max_request_tokens is None else max_request_tokens, heads, kv_heads, head_dim,
+        head_dim ** -0.5 if scale is None else scale, q_, k_, ks_, v_, vs_, cu_, to_, o_, ws.data_ptr(), ws.numel() * ws.element_size(), st))
 
 
 def fd_timer_arm(kernel: str, capacity: int) -> None:
