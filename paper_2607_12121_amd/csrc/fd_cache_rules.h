@@ -1,0 +1,18 @@
+// How the attention over an 8-bit cache goes through its work.  Plain C++, shared by the device code (row counts are
+// only known there), the host code and a CPU build.
+#pragma once
+
+#include "fd_rules.h"
+
+namespace fd {
+
+constexpr int kFewRows = 32;                                                  // rows of an item of few rows
+FD_RULE constexpr int cache_tile_rows(int dh) { return dh >= 64 ? 256 : 128; }   // ... of a tile
+
+// Few rows rather than tiles, by the items that each way has: all waves of a workgroup work on 32 rows, each on its own
+// keys, where tiles would leave most waves without rows.
+FD_RULE bool cache_few_rows(int few, int tiles) { return few <= 4 * tiles; }
+// Whether every request of a call of at most `rows` rows is of few: 4 items of 32 rows make a tile or less.
+FD_RULE bool cache_always_few(long long rows) { return rows <= 4 * kFewRows; }
+
+}  // namespace fd

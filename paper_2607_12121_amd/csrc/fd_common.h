@@ -228,6 +228,7 @@ hipError_t launch_int_linear(const IntLinearArgs& g, hipStream_t s);
 
 struct CacheAttnArgs {
   int n_rows, n_tokens, n_req, heads, kv_heads, dh, max_req_tokens;
+  bool may_cut;                                 // set per launch: pieces of items have their places, and are joined
   float scale;
   const uint16_t* q; uint16_t* o;               // [n_rows][heads * dh]
   const uint8_t* k; const uint8_t* v;           // [n_tokens][kv_heads * dh] codes

@@ -3,8 +3,28 @@
 // contractions run on v_mfma_f32_32x32x16_bf16 as for a bf16 cache; fp32 online softmax, base 2.
 //
 // The query heads that share a key head are rows of one problem: row r of a request under key head kh is query
-// r / group, head kh * group + r % group.  An item is (key head, 256 of these rows), eight waves of 32 rows.
+// r / group, head kh * group + r % group.  A wave computes S^T = K Q^T (64 keys x 32 rows), so that a lane owns one
+// row: its maximum needs one exchange between the half-waves per tile, its sum none until the end, and S^T feeds
+// O^T = V^T P^T as the second operand.
+//
+// Two ways through the work, chosen by the row counts on the device (fd_cache_rules.h):
+//
+// - Tiles: an item is (key head, 256 rows), a wave per 32 rows (head dim 16: 128 rows, four waves).  The key tile's
+//   codes go to LDS as bf16 values, converted once for all waves (8 conversions a wave and tile; fragments converted
+//   by the wave that uses them would take 128).  Software pipeline: the iteration of key tile t runs the matrix
+//   instructions of S(t + 1) and of O += V P(t) between the element pairs of tile t's softmax, with the codes of K's
+//   tile t + 2 and V's t + 1 on their way to registers.
+// - Few rows: an item is (key head, 32 rows), every wave has key tiles of its own, 64 keys at a time, K straight
+//   from memory into fragments, V through a tile of the wave's own in LDS that transposes it; the waves' results
+//   meet in LDS.  What bounds it is the cache's bytes: 128 KB are on their way to a CU.
+//
+// Schedule: the key steps of all items, head-major, are one range cut into equal shares, one per workgroup.  Pieces of
+// a cut item go to scratch as O / sum with their maximum and sum, and a second kernel joins them in key order (the same
+// bits for the same sizes); no workgroup waits for another.
+#include <type_traits>
+
 #include "fd_attn_sched.h"
+#include "fd_cache_rules.h"
 #include "fd_scaled.h"
 
 namespace {
@@ -13,18 +33,25 @@ constexpr int KB = fd::kKeyTile;
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 typedef short short4_t __attribute__((ext_vector_type(4)));
 using fd::bf16x2_t;
+using fd::f32x2_t;
 using fd::SchedTables;
 typedef __attribute__((address_space(3))) void* lds_ptr_t;
 
 template <int DH>
 struct Cfg {
-  static constexpr int WAVES = DH >= 64 ? 8 : 4, THREADS = 64 * WAVES, QB = 32 * WAVES;
-  static constexpr int KCH = DH / 8;                 // 16-byte chunks of a row of bf16 values in LDS
-  static constexpr int TILE = KB * KCH;              // chunks of a tile
+  static constexpr int WAVES = DH >= 64 ? 8 : 4, THREADS = 64 * WAVES;
+  static constexpr int QB = fd::cache_tile_rows(DH);   // rows of an item, in tiles and of few rows
+  static constexpr int QF = fd::kFewRows;
+  static constexpr int KCH = DH / 8;                   // 16-byte chunks of a key row of bf16 values in LDS
+  static constexpr int TILE = KB * KCH;                // chunks of a tile
   static constexpr int KS = DH / 16, DT = (DH + 31) / 32;
-  static constexpr int PIECE = KB * DH / THREADS;    // codes of a tile that a thread brings: 4, 8 or 16 of a row
+  static constexpr int PIECE = KB * DH / THREADS;      // codes of a tile that a thread brings: 4, 8 or 16 of a row
+  static constexpr int FEW_KEYS = KB * WAVES;          // keys of a step of few rows
+  static constexpr int AHEAD = DH >= 128 ? 2 : 3;      // operand reads ahead of their matrix instructions (registers)
+  static constexpr int E = DT * 16 + 2;                // floats of a thread in a tile's piece
+  static_assert(QB == 32 * WAVES, "a wave per 32 rows");
   // chunk c of key row r lies at c ^ fk(r) of K's tile and c ^ fv(r) of V's, so that the lanes that read together
-  // meet different bank groups
+  // meet different bank groups.  fk(r + 32) = fk(r), fv(r + 8) = fv(r).
   static FD_DEVICE int fk(int r) { return KCH >= 16 ? (r & 15) : KCH == 8 ? ((r >> 1) & 7) : ((r >> 3) & (KCH - 1)); }
   static FD_DEVICE int fv(int r) { return KCH >= 16 ? 4 * (r & 3) : KCH == 8 ? 4 * ((r >> 1) & 1) : 0; }
 };
@@ -37,192 +64,685 @@ FD_DEVICE float half_sum(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+FD_DEVICE float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
+// This wave's LDS writes are done; then the barrier.
+FD_DEVICE void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+FD_DEVICE float scale_of(uint32_t s) { return __uint_as_float(s << 23); }
+// Four codes times a scale as two pairs of bf16 (exact).
+FD_DEVICE uint2 values4(uint32_t codes, float scale) {
+  return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true)));
+}
+FD_DEVICE bf16x8_t lds_chunk(uint32_t addr) {
+  return __builtin_bit_cast(bf16x8_t, *(__attribute__((address_space(3))) const u32x4_t*)(uintptr_t)addr);
+}
+// Eight keys of one d of V's tile: ds_read_b64_tr_b16 twice, the second 8 keys on.
+FD_DEVICE u32x4_t lds_transposed(uint32_t addr, uint32_t eight_keys) {
+  const short4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)(uintptr_t)addr);
+  const short4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)(uintptr_t)(addr + eight_keys));
+  const short v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  return __builtin_bit_cast(u32x4_t, v);
+}
 
-// Prefix tables over the requests: tiles of QB rows and their tile-steps (tiles x key tiles), of one key head.
-// Requests without tokens have no tile-steps; returns whether one of them has rows.
-template <int THREADS>
-FD_DEVICE bool build_tables(SchedTables& t, const fdh::CacheAttnArgs& g, int group, int QB) {
-  __shared__ int empty;
-  const int tid = threadIdx.x;
-  if (tid == 0) empty = 0;
-  __syncthreads();
-  for (int b = tid; b < g.n_req; b += THREADS) {
-    const int rows = (g.cu_q[b + 1] - g.cu_q[b]) * group, keys = g.tok_off[b + 1] - g.tok_off[b];
-    if (rows > 0 && keys <= 0) empty = 1;
-    t.tpre[b] = rows > 0 && keys > 0 ? (rows + QB - 1) / QB : 0;
-    t.wpre[b] = rows > 0 && keys > 0 ? static_cast<long long>(t.tpre[b]) * ((keys + KB - 1) / KB) : 0;
+// Requests with rows and keys: their items of QB rows and key steps.
+struct Lengths {
+  const fdh::CacheAttnArgs* g;
+  int group;
+  FD_DEVICE int rows(int b) const { return (g->cu_q[b + 1] - g->cu_q[b]) * group; }
+  FD_DEVICE int keys(int b) const { return g->tok_off[b + 1] - g->tok_off[b]; }
+  FD_DEVICE int items(int b, int qb) const {
+    const int r = rows(b);
+    return r > 0 && keys(b) > 0 ? (r + qb - 1) / qb : 0;
+  }
+};
+
+// What the schedule is built from, by every workgroup of both kernels alike: the way, and the prefix tables of its items
+// and key steps over the requests.  Each thread takes a run of requests, the runs' sums are scanned over the
+// waves and the workgroup.
+struct Way { bool few, empty; };   // empty: a request has rows but no keys
+template <int DH>
+FD_DEVICE Way build_tables(SchedTables& t, const fdh::CacheAttnArgs& g, int group) {
+  using C = Cfg<DH>;
+  constexpr int NW = C::WAVES;
+  __shared__ int s_items[2][NW], s_empty[NW];
+  __shared__ long long s_steps[NW];
+  const Lengths len{&g, group};
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int per = (g.n_req + C::THREADS - 1) / C::THREADS, b0 = min(tid * per, g.n_req), b1 = min(b0 + per, g.n_req);
+  int few = 0, tiles = 0, empty = 0;
+  for (int b = b0; b < b1; ++b) {
+    few += len.items(b, C::QF);
+    tiles += len.items(b, C::QB);
+    empty |= len.rows(b) > 0 && len.keys(b) <= 0;
+  }
+  few = fd::wave_sum(few);
+  tiles = fd::wave_sum(tiles);
+  empty = __any(empty);
+  if (lane == 0) {
+    s_items[0][wave] = few;
+    s_items[1][wave] = tiles;
+    s_empty[wave] = empty;
   }
   __syncthreads();
-  if (tid == 0) {
-    int tiles = 0;
-    long long steps = 0;
-    for (int b = 0; b < g.n_req; ++b) {
-      const int nt = t.tpre[b];
-      const long long nw = t.wpre[b];
-      t.tpre[b] = tiles;
-      t.wpre[b] = steps;
-      tiles += nt;
-      steps += nw;
+  few = tiles = empty = 0;
+  for (int w = 0; w < NW; ++w) {
+    few += s_items[0][w];
+    tiles += s_items[1][w];
+    empty |= s_empty[w];
+  }
+  const Way way{fd::cache_few_rows(few, tiles), empty != 0};
+  const int qb = way.few ? C::QF : C::QB, kb = way.few ? C::FEW_KEYS : KB;
+  int it = 0;
+  long long st = 0;
+  for (int b = b0; b < b1; ++b) {
+    const int n = len.items(b, qb);
+    it += n;
+    st += static_cast<long long>(n) * ((len.keys(b) + kb - 1) / kb);
+  }
+  int it_in = it;
+  long long st_in = st;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int x = __shfl_up(it_in, o, 64);
+    const long long y = __shfl_up(st_in, o, 64);
+    if (lane >= o) {
+      it_in += x;
+      st_in += y;
     }
-    t.tpre[g.n_req] = tiles;
-    t.wpre[g.n_req] = steps;
   }
   __syncthreads();
-  return empty != 0;
+  if (lane == 63) {
+    s_items[0][wave] = it_in;
+    s_steps[wave] = st_in;
+  }
+  __syncthreads();
+  int pi = it_in - it;
+  long long ps = st_in - st;
+  for (int w = 0; w < wave; ++w) {
+    pi += s_items[0][w];
+    ps += s_steps[w];
+  }
+  for (int b = b0; b < b1; ++b) {
+    t.tpre[b] = pi;
+    t.wpre[b] = ps;
+    const int n = len.items(b, qb);
+    pi += n;
+    ps += static_cast<long long>(n) * ((len.keys(b) + kb - 1) / kb);
+  }
+  if (b0 < b1 && b1 == g.n_req) {
+    t.tpre[g.n_req] = pi;
+    t.wpre[g.n_req] = ps;
+  }
+  __syncthreads();
+  return way;
+}
+
+// The shares.  In tiles attn_cuts decides whether items are cut; few rows always are, into shares of a step at least.
+template <int DH>
+struct Sched : fd::AttnSched<Cfg<DH>::QB, DH, true, true> {
+  using Base = fd::AttnSched<Cfg<DH>::QB, DH, true, true>;
+  FD_DEVICE Sched(const SchedTables* t, const fdh::CacheAttnArgs& g, bool few, int grid)
+      : Base(t, g.cu_q, g.tok_off, g.n_req, g.kv_heads, grid, (g.max_req_tokens + KB - 1) / KB) {
+    if (!few && g.may_cut) return;
+    this->cut = few && g.may_cut;
+    this->G = grid;
+    this->per = fd::div_steps(this->work, grid);
+    this->extra = static_cast<int>(this->work - this->per * grid);
+    if (this->cut && this->work < grid) {   // shares of one step, so that the empty ones come last
+      this->G = static_cast<int>((this->work + fd::kXcds - 1) / fd::kXcds * fd::kXcds);
+      this->per = 1;
+      this->extra = 0;
+    }
+  }
+};
+
+// One lane's row of an item: where its query (and result) begins, and whether there is one.
+struct RowAt { size_t at; bool live; };
+template <int DH>
+FD_DEVICE RowAt row_at(const fdh::CacheAttnArgs& g, int group, int b, int head, int r) {
+  const int q0 = g.cu_q[b], rows = (g.cu_q[b + 1] - q0) * group;
+  const int query = group == 1 ? r : r / group;
+  return {(static_cast<size_t>(q0 + query) * g.heads + static_cast<size_t>(head) * group + (r - query * group)) * DH, r < rows};
+}
+
+// This lane's part of O^T blocks as a bf16 row: register 4 r4 + e of block dt is d = 32 dt + 8 r4 + 4 lg + e.
+template <int DH>
+FD_DEVICE void store_o(uint16_t* row, int lg, const f32x16_t (&o)[Cfg<DH>::DT], float inv) {
+#pragma unroll
+  for (int d = 0; d < Cfg<DH>::DT; ++d)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const int d0 = 32 * d + 8 * r4 + 4 * lg;
+      if (d0 >= DH) continue;
+      *reinterpret_cast<uint2*>(row + d0) = make_uint2(fd::pack_bf2(o[d][4 * r4] * inv, o[d][4 * r4 + 1] * inv),
+                                                       fd::pack_bf2(o[d][4 * r4 + 2] * inv, o[d][4 * r4 + 3] * inv));
+    }
+}
+
+// The running maximum of a row takes a tile's scores s (64 keys, 32 of them in this lane) and O and the sum are rescaled
+// where it grew by more than 8 (P stays below 2^8; the softmax does not depend on what is subtracted).  Returns what to
+// subtract.  LIMIT: the scores of the lane's keys from `lim` on are not the request's.
+template <int DH, bool LIMIT>
+FD_DEVICE float take_max(f32x16_t (&s)[2], int lim, float scale_log2, float& m_run, float& l_run, f32x16_t (&o)[Cfg<DH>::DT]) {
+  if constexpr (LIMIT) {
+#pragma unroll
+    for (int kh = 0; kh < 2; ++kh)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (32 * kh + 8 * (r >> 2) + (r & 3) >= lim) s[kh][r] = -INFINITY;
+  }
+  float mx[4];   // four independent chains
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const int kh = c >> 1, r0 = 8 * (c & 1);
+    mx[c] = __builtin_elementwise_maximum(s[kh][r0], s[kh][r0 + 1]);
+#pragma unroll
+    for (int r = r0 + 2; r < r0 + 8; r += 2) mx[c] = max3(mx[c], s[kh][r], s[kh][r + 1]);
+  }
+  const float top = half_max(__builtin_elementwise_maximum(__builtin_elementwise_maximum(mx[0], mx[1]), __builtin_elementwise_maximum(mx[2], mx[3]))) * scale_log2;
+  const bool grow = top > m_run + 8.0f;
+  const float m_new = grow ? top : m_run;
+  if (__any(grow)) {
+    const float alpha = grow ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.0f;
+    l_run *= alpha;
+#pragma unroll
+    for (int d = 0; d < Cfg<DH>::DT; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
+  }
+  m_run = m_new;
+  return m_new == -INFINITY ? 0.0f : m_new;   // no finite score yet: exp2(-inf) is zero, not NaN
+}
+
+// P = exp2(s scale - sub) in bf16, the second operand of O^T, and its sum: of the rounded values that the product takes.
+FD_DEVICE void take_p(const f32x16_t (&s)[2], float scale_log2, float sub, bf16x8_t (&pk)[4], float& l_run) {
+  float sum[2] = {0.f, 0.f};
+#pragma unroll
+  for (int st = 0; st < 4; ++st)
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const f32x2_t f = {__builtin_amdgcn_exp2f(fmaf(s[st >> 1][8 * (st & 1) + e], scale_log2, -sub)),
+                         __builtin_amdgcn_exp2f(fmaf(s[st >> 1][8 * (st & 1) + e + 1], scale_log2, -sub))};
+      const bf16x2_t pb = __builtin_convertvector(f, bf16x2_t);
+      sum[(e >> 1) & 1] = __builtin_amdgcn_fdot2_f32_bf16(pb, bf16x2_t{(__bf16)1.0f, (__bf16)1.0f}, sum[(e >> 1) & 1], false);
+      pk[st][e] = pb[0];
+      pk[st][e + 1] = pb[1];
+    }
+  l_run += sum[0] + sum[1];
 }
 
 template <int DH>
-__global__ __launch_bounds__(Cfg<DH>::THREADS) void cache_attn_kernel(fdh::CacheAttnArgs g) {
+struct Lane {   // addressing that does not depend on the work
+  uint32_t k_off[Cfg<DH>::KS], v_off[Cfg<DH>::DT];   // byte offsets in a tile of this lane's fragments
+  bool tr_live;                                      // d is below the head dim, else the operand's rows are zeros
+  FD_DEVICE explicit Lane(int lane) {
+    using C = Cfg<DH>;
+    const int l32 = lane & 31, lg = lane >> 5, grp = lane >> 4, jj = lane & 15;
+    // ds_read_b64_tr_b16: in a group of 16 lanes lane j addresses four d of key K0 + j / 4, and gets its own d of the
+    // keys K0 .. K0 + 3
+    const int tr_key = 4 * lg + (jj >> 2), tr_d = 16 * (grp & 1) + 4 * (jj & 3);
+    tr_live = DH >= 32 || (grp & 1) == 0;
+#pragma unroll
+    for (int ks = 0; ks < C::KS; ++ks) k_off[ks] = static_cast<uint32_t>((l32 * C::KCH + ((2 * ks + lg) ^ C::fk(l32))) * 16);
+#pragma unroll
+    for (int d = 0; d < C::DT; ++d) {
+      const int at = 32 * d + tr_d;
+      v_off[d] = static_cast<uint32_t>((tr_key * C::KCH + ((at >> 3) ^ C::fv(tr_key))) * 16 + (at & 7) * 2);
+    }
+  }
+  // V^T of 16-key step st, block d, of the tile at `tile`
+  FD_DEVICE u32x4_t v_frag(uint32_t tile, int st, int d) const {
+    u32x4_t v = {0, 0, 0, 0};
+    if (tr_live) v = lds_transposed(tile + v_off[d] + static_cast<uint32_t>(16 * st * Cfg<DH>::KCH * 16), 8 * Cfg<DH>::KCH * 16);
+    return v;
+  }
+};
+
+// ---------------------------------------------------------------- tiles
+
+// Key tiles [kt0, kt1) of query tile `tile` of request b under key head `head`, to the outputs or, of a cut item, to
+// scratch slot `slot_no`.
+template <int DH>
+FD_DEVICE void tile_piece(const fdh::CacheAttnArgs& g, int group, float scale_log2, const Lane<DH>& ln, uint32_t lds, int head, int tile,
+                          int b, int kt0, int kt1, int slot_no) {
   using C = Cfg<DH>;
-  constexpr int KS = C::KS, DT = C::DT, KCH = C::KCH;
-  __shared__ uint4 kt[C::TILE], vt[C::TILE];
-  __shared__ SchedTables tabs;
-  const int group = g.heads / g.kv_heads, ldq = g.heads * DH, ldk = g.kv_heads * DH;
-  const bool empty = build_tables<C::THREADS>(tabs, g, group, C::QB);
+  constexpr int DT = C::DT, KS = C::KS, KCH = C::KCH;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, lg = lane >> 5;
-  if (empty)   // a request without tokens: its rows are zeros
+  const int k_beg = g.tok_off[b], k_end = g.tok_off[b + 1], nkt = kt1 - kt0, ldk = g.kv_heads * DH;
+  const RowAt me = row_at<DH>(g, group, b, head, tile * C::QB + 32 * wave + l32);
+  bf16x8_t qf[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    u32x4_t t = {0, 0, 0, 0};
+    if (me.live) t = *reinterpret_cast<const u32x4_t*>(g.q + me.at + ks * 16 + lg * 8);
+    qf[ks] = __builtin_bit_cast(bf16x8_t, t);
+  }
+
+  // a thread's codes of a tile: PIECE of row `row` from column c0 on; rows past the end repeat the last one
+  constexpr int PER_ROW = DH / C::PIECE;
+  const int row = tid / PER_ROW, c0 = tid % PER_ROW * C::PIECE;
+  struct Codes { uint32_t c[C::PIECE / 4]; uint32_t scale; };
+  const uint32_t off = static_cast<uint32_t>(row) * static_cast<uint32_t>(ldk) + static_cast<uint32_t>(c0);
+  auto fetch = [&](const uint8_t* cache, const uint8_t* scale, int t) {   // of local tile t
+    const int key0 = k_beg + (kt0 + fd::uniform(min(t, nkt - 1))) * KB, last = k_end - 1 - key0;
+    const bool in = row <= last;
+    const uint8_t* base = cache + static_cast<size_t>(key0) * ldk + static_cast<size_t>(head) * DH;
+    Codes x;
+    __builtin_memcpy(x.c, base + (in ? off : static_cast<uint32_t>(last) * static_cast<uint32_t>(ldk) + static_cast<uint32_t>(c0)), C::PIECE);
+    x.scale = (scale + static_cast<size_t>(head) * g.n_tokens + key0)[in ? row : last];
+    return x;
+  };
+  const uint32_t put_k = static_cast<uint32_t>((row * KCH + ((c0 / 8) ^ C::fk(row))) * 16 + c0 % 8 * 2);
+  const uint32_t put_v = static_cast<uint32_t>((row * KCH + ((c0 / 8) ^ C::fv(row))) * 16 + c0 % 8 * 2);
+  auto put = [&](const Codes& x, uint32_t at) {   // as bf16 values to LDS
+    const float s = scale_of(x.scale);
+    if constexpr (C::PIECE == 4) {
+      const uint2 v = values4(x.c[0], s);
+      *(__attribute__((address_space(3))) uint64_t*)(uintptr_t)at = __builtin_bit_cast(uint64_t, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < C::PIECE / 8; ++i) {
+        const uint2 lo = values4(x.c[2 * i], s), hi = values4(x.c[2 * i + 1], s);
+        // the piece's second chunk is the first one's neighbour: c0 / 8 is even
+        *(__attribute__((address_space(3))) u32x4_t*)(uintptr_t)(at ^ (16u * i)) = u32x4_t{lo.x, lo.y, hi.x, hi.y};
+      }
+    }
+  };
+  // rings of two tiles each: K, then V
+  auto k_tile = [&](int t) { return lds + static_cast<uint32_t>((t & 1) * C::TILE * 16); };
+  auto v_tile = [&](int t) { return lds + static_cast<uint32_t>((2 + (t & 1)) * C::TILE * 16); };
+
+  f32x16_t o[DT] = {};
+  float m_run = -INFINITY, l_run = 0.f;
+  bf16x8_t pk[4];
+  auto s_step = [&](uint32_t tile_at, f32x16_t (&s)[2], int ks) {
+    const f32x16_t zero = {};
+#pragma unroll
+    for (int kh = 0; kh < 2; ++kh) {
+      const bf16x8_t a = lds_chunk(tile_at + ln.k_off[ks] + static_cast<uint32_t>(kh * 32 * KCH * 16));
+      s[kh] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[ks], ks == 0 ? zero : s[kh], 0, 0, 0);
+    }
+  };
+
+  // Iteration t: S(t + 1), the softmax of tile t and O += V P(t).  At its barrier K(t + 1) and V(t) are in LDS and every
+  // wave is done with K(t) and V(t - 1), whose places K(t + 2) and V(t + 1) take.
+  auto body = [&](int t, f32x16_t (&cur)[2], f32x16_t (&nxt)[2]) {
+    lds_barrier();
+    const Codes ck = fetch(g.k, g.k_scale, t + 2), cv = fetch(g.v, g.v_scale, t + 1);
+    const uint32_t kt_at = k_tile(t + 1), vt_at = v_tile(t);
+    // jobs: one operand read feeding one matrix instruction; first the rest of S(t + 1) (its first step runs beside the
+    // maximum), then O by quarters of P as they come; reads run AH jobs ahead
+    constexpr int NS = (KS - 1) * 2, NJ = NS + DT * 4, AH = C::AHEAD < NJ ? C::AHEAD : NJ, PAIRS = 16, PER = (NJ + PAIRS - 1) / PAIRS;
+    auto read = [&](int j) -> u32x4_t {
+      if (j < NS) return __builtin_bit_cast(u32x4_t, lds_chunk(kt_at + ln.k_off[1 + j / 2] + static_cast<uint32_t>(j % 2 * 32 * KCH * 16)));
+      return ln.v_frag(vt_at, (j - NS) / DT, (j - NS) % DT);
+    };
+    auto run = [&](int j, u32x4_t op) {
+      const bf16x8_t a = __builtin_bit_cast(bf16x8_t, op);
+      if (j < NS) nxt[j % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[1 + j / 2], nxt[j % 2], 0, 0, 0);
+      else o[(j - NS) % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pk[(j - NS) / DT], o[(j - NS) % DT], 0, 0, 0);
+    };
+    auto earliest = [&](int j) { return j < NS ? 0 : 4 * ((j - NS) / DT + 1); };   // pair behind which job j may run
+    s_step(kt_at, nxt, 0);
+    const float sub = take_max<DH, false>(cur, 0, scale_log2, m_run, l_run, o);
+    u32x4_t ops[AH];
+#pragma unroll
+    for (int j = 0; j < AH; ++j) ops[j] = read(j);
+    // P in three stages that overlap across pairs: exponentials of pair pp, scaled scores of pp + 1, packing and sum of pp - 1
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    int cursor = 0;
+    auto next_job = [&] {
+      run(cursor, ops[cursor % AH]);
+      if (cursor + AH < NJ) ops[cursor % AH] = read(cursor + AH);
+      ++cursor;
+    };
+    auto arg = [&](int pp, float (&x)[2]) {
+      const int st = pp / 4, e = 2 * (pp % 4);
+      x[0] = fmaf(cur[st / 2][(st % 2) * 8 + e], scale_log2, -sub);
+      x[1] = fmaf(cur[st / 2][(st % 2) * 8 + e + 1], scale_log2, -sub);
+    };
+    auto pack = [&](int pp, float p0, float p1) {
+      const int st = pp / 4, e = 2 * (pp % 4);
+      const f32x2_t f = {p0, p1};
+      const bf16x2_t pb = __builtin_convertvector(f, bf16x2_t);
+      sum[pp % 4] = __builtin_amdgcn_fdot2_f32_bf16(pb, bf16x2_t{(__bf16)1.0f, (__bf16)1.0f}, sum[pp % 4], false);
+      pk[st][e] = pb[0];
+      pk[st][e + 1] = pb[1];
+    };
+    float x[2], p0 = 0.f, p1 = 0.f;
+    arg(0, x);
+#pragma unroll
+    for (int pp = 0; pp < PAIRS; ++pp) {
+      const float e0 = __builtin_amdgcn_exp2f(x[0]), e1 = __builtin_amdgcn_exp2f(x[1]);
+      if (pp + 1 < PAIRS) arg(pp + 1, x);
+      if (pp > 0) pack(pp - 1, p0, p1);
+      p0 = e0;
+      p1 = e1;
+#pragma unroll
+      for (int k = 0; k < PER; ++k)
+        if (cursor < NJ && earliest(cursor) <= pp) next_job();
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    pack(PAIRS - 1, p0, p1);
+#pragma unroll
+    for (int k = 0; k < NJ; ++k)
+      if (cursor < NJ) next_job();
+    put(ck, k_tile(t + 2) + put_k);
+    put(cv, v_tile(t + 1) + put_v);
+    l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  };
+  auto tail = [&](int t, f32x16_t (&cur)[2]) {
+    lds_barrier();
+    const int lim = k_end - (k_beg + (kt0 + t) * KB) - 4 * lg;   // this lane's keys below it are the request's
+    const float sub = take_max<DH, true>(cur, lim, scale_log2, m_run, l_run, o);
+    take_p(cur, scale_log2, sub, pk, l_run);
+#pragma unroll
+    for (int st = 0; st < 4; ++st)
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, ln.v_frag(v_tile(t), st, d)), pk[st], o[d], 0, 0, 0);
+  };
+  {
+    const Codes k0 = fetch(g.k, g.k_scale, 0), k1 = fetch(g.k, g.k_scale, 1), v0 = fetch(g.v, g.v_scale, 0);
+    put(k0, k_tile(0) + put_k);
+    put(k1, k_tile(1) + put_k);
+    put(v0, v_tile(0) + put_v);
+  }
+  lds_barrier();
+  f32x16_t sa[2], sb[2];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) s_step(k_tile(0), sa, ks);
+  int t = 0;
+  for (; t + 2 <= nkt - 1; t += 2) {
+    body(t, sa, sb);
+    body(t + 1, sb, sa);
+  }
+  if (t < nkt - 1) {
+    body(t, sa, sb);
+    tail(t + 1, sb);
+  } else {
+    tail(t, sa);
+  }
+  lds_barrier();   // the rings are filled again by the next piece
+  l_run = half_sum(l_run);
+  const float inv = 1.0f / l_run;
+  if (slot_no < 0) {
+    if (me.live) store_o<DH>(g.o + me.at, lg, o, inv);
+    return;
+  }
+  // a piece: O / sum in quads, then (maximum, sum), lane-major
+  float* slot = g.partial + static_cast<size_t>(slot_no) * (C::E * C::THREADS);
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4)
+      reinterpret_cast<float4*>(slot)[(4 * d + r4) * C::THREADS + tid] =
+          make_float4(o[d][4 * r4] * inv, o[d][4 * r4 + 1] * inv, o[d][4 * r4 + 2] * inv, o[d][4 * r4 + 3] * inv);
+  reinterpret_cast<f32x2_t*>(slot + DT * 16 * C::THREADS)[tid] = f32x2_t{m_run, l_run};
+}
+
+// ---------------------------------------------------------------- few rows
+
+// Key steps [s0, s1) of 32 rows; the piece's slot holds O / sum [32][DH] and (maximum, sum) [32].
+template <int DH>
+FD_DEVICE void few_piece(const fdh::CacheAttnArgs& g, int group, float scale_log2, const Lane<DH>& ln, uint4* ring, uint32_t lds, int head,
+                         int tile, int b, int s0, int s1, int slot_no) {
+  using C = Cfg<DH>;
+  constexpr int DT = C::DT, KS = C::KS, KCH = C::KCH;
+  constexpr int KL = DH / 2;                               // codes of a key in a lane: its half of the head
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, lg = lane >> 5;
+  const int k_beg = g.tok_off[b], k_end = g.tok_off[b + 1], ldk = g.kv_heads * DH;
+  const RowAt me = row_at<DH>(g, group, b, head, tile * C::QF + l32);
+  // the contraction's order is free: value i of step ks is d = lg * DH / 2 + 8 ks + i, so that a lane's part of a key
+  // is one run of codes
+  bf16x8_t qf[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    u32x4_t t = {0, 0, 0, 0};
+    if (me.live) t = *reinterpret_cast<const u32x4_t*>(g.q + me.at + lg * KL + 8 * ks);
+    qf[ks] = __builtin_bit_cast(bf16x8_t, t);
+  }
+  constexpr int PER_ROW = DH / 16, VROWS = 64 / PER_ROW, VN = KB / VROWS;   // V: 16 codes a lane, VROWS rows a load
+  const int vrow = lane / PER_ROW, vc = lane % PER_ROW * 16;
+  struct Tile { uint32_t k[2][KL / 4]; u32x4_t v[VN]; uint32_t ks, vs; };
+  const uint8_t* ksc = g.k_scale + static_cast<size_t>(head) * g.n_tokens;
+  const uint8_t* vsc = g.v_scale + static_cast<size_t>(head) * g.n_tokens;
+  auto fetch = [&](Tile& x, int key0) {   // keys past the end repeat the last one
+    const int last = k_end - 1 - key0;
+    const uint8_t* kp = g.k + static_cast<size_t>(key0) * ldk + static_cast<size_t>(head) * DH;
+    const uint8_t* vp = g.v + static_cast<size_t>(key0) * ldk + static_cast<size_t>(head) * DH;
+#pragma unroll
+    for (int kh = 0; kh < 2; ++kh) {
+      const uint8_t* p = kp + static_cast<uint32_t>(min(32 * kh + l32, last)) * static_cast<uint32_t>(ldk) + lg * KL;
+      __builtin_memcpy(x.k[kh], __builtin_assume_aligned(p, KL < 16 ? KL : 16), KL);
+    }
+#pragma unroll
+    for (int i = 0; i < VN; ++i)
+      x.v[i] = *reinterpret_cast<const u32x4_t*>(vp + static_cast<uint32_t>(min(VROWS * i + vrow, last)) * static_cast<uint32_t>(ldk) + vc);
+    x.ks = ksc[key0 + min(lane, last)];
+    x.vs = vsc[key0 + min(lane, last)];
+  };
+  const uint32_t vt_at = lds + static_cast<uint32_t>(wave * C::TILE * 16);   // this wave's tile of V
+  f32x16_t o[DT] = {};
+  float m_run = -INFINITY, l_run = 0.f;
+  Tile x;
+  auto step = [&](int key0, int next) {   // the tile in x, whose place the one from `next` on takes
+    f32x16_t s[2] = {};
+#pragma unroll
+    for (int kh = 0; kh < 2; ++kh) {
+      const float sc = scale_of(__shfl(static_cast<int>(x.ks), 32 * kh + l32, fd::kWave));
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const uint2 lo = values4(x.k[kh][2 * ks], sc), hi = values4(x.k[kh][2 * ks + 1], sc);
+        s[kh] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, u32x4_t{lo.x, lo.y, hi.x, hi.y}), qf[ks], s[kh], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < VN; ++i) {   // V as bf16 values to the wave's tile
+      const int r = VROWS * i + vrow;
+      const float sc = scale_of(__shfl(static_cast<int>(x.vs), r, fd::kWave));
+      const uint2 a = values4(x.v[i][0], sc), b2 = values4(x.v[i][1], sc), c = values4(x.v[i][2], sc), d = values4(x.v[i][3], sc);
+      const uint32_t at = vt_at + static_cast<uint32_t>((r * KCH + ((vc / 8) ^ C::fv(r))) * 16);
+      *(__attribute__((address_space(3))) u32x4_t*)(uintptr_t)at = u32x4_t{a.x, a.y, b2.x, b2.y};
+      *(__attribute__((address_space(3))) u32x4_t*)(uintptr_t)(at ^ 16u) = u32x4_t{c.x, c.y, d.x, d.y};
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    fetch(x, next);
+    __builtin_amdgcn_sched_barrier(0);
+    const float sub = take_max<DH, true>(s, k_end - key0 - 4 * lg, scale_log2, m_run, l_run, o);
+    bf16x8_t pk[4];
+    take_p(s, scale_log2, sub, pk, l_run);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the tile is the wave's own: no barrier
+#pragma unroll
+    for (int st = 0; st < 4; ++st)
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, ln.v_frag(vt_at, st, d)), pk[st], o[d], 0, 0, 0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  };
+  const int key_end = min(k_end, k_beg + s1 * C::FEW_KEYS);
+  int key0 = k_beg + s0 * C::FEW_KEYS + wave * KB;
+  if (key0 < key_end) {
+    fetch(x, key0);
+    for (; key0 < key_end; key0 += C::FEW_KEYS) step(key0, min(key0 + C::FEW_KEYS, k_end - 1));   // the last one fetches in vain
+  }
+  l_run = half_sum(l_run);
+  // the waves' results: O [wave][32][DH + 4] unnormalised, (maximum, sum) [wave][32]
+  __syncthreads();
+  constexpr int LD = DH + 4;
+  float* part = reinterpret_cast<float*>(ring);
+  f32x2_t* ml = reinterpret_cast<f32x2_t*>(part + C::WAVES * 32 * LD);
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const int d0 = 32 * d + 8 * r4 + 4 * lg;
+      if (d0 < DH)
+        *reinterpret_cast<float4*>(part + (wave * 32 + l32) * LD + d0) = make_float4(o[d][4 * r4], o[d][4 * r4 + 1], o[d][4 * r4 + 2], o[d][4 * r4 + 3]);
+    }
+  if (lg == 0) ml[wave * 32 + l32] = f32x2_t{m_run, l_run};
+  __syncthreads();
+  const int rows = min(C::QF, (g.cu_q[b + 1] - g.cu_q[b]) * group - tile * C::QF);
+  float* slot = g.partial + static_cast<size_t>(max(slot_no, 0)) * (32 * (DH + 2));
+  for (int i = tid; i < rows * (DH / 4); i += C::THREADS) {
+    const int r = i / (DH / 4), d0 = i % (DH / 4) * 4;
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < C::WAVES; ++w) m = __builtin_elementwise_maximum(m, ml[w * 32 + r][0]);
+    float4 sum = make_float4(0, 0, 0, 0);
+#pragma unroll
+    for (int w = 0; w < C::WAVES; ++w) {
+      const f32x2_t p = ml[w * 32 + r];
+      const float4 v = *reinterpret_cast<const float4*>(part + (w * 32 + r) * LD + d0);
+      // a wave without keys, or without a finite score, has the sum 0 (or NaN)
+      const float a = p[0] == -INFINITY ? (p[1] == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(p[0] - m);
+      l += a * p[1];
+      sum.x += a * v.x; sum.y += a * v.y; sum.z += a * v.z; sum.w += a * v.w;
+    }
+    const float inv = 1.0f / l;
+    sum = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
+    if (slot_no < 0) {
+      const RowAt to = row_at<DH>(g, group, b, head, tile * C::QF + r);
+      *reinterpret_cast<uint2*>(g.o + to.at + d0) = make_uint2(fd::pack_bf2(sum.x, sum.y), fd::pack_bf2(sum.z, sum.w));
+    } else {
+      *reinterpret_cast<float4*>(slot + r * DH + d0) = sum;
+      if (d0 == 0) reinterpret_cast<f32x2_t*>(slot + 32 * DH)[r] = f32x2_t{m, l};
+    }
+  }
+  __syncthreads();   // the next piece fills the tiles again
+}
+
+template <int DH>
+__global__ __launch_bounds__(Cfg<DH>::THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) void cache_attn_kernel(fdh::CacheAttnArgs g) {
+  using C = Cfg<DH>;
+  // tiles: two of K and two of V; few rows: one per wave, then the waves' results
+  constexpr int kFewBytes = C::WAVES * 32 * (DH + 4) * 4 + C::WAVES * 32 * 8;
+  constexpr int kTiles = C::WAVES > 4 ? C::WAVES : 4, kBytes = kTiles * C::TILE * 16 > kFewBytes ? kTiles * C::TILE * 16 : kFewBytes;
+  __shared__ __align__(256) uint4 ring[(kBytes + 15) / 16];   // chunk addresses are formed by exclusive or
+  __shared__ SchedTables tabs;
+  const int group = fd::uniform(g.heads / g.kv_heads);
+  const Way way = build_tables<DH>(tabs, g, group);
+  const int tid = threadIdx.x;
+  if (way.empty)   // a request without tokens: its rows are zeros
     for (int b = blockIdx.x; b < g.n_req; b += gridDim.x) {
       if (g.tok_off[b + 1] > g.tok_off[b]) continue;
-      for (long long i = static_cast<long long>(g.cu_q[b]) * ldq / 8 + tid; i < static_cast<long long>(g.cu_q[b + 1]) * ldq / 8; i += C::THREADS)
-        reinterpret_cast<uint4*>(g.o)[i] = make_uint4(0, 0, 0, 0);
+      const long long per = static_cast<long long>(g.heads) * DH / 8, end = per * g.cu_q[b + 1];
+      for (long long i = per * g.cu_q[b] + tid; i < end; i += C::THREADS) reinterpret_cast<uint4*>(g.o)[i] = make_uint4(0, 0, 0, 0);
     }
-  using Sched = fd::AttnSched<C::QB, DH, true, false>;
-  const Sched sch(&tabs, g.cu_q, g.tok_off, g.n_req, g.kv_heads, static_cast<int>(gridDim.x), 0);
+  const bool few = fd::uniform(static_cast<int>(way.few)) != 0;
+  const Sched<DH> sch(&tabs, g, few, static_cast<int>(gridDim.x));
   if (sch.work == 0) return;
   const float scale_log2 = g.scale * 1.4426950408889634f;
-  const uint32_t k_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr_t)&kt[0]));
-  const uint32_t v_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr_t)&vt[0]));
-  // V^T operand, ds_read_b64_tr_b16: in a group of 16 lanes lane j addresses four d of key K0 + j / 4 and gets its own
-  // d for the keys K0 .. K0 + 3
-  const int grp = lane >> 4, jj = lane & 15, tr_key = 4 * lg + (jj >> 2), tr_d = 16 * (grp & 1) + 4 * (jj & 3);
-  const bool tr_live = DH >= 32 || (grp & 1) == 0;
-
+  const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr_t)&ring[0]));
+  const Lane<DH> ln(tid & 63);
+  // waves w and w + WAVES / 2 share a SIMD: the second issues first when both are ready, so that the pair drifts apart
+  if (__builtin_amdgcn_readfirstlane(tid >> 6) >= C::WAVES / 2) __builtin_amdgcn_s_setprio(1);
   const int w = sch.share(static_cast<int>(blockIdx.x));
   long long p = sch.bound(w);
   const long long p_end = sch.bound(w + 1);
   while (p < p_end) {
     long long i_start;
-    int nkv, head, b, first, tau;
-    sch.locate(p, i_start, nkv, head, b, first, tau);
-    const int q0 = g.cu_q[b], rows = (g.cu_q[b + 1] - q0) * group, k_beg = g.tok_off[b], k_end = g.tok_off[b + 1];
-    const int r = (tau - first) * C::QB + 32 * wave + l32;   // this lane's row
-    const bool live = r < rows;
-    const size_t at = static_cast<size_t>(q0 + r / group) * ldq + static_cast<size_t>(head * group + r % group) * DH;
-    bf16x8_t qf[KS];
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      u32x4_t t = {0, 0, 0, 0};
-      if (live) t = *reinterpret_cast<const u32x4_t*>(g.q + at + ks * 16 + lg * 8);
-      qf[ks] = __builtin_bit_cast(bf16x8_t, t);
-    }
-    f32x16_t o[DT] = {};
-    float m_run = -INFINITY, l_run = 0.f;
-    for (int kt0 = 0; kt0 < nkv; ++kt0) {
-      const int key0 = k_beg + kt0 * KB;
-      {   // the tile's codes as bf16 values to LDS; rows past the end repeat the last
-        constexpr int PER_ROW = DH / C::PIECE;
-        const int row = tid / PER_ROW, c0 = tid % PER_ROW * C::PIECE;
-        const size_t tok = min(key0 + row, k_end - 1);
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-          const uint8_t* src = (kv ? g.v : g.k) + tok * ldk + static_cast<size_t>(head) * DH + c0;
-          const float sc = __uint_as_float(static_cast<uint32_t>((kv ? g.v_scale : g.k_scale)[static_cast<size_t>(head) * g.n_tokens + tok]) << 23);
-          uint32_t codes[C::PIECE / 4], vals[C::PIECE / 2];
-          __builtin_memcpy(codes, src, C::PIECE);
-#pragma unroll
-          for (int i = 0; i < C::PIECE / 4; ++i) {
-            vals[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[i], sc, false));
-            vals[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[i], sc, true));
-          }
-          char* dst = reinterpret_cast<char*>(kv ? vt : kt);
-#pragma unroll
-          for (int i = 0; i < C::PIECE; i += 4) {
-            const int c = (c0 + i) / 8;
-            *reinterpret_cast<uint2*>(dst + (row * KCH + (c ^ (kv ? C::fv(row) : C::fk(row)))) * 16 + (c0 + i) % 8 * 2) = make_uint2(vals[i / 2], vals[i / 2 + 1]);
-          }
-        }
-      }
-      __syncthreads();
-      f32x16_t s[2] = {};
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-        for (int kh = 0; kh < 2; ++kh) {
-          const int key = 32 * kh + l32;
-          const bf16x8_t a = __builtin_bit_cast(bf16x8_t, kt[key * KCH + ((2 * ks + lg) ^ C::fk(key))]);
-          s[kh] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[ks], s[kh], 0, 0, 0);
-        }
-      const int lim = k_end - key0 - 4 * lg;
-      float top = -INFINITY;
-#pragma unroll
-      for (int kh = 0; kh < 2; ++kh)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          if (32 * kh + 8 * (e >> 2) + (e & 3) >= lim) s[kh][e] = -INFINITY;
-          top = __builtin_elementwise_maximum(top, s[kh][e]);
-        }
-      top = half_max(top) * scale_log2;
-      const float m_new = top > m_run ? top : m_run, alpha = m_run == m_new ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
-      const float sub = m_new == -INFINITY ? 0.f : m_new;
-      m_run = m_new;
-      l_run *= alpha;
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[d][e] *= alpha;
-      bf16x8_t pk[4];
-#pragma unroll
-      for (int st = 0; st < 4; ++st)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float x = __builtin_amdgcn_exp2f(fmaf(s[st >> 1][8 * (st & 1) + e], scale_log2, -sub));
-          pk[st][e] = static_cast<__bf16>(x);
-          l_run += static_cast<float>(pk[st][e]);   // of the rounded values that the product takes
-        }
-#pragma unroll
-      for (int st = 0; st < 4; ++st)
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          short4_t lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
-          if (tr_live) {
-            const int c = (32 * d + tr_d) >> 3;
-            const uint32_t a_lo = v_base + static_cast<uint32_t>(((16 * st + tr_key) * KCH + (c ^ C::fv(tr_key))) * 16 + (tr_d & 7) * 2);
-            lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)(uintptr_t)a_lo);
-            hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)(uintptr_t)(a_lo + 8 * KCH * 16));
-          }
-          const short lo_hi[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, lo_hi), pk[st], o[d], 0, 0, 0);
-        }
-      __syncthreads();
-    }
-    const float inv = 1.0f / half_sum(l_run);
-    if (live)
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) {
-          const int d0 = 32 * d + 8 * r4 + 4 * lg;
-          if (d0 < DH)
-            *reinterpret_cast<uint2*>(g.o + at + d0) = make_uint2(fd::pack_bf2(o[d][4 * r4] * inv, o[d][4 * r4 + 1] * inv),
-                                                                  fd::pack_bf2(o[d][4 * r4 + 2] * inv, o[d][4 * r4 + 3] * inv));
-        }
-    p += nkv;
+    int n, head, b, first, tau;
+    sch.locate(p, i_start, n, head, b, first, tau);
+    const int s0 = static_cast<int>(p - i_start), s1 = static_cast<int>(min(p_end, i_start + n) - i_start);
+    const int slot = sch.cut ? sch.slot_of(w, s0, s1, n) : -1;
+    if (few) few_piece<DH>(g, group, scale_log2, ln, ring, lds, head, tau - first, b, s0, s1, slot);
+    else tile_piece<DH>(g, group, scale_log2, ln, lds, head, tau - first, b, s0, s1, slot);
+    p = i_start + s1;
   }
-  (void)k_base;
+}
+
+// The pieces of the cut items, joined in key order: workgroup x takes the cut item whose first piece share x holds.
+// Each piece's O is divided by its own sum: its weight is 2^(maximum - the largest) * sum.
+template <int DH>
+__global__ __launch_bounds__(Cfg<DH>::THREADS) void cache_join_kernel(fdh::CacheAttnArgs g) {
+  using C = Cfg<DH>;
+  constexpr int DT = C::DT;
+  __shared__ SchedTables tabs;
+  const int group = fd::uniform(g.heads / g.kv_heads);
+  const bool few = fd::uniform(static_cast<int>(build_tables<DH>(tabs, g, group).few)) != 0;
+  const Sched<DH> sch(&tabs, g, few, static_cast<int>(gridDim.x));
+  if (sch.work == 0 || !sch.cut) return;
+  const int x = sch.share(static_cast<int>(blockIdx.x));
+  const long long p0 = sch.bound(x), p_end = sch.bound(x + 1);
+  if (p_end <= p0) return;
+  long long i_start;
+  int n, head, b, first, tau;
+  sch.locate(p_end - 1, i_start, n, head, b, first, tau);
+  if (i_start < p0 || i_start + n <= p_end) return;   // no item begins here and goes on
+  const int pieces = sch.last_share(x, i_start + n) - x + 1, tile = tau - first;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, lg = lane >> 5;
+  auto weight = [](f32x2_t ml, float top) { return ml[0] == -INFINITY ? (ml[1] == 0.f ? 0.f : ml[1]) : __builtin_amdgcn_exp2f(ml[0] - top) * ml[1]; };
+  if (few) {
+    constexpr int SLOT = 32 * (DH + 2);
+    auto slot = [&](int j) { return g.partial + static_cast<size_t>(sch.slot_at(x, j)) * SLOT; };
+    const int rows = min(C::QF, (g.cu_q[b + 1] - g.cu_q[b]) * group - tile * C::QF);
+    for (int i = tid; i < rows * (DH / 4); i += C::THREADS) {
+      const int r = i / (DH / 4), d0 = i % (DH / 4) * 4;
+      auto ml = [&](int j) { return reinterpret_cast<const f32x2_t*>(slot(j) + 32 * DH)[r]; };
+      float top = -INFINITY, l = 0.f;
+      for (int j = 0; j < pieces; ++j) top = __builtin_elementwise_maximum(top, ml(j)[0]);
+      float4 sum = make_float4(0, 0, 0, 0);
+      for (int j = 0; j < pieces; ++j) {
+        const float a = weight(ml(j), top);
+        const float4 v = *reinterpret_cast<const float4*>(slot(j) + r * DH + d0);
+        l += a;
+        sum.x += a * v.x; sum.y += a * v.y; sum.z += a * v.z; sum.w += a * v.w;
+      }
+      const float inv = 1.0f / l;
+      const RowAt to = row_at<DH>(g, group, b, head, tile * C::QF + r);
+      *reinterpret_cast<uint2*>(g.o + to.at + d0) = make_uint2(fd::pack_bf2(sum.x * inv, sum.y * inv), fd::pack_bf2(sum.z * inv, sum.w * inv));
+    }
+    return;
+  }
+  const RowAt me = row_at<DH>(g, group, b, head, tile * C::QB + 32 * wave + l32);
+  if (!me.live) return;
+  auto slot = [&](int j) { return g.partial + static_cast<size_t>(sch.slot_at(x, j)) * (C::E * C::THREADS); };
+  auto ml = [&](int j) { return reinterpret_cast<const f32x2_t*>(slot(j) + DT * 16 * C::THREADS)[tid]; };
+  float top = -INFINITY, l = 0.f;
+  for (int j = 0; j < pieces; ++j) top = __builtin_elementwise_maximum(top, ml(j)[0]);
+  f32x16_t o[DT] = {};
+  for (int j = 0; j < pieces; ++j) {
+    const float a = weight(ml(j), top);
+    l += a;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const float4 v = reinterpret_cast<const float4*>(slot(j))[(4 * d + r4) * C::THREADS + tid];
+        o[d][4 * r4] += a * v.x; o[d][4 * r4 + 1] += a * v.y; o[d][4 * r4 + 2] += a * v.z; o[d][4 * r4 + 3] += a * v.w;
+      }
+  }
+  store_o<DH>(g.o + me.at, lg, o, 1.0f / l);
 }
 
 }  // namespace
 
 namespace fdh {
 
-size_t cache_attention_scratch_bytes(int, int, int, int) { return 256; }
+namespace {
+int cache_grid() { return (num_cus() + fd::kXcds - 1) / fd::kXcds * fd::kXcds; }
+}  // namespace
 
-hipError_t launch_cache_attention(const CacheAttnArgs& g, hipStream_t s) {
-  const int grid = (num_cus() + fd::kXcds - 1) / fd::kXcds * fd::kXcds;
+size_t cache_attention_scratch_bytes(int n_rows, int heads, int kv_heads, int dh) {
+  // two slots per share: 32 rows where no call of these rows runs in tiles
+  const bool few = fd::cache_always_few(static_cast<long long>(n_rows) * (heads / kv_heads));
+  const size_t floats = few ? 32 * (dh + 2) : static_cast<size_t>(2 * fd::cache_tile_rows(dh)) * ((dh + 31) / 32 * 16 + 2);
+  return 2 * static_cast<size_t>(cache_grid()) * floats * sizeof(float);
+}
+
+hipError_t launch_cache_attention(const CacheAttnArgs& args, hipStream_t s) {
+  CacheAttnArgs g = args;
+  g.may_cut = g.max_req_tokens > (g.dh >= 64 ? Cfg<64>::FEW_KEYS : Cfg<16>::FEW_KEYS);
+  auto run = [&](auto tag) {
+    constexpr int DH = decltype(tag)::value;
+    cache_attn_kernel<DH><<<cache_grid(), Cfg<DH>::THREADS, 0, s>>>(g);
+    if (g.may_cut) cache_join_kernel<DH><<<cache_grid(), Cfg<DH>::THREADS, 0, s>>>(g);
+  };
   switch (g.dh) {
-    case 16: cache_attn_kernel<16><<<grid, Cfg<16>::THREADS, 0, s>>>(g); break;
-    case 64: cache_attn_kernel<64><<<grid, Cfg<64>::THREADS, 0, s>>>(g); break;
-    default: cache_attn_kernel<128><<<grid, Cfg<128>::THREADS, 0, s>>>(g);
+    case 16: run(std::integral_constant<int, 16>{}); break;
+    case 64: run(std::integral_constant<int, 64>{}); break;
+    default: run(std::integral_constant<int, 128>{});
   }
   return hipGetLastError();
 }
