@@ -31,6 +31,7 @@ namespace {
 
 constexpr int KB = fd::kKeyTile;
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
 typedef short short4_t __attribute__((ext_vector_type(4)));
 using fd::bf16x2_t;
 using fd::f32x2_t;
@@ -47,6 +48,8 @@ struct Cfg {
   static constexpr int KS = DH / 16, DT = (DH + 31) / 32;
   static constexpr int PIECE = KB * DH / THREADS;      // codes of a tile that a thread brings: 4, 8 or 16 of a row
   static constexpr int FEW_KEYS = KB * WAVES;          // keys of a step of few rows
+  static constexpr int VHALVES = DH >= 128 ? 2 : 1;    // parts in which V's values of 64 keys pass a wave's LDS
+  static constexpr int FEW_WAVE_BYTES = KB * DH + TILE * 16 / VHALVES;   // K's codes and V's values
   static constexpr int AHEAD = DH >= 128 ? 2 : 3;      // operand reads ahead of their matrix instructions (registers)
   static constexpr int E = DT * 16 + 2;                // floats of a thread in a tile's piece
   static_assert(QB == 32 * WAVES, "a wave per 32 rows");
@@ -489,81 +492,120 @@ FD_DEVICE void few_piece(const fdh::CacheAttnArgs& g, int group, float scale_log
                          int tile, int b, int s0, int s1, int slot_no) {
   using C = Cfg<DH>;
   constexpr int DT = C::DT, KS = C::KS, KCH = C::KCH;
-  constexpr int KL = DH / 2;                               // codes of a key in a lane: its half of the head
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, lg = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = fd::uniform(tid >> 6), l32 = lane & 31, lg = lane >> 5;
   const int k_beg = g.tok_off[b], k_end = g.tok_off[b + 1], ldk = g.kv_heads * DH;
   const RowAt me = row_at<DH>(g, group, b, head, tile * C::QF + l32);
-  // the contraction's order is free: value i of step ks is d = lg * DH / 2 + 8 ks + i, so that a lane's part of a key
-  // is one run of codes
+  // A tile's codes come 16 a lane, whole rows side by side.  K's go to LDS as they are and come back as fragments: the
+  // contraction's order is free, so that a lane's two steps 2 j and 2 j + 1 take its chunk 2 j + lg of the key's row (head dim 16,
+  // of one step: 8 codes of the chunk).  V's go there as values, head dim 128 half the keys at a time.
+  constexpr int PER_ROW = DH / 16, ROWS = 64 / PER_ROW, N = KB / ROWS;   // ROWS rows a load, N loads
+  constexpr int VH = C::VHALVES;
   bf16x8_t qf[KS];
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
     u32x4_t t = {0, 0, 0, 0};
-    if (me.live) t = *reinterpret_cast<const u32x4_t*>(g.q + me.at + lg * KL + 8 * ks);
+    const int d = DH == 16 ? 8 * lg : 16 * (2 * (ks >> 1) + lg) + 8 * (ks & 1);
+    if (me.live) t = *reinterpret_cast<const u32x4_t*>(g.q + me.at + d);
     qf[ks] = __builtin_bit_cast(bf16x8_t, t);
   }
-  constexpr int PER_ROW = DH / 16, VROWS = 64 / PER_ROW, VN = KB / VROWS;   // V: 16 codes a lane, VROWS rows a load
-  const int vrow = lane / PER_ROW, vc = lane % PER_ROW * 16;
-  struct Tile { uint32_t k[2][KL / 4]; u32x4_t v[VN]; uint32_t ks, vs; };
+  // The lane's rows of a load are ROWS apart, which leaves the swizzles: addresses are a base and a constant.
+  const int lrow = lane / PER_ROW, lc = lane % PER_ROW;
+  auto kswz = [](int r) { return PER_ROW == 8 ? (r & 7) : PER_ROW == 4 ? ((r >> 1) & 3) : 0; };
+  const uint32_t k_at = lds + static_cast<uint32_t>(wave * C::FEW_WAVE_BYTES), v_at = k_at + KB * DH;   // this wave's own: no barriers
+  const uint32_t put_k = k_at + static_cast<uint32_t>(lrow * DH + (lc ^ kswz(lrow)) * 16);
+  const uint32_t put_v0 = v_at + static_cast<uint32_t>((lrow * KCH + ((2 * lc) ^ C::fv(lrow))) * 16), put_v1 = put_v0 ^ 16u;
+  uint32_t get_k[(KS + 1) / 2];   // of key l32; key l32 + 32 has the same swizzle
+#pragma unroll
+  for (int j = 0; j < (KS + 1) / 2; ++j)
+    get_k[j] = k_at + static_cast<uint32_t>(l32 * DH + (DH == 16 ? 8 * lg : ((2 * j + lg) ^ kswz(l32)) * 16));
   const uint8_t* ksc = g.k_scale + static_cast<size_t>(head) * g.n_tokens;
   const uint8_t* vsc = g.v_scale + static_cast<size_t>(head) * g.n_tokens;
-  auto fetch = [&](Tile& x, int key0) {   // keys past the end repeat the last one
+  const uint32_t off = static_cast<uint32_t>(lrow) * static_cast<uint32_t>(ldk) + static_cast<uint32_t>(16 * lc);
+  auto fetch = [&](const uint8_t* cache, const uint8_t* scale, int key0, u32x4_t (&x)[N], uint32_t& sc) {   // keys past the end repeat the last one
     const int last = k_end - 1 - key0;
-    const uint8_t* kp = g.k + static_cast<size_t>(key0) * ldk + static_cast<size_t>(head) * DH;
-    const uint8_t* vp = g.v + static_cast<size_t>(key0) * ldk + static_cast<size_t>(head) * DH;
+    const uint8_t* p = cache + static_cast<size_t>(key0) * ldk + static_cast<size_t>(head) * DH;
+    if (last >= KB - 1) {
 #pragma unroll
-    for (int kh = 0; kh < 2; ++kh) {
-      const uint8_t* p = kp + static_cast<uint32_t>(min(32 * kh + l32, last)) * static_cast<uint32_t>(ldk) + lg * KL;
-      __builtin_memcpy(x.k[kh], __builtin_assume_aligned(p, KL < 16 ? KL : 16), KL);
+      for (int i = 0; i < N; ++i) x[i] = *reinterpret_cast<const u32x4_t*>(p + static_cast<size_t>(ROWS * i) * ldk + off);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        x[i] = *reinterpret_cast<const u32x4_t*>(p + static_cast<uint32_t>(min(ROWS * i + lrow, last)) * static_cast<uint32_t>(ldk) + 16 * lc);
     }
-#pragma unroll
-    for (int i = 0; i < VN; ++i)
-      x.v[i] = *reinterpret_cast<const u32x4_t*>(vp + static_cast<uint32_t>(min(VROWS * i + vrow, last)) * static_cast<uint32_t>(ldk) + vc);
-    x.ks = ksc[key0 + min(lane, last)];
-    x.vs = vsc[key0 + min(lane, last)];
+    sc = (scale + key0)[min(lane, last)];
   };
-  const uint32_t vt_at = lds + static_cast<uint32_t>(wave * C::TILE * 16);   // this wave's tile of V
   f32x16_t o[DT] = {};
   float m_run = -INFINITY, l_run = 0.f;
-  Tile x;
-  auto step = [&](int key0, int next) {   // the tile in x, whose place the one from `next` on takes
+  u32x4_t xk[N], xv[N];
+  uint32_t sk, sv;
+  auto own_lds = [] { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
+  auto put_v = [&](int half) {
+#pragma unroll
+    for (int i = half * (N / VH); i < (half + 1) * (N / VH); ++i) {
+      const float sc = scale_of(__shfl(static_cast<int>(sv), ROWS * i + lrow, fd::kWave));
+      const uint2 a = values4(xv[i][0], sc), b2 = values4(xv[i][1], sc), c = values4(xv[i][2], sc), d = values4(xv[i][3], sc);
+      const uint32_t on = static_cast<uint32_t>((i - half * (N / VH)) * ROWS * KCH * 16);
+      *(__attribute__((address_space(3))) u32x4_t*)(uintptr_t)(put_v0 + on) = u32x4_t{a.x, a.y, b2.x, b2.y};
+      *(__attribute__((address_space(3))) u32x4_t*)(uintptr_t)(put_v1 + on) = u32x4_t{c.x, c.y, d.x, d.y};
+    }
+  };
+  auto step = [&](int key0, int next) {   // the tile in xk and xv, whose places the one from `next` on takes
+#pragma unroll
+    for (int i = 0; i < N; ++i) *(__attribute__((address_space(3))) u32x4_t*)(uintptr_t)(put_k + static_cast<uint32_t>(ROWS * i * DH)) = xk[i];
+    float ksl[2];
+#pragma unroll
+    for (int kh = 0; kh < 2; ++kh) ksl[kh] = scale_of(__shfl(static_cast<int>(sk), 32 * kh + l32, fd::kWave));
+    own_lds();
     f32x16_t s[2] = {};
 #pragma unroll
     for (int kh = 0; kh < 2; ++kh) {
-      const float sc = scale_of(__shfl(static_cast<int>(x.ks), 32 * kh + l32, fd::kWave));
+      constexpr int kHalf = 32 * DH;
+      __builtin_amdgcn_sched_barrier(0);   // as many fragments at once as there are registers for
+      if constexpr (DH == 16) {
+        const u32x2_t c = *(__attribute__((address_space(3))) const u32x2_t*)(uintptr_t)(get_k[0] + static_cast<uint32_t>(kh * kHalf));
+        const uint2 lo = values4(c[0], ksl[kh]), hi = values4(c[1], ksl[kh]);
+        s[kh] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, u32x4_t{lo.x, lo.y, hi.x, hi.y}), qf[0], s[kh], 0, 0, 0);
+      } else {
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const uint2 lo = values4(x.k[kh][2 * ks], sc), hi = values4(x.k[kh][2 * ks + 1], sc);
-        s[kh] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, u32x4_t{lo.x, lo.y, hi.x, hi.y}), qf[ks], s[kh], 0, 0, 0);
+        for (int j = 0; j < KS / 2; ++j) {
+          const u32x4_t c = *(__attribute__((address_space(3))) const u32x4_t*)(uintptr_t)(get_k[j] + static_cast<uint32_t>(kh * kHalf));
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint2 lo = values4(c[2 * i], ksl[kh]), hi = values4(c[2 * i + 1], ksl[kh]);
+            s[kh] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, u32x4_t{lo.x, lo.y, hi.x, hi.y}), qf[2 * j + i], s[kh], 0, 0, 0);
+          }
+        }
       }
     }
-#pragma unroll
-    for (int i = 0; i < VN; ++i) {   // V as bf16 values to the wave's tile
-      const int r = VROWS * i + vrow;
-      const float sc = scale_of(__shfl(static_cast<int>(x.vs), r, fd::kWave));
-      const uint2 a = values4(x.v[i][0], sc), b2 = values4(x.v[i][1], sc), c = values4(x.v[i][2], sc), d = values4(x.v[i][3], sc);
-      const uint32_t at = vt_at + static_cast<uint32_t>((r * KCH + ((vc / 8) ^ C::fv(r))) * 16);
-      *(__attribute__((address_space(3))) u32x4_t*)(uintptr_t)at = u32x4_t{a.x, a.y, b2.x, b2.y};
-      *(__attribute__((address_space(3))) u32x4_t*)(uintptr_t)(at ^ 16u) = u32x4_t{c.x, c.y, d.x, d.y};
-    }
+    put_v(0);
     __builtin_amdgcn_sched_barrier(0);
-    fetch(x, next);
-    __builtin_amdgcn_sched_barrier(0);
+    fetch(g.k, ksc, next, xk, sk);   // not before: the fragments need the registers
     const float sub = take_max<DH, true>(s, k_end - key0 - 4 * lg, scale_log2, m_run, l_run, o);
     bf16x8_t pk[4];
     take_p(s, scale_log2, sub, pk, l_run);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the tile is the wave's own: no barrier
 #pragma unroll
-    for (int st = 0; st < 4; ++st)
+    for (int half = 0; half < VH; ++half) {
+      if (half) put_v(half);
+      if (half == VH - 1) {
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(g.v, vsc, next, xv, sv);
+      }
+      own_lds();
 #pragma unroll
-      for (int d = 0; d < DT; ++d)
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, ln.v_frag(vt_at, st, d)), pk[st], o[d], 0, 0, 0);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      for (int st = 0; st < 4 / VH; ++st) {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, ln.v_frag(v_at, st, d)), pk[half * (4 / VH) + st], o[d], 0, 0, 0);
+      }
+      own_lds();
+    }
   };
   const int key_end = min(k_end, k_beg + s1 * C::FEW_KEYS);
   int key0 = k_beg + s0 * C::FEW_KEYS + wave * KB;
   if (key0 < key_end) {
-    fetch(x, key0);
+    fetch(g.k, ksc, key0, xk, sk);
+    fetch(g.v, vsc, key0, xv, sv);
     for (; key0 < key_end; key0 += C::FEW_KEYS) step(key0, min(key0 + C::FEW_KEYS, k_end - 1));   // the last one fetches in vain
   }
   l_run = half_sum(l_run);
@@ -612,12 +654,13 @@ FD_DEVICE void few_piece(const fdh::CacheAttnArgs& g, int group, float scale_log
   __syncthreads();   // the next piece fills the tiles again
 }
 
-template <int DH>
+// FEW_ONLY: no call of this many rows runs in tiles, and the kernel does without their code and registers.
+template <int DH, bool FEW_ONLY>
 __global__ __launch_bounds__(Cfg<DH>::THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) void cache_attn_kernel(fdh::CacheAttnArgs g) {
   using C = Cfg<DH>;
-  // tiles: two of K and two of V; few rows: one per wave, then the waves' results
-  constexpr int kFewBytes = C::WAVES * 32 * (DH + 4) * 4 + C::WAVES * 32 * 8;
-  constexpr int kTiles = C::WAVES > 4 ? C::WAVES : 4, kBytes = kTiles * C::TILE * 16 > kFewBytes ? kTiles * C::TILE * 16 : kFewBytes;
+  // tiles: two of K and two of V; few rows: the waves' own, then their results
+  constexpr int kTileBytes = FEW_ONLY ? 0 : 4 * C::TILE * 16, kFewBytes = C::WAVES * C::FEW_WAVE_BYTES, kJoinBytes = C::WAVES * 32 * ((DH + 4) * 4 + 8);
+  constexpr int kMore = kFewBytes > kJoinBytes ? kFewBytes : kJoinBytes, kBytes = kMore > kTileBytes ? kMore : kTileBytes;
   __shared__ __align__(256) uint4 ring[(kBytes + 15) / 16];   // chunk addresses are formed by exclusive or
   __shared__ SchedTables tabs;
   const int group = fd::uniform(g.heads / g.kv_heads);
@@ -646,8 +689,8 @@ __global__ __launch_bounds__(Cfg<DH>::THREADS) __attribute__((amdgpu_waves_per_e
     sch.locate(p, i_start, n, head, b, first, tau);
     const int s0 = static_cast<int>(p - i_start), s1 = static_cast<int>(min(p_end, i_start + n) - i_start);
     const int slot = sch.cut ? sch.slot_of(w, s0, s1, n) : -1;
-    if (few) few_piece<DH>(g, group, scale_log2, ln, ring, lds, head, tau - first, b, s0, s1, slot);
-    else tile_piece<DH>(g, group, scale_log2, ln, lds, head, tau - first, b, s0, s1, slot);
+    if (FEW_ONLY || few) few_piece<DH>(g, group, scale_log2, ln, ring, lds, head, tau - first, b, s0, s1, slot);
+    else if constexpr (!FEW_ONLY) tile_piece<DH>(g, group, scale_log2, ln, lds, head, tau - first, b, s0, s1, slot);
     p = i_start + s1;
   }
 }
@@ -679,15 +722,33 @@ __global__ __launch_bounds__(Cfg<DH>::THREADS) void cache_join_kernel(fdh::Cache
     const int rows = min(C::QF, (g.cu_q[b + 1] - g.cu_q[b]) * group - tile * C::QF);
     for (int i = tid; i < rows * (DH / 4); i += C::THREADS) {
       const int r = i / (DH / 4), d0 = i % (DH / 4) * 4;
-      auto ml = [&](int j) { return reinterpret_cast<const f32x2_t*>(slot(j) + 32 * DH)[r]; };
+      // 24 pieces at a time, their loads in flight together; what came before is rescaled to the new maximum
+      constexpr int AT_ONCE = 24;
       float top = -INFINITY, l = 0.f;
-      for (int j = 0; j < pieces; ++j) top = __builtin_elementwise_maximum(top, ml(j)[0]);
       float4 sum = make_float4(0, 0, 0, 0);
-      for (int j = 0; j < pieces; ++j) {
-        const float a = weight(ml(j), top);
-        const float4 v = *reinterpret_cast<const float4*>(slot(j) + r * DH + d0);
-        l += a;
-        sum.x += a * v.x; sum.y += a * v.y; sum.z += a * v.z; sum.w += a * v.w;
+      for (int j0 = 0; j0 < pieces; j0 += AT_ONCE) {
+        f32x2_t ml[AT_ONCE];
+        float4 v[AT_ONCE];
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+          const float* from = slot(min(j0 + j, pieces - 1));
+          ml[j] = reinterpret_cast<const f32x2_t*>(from + 32 * DH)[r];
+          v[j] = *reinterpret_cast<const float4*>(from + r * DH + d0);
+        }
+        float next = top;
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) next = __builtin_elementwise_maximum(next, ml[j][0]);
+        const float back = top == -INFINITY ? (l == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(top - next);
+        l *= back;
+        sum.x *= back; sum.y *= back; sum.z *= back; sum.w *= back;
+        top = next;
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+          const float a = weight(ml[j], top);
+          if (j0 + j >= pieces) continue;
+          l += a;
+          sum.x += a * v[j].x; sum.y += a * v[j].y; sum.z += a * v[j].z; sum.w += a * v[j].w;
+        }
       }
       const float inv = 1.0f / l;
       const RowAt to = row_at<DH>(g, group, b, head, tile * C::QF + r);
@@ -736,7 +797,8 @@ hipError_t launch_cache_attention(const CacheAttnArgs& args, hipStream_t s) {
   g.may_cut = g.max_req_tokens > (g.dh >= 64 ? Cfg<64>::FEW_KEYS : Cfg<16>::FEW_KEYS);
   auto run = [&](auto tag) {
     constexpr int DH = decltype(tag)::value;
-    cache_attn_kernel<DH><<<cache_grid(), Cfg<DH>::THREADS, 0, s>>>(g);
+    if (fd::cache_always_few(static_cast<long long>(g.n_rows) * (g.heads / g.kv_heads))) cache_attn_kernel<DH, true><<<cache_grid(), Cfg<DH>::THREADS, 0, s>>>(g);
+    else cache_attn_kernel<DH, false><<<cache_grid(), Cfg<DH>::THREADS, 0, s>>>(g);
     if (g.may_cut) cache_join_kernel<DH><<<cache_grid(), Cfg<DH>::THREADS, 0, s>>>(g);
   };
   switch (g.dh) {
