@@ -1,70 +1,404 @@
 // The product of 8-bit integers with a scale per row and per column:
 //   Y[M][N] = act(float(sum_k A[i][k] W[j][k]) * (a_scale[i] * w_scale[j]) + bias[j])
-// on v_mfma_i32_32x32x32_i8: the sums are whole numbers below 2^31 (K <= 2^16) and exact.
+// on v_mfma_i32_16x16x64_i8 and 32x32x32: the sums are whole numbers of at most 2^30 (K <= 2^16) and exact.
 #include <type_traits>
 
 #include "fd_int.h"
+#include "fd_scaled_rules.h"
+#include "fd_tile_loads.h"
 
 namespace {
 
-typedef int i32x4_t __attribute__((ext_vector_type(4)));
 typedef int i32x16_t __attribute__((ext_vector_type(16)));
+constexpr int kBlock = 128;   // bytes of K in a step
 
-constexpr int BM = 128, BN = 128, BK = 128, kPitch = BK + 16;   // bytes of a tile row in LDS
+FD_DEVICE i32x4_t half_of(const i32x8_t& x, int c) { return c ? i32x4_t{x[4], x[5], x[6], x[7]} : i32x4_t{x[0], x[1], x[2], x[3]}; }
+// The lanes' 32 bytes of both operands are the same ones of K, which is all that a sum asks of their order.
+FD_DEVICE i32x4_t mma(const i32x8_t& w, const i32x8_t& a, i32x4_t c) {
+  c = __builtin_amdgcn_mfma_i32_16x16x64_i8(half_of(w, 0), half_of(a, 0), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_i32_16x16x64_i8(half_of(w, 1), half_of(a, 1), c, 0, 0, 0);
+}
+FD_DEVICE i32x16_t mma(const i32x8_t& a, const i32x8_t& w, i32x16_t c) {
+  c = __builtin_amdgcn_mfma_i32_32x32x32_i8(half_of(a, 0), half_of(w, 0), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_i32_32x32x32_i8(half_of(a, 1), half_of(w, 1), c, 0, 0, 0);
+}
 
-template <bool WIDE>   // fp32 results, else bf16
-__global__ __launch_bounds__(256) void int_tile_kernel(fdh::IntLinearArgs g) {
-  __shared__ __align__(16) uint8_t ta[BM * kPitch], tw[BN * kPitch];
-  const int M = g.m ? min(*g.m, g.n_rows) : g.n_rows, K = g.K, N = g.N;
-  const int m0 = blockIdx.y * BM, n0 = blockIdx.x * BN;
+// ---------------------------------------------------------------- few rows
+
+// As the few-row kernel of the block-scaled product: what counts is how many of the weights' bytes are on the way.  A
+// workgroup takes the rows' FM fragments and 16 NF columns, its waves the K-blocks in turn, operands straight from memory
+// into registers, DEEP blocks at a time; the waves' sums meet in LDS.  The first operand is the weights, so that a lane
+// holds a row (l & 15) and, of its NF fragments, 4 NF consecutive columns.
+constexpr int kFewWaves = 8;
+
+template <bool WIDE, int FM, int NF, int DEEP>
+__global__ __launch_bounds__(kFewWaves * 64) void int_few_kernel(fdh::IntLinearArgs g) {
+  __shared__ i32x4_t part[kFewWaves][FM][NF][64];
+  const int M = g.m ? min(*g.m, g.n_rows) : g.n_rows;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, lg = lane >> 4;
+  const int K = g.K, nk = (K + kBlock - 1) / kBlock;
+  const int n0 = blockIdx.x * 16 * NF, m0 = blockIdx.y * 16 * FM;
   if (m0 >= M) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, half = lane >> 5;
-  i32x16_t acc[4] = {};
-  for (int k0 = 0; k0 < K; k0 += BK) {
-    for (int i = threadIdx.x; i < BM * BK / 16; i += 256) {
-      const int r = i / (BK / 16), c = i % (BK / 16) * 16, k = k0 + c;
-      const uint4 none = make_uint4(0, 0, 0, 0);
-      *reinterpret_cast<uint4*>(ta + r * kPitch + c) = m0 + r < M && k < K ? *reinterpret_cast<const uint4*>(g.a + static_cast<size_t>(m0 + r) * K + k) : none;
-      *reinterpret_cast<uint4*>(tw + r * kPitch + c) = n0 + r < N && k < K ? *reinterpret_cast<const uint4*>(g.w + static_cast<size_t>(n0 + r) * K + k) : none;
-    }
-    __syncthreads();
+  const uint8_t* w[NF];
 #pragma unroll
-    for (int ks = 0; ks < BK / 32; ++ks) {
-      const i32x4_t a = *reinterpret_cast<const i32x4_t*>(ta + (32 * wave + l32) * kPitch + 32 * ks + 16 * half);
+  for (int j = 0; j < NF; ++j)
+    w[j] = reinterpret_cast<const uint8_t*>(g.w) + static_cast<size_t>(min(n0 + 4 * NF * (l16 >> 2) + 4 * j + (l16 & 3), g.N - 1)) * K;
+  i32x4_t acc[FM][NF] = {};
+  for (int kb = wave; kb < nk; kb += kFewWaves * DEEP) {
+    Piece wf[DEEP][NF], af[DEEP][FM];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const i32x4_t w = *reinterpret_cast<const i32x4_t*>(tw + (32 * j + l32) * kPitch + 32 * ks + 16 * half);
-        acc[j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a, w, acc[j], 0, 0, 0);
+    for (int d = 0; d < DEEP; ++d) {
+      const int b = kb + d * kFewWaves, k = b * kBlock + 32 * lg;
+      if (b >= nk) break;
+#pragma unroll
+      for (int j = 0; j < NF; ++j) wf[d][j] = load32(w[j], k, K);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const size_t row = min(m0 + 16 * i + l16, M - 1);
+        af[d][i] = load32(reinterpret_cast<const uint8_t*>(g.a) + row * K, k, K);
       }
     }
-    __syncthreads();
-  }
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int col = n0 + 32 * j + l32;
-    if (col >= N) continue;
-    const float sw = g.w_scale[col], bias = g.bias ? g.bias[col] : 0.f;
+    for (int d = 0; d < DEEP; ++d) {
+      const int b = kb + d * kFewWaves, k = b * kBlock + 32 * lg;
+      if (b >= nk) break;
+      i32x8_t wd[NF];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int row = m0 + 32 * wave + 8 * (r >> 2) + 4 * half + (r & 3);
-      if (row >= M) continue;
-      float v = static_cast<float>(acc[j][r]) * (g.a_scale[row] * sw) + bias;
-      if (g.gelu) v = fd::gelu(v);
-      const size_t at = static_cast<size_t>(row) * N + col;
-      if constexpr (WIDE) g.y_f32[at] = v;
-      else g.y_bf16[at] = fd::f2bf(v);
+      for (int j = 0; j < NF; ++j) wd[j] = inside(wf[d][j], k, K);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const i32x8_t ad = inside(af[d][i], k, K);
+#pragma unroll
+        for (int j = 0; j < NF; ++j) acc[i][j] = mma(wd[j], ad, acc[i][j]);
+      }
     }
   }
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < NF; ++j) part[wave][i][j][lane] = acc[i][j];
+  __syncthreads();
+  if (wave >= FM) return;
+  // a wave per 16 rows adds the waves' sums
+  const int row = m0 + 16 * wave + l16, col = n0 + 4 * NF * lg;
+  const float sa = g.a_scale[min(row, M - 1)];
+#pragma unroll
+  for (int j = 0; j < NF; ++j) {
+    i32x4_t sum = part[0][wave][j][lane];
+#pragma unroll
+    for (int p = 1; p < kFewWaves; ++p) sum += part[p][wave][j][lane];
+    const int c = min(col + 4 * j, g.N - 4);
+    const float4 sw = *reinterpret_cast<const float4*>(g.w_scale + c), bias = g.bias ? *reinterpret_cast<const float4*>(g.bias + c) : make_float4(0, 0, 0, 0);
+    float v[4] = {static_cast<float>(sum[0]) * (sa * sw.x) + bias.x, static_cast<float>(sum[1]) * (sa * sw.y) + bias.y,
+                  static_cast<float>(sum[2]) * (sa * sw.z) + bias.z, static_cast<float>(sum[3]) * (sa * sw.w) + bias.w};
+    if (g.gelu) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = fd::gelu(v[e]);
+    }
+    if (row >= M || col + 4 * j >= g.N) continue;
+    const size_t at = static_cast<size_t>(row) * g.N + col + 4 * j;
+    if constexpr (WIDE) *reinterpret_cast<float4*>(g.y_f32 + at) = make_float4(v[0], v[1], v[2], v[3]);
+    else *reinterpret_cast<uint2*>(g.y_bf16 + at) = make_uint2(fd::pack_bf2(v[0], v[1]), fd::pack_bf2(v[2], v[3]));
+  }
+}
+
+// ---------------------------------------------------------------- tiles
+
+// A workgroup of WM x WN waves with a tile of 32 FI WM rows x 32 NJ WN columns, K-steps of one block; a wave owns FI x NJ
+// blocks of 32 x 32.  In LDS a tile row is eight 16-byte chunks, chunk c of row r at c ^ swz(r), so that the 16 lanes
+// that read a fragment together meet 16 different 16-byte bank groups.  A tile's scales and bias come with its first stage.
+template <int FI_, int NJ_, int WM_, int WN_, int STAGES_>
+struct IntTile {
+  static constexpr int FI = FI_, NJ = NJ_, WM = WM_, WN = WN_, STAGES = STAGES_;
+  static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
+  static constexpr int BM = 32 * FI * WM, BN = 32 * NJ * WN;
+  static constexpr int LOADS_A = BM / 8 / WAVES, LOADS_W = BN / 8 / WAVES;        // 8 rows of 128 bytes per wave-load
+  static constexpr int ISSUED = LOADS_A + LOADS_W;
+  static constexpr int CHUNKS = (BM + BN) * 8;                                    // of a stage
+  static constexpr int SIDE = STAGES * CHUNKS;                                    // four slots of column scales, bias and row scales
+  static constexpr int SIDE_FLOATS = 2 * BN + BM;
+  static constexpr int TOTAL = SIDE + 4 * SIDE_FLOATS / 4;
+  static_assert(NJ == 4 || NJ == 2, "a step's parts");
+  static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && BN % 64 == 0 && BM % 64 == 0 && BN <= 64 * WAVES && BM <= 64 * WAVES, "whole wave-loads");
+  static FD_DEVICE int swz(int r) { return (r >> 1) & 7; }
+  // Column of LDS row p: fragment j of a wave's columns holds every NJ-th, from j on, so that a lane has NJ consecutive
+  // columns in its NJ fragments.
+  static FD_DEVICE int column(int p) { return (p & ~(32 * NJ - 1)) + NJ * (p & 31) + ((p >> 5) & (NJ - 1)); }
+};
+
+// The K-steps of all of a workgroup's tiles are one sequence: the loads run STAGES steps ahead of the products, into the
+// next tile too, and a tile's results leave while the next one's first stages land.  A step's 2 NJ sub-steps (half of K,
+// column fragment) read their weight fragment two sub-steps ahead; after the barrier behind sub-step 1 the stage's rows
+// may be loaded over, after the one before the last two its columns, and the next stage is there (waves of two
+// fragments: the one barrier frees all of it).  A step is one basic block, its loads go out behind products.
+template <class T, bool WIDE>
+FD_DEVICE void int_tiles(const fdh::IntLinearArgs& g, int M, uint4* ring) {
+  constexpr int FI = T::FI, NJ = T::NJ, STAGES = T::STAGES, kSubs = 2 * NJ, kSize = WIDE ? 4 : 2;
+  constexpr int kStores = FI * 16;
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / T::WN, wn = wave % T::WN;
+  const int K = g.K, blocks = (K + kBlock - 1) / kBlock, nk = max(blocks, STAGES);
+  const int tiles_m = (M + T::BM - 1) / T::BM, tiles_n = (g.N + T::BN - 1) / T::BN, tiles = tiles_m * tiles_n;
+  const int per_xcd = (tiles + 7) / 8;
+  const uint32_t ring_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr_t)ring));
+
+  // Tile of turn u of this workgroup: consecutive tiles on one XCD, in groups of 8 row tiles x every column tile, row tile
+  // fastest, so that the tiles an XCD runs at once share operand rows in its L2.
+  auto tile_at = [&](int u, int& m0, int& n0) -> bool {
+    const int tile = (u % 8) * per_xcd + u / 8;
+    if (u >= per_xcd * 8 || tile >= tiles) return false;
+    const int grp = tile / (8 * tiles_n), in = tile - grp * 8 * tiles_n, gm = min(8, tiles_m - 8 * grp);
+    m0 = (8 * grp + in % gm) * T::BM;
+    n0 = in / gm * T::BN;
+    return true;
+  };
+
+  // ---- the loads: of K-block lk of the tile at (lm0, ln0)
+  int u = blockIdx.x, lk = 0, lm0, ln0;
+  if (!tile_at(u, lm0, ln0)) return;
+  i32x4_t ra, rw;
+  int turn = 3;
+  uint32_t off_a[T::LOADS_A], off_w[T::LOADS_W];
+  auto row_of = [&](int q) { return (wave + T::WAVES * q) * 8 + (lane >> 3); };
+  const int chunk = (lane & 7) ^ T::swz(row_of(0));   // of every load's row: 8 WAVES q leaves the swizzle
+  auto side_at = [&](int slot) { return static_cast<uint32_t>(T::SIDE * 16 + slot * T::SIDE_FLOATS * 4); };
+  auto aim = [&] {   // the tile's bases, and this lane's row and chunk of each load (rows past the end re-read the last)
+    ra = buffer_of(g.a + static_cast<size_t>(lm0) * K);
+    rw = buffer_of(g.w + static_cast<size_t>(ln0) * K);
+#pragma unroll
+    for (int q = 0; q < T::LOADS_A; ++q) off_a[q] = static_cast<uint32_t>(min(row_of(q), M - lm0 - 1)) * static_cast<uint32_t>(K) + 16 * chunk;
+#pragma unroll
+    for (int q = 0; q < T::LOADS_W; ++q) off_w[q] = static_cast<uint32_t>(min(T::column(row_of(q)), g.N - ln0 - 1)) * static_cast<uint32_t>(K) + 16 * chunk;
+    // the columns' scales and bias (zeros without one) and the rows' scales, ahead of the tile's first stage.  The tile before this
+    // one has yet to read its own, and with STAGES blocks no barrier has passed since the one before that did: four slots.
+    turn = (turn + 1) & 3;
+    const int c = 64 * (wave % (T::BN / 64)), r = 64 * (wave % (T::BM / 64));
+    const uint32_t to = ring_at + side_at(turn);
+    dma4(to + static_cast<uint32_t>(c * 4), static_cast<uint32_t>(ln0 + c + lane) * 4, buffer_of(g.w_scale, 4u * g.N), 0);
+    dma4(to + static_cast<uint32_t>((T::BN + c) * 4), static_cast<uint32_t>(ln0 + c + lane) * 4, buffer_of(g.bias, g.bias ? 4u * g.N : 0u), 0);
+    dma4(to + static_cast<uint32_t>((2 * T::BN + r) * 4), static_cast<uint32_t>(r + lane) * 4, buffer_of(g.a_scale + lm0, 4u * min(T::BM, M - lm0)), 0);
+  };
+  // The chunks past K of a last, shorter K-block read zeros, and all of those that fill a short sum up to STAGES
+  // blocks: called before such a block's loads.  The next tile's aim sets the offsets anew.
+  auto last_block = [&] {
+    const bool in = lk * kBlock + 16 * chunk < K;
+#pragma unroll
+    for (int q = 0; q < T::LOADS_A; ++q) off_a[q] = in ? off_a[q] : kNowhere;
+#pragma unroll
+    for (int q = 0; q < T::LOADS_W; ++q) off_w[q] = in ? off_w[q] : kNowhere;
+  };
+  // Loads `from` to `to` of the rows (q < LOADS_A) and of the columns (the rest) into a slot.
+  constexpr int kSlot = T::CHUNKS * 16;
+  const uint32_t wave_at = ring_at + wave * 1024;
+  auto issue = [&](uint32_t slot_at, auto from, auto to) {
+    constexpr int FROM = decltype(from)::value, TO = decltype(to)::value;
+    auto go = [&](auto self, auto i) {
+      constexpr int q = decltype(i)::value;
+      if constexpr (q < TO) {
+        // tile rows are 128 bytes, the columns' follow the rows', and WAVES loads of 1024 bytes lie between q and q + 1
+        if constexpr (q < T::LOADS_A) dma16<T::WAVES * q * 1024>(wave_at + slot_at, off_a[q], ra, static_cast<uint32_t>(lk * kBlock));
+        else dma16<T::WAVES * q * 1024>(wave_at + slot_at, off_w[q - T::LOADS_A], rw, static_cast<uint32_t>(lk * kBlock));
+        self(self, std::integral_constant<int, q + 1>{});
+      }
+    };
+    go(go, std::integral_constant<int, FROM>{});
+  };
+
+  // ---- the products
+  const int arow = 32 * FI * wm + l32;
+  const int wrow = 32 * NJ * wn + l32;
+  // byte offsets in a stage of this lane's two chunks of a half K-block, of its first row and its first column (32 rows on: 4096 bytes)
+  uint32_t at_a[2][2], at_w[2][2];
+#pragma unroll
+  for (int kh = 0; kh < 2; ++kh)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      at_a[kh][c] = arow * 128 + ((4 * kh + 2 * half + c) ^ T::swz(arow)) * 16;
+      at_w[kh][c] = (T::BM + wrow) * 128 + ((4 * kh + 2 * half + c) ^ T::swz(wrow)) * 16;
+    }
+  const char* lds = reinterpret_cast<const char*>(ring);
+  auto read = [&](const char* lo_at, const char* hi_at) {
+    const uint4 lo = *reinterpret_cast<const uint4*>(lo_at), hi = *reinterpret_cast<const uint4*>(hi_at);
+    return i32x8_t{static_cast<int>(lo.x), static_cast<int>(lo.y), static_cast<int>(lo.z), static_cast<int>(lo.w),
+                   static_cast<int>(hi.x), static_cast<int>(hi.y), static_cast<int>(hi.z), static_cast<int>(hi.w)};
+  };
+  i32x8_t a[2][FI], w[4];
+  auto read_a = [&](uint32_t slot_at, int kh) {
+#pragma unroll
+    for (int i = 0; i < FI; ++i) a[kh][i] = read(lds + (slot_at + at_a[kh][0]) + 4096 * i, lds + (slot_at + at_a[kh][1]) + 4096 * i);
+  };
+  auto read_w = [&](uint32_t slot_at, int s) {
+    const int kh = s / NJ, j = s % NJ;
+    w[s & 3] = read(lds + (slot_at + at_w[kh][0]) + 4096 * j, lds + (slot_at + at_w[kh][1]) + 4096 * j);
+  };
+
+  aim();
+#pragma unroll
+  for (int p = 0; p < STAGES; ++p) {
+    if (lk >= blocks - 1) last_block();
+    issue(p * kSlot, std::integral_constant<int, 0>{}, std::integral_constant<int, T::LOADS_A + T::LOADS_W>{});
+    ++lk;
+  }
+  wait_barrier<(STAGES - 1) * T::ISSUED, 0>(0);
+  read_a(0, 0);
+  read_w(0, 0);
+  read_w(0, 1);
+
+  uint32_t slot = 0;   // byte offset of the step's stage
+  int stored = 0;   // in a tile's first step: the previous tile's stores were issued after the last stage's loads
+  for (;;) {
+    const int m0 = lm0, n0 = ln0;
+    i32x16_t acc[FI][NJ] = {};
+    bool more = false;
+    int kb = 0;
+    // the steps that load this tile, then the last STAGES, which load the next one (or this one's end again)
+    for (int part = 0; part < 2; ++part) {
+      if (part == 1) {
+        more = tile_at(u + gridDim.x, lm0, ln0);
+        lk = more ? 0 : nk - STAGES;
+        if (more) aim();
+      }
+      for (const int end = part == 0 ? nk - STAGES : nk; kb < end; ++kb, ++lk) {
+        if (lk >= blocks - 1) last_block();
+        const uint32_t next = slot == (STAGES - 1) * kSlot ? 0 : slot + kSlot;
+#pragma unroll
+        for (int s = 0; s < kSubs; ++s) {
+          if (NJ == 4 && s == 2) wait_reads_barrier();
+          if (s == kSubs - 2) wait_barrier<(STAGES - 2) * T::ISSUED + (NJ == 4 ? T::LOADS_A : 0), kStores>(stored);
+          if (s == 0) read_a(slot, 1);
+          if (s < kSubs - 2) read_w(slot, s + 2);
+          if (s == kSubs - 2) {
+            read_a(next, 0);
+            read_w(next, 0);
+          }
+          if (s == kSubs - 1) read_w(next, 1);
+#pragma unroll
+          for (int i = 0; i < FI; ++i) acc[i][s % NJ] = mma(a[s / NJ][i], w[s & 3], acc[i][s % NJ]);
+          __builtin_amdgcn_sched_barrier(0);
+          if (s == 2) issue(slot, std::integral_constant<int, 0>{}, std::integral_constant<int, T::LOADS_A / 2>{});
+          if (s == (NJ == 4 ? 4 : 2)) issue(slot, std::integral_constant<int, T::LOADS_A / 2>{}, std::integral_constant<int, T::LOADS_A>{});
+          if (s == kSubs - 2) issue(slot, std::integral_constant<int, T::LOADS_A>{}, std::integral_constant<int, T::LOADS_A + T::LOADS_W / 2>{});
+          if (s == kSubs - 1) issue(slot, std::integral_constant<int, T::LOADS_A + T::LOADS_W / 2>{}, std::integral_constant<int, T::LOADS_A + T::LOADS_W>{});
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        slot = next;
+        stored = 0;
+      }
+    }
+
+    stored = 1;
+    const int col = 32 * NJ * wn + NJ * l32;   // this lane's first column of the tile
+    const bool col_ok = n0 + col < g.N;
+    const float* side = reinterpret_cast<const float*>(lds + side_at(turn - (more ? 1 : 0) & 3));
+    float sw[NJ], bias[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      sw[j] = side[col + j];
+      bias[j] = side[T::BN + col + j];
+    }
+    const int row0 = 32 * FI * wm;
+    uint8_t* base = WIDE ? reinterpret_cast<uint8_t*>(g.y_f32) : reinterpret_cast<uint8_t*>(g.y_bf16);
+    const auto y = __builtin_amdgcn_make_buffer_rsrc(base + (static_cast<size_t>(m0 + row0) * g.N + n0) * kSize, 0, 0x7fffffff, 0x00020000);
+    const bool block_ok = n0 + 32 * NJ * wn < g.N;   // else no column of this wave
+    const uint32_t pitch = static_cast<uint32_t>(g.N) * kSize;
+#pragma unroll
+    for (int i = 0; i < FI; ++i) {
+      // acc[i][j][r] is row 8 (r >> 2) + 4 half + (r & 3) of 32: 32 lanes store a row's columns side by side.  Every store
+      // issues, rows and columns outside go nowhere: the waits count the stores.
+      const int rows = block_ok ? M - m0 - row0 - 32 * i - 4 * half : 0;
+      const uint32_t off = (static_cast<uint32_t>(32 * i + 4 * half) * g.N + col) * kSize;
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const float4 sa4 = *reinterpret_cast<const float4*>(side + 2 * T::BN + row0 + 32 * i + 8 * r4 + 4 * half);
+        const float sa[4] = {sa4.x, sa4.y, sa4.z, sa4.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int row = 8 * r4 + e;
+          float v[NJ];
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) {
+            v[j] = static_cast<float>(acc[i][j][4 * r4 + e]) * (sa[e] * sw[j]) + bias[j];
+            if (g.gelu) v[j] = fd::gelu(v[j]);
+          }
+          const uint32_t to = col_ok && row < rows ? off : kNowhere;
+          typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+          typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+          if constexpr (!WIDE && NJ == 2)
+            __builtin_amdgcn_raw_buffer_store_b32(fd::pack_bf2(v[0], v[1]), y, to, row * pitch, kStream);
+          else if constexpr (NJ == 2)
+            __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(v[0]), __float_as_uint(v[1])}, y, to, row * pitch, kStream);
+          else if constexpr (!WIDE)
+            __builtin_amdgcn_raw_buffer_store_b64(u32x2{fd::pack_bf2(v[0], v[1]), fd::pack_bf2(v[2], v[3])}, y, to, row * pitch, kStream);
+          else
+            __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}, y, to, row * pitch, kStream);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);   // 32 rows at a time: fewer registers
+    }
+    if (!more) break;
+    u += gridDim.x;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the repeats of the last stage
+}
+
+using Tile64 = IntTile<1, 2, 2, 2, 3>;      // 64 x 128, two workgroups per CU
+using Tile128 = IntTile<1, 4, 4, 1, 2>;     // 128 x 128, two
+using TileLarge = IntTile<2, 4, 4, 2, 2>;   // 256 x 256, one
+
+// Where both kernels are launched (cus > 0), the one that the row count does not call for ends at once.
+template <bool WIDE, class T, int PER_CU>
+__global__ __launch_bounds__(T::THREADS, (PER_CU * T::WAVES + 3) / 4) void int_tile_kernel(fdh::IntLinearArgs g, int cus) {
+  __shared__ uint4 ring[T::TOTAL];
+  static_assert(T::TOTAL * 16 * PER_CU <= 160 * 1024, "the LDS of a CU");
+  const int M = g.m ? min(*g.m, g.n_rows) : g.n_rows;
+  if (M <= 0 || (cus > 0 && fd::scaled_large(M, g.N, g.K, false, cus) != (T::BM == TileLarge::BM))) return;
+  int_tiles<T, WIDE>(g, M, ring);
 }
 
 }  // namespace
 
 namespace fdh {
 
+// The block-scaled product's rules: the loads, the tiles and the rate of the matrix instructions are the same.
 hipError_t launch_int_linear(const IntLinearArgs& g, hipStream_t s) {
-  const dim3 grid((g.N + BN - 1) / BN, (g.n_rows + BM - 1) / BM);
-  if (g.y_f32) int_tile_kernel<true><<<grid, 256, 0, s>>>(g);
-  else int_tile_kernel<false><<<grid, 256, 0, s>>>(g);
+  auto run = [&](auto wide) {
+    constexpr bool WIDE = decltype(wide)::value;
+    using std::integral_constant;
+    if (fd::scaled_few(g.n_rows, g.N, g.K, false, false, num_cus())) {
+      auto few = [&](auto fm, auto nf, auto deep) {
+        constexpr int FM = decltype(fm)::value, NF = decltype(nf)::value;
+        int_few_kernel<WIDE, FM, NF, decltype(deep)::value><<<dim3((g.N + 16 * NF - 1) / (16 * NF), (g.n_rows + 16 * FM - 1) / (16 * FM)), kFewWaves * 64, 0, s>>>(g);
+      };
+      const integral_constant<int, 1> one{};
+      const integral_constant<int, 2> two{};
+      const integral_constant<int, 3> three{};
+      const integral_constant<int, 4> four{};
+      const int frags = fd::scaled_few_frags(g.n_rows);
+      if (fd::scaled_few_wide(g.N, num_cus())) {
+        if (frags == 1) few(one, two, two);
+        else if (frags == 2) few(two, two, two);
+        else few(four, two, one);
+      } else {
+        if (frags == 1) few(one, one, three);
+        else if (frags == 2) few(two, one, two);
+        else few(four, one, one);
+      }
+      return;
+    }
+    const int cus = num_cus() / 8 * 8;   // the tile order counts on whole rounds of the 8 XCDs
+    const bool both = g.m && fd::scaled_both(g.n_rows, g.N, g.K, false, cus), large = !g.m && fd::scaled_large(g.n_rows, g.N, g.K, false, cus);
+    auto tiles = [&](auto tile, auto per_cu, int check) {
+      using T = decltype(tile);
+      constexpr int PER_CU = decltype(per_cu)::value;
+      const long long all = static_cast<long long>((g.n_rows + T::BM - 1) / T::BM) * ((g.N + T::BN - 1) / T::BN), most = PER_CU * cus;
+      int_tile_kernel<WIDE, T, PER_CU><<<static_cast<int>(all < most ? (all + 7) / 8 * 8 : most), T::THREADS, 0, s>>>(g, check);
+    };
+    if (fd::scaled_small(g.n_rows, g.N, cus)) return tiles(Tile64{}, integral_constant<int, 2>{}, 0);
+    if (both || !large) tiles(Tile128{}, integral_constant<int, 2>{}, both ? cus : 0);
+    if (both || large) tiles(TileLarge{}, integral_constant<int, 1>{}, both ? cus : 0);
+  };
+  if (g.y_f32) run(std::true_type{});
+  else run(std::false_type{});
   return hipGetLastError();
 }
 

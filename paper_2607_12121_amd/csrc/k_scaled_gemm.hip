@@ -6,13 +6,12 @@
 
 #include "fd_scaled.h"
 #include "fd_scaled_rules.h"
+#include "fd_tile_loads.h"
 
 namespace {
 
 using fd::bf16x2_t;
 using fd::kScaleBlock;
-typedef int i32x8_t __attribute__((ext_vector_type(8)));
-typedef int i32x4_t __attribute__((ext_vector_type(4)));
 
 enum { kToBf16, kToF32, kToCodes };
 
@@ -96,17 +95,6 @@ FD_DEVICE void store_row(const fdh::ScaledArgs& g, bool row_ok, int row, int col
       if (row_ok && col + (4 * i & 16) < g.N) *reinterpret_cast<float4*>(g.y_f32 + at + 4 * i) = make_float4(x[0], x[1], x[2], x[3]);
     }
   }
-}
-
-// 32 bytes at p + k of a row of K bytes, K a multiple of 16; past its end the last 16 bytes again, for inside() to clear.
-struct Piece { uint4 lo, hi; };
-FD_DEVICE Piece load32(const uint8_t* p, int k, int K) {
-  return {*reinterpret_cast<const uint4*>(p + min(k, K - 16)), *reinterpret_cast<const uint4*>(p + min(k + 16, K - 16))};
-}
-FD_DEVICE i32x8_t inside(const Piece& x, int k, int K) {
-  const uint4 none = make_uint4(0, 0, 0, 0), lo = k < K ? x.lo : none, hi = k + 16 < K ? x.hi : none;
-  return i32x8_t{static_cast<int>(lo.x), static_cast<int>(lo.y), static_cast<int>(lo.z), static_cast<int>(lo.w),
-                 static_cast<int>(hi.x), static_cast<int>(hi.y), static_cast<int>(hi.z), static_cast<int>(hi.w)};
 }
 
 // ---------------------------------------------------------------- few rows
@@ -210,44 +198,6 @@ struct Tile {
   // has NJ consecutive columns in its NJ fragments.
   static FD_DEVICE int column(int p) { return (p & ~(32 * NJ - 1)) + NJ * (p & 31) + ((p >> 5) & (NJ - 1)); }
 };
-
-typedef __attribute__((address_space(3))) void* lds_ptr_t;
-
-FD_DEVICE i32x4_t buffer_of(const void* base, uint32_t bytes = 0x7fffffffu) {
-  const uint64_t p = reinterpret_cast<uint64_t>(base);
-  return i32x4_t{static_cast<int>(static_cast<uint32_t>(p)), static_cast<int>(static_cast<uint32_t>(p >> 32) & 0xffffu), static_cast<int>(bytes), 0x00020000};
-}
-constexpr uint32_t kNowhere = 0x80000000u;   // an offset past every buffer: loads read zeros, stores are dropped
-// Cache policy of wide results: non-temporal, so that they leave the L2 to the operands (9828 x 4608 x 1536 to bf16
-// 77.4 -> 74.8 us, x 1536 x 6144 84.3 -> 79.7; codes, a quarter to a half of the bytes, the same either way).
-constexpr int kStream = 2;
-// 16 (4) bytes per lane from buffer offset voff + soff into LDS at lds + MORE + 16 (4) * lane.  In assembly so that
-// the compiler does not wait for it before unrelated LDS reads.  A load to LDS takes M0 one wait state after its write.
-template <int MORE>
-FD_DEVICE void dma16(uint32_t lds, uint32_t voff, i32x4_t rsrc, uint32_t soff) {
-  asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(lds), "v"(voff), "s"(rsrc), "s"(soff), "n"(MORE) : "scc");
-}
-FD_DEVICE void dma4(uint32_t lds, uint32_t voff, i32x4_t rsrc, uint32_t soff) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" : : "s"(lds), "v"(voff), "s"(rsrc), "s"(soff));
-}
-// This wave's LDS reads are done; then the barrier.
-FD_DEVICE void wait_reads_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
-// ... and at most N of its vector memory operations are in flight (N + MORE where `more`).  One block of assembly:
-// a branch around the wait would end the basic block, across which the compiler moves the products.
-template <int N, int MORE>
-FD_DEVICE void wait_barrier(int more) {
-  static_assert(N + MORE < 64, "the counter's range");
-  asm volatile(
-      "s_waitcnt vmcnt(%1) lgkmcnt(0)\n\t"
-      "s_cmp_lg_u32 %0, 0\n\t"
-      "s_cbranch_scc1 .Lfd_wait_%=\n\t"
-      "s_waitcnt vmcnt(%2)\n"
-      ".Lfd_wait_%=:\n\t"
-      "s_barrier"
-      :
-      : "s"(more), "n"(N + MORE), "n"(N)
-      : "memory", "scc");
-}
 
 // 32 rows x 32 NJ columns to memory: acc[j][r] is row 8 (r >> 2) + 4 half + (r & 3) and column NJ l32 + j, so that
 // 32 lanes store one row's columns side by side (with rows spread over the lanes, 16 bytes of 64 rows a store,
