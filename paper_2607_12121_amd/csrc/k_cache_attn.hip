@@ -222,11 +222,24 @@ FD_DEVICE void store_o(uint16_t* row, int lg, const f32x16_t (&o)[Cfg<DH>::DT], 
     }
 }
 
-// The running maximum of a row takes a tile's scores s (64 keys, 32 of them in this lane) and O and the sum are rescaled
-// where it grew by more than 8 (P stays below 2^8; the softmax does not depend on what is subtracted).  Returns what to
-// subtract.  LIMIT: the scores of the lane's keys from `lim` on are not the request's.
-template <int DH, bool LIMIT>
-FD_DEVICE float take_max(f32x16_t (&s)[2], int lim, float scale_log2, float& m_run, float& l_run, f32x16_t (&o)[Cfg<DH>::DT]) {
+// The largest of a lane's 32 scores of a tile in eight steps of two, four independent chains; then of the row's.
+struct TileMax {
+  float mx[4];
+  FD_DEVICE void first(const f32x16_t (&s)[2]) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) mx[c] = __builtin_elementwise_maximum(s[c >> 1][8 * (c & 1)], s[c >> 1][8 * (c & 1) + 1]);
+  }
+  FD_DEVICE void next(const f32x16_t (&s)[2], int i) {   // i = 0 .. 11
+    const int c = i & 3, r = 8 * (c & 1) + 2 + 2 * (i >> 2);
+    mx[c] = max3(mx[c], s[c >> 1][r], s[c >> 1][r + 1]);
+  }
+  FD_DEVICE float row(float scale_log2) const {
+    return half_max(__builtin_elementwise_maximum(__builtin_elementwise_maximum(mx[0], mx[1]), __builtin_elementwise_maximum(mx[2], mx[3]))) * scale_log2;
+  }
+};
+// LIMIT: the scores of the lane's keys from `lim` on are not the request's.
+template <bool LIMIT>
+FD_DEVICE float tile_max(f32x16_t (&s)[2], int lim, float scale_log2) {
   if constexpr (LIMIT) {
 #pragma unroll
     for (int kh = 0; kh < 2; ++kh)
@@ -234,15 +247,17 @@ FD_DEVICE float take_max(f32x16_t (&s)[2], int lim, float scale_log2, float& m_r
       for (int r = 0; r < 16; ++r)
         if (32 * kh + 8 * (r >> 2) + (r & 3) >= lim) s[kh][r] = -INFINITY;
   }
-  float mx[4];   // four independent chains
+  TileMax m;
+  m.first(s);
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const int kh = c >> 1, r0 = 8 * (c & 1);
-    mx[c] = __builtin_elementwise_maximum(s[kh][r0], s[kh][r0 + 1]);
-#pragma unroll
-    for (int r = r0 + 2; r < r0 + 8; r += 2) mx[c] = max3(mx[c], s[kh][r], s[kh][r + 1]);
-  }
-  const float top = half_max(__builtin_elementwise_maximum(__builtin_elementwise_maximum(mx[0], mx[1]), __builtin_elementwise_maximum(mx[2], mx[3]))) * scale_log2;
+  for (int i = 0; i < 12; ++i) m.next(s, i);
+  return m.row(scale_log2);
+}
+
+// The running maximum of a row takes a tile's, and O and the sum are rescaled where it grew by more than 8 (P stays below 2^8;
+// the softmax does not depend on what is subtracted).  Returns what to subtract.
+template <int DH>
+FD_DEVICE float take_max(float top, float& m_run, float& l_run, f32x16_t (&o)[Cfg<DH>::DT]) {
   const bool grow = top > m_run + 8.0f;
   const float m_new = grow ? top : m_run;
   if (__any(grow)) {
@@ -326,15 +341,32 @@ FD_DEVICE void tile_piece(const fdh::CacheAttnArgs& g, int group, float scale_lo
   const int row = tid / PER_ROW, c0 = tid % PER_ROW * C::PIECE;
   struct Codes { uint32_t c[C::PIECE / 4]; uint32_t scale; };
   const uint32_t off = static_cast<uint32_t>(row) * static_cast<uint32_t>(ldk) + static_cast<uint32_t>(c0);
-  auto fetch = [&](const uint8_t* cache, const uint8_t* scale, int t) {   // of local tile t
-    const int key0 = k_beg + (kt0 + fd::uniform(min(t, nkt - 1))) * KB, last = k_end - 1 - key0;
-    const bool in = row <= last;
-    const uint8_t* base = cache + static_cast<size_t>(key0) * ldk + static_cast<size_t>(head) * DH;
+  // Successive tiles of a cache: the next tile's place and its last row of the request, in scalar registers.  (Formed anew from the
+  // tile's number, the addresses took 300 to 400 clocks of an iteration's 2700 at head dim 64.)
+  struct Stream { const uint8_t* codes; const uint8_t* scale; int last, left; };
+  auto stream = [&](const uint8_t* cache, const uint8_t* scale) {
+    const int key0 = k_beg + kt0 * KB;
+    return Stream{cache + static_cast<size_t>(key0) * ldk + static_cast<size_t>(head) * DH, scale + static_cast<size_t>(head) * g.n_tokens + key0,
+                  k_end - 1 - key0, nkt};
+  };
+  // without a branch: the iteration stays one block, in which the compiler may order
+  auto fetch_codes = [&](const Stream& from, Codes& x) {
+    __builtin_memcpy(x.c, __builtin_assume_aligned(from.codes + (row <= from.last ? off : static_cast<uint32_t>(from.last) * static_cast<uint32_t>(ldk) + static_cast<uint32_t>(c0)), C::PIECE), C::PIECE);
+  };
+  auto fetch_scale = [&](Stream& from, Codes& x) {   // and on to the next tile; past the piece's last one that one again
+    x.scale = from.scale[min(row, from.last)];
+    const bool more = --from.left > 0;
+    from.codes += more ? KB * ldk : 0;
+    from.scale += more ? KB : 0;
+    from.last -= more ? KB : 0;
+  };
+  auto fetch = [&](Stream& from) {
     Codes x;
-    __builtin_memcpy(x.c, base + (in ? off : static_cast<uint32_t>(last) * static_cast<uint32_t>(ldk) + static_cast<uint32_t>(c0)), C::PIECE);
-    x.scale = (scale + static_cast<size_t>(head) * g.n_tokens + key0)[in ? row : last];
+    fetch_codes(from, x);
+    fetch_scale(from, x);
     return x;
   };
+  Stream from_k = stream(g.k, g.k_scale), from_v = stream(g.v, g.v_scale);
   const uint32_t put_k = static_cast<uint32_t>((row * KCH + ((c0 / 8) ^ C::fk(row))) * 16 + c0 % 8 * 2);
   const uint32_t put_v = static_cast<uint32_t>((row * KCH + ((c0 / 8) ^ C::fv(row))) * 16 + c0 % 8 * 2);
   auto put = [&](const Codes& x, uint32_t at) {   // as bf16 values to LDS
@@ -358,6 +390,7 @@ FD_DEVICE void tile_piece(const fdh::CacheAttnArgs& g, int group, float scale_lo
   f32x16_t o[DT] = {};
   float m_run = -INFINITY, l_run = 0.f;
   bf16x8_t pk[4];
+  float top = 0.f;   // the maximum of the next iteration's scores
   auto s_step = [&](uint32_t tile_at, f32x16_t (&s)[2], int ks) {
     const f32x16_t zero = {};
 #pragma unroll
@@ -371,29 +404,31 @@ FD_DEVICE void tile_piece(const fdh::CacheAttnArgs& g, int group, float scale_lo
   // wave is done with K(t) and V(t - 1), whose places K(t + 2) and V(t + 1) take.
   auto body = [&](int t, f32x16_t (&cur)[2], f32x16_t (&nxt)[2]) {
     lds_barrier();
-    const Codes ck = fetch(g.k, g.k_scale, t + 2), cv = fetch(g.v, g.v_scale, t + 1);
     const uint32_t kt_at = k_tile(t + 1), vt_at = v_tile(t);
-    // jobs: one operand read feeding one matrix instruction; first the rest of S(t + 1) (its first step runs beside the
-    // maximum), then O by quarters of P as they come; reads run AH jobs ahead
-    constexpr int NS = (KS - 1) * 2, NJ = NS + DT * 4, AH = C::AHEAD < NJ ? C::AHEAD : NJ, PAIRS = 16, PER = (NJ + PAIRS - 1) / PAIRS;
+    // jobs: one operand read feeding one matrix instruction; first S(t + 1), then O by quarters of P as they come; reads run
+    // AH jobs ahead
+    constexpr int NS = KS * 2, NJ = NS + DT * 4, AH = C::AHEAD < NJ ? C::AHEAD : NJ, PAIRS = 16, PER = (NJ + PAIRS - 1) / PAIRS;
+    constexpr int S_DONE = (NS + PER - 1) / PER;   // the pair from which on S(t + 1) is complete
+    const f32x16_t zero = {};
     auto read = [&](int j) -> u32x4_t {
-      if (j < NS) return __builtin_bit_cast(u32x4_t, lds_chunk(kt_at + ln.k_off[1 + j / 2] + static_cast<uint32_t>(j % 2 * 32 * KCH * 16)));
+      if (j < NS) return __builtin_bit_cast(u32x4_t, lds_chunk(kt_at + ln.k_off[j / 2] + static_cast<uint32_t>(j % 2 * 32 * KCH * 16)));
       return ln.v_frag(vt_at, (j - NS) / DT, (j - NS) % DT);
     };
     auto run = [&](int j, u32x4_t op) {
       const bf16x8_t a = __builtin_bit_cast(bf16x8_t, op);
-      if (j < NS) nxt[j % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[1 + j / 2], nxt[j % 2], 0, 0, 0);
+      if (j < NS) nxt[j % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[j / 2], j < 2 ? zero : nxt[j % 2], 0, 0, 0);
       else o[(j - NS) % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pk[(j - NS) / DT], o[(j - NS) % DT], 0, 0, 0);
     };
     auto earliest = [&](int j) { return j < NS ? 0 : 4 * ((j - NS) / DT + 1); };   // pair behind which job j may run
-    s_step(kt_at, nxt, 0);
-    const float sub = take_max<DH, false>(cur, 0, scale_log2, m_run, l_run, o);
     u32x4_t ops[AH];
 #pragma unroll
     for (int j = 0; j < AH; ++j) ops[j] = read(j);
+    const float sub = take_max<DH>(top, m_run, l_run, o);
+    Codes ck, cv;   // K's tile t + 2 and V's t + 1
+    TileMax nm;
     // P in three stages that overlap across pairs: exponentials of pair pp, scaled scores of pp + 1, packing and sum of pp - 1
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    int cursor = 0;
+    int cursor = 0, compared = 0;
     auto next_job = [&] {
       run(cursor, ops[cursor % AH]);
       if (cursor + AH < NJ) ops[cursor % AH] = read(cursor + AH);
@@ -424,20 +459,35 @@ FD_DEVICE void tile_piece(const fdh::CacheAttnArgs& g, int group, float scale_lo
 #pragma unroll
       for (int k = 0; k < PER; ++k)
         if (cursor < NJ && earliest(cursor) <= pp) next_job();
+      // the loads apart from each other: all waves' at once wait for the address unit
+      if (pp == 0) fetch_codes(from_k, ck);
+      if (pp == 2) fetch_codes(from_v, cv);
+      if (pp == 4) fetch_scale(from_k, ck);
+      if (pp == 6) fetch_scale(from_v, cv);
+      // the maximum of S(t + 1), two steps a pair
+      if (pp == S_DONE + 1) nm.first(nxt);
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        if (pp > S_DONE + 1 && compared < 12) nm.next(nxt, compared++);
       __builtin_amdgcn_sched_barrier(0);
     }
     pack(PAIRS - 1, p0, p1);
 #pragma unroll
     for (int k = 0; k < NJ; ++k)
       if (cursor < NJ) next_job();
+#pragma unroll
+    for (int k = 0; k < 12; ++k)
+      if (compared < 12) nm.next(nxt, compared++);
+    top = nm.row(scale_log2);
     put(ck, k_tile(t + 2) + put_k);
     put(cv, v_tile(t + 1) + put_v);
     l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    asm volatile("" : "+v"(l_run));   // here, and not beside the next iteration's work with P kept until then
   };
   auto tail = [&](int t, f32x16_t (&cur)[2]) {
     lds_barrier();
     const int lim = k_end - (k_beg + (kt0 + t) * KB) - 4 * lg;   // this lane's keys below it are the request's
-    const float sub = take_max<DH, true>(cur, lim, scale_log2, m_run, l_run, o);
+    const float sub = take_max<DH>(tile_max<true>(cur, lim, scale_log2), m_run, l_run, o);
     take_p(cur, scale_log2, sub, pk, l_run);
 #pragma unroll
     for (int st = 0; st < 4; ++st)
@@ -446,7 +496,7 @@ FD_DEVICE void tile_piece(const fdh::CacheAttnArgs& g, int group, float scale_lo
         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, ln.v_frag(v_tile(t), st, d)), pk[st], o[d], 0, 0, 0);
   };
   {
-    const Codes k0 = fetch(g.k, g.k_scale, 0), k1 = fetch(g.k, g.k_scale, 1), v0 = fetch(g.v, g.v_scale, 0);
+    const Codes k0 = fetch(from_k), k1 = fetch(from_k), v0 = fetch(from_v);
     put(k0, k_tile(0) + put_k);
     put(k1, k_tile(1) + put_k);
     put(v0, v_tile(0) + put_v);
@@ -455,6 +505,7 @@ FD_DEVICE void tile_piece(const fdh::CacheAttnArgs& g, int group, float scale_lo
   f32x16_t sa[2], sb[2];
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) s_step(k_tile(0), sa, ks);
+  if (nkt > 1) top = tile_max<false>(sa, 0, scale_log2);   // of the tile whose turn is next: all but the last one's are the request's
   int t = 0;
   for (; t + 2 <= nkt - 1; t += 2) {
     body(t, sa, sb);
@@ -580,7 +631,7 @@ FD_DEVICE void few_piece(const fdh::CacheAttnArgs& g, int group, float scale_log
     put_v(0);
     __builtin_amdgcn_sched_barrier(0);
     fetch(g.k, ksc, next, xk, sk);   // not before: the fragments need the registers
-    const float sub = take_max<DH, true>(s, k_end - key0 - 4 * lg, scale_log2, m_run, l_run, o);
+    const float sub = take_max<DH>(tile_max<true>(s, k_end - key0 - 4 * lg, scale_log2), m_run, l_run, o);
     bf16x8_t pk[4];
     take_p(s, scale_log2, sub, pk, l_run);
 #pragma unroll
@@ -782,14 +833,15 @@ __global__ __launch_bounds__(Cfg<DH>::THREADS) void cache_join_kernel(fdh::Cache
 namespace fdh {
 
 namespace {
-int cache_grid() { return (num_cus() + fd::kXcds - 1) / fd::kXcds * fd::kXcds; }
+// Workgroups: eight waves a CU, two a SIMD.
+int cache_grid(int dh) { return (num_cus() + fd::kXcds - 1) / fd::kXcds * fd::kXcds * (256 / fd::cache_tile_rows(dh)); }
 }  // namespace
 
 size_t cache_attention_scratch_bytes(int n_rows, int heads, int kv_heads, int dh) {
   // two slots per share: 32 rows where no call of these rows runs in tiles
   const bool few = fd::cache_always_few(static_cast<long long>(n_rows) * (heads / kv_heads));
   const size_t floats = few ? 32 * (dh + 2) : static_cast<size_t>(2 * fd::cache_tile_rows(dh)) * ((dh + 31) / 32 * 16 + 2);
-  return 2 * static_cast<size_t>(cache_grid()) * floats * sizeof(float);
+  return 2 * static_cast<size_t>(cache_grid(dh)) * floats * sizeof(float);
 }
 
 hipError_t launch_cache_attention(const CacheAttnArgs& args, hipStream_t s) {
@@ -797,9 +849,9 @@ hipError_t launch_cache_attention(const CacheAttnArgs& args, hipStream_t s) {
   g.may_cut = g.max_req_tokens > (g.dh >= 64 ? Cfg<64>::FEW_KEYS : Cfg<16>::FEW_KEYS);
   auto run = [&](auto tag) {
     constexpr int DH = decltype(tag)::value;
-    if (fd::cache_always_few(static_cast<long long>(g.n_rows) * (g.heads / g.kv_heads))) cache_attn_kernel<DH, true><<<cache_grid(), Cfg<DH>::THREADS, 0, s>>>(g);
-    else cache_attn_kernel<DH, false><<<cache_grid(), Cfg<DH>::THREADS, 0, s>>>(g);
-    if (g.may_cut) cache_join_kernel<DH><<<cache_grid(), Cfg<DH>::THREADS, 0, s>>>(g);
+    if (fd::cache_always_few(static_cast<long long>(g.n_rows) * (g.heads / g.kv_heads))) cache_attn_kernel<DH, true><<<cache_grid(DH), Cfg<DH>::THREADS, 0, s>>>(g);
+    else cache_attn_kernel<DH, false><<<cache_grid(DH), Cfg<DH>::THREADS, 0, s>>>(g);
+    if (g.may_cut) cache_join_kernel<DH><<<cache_grid(DH), Cfg<DH>::THREADS, 0, s>>>(g);
   };
   switch (g.dh) {
     case 16: run(std::integral_constant<int, 16>{}); break;
