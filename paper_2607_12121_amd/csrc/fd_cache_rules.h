@@ -15,4 +15,8 @@ FD_RULE bool cache_few_rows(int few, int tiles) { return few <= 4 * tiles; }
 // Whether every request of a call of at most `rows` rows is of few: 4 items of 32 rows make a tile or less.
 FD_RULE bool cache_always_few(long long rows) { return rows <= 4 * kFewRows; }
 
+// Key tiles that the start of an item of tiles counts for in the shares: its queries and first key tiles on their way.  Every share has one
+// start; where they have more, those of short items would end late.
+FD_RULE int cache_item_steps(long long items, int shares) { return items > shares ? 3 : 0; }
+
 }  // namespace fd

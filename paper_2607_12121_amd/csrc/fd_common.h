@@ -234,7 +234,8 @@ struct CacheAttnArgs {
   const uint8_t* k; const uint8_t* v;           // [n_tokens][kv_heads * dh] codes
   const uint8_t* k_scale; const uint8_t* v_scale;   // [kv_heads][n_tokens]
   const int32_t* cu_q; const int32_t* tok_off;
-  float* partial;
+  float* partial;                               // the workspace
+  void* cut_items;                              // set per launch
 };
 size_t cache_attention_scratch_bytes(int n_rows, int heads, int kv_heads, int dh);
 hipError_t launch_cache_attention(const CacheAttnArgs& g, hipStream_t s);

@@ -52,6 +52,8 @@ struct Cfg {
   static constexpr int FEW_WAVE_BYTES = KB * DH + TILE * 16 / VHALVES;   // K's codes and V's values
   static constexpr int AHEAD = DH >= 128 ? 2 : 3;      // operand reads ahead of their matrix instructions (registers)
   static constexpr int E = DT * 16 + 2;                // floats of a thread in a tile's piece
+  static constexpr int FEW_SLOT = 32 * (DH + 2);       // floats of a piece of few rows
+  static constexpr int JOIN_PARTS = DT * 2;            // workgroups that join an item: two quads of a thread each
   static_assert(QB == 32 * WAVES, "a wave per 32 rows");
   // chunk c of key row r lies at c ^ fk(r) of K's tile and c ^ fv(r) of V's, so that the lanes that read together
   // meet different bank groups.  fk(r + 32) = fk(r), fv(r + 8) = fv(r).
@@ -102,7 +104,7 @@ struct Lengths {
 // What the schedule is built from, by every workgroup of both kernels alike: the way, and the prefix tables of its items
 // and key steps over the requests.  Each thread takes a run of requests, the runs' sums are scanned over the
 // waves and the workgroup.
-struct Way { bool few, empty; };   // empty: a request has rows but no keys
+struct Way { bool few, empty; int extra; };   // empty: a request has rows but no keys; extra: key steps that an item's start counts for
 template <int DH>
 FD_DEVICE Way build_tables(SchedTables& t, const fdh::CacheAttnArgs& g, int group) {
   using C = Cfg<DH>;
@@ -133,14 +135,15 @@ FD_DEVICE Way build_tables(SchedTables& t, const fdh::CacheAttnArgs& g, int grou
     tiles += s_items[1][w];
     empty |= s_empty[w];
   }
-  const Way way{fd::cache_few_rows(few, tiles), empty != 0};
-  const int qb = way.few ? C::QF : C::QB, kb = way.few ? C::FEW_KEYS : KB;
+  const bool is_few = fd::cache_few_rows(few, tiles);
+  const Way way{is_few, empty != 0, is_few ? 0 : fd::cache_item_steps(static_cast<long long>(tiles) * g.kv_heads, static_cast<int>(gridDim.x))};
+  const int qb = way.few ? C::QF : C::QB, kb = way.few ? C::FEW_KEYS : KB, more = way.extra;
   int it = 0;
   long long st = 0;
   for (int b = b0; b < b1; ++b) {
     const int n = len.items(b, qb);
     it += n;
-    st += static_cast<long long>(n) * ((len.keys(b) + kb - 1) / kb);
+    st += static_cast<long long>(n) * ((len.keys(b) + kb - 1) / kb + more);
   }
   int it_in = it;
   long long st_in = st;
@@ -170,7 +173,7 @@ FD_DEVICE Way build_tables(SchedTables& t, const fdh::CacheAttnArgs& g, int grou
     t.wpre[b] = ps;
     const int n = len.items(b, qb);
     pi += n;
-    ps += static_cast<long long>(n) * ((len.keys(b) + kb - 1) / kb);
+    ps += static_cast<long long>(n) * ((len.keys(b) + kb - 1) / kb + more);
   }
   if (b0 < b1 && b1 == g.n_req) {
     t.tpre[g.n_req] = pi;
@@ -184,8 +187,9 @@ FD_DEVICE Way build_tables(SchedTables& t, const fdh::CacheAttnArgs& g, int grou
 template <int DH>
 struct Sched : fd::AttnSched<Cfg<DH>::QB, DH, true, true> {
   using Base = fd::AttnSched<Cfg<DH>::QB, DH, true, true>;
-  FD_DEVICE Sched(const SchedTables* t, const fdh::CacheAttnArgs& g, bool few, int grid)
-      : Base(t, g.cu_q, g.tok_off, g.n_req, g.kv_heads, grid, (g.max_req_tokens + KB - 1) / KB) {
+  int extra_steps;   // of an item: what its start takes
+  FD_DEVICE Sched(const SchedTables* t, const fdh::CacheAttnArgs& g, bool few, int start, int grid)
+      : Base(t, g.cu_q, g.tok_off, g.n_req, g.kv_heads, grid, (g.max_req_tokens + KB - 1) / KB + start), extra_steps(start) {
     if (!few && g.may_cut) return;
     this->cut = few && g.may_cut;
     this->G = grid;
@@ -197,7 +201,22 @@ struct Sched : fd::AttnSched<Cfg<DH>::QB, DH, true, true> {
       this->extra = 0;
     }
   }
+  // A share does not end among the steps that stand for an item's start, but before it: no piece is without keys (a share is
+  // longer than those steps).
+  FD_DEVICE long long bound(long long x) const {
+    const long long q = Base::bound(x);
+    if (!this->cut || extra_steps == 0 || q >= this->work) return q;
+    long long i_start;
+    int n, head, b, first, tau;
+    this->locate(q, i_start, n, head, b, first, tau);
+    return q - i_start <= extra_steps ? i_start : q;
+  }
+  FD_DEVICE int tile(int step) const { return step > 0 ? step - extra_steps : 0; }   // key tile (or step of few rows) of an item's step
 };
+
+// The cut item whose first piece a workgroup has, for the join; no pieces: none.  Every workgroup writes its own.
+struct CutItem { int pieces, share, head, request, tile_few; };
+FD_DEVICE CutItem* g_cut_items(const fdh::CacheAttnArgs& g) { return static_cast<CutItem*>(g.cut_items); }
 
 // One lane's row of an item: where its query (and result) begins, and whether there is one.
 struct RowAt { size_t at; bool live; };
@@ -676,7 +695,7 @@ FD_DEVICE void few_piece(const fdh::CacheAttnArgs& g, int group, float scale_log
   if (lg == 0) ml[wave * 32 + l32] = f32x2_t{m_run, l_run};
   __syncthreads();
   const int rows = min(C::QF, (g.cu_q[b + 1] - g.cu_q[b]) * group - tile * C::QF);
-  float* slot = g.partial + static_cast<size_t>(max(slot_no, 0)) * (32 * (DH + 2));
+  float* slot = g.partial + static_cast<size_t>(max(slot_no, 0)) * C::FEW_SLOT;
   for (int i = tid; i < rows * (DH / 4); i += C::THREADS) {
     const int r = i / (DH / 4), d0 = i % (DH / 4) * 4;
     float m = -INFINITY, l = 0.f;
@@ -724,7 +743,8 @@ __global__ __launch_bounds__(Cfg<DH>::THREADS) __attribute__((amdgpu_waves_per_e
       for (long long i = per * g.cu_q[b] + tid; i < end; i += C::THREADS) reinterpret_cast<uint4*>(g.o)[i] = make_uint4(0, 0, 0, 0);
     }
   const bool few = fd::uniform(static_cast<int>(way.few)) != 0;
-  const Sched<DH> sch(&tabs, g, few, static_cast<int>(gridDim.x));
+  const Sched<DH> sch(&tabs, g, few, fd::uniform(way.extra), static_cast<int>(gridDim.x));
+  if (tid == 0 && g.may_cut) g_cut_items(g)[blockIdx.x] = CutItem{};
   if (sch.work == 0) return;
   const float scale_log2 = g.scale * 1.4426950408889634f;
   const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr_t)&ring[0]));
@@ -740,92 +760,90 @@ __global__ __launch_bounds__(Cfg<DH>::THREADS) __attribute__((amdgpu_waves_per_e
     sch.locate(p, i_start, n, head, b, first, tau);
     const int s0 = static_cast<int>(p - i_start), s1 = static_cast<int>(min(p_end, i_start + n) - i_start);
     const int slot = sch.cut ? sch.slot_of(w, s0, s1, n) : -1;
-    if (FEW_ONLY || few) few_piece<DH>(g, group, scale_log2, ln, ring, lds, head, tau - first, b, s0, s1, slot);
-    else if constexpr (!FEW_ONLY) tile_piece<DH>(g, group, scale_log2, ln, lds, head, tau - first, b, s0, s1, slot);
+    if (tid == 0 && slot >= 0 && s0 == 0)   // its first piece
+      g_cut_items(g)[blockIdx.x] = CutItem{sch.last_share(w, i_start + n) - w + 1, w, head, b, 2 * (tau - first) + few};
+    const int t0 = sch.tile(s0), t1 = sch.tile(s1);
+    if (FEW_ONLY || few) few_piece<DH>(g, group, scale_log2, ln, ring, lds, head, tau - first, b, t0, t1, slot);
+    else if constexpr (!FEW_ONLY) tile_piece<DH>(g, group, scale_log2, ln, lds, head, tau - first, b, t0, t1, slot);
     p = i_start + s1;
   }
 }
 
-// The pieces of the cut items, joined in key order: workgroup x takes the cut item whose first piece share x holds.
-// Each piece's O is divided by its own sum: its weight is 2^(maximum - the largest) * sum.
+// The pieces of the cut items, joined in key order: workgroups (x, 0 ..) take the item whose first piece workgroup x of
+// the attention had, a part of its values each (one workgroup an item: 256 rows of 12 heads, 21 pieces each, 45 us).  Each piece's
+// O is divided by its own sum: its weight is 2^(maximum - the largest) * sum.  Eight pieces' loads are in flight together; what
+// came before is rescaled to the new maximum.
+template <int VALUES>
+struct Joined {
+  float top = -INFINITY, l = 0.f;
+  float4 o[VALUES] = {};
+  template <int AT_ONCE, class Ml, class Value>
+  FD_DEVICE void add(int pieces, Ml ml_of, Value value_of) {
+    for (int j0 = 0; j0 < pieces; j0 += AT_ONCE) {
+      f32x2_t ml[AT_ONCE];
+      float4 v[AT_ONCE][VALUES];
+#pragma unroll
+      for (int j = 0; j < AT_ONCE; ++j) {
+        const int p = min(j0 + j, pieces - 1);
+        ml[j] = ml_of(p);
+#pragma unroll
+        for (int i = 0; i < VALUES; ++i) v[j][i] = value_of(p, i);
+      }
+      float next = top;
+#pragma unroll
+      for (int j = 0; j < AT_ONCE; ++j) next = __builtin_elementwise_maximum(next, ml[j][0]);
+      const float back = top == -INFINITY ? (l == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(top - next);
+      l *= back;
+#pragma unroll
+      for (int i = 0; i < VALUES; ++i) o[i] = make_float4(o[i].x * back, o[i].y * back, o[i].z * back, o[i].w * back);
+      top = next;
+#pragma unroll
+      for (int j = 0; j < AT_ONCE; ++j) {
+        if (j0 + j >= pieces) continue;
+        // a piece without a finite score has the sum 0 (or NaN)
+        const float a = ml[j][0] == -INFINITY ? ml[j][1] : __builtin_amdgcn_exp2f(ml[j][0] - top) * ml[j][1];
+        l += a;
+#pragma unroll
+        for (int i = 0; i < VALUES; ++i)
+          o[i] = make_float4(o[i].x + a * v[j][i].x, o[i].y + a * v[j][i].y, o[i].z + a * v[j][i].z, o[i].w + a * v[j][i].w);
+      }
+    }
+  }
+  FD_DEVICE uint2 row(int i) const {
+    const float inv = 1.0f / l;
+    return make_uint2(fd::pack_bf2(o[i].x * inv, o[i].y * inv), fd::pack_bf2(o[i].z * inv, o[i].w * inv));
+  }
+};
 template <int DH>
 __global__ __launch_bounds__(Cfg<DH>::THREADS) void cache_join_kernel(fdh::CacheAttnArgs g) {
   using C = Cfg<DH>;
-  constexpr int DT = C::DT;
-  __shared__ SchedTables tabs;
-  const int group = fd::uniform(g.heads / g.kv_heads);
-  const bool few = fd::uniform(static_cast<int>(build_tables<DH>(tabs, g, group).few)) != 0;
-  const Sched<DH> sch(&tabs, g, few, static_cast<int>(gridDim.x));
-  if (sch.work == 0 || !sch.cut) return;
-  const int x = sch.share(static_cast<int>(blockIdx.x));
-  const long long p0 = sch.bound(x), p_end = sch.bound(x + 1);
-  if (p_end <= p0) return;
-  long long i_start;
-  int n, head, b, first, tau;
-  sch.locate(p_end - 1, i_start, n, head, b, first, tau);
-  if (i_start < p0 || i_start + n <= p_end) return;   // no item begins here and goes on
-  const int pieces = sch.last_share(x, i_start + n) - x + 1, tile = tau - first;
+  const CutItem it = g_cut_items(g)[blockIdx.x];
+  if (it.pieces == 0) return;
+  const int group = g.heads / g.kv_heads, few = it.tile_few & 1, tile = it.tile_few >> 1, head = it.head, b = it.request, x = it.share;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, lg = lane >> 5;
-  auto weight = [](f32x2_t ml, float top) { return ml[0] == -INFINITY ? (ml[1] == 0.f ? 0.f : ml[1]) : __builtin_amdgcn_exp2f(ml[0] - top) * ml[1]; };
+  auto slot = [&](int j, int floats) { return g.partial + static_cast<size_t>(Sched<DH>::slot_at(x, j)) * floats; };
   if (few) {
-    constexpr int SLOT = 32 * (DH + 2);
-    auto slot = [&](int j) { return g.partial + static_cast<size_t>(sch.slot_at(x, j)) * SLOT; };
     const int rows = min(C::QF, (g.cu_q[b + 1] - g.cu_q[b]) * group - tile * C::QF);
-    for (int i = tid; i < rows * (DH / 4); i += C::THREADS) {
+    for (int i = blockIdx.y * C::THREADS + tid; i < rows * (DH / 4); i += gridDim.y * C::THREADS) {
       const int r = i / (DH / 4), d0 = i % (DH / 4) * 4;
-      // 24 pieces at a time, their loads in flight together; what came before is rescaled to the new maximum
-      constexpr int AT_ONCE = 24;
-      float top = -INFINITY, l = 0.f;
-      float4 sum = make_float4(0, 0, 0, 0);
-      for (int j0 = 0; j0 < pieces; j0 += AT_ONCE) {
-        f32x2_t ml[AT_ONCE];
-        float4 v[AT_ONCE];
-#pragma unroll
-        for (int j = 0; j < AT_ONCE; ++j) {
-          const float* from = slot(min(j0 + j, pieces - 1));
-          ml[j] = reinterpret_cast<const f32x2_t*>(from + 32 * DH)[r];
-          v[j] = *reinterpret_cast<const float4*>(from + r * DH + d0);
-        }
-        float next = top;
-#pragma unroll
-        for (int j = 0; j < AT_ONCE; ++j) next = __builtin_elementwise_maximum(next, ml[j][0]);
-        const float back = top == -INFINITY ? (l == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(top - next);
-        l *= back;
-        sum.x *= back; sum.y *= back; sum.z *= back; sum.w *= back;
-        top = next;
-#pragma unroll
-        for (int j = 0; j < AT_ONCE; ++j) {
-          const float a = weight(ml[j], top);
-          if (j0 + j >= pieces) continue;
-          l += a;
-          sum.x += a * v[j].x; sum.y += a * v[j].y; sum.z += a * v[j].z; sum.w += a * v[j].w;
-        }
-      }
-      const float inv = 1.0f / l;
-      const RowAt to = row_at<DH>(g, group, b, head, tile * C::QF + r);
-      *reinterpret_cast<uint2*>(g.o + to.at + d0) = make_uint2(fd::pack_bf2(sum.x * inv, sum.y * inv), fd::pack_bf2(sum.z * inv, sum.w * inv));
+      Joined<1> sum;
+      sum.template add<24>(it.pieces, [&](int j) { return reinterpret_cast<const f32x2_t*>(slot(j, C::FEW_SLOT) + 32 * DH)[r]; },
+                           [&](int j, int) { return *reinterpret_cast<const float4*>(slot(j, C::FEW_SLOT) + r * DH + d0); });
+      *reinterpret_cast<uint2*>(g.o + row_at<DH>(g, group, b, head, tile * C::QF + r).at + d0) = sum.row(0);
     }
     return;
   }
   const RowAt me = row_at<DH>(g, group, b, head, tile * C::QB + 32 * wave + l32);
   if (!me.live) return;
-  auto slot = [&](int j) { return g.partial + static_cast<size_t>(sch.slot_at(x, j)) * (C::E * C::THREADS); };
-  auto ml = [&](int j) { return reinterpret_cast<const f32x2_t*>(slot(j) + DT * 16 * C::THREADS)[tid]; };
-  float top = -INFINITY, l = 0.f;
-  for (int j = 0; j < pieces; ++j) top = __builtin_elementwise_maximum(top, ml(j)[0]);
-  f32x16_t o[DT] = {};
-  for (int j = 0; j < pieces; ++j) {
-    const float a = weight(ml(j), top);
-    l += a;
+  const int q0 = blockIdx.y * 2;   // this workgroup's quads q0 and q0 + 1: d = 8 q + 4 lg ..
+  Joined<2> sum;
+  sum.template add<8>(it.pieces, [&](int j) { return reinterpret_cast<const f32x2_t*>(slot(j, C::E * C::THREADS) + C::DT * 16 * C::THREADS)[tid]; },
+                      [&](int j, int i) { return reinterpret_cast<const float4*>(slot(j, C::E * C::THREADS))[(q0 + i) * C::THREADS + tid]; });
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4) {
-        const float4 v = reinterpret_cast<const float4*>(slot(j))[(4 * d + r4) * C::THREADS + tid];
-        o[d][4 * r4] += a * v.x; o[d][4 * r4 + 1] += a * v.y; o[d][4 * r4 + 2] += a * v.z; o[d][4 * r4 + 3] += a * v.w;
-      }
+  for (int i = 0; i < 2; ++i) {
+    const int d0 = 8 * (q0 + i) + 4 * lg;
+    if (d0 < DH) *reinterpret_cast<uint2*>(g.o + me.at + d0) = sum.row(i);
   }
-  store_o<DH>(g.o + me.at, lg, o, 1.0f / l);
 }
 
 }  // namespace
@@ -835,23 +853,27 @@ namespace fdh {
 namespace {
 // Workgroups: eight waves a CU, two a SIMD.
 int cache_grid(int dh) { return (num_cus() + fd::kXcds - 1) / fd::kXcds * fd::kXcds * (256 / fd::cache_tile_rows(dh)); }
+// The items' records come first in the workspace, then the pieces.
+size_t cut_items_bytes(int dh) { return (cache_grid(dh) * sizeof(CutItem) + 255) / 256 * 256; }
 }  // namespace
 
 size_t cache_attention_scratch_bytes(int n_rows, int heads, int kv_heads, int dh) {
   // two slots per share: 32 rows where no call of these rows runs in tiles
   const bool few = fd::cache_always_few(static_cast<long long>(n_rows) * (heads / kv_heads));
   const size_t floats = few ? 32 * (dh + 2) : static_cast<size_t>(2 * fd::cache_tile_rows(dh)) * ((dh + 31) / 32 * 16 + 2);
-  return 2 * static_cast<size_t>(cache_grid(dh)) * floats * sizeof(float);
+  return cut_items_bytes(dh) + 2 * static_cast<size_t>(cache_grid(dh)) * floats * sizeof(float);
 }
 
 hipError_t launch_cache_attention(const CacheAttnArgs& args, hipStream_t s) {
   CacheAttnArgs g = args;
+  g.cut_items = args.partial;
+  g.partial = args.partial + cut_items_bytes(g.dh) / sizeof(float);
   g.may_cut = g.max_req_tokens > (g.dh >= 64 ? Cfg<64>::FEW_KEYS : Cfg<16>::FEW_KEYS);
   auto run = [&](auto tag) {
     constexpr int DH = decltype(tag)::value;
     if (fd::cache_always_few(static_cast<long long>(g.n_rows) * (g.heads / g.kv_heads))) cache_attn_kernel<DH, true><<<cache_grid(DH), Cfg<DH>::THREADS, 0, s>>>(g);
     else cache_attn_kernel<DH, false><<<cache_grid(DH), Cfg<DH>::THREADS, 0, s>>>(g);
-    if (g.may_cut) cache_join_kernel<DH><<<cache_grid(DH), Cfg<DH>::THREADS, 0, s>>>(g);
+    if (g.may_cut) cache_join_kernel<DH><<<dim3(cache_grid(DH), Cfg<DH>::JOIN_PARTS), Cfg<DH>::THREADS, 0, s>>>(g);
   };
   switch (g.dh) {
     case 16: run(std::integral_constant<int, 16>{}); break;
