@@ -11,9 +11,9 @@ FD_RULE constexpr int cache_tile_rows(int dh) { return dh >= 64 ? 256 : 128; }  
 
 // Few rows rather than tiles, by the items that each way has: all waves of a workgroup work on 32 rows, each on its own
 // keys, where tiles would leave most waves without rows.
-FD_RULE bool cache_few_rows(int few, int tiles) { return few <= 4 * tiles; }
-// Whether every request of a call of at most `rows` rows is of few: 4 items of 32 rows make a tile or less.
-FD_RULE bool cache_always_few(long long rows) { return rows <= 4 * kFewRows; }
+FD_RULE bool cache_few_rows(int few, int tiles) { return few <= 3 * tiles; }
+// Whether every request of a call of at most `rows` rows is of few: 3 items of 32 rows are not too many for a tile.
+FD_RULE bool cache_always_few(long long rows) { return rows <= 3 * kFewRows; }
 
 // Key tiles that the start of an item of tiles counts for in the shares: its queries and first key tiles on their way.  Every share has one
 // start; where they have more, those of short items would end late.
