@@ -36,9 +36,15 @@ __global__ __launch_bounds__(256) void rope_kernel(fdh::RopeArgs g, int row0) {
     int axis = 0, first = 0;
     while (lane >= first + g.dim[axis] / 2) first += g.dim[axis++] / 2;
     const double turns = static_cast<double>(g.coord[static_cast<size_t>(tok) * g.n_axes + axis]) * g.turns[lane];
-    const float rest = static_cast<float>(turns - rint(turns));
     float2 cs;
-    sincospif(2.f * rest, &cs.y, &cs.x);
+    if constexpr (CODES) {   // rounded once: a code near a tie goes the way of the exact angle's as often as fp32 lets it
+      double c, n;
+      sincospi(2.0 * (turns - rint(turns)), &n, &c);
+      cs = make_float2(static_cast<float>(c), static_cast<float>(n));
+    } else {
+      const float rest = static_cast<float>(turns - rint(turns));
+      sincospif(2.f * rest, &cs.y, &cs.x);
+    }
     turn[wave][lane] = cs;
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
