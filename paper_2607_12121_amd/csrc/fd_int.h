@@ -30,10 +30,5 @@ FD_DEVICE uint2 pack_ints(const float (&v)[8], float up) {
   }
   return make_uint2(w[0], w[1]);
 }
-FD_DEVICE uint32_t wave_top(uint32_t t) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) t = max(t, static_cast<uint32_t>(__shfl_xor(static_cast<int>(t), o, kWave)));
-  return t;
-}
 
 }  // namespace fd
