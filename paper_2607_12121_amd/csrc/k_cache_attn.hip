@@ -7,7 +7,7 @@
 // row: its maximum needs one exchange between the half-waves per tile, its sum none until the end, and S^T feeds
 // O^T = V^T P^T as the second operand.
 //
-// Two ways through the work, chosen by the row counts on the device (fd_cache_rules.h):
+// Two ways through the work, chosen by the row counts on the device (fd_cache_sched.h):
 //
 // - Tiles: an item is (key head, 256 rows), a wave per 32 rows (head dim 16: 128 rows, four waves).  The key tile's
 //   codes go to LDS as bf16 values, converted once for all waves (8 conversions a wave and tile; fragments converted
@@ -23,8 +23,7 @@
 // bits for the same sizes); no workgroup waits for another.
 #include <type_traits>
 
-#include "fd_attn_sched.h"
-#include "fd_cache_rules.h"
+#include "fd_cache_sched.h"
 #include "fd_scaled.h"
 
 namespace {
@@ -47,7 +46,8 @@ struct Cfg {
   static constexpr int TILE = KB * KCH;                // chunks of a tile
   static constexpr int KS = DH / 16, DT = (DH + 31) / 32;
   static constexpr int PIECE = KB * DH / THREADS;      // codes of a tile that a thread brings: 4, 8 or 16 of a row
-  static constexpr int FEW_KEYS = KB * WAVES;          // keys of a step of few rows
+  static constexpr int FEW_KEYS = fd::cache_few_keys(DH);   // keys of a step of few rows
+  static_assert(FEW_KEYS == KB * WAVES, "a tile a wave");
   static constexpr int VHALVES = DH >= 128 ? 2 : 1;    // parts in which V's values of 64 keys pass a wave's LDS
   static constexpr int FEW_WAVE_BYTES = KB * DH + TILE * 16 / VHALVES;   // K's codes and V's values
   static constexpr int AHEAD = DH >= 128 ? 2 : 3;      // operand reads ahead of their matrix instructions (registers)
@@ -218,41 +218,13 @@ FD_DEVICE Way build_tables(SchedTables& t, const fdh::CacheAttnArgs& g, int grou
   return way;
 }
 
-// The shares.  In tiles attn_cuts decides whether items are cut; few rows always are, into shares of a step at least.
 template <int DH>
-struct Sched : fd::AttnSched<Cfg<DH>::QB, DH, true, true> {
-  using Base = fd::AttnSched<Cfg<DH>::QB, DH, true, true>;
-  int extra_steps;   // of an item: what its start takes
-  FD_DEVICE Sched(const SchedTables* t, const fdh::CacheAttnArgs& g, bool few, int start, int grid)
-      : Base(t, g.cu_q, g.tok_off, g.n_req, g.kv_heads, grid, (g.max_req_tokens + KB - 1) / KB + start), extra_steps(start) {
-    if (!few && g.may_cut) return;
-    this->cut = few && g.may_cut;
-    this->G = grid;
-    this->per = fd::div_steps(this->work, grid);
-    this->extra = static_cast<int>(this->work - this->per * grid);
-    if (this->cut && this->work < grid) {   // shares of one step, so that the empty ones come last
-      this->G = static_cast<int>((this->work + fd::kXcds - 1) / fd::kXcds * fd::kXcds);
-      this->per = 1;
-      this->extra = 0;
-    }
-  }
-  // A share does not end among the steps that stand for an item's start, but before it: no piece is without keys (a share is
-  // longer than those steps).
-  FD_DEVICE long long bound(long long x) const {
-    const long long q = Base::bound(x);
-    if (!this->cut || extra_steps == 0 || q >= this->work) return q;
-    long long i_start;
-    int n, head, b, first, tau;
-    this->locate(q, i_start, n, head, b, first, tau);
-    return q - i_start <= extra_steps ? i_start : q;
-  }
-  // Last share that holds a piece of the item that ends at step i_end: the largest x whose bound, x work / G rounded down or
-  // x per, is below it.  (Walked to from the item's first share it takes 5 us of 21 pieces.)
-  FD_DEVICE int last_share(long long i_end) const {
-    return static_cast<int>(this->extra == 0 ? fd::div_steps(i_end - 1, this->per) : fd::div_steps(i_end * this->G - 1, this->work));
-  }
-  FD_DEVICE int tile(int step) const { return step > 0 ? step - extra_steps : 0; }   // key tile (or step of few rows) of an item's step
-};
+using Sched = fd::CacheSched<DH>;
+template <int DH>
+FD_DEVICE Sched<DH> schedule(const SchedTables* t, const fdh::CacheAttnArgs& g, const Way& way) {
+  return Sched<DH>(t, g.cu_q, g.tok_off, g.n_req, g.kv_heads, static_cast<int>(gridDim.x), (g.max_req_tokens + KB - 1) / KB,
+                   fd::uniform(static_cast<int>(way.few)) != 0, g.may_cut, fd::uniform(way.extra));
+}
 
 // The cut item whose first piece a workgroup has, for the join; no pieces: none.  Every workgroup writes its own.
 struct CutItem { int pieces, share, head, request, tile_few; };
@@ -783,7 +755,7 @@ __global__ __launch_bounds__(Cfg<DH>::THREADS) __attribute__((amdgpu_waves_per_e
       for (long long i = per * g.cu_q[b] + tid; i < end; i += C::THREADS) reinterpret_cast<uint4*>(g.o)[i] = make_uint4(0, 0, 0, 0);
     }
   const bool few = fd::uniform(static_cast<int>(way.few)) != 0;
-  const Sched<DH> sch(&tabs, g, few, fd::uniform(way.extra), static_cast<int>(gridDim.x));
+  const Sched<DH> sch = schedule<DH>(&tabs, g, way);
   if (tid == 0 && g.may_cut) g_cut_items(g)[blockIdx.x] = CutItem{};
   if (sch.work == 0) return;
   const float scale_log2 = g.scale * 1.4426950408889634f;
@@ -908,7 +880,7 @@ hipError_t launch_cache_attention(const CacheAttnArgs& args, hipStream_t s) {
   CacheAttnArgs g = args;
   g.cut_items = args.partial;
   g.partial = args.partial + cut_items_bytes(g.dh) / sizeof(float);
-  g.may_cut = g.max_req_tokens > (g.dh >= 64 ? Cfg<64>::FEW_KEYS : Cfg<16>::FEW_KEYS);
+  g.may_cut = g.max_req_tokens > fd::cache_few_keys(g.dh);
   auto run = [&](auto tag) {
     constexpr int DH = decltype(tag)::value;
     if (fd::cache_always_few(static_cast<long long>(g.n_rows) * (g.heads / g.kv_heads))) cache_attn_kernel<DH, true><<<cache_grid(DH), Cfg<DH>::THREADS, 0, s>>>(g);

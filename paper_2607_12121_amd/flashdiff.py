@@ -679,13 +679,18 @@ def fd_norm_residual(h, a, cu_q, m, y=None, post_weight=None, gate=None, residua
 
 # ------------------------------------------------------------------ 8-bit cache
 
-def _cache(name: str, t, scale, kv_heads: int, head_dim: int) -> int:
-    """Tokens of a cache [tokens, kv_heads * head_dim] with scales [kv_heads, tokens]."""
-    tokens, cols = _rows(name, t)
-    if cols != kv_heads * head_dim:
-        raise FlashDiffError(f"{name} has {cols} columns, needs {kv_heads * head_dim}")
-    if tuple(_rows(name + "_scale", scale)) != (kv_heads, tokens):
-        raise FlashDiffError(f"{name}_scale must be [{kv_heads}, {tokens}], got {tuple(scale.shape)}")
+def _cache(k, k_scale, v, v_scale, kv_heads: int, head_dim: int) -> int:
+    """Tokens of an 8-bit cache: k and v [tokens, kv_heads * head_dim] with scales [kv_heads, tokens]."""
+    tokens, cols = _rows("k", k)
+    want = (kv_heads, tokens)
+    for name, t, scale in (("k", k, k_scale), ("v", v, v_scale)):
+        if t is None or scale is None:
+            raise FlashDiffError(f"{name if t is None else name + '_scale'} is required")
+        if t.shape != (tokens, kv_heads * head_dim):
+            raise FlashDiffError(f"{name} has {t.shape[-1]} columns, needs {kv_heads * head_dim}" if t.shape[-1:] != (kv_heads * head_dim,)
+                                 else "k and v must have the same tokens")
+        if scale.shape != want:
+            raise FlashDiffError(f"{name}_scale must be [{kv_heads}, {tokens}], got {tuple(scale.shape)}")
     return tokens
 
 
@@ -699,10 +704,8 @@ def fd_cache_write(qkv, coord, idx, m, q, k, k_scale, v, v_scale, heads: int, kv
     rows, cols = _rows("qkv", qkv)
     if cols != (heads + 2 * kv_heads) * head_dim:
         raise FlashDiffError(f"qkv has {cols} columns, needs {(heads + 2 * kv_heads) * head_dim}")
-    tokens = _cache("k", k, k_scale, kv_heads, head_dim)
-    if _cache("v", v, v_scale, kv_heads, head_dim) != tokens:
-        raise FlashDiffError("k and v must have the same tokens")
-    if coord is not None and tuple(coord.shape) != (tokens, r.n_axes):
+    tokens = _cache(k, k_scale, v, v_scale, kv_heads, head_dim)
+    if coord is not None and coord.shape != (tokens, r.n_axes):
         raise FlashDiffError(f"coord must be [{tokens}, {r.n_axes}], got {tuple(coord.shape)}")
     kv = tokens * kv_heads
     p = _pointers(stream, ("coord", coord, "i32", -1 if r is None else tokens * r.n_axes), ("qkv", qkv, "b16", rows * cols), ("idx", idx, "i32", -rows),
@@ -721,9 +724,9 @@ def fd_cache_attention(q, k, k_scale, v, v_scale, o, cu_q, req_tok_off, heads: i
     tokens (req_tok_off) in an 8-bit cache, to o [rows, heads head_dim] bf16; scale None: 1 / sqrt(head_dim).  ws of
     fd_cache_attention_ws_size bytes, its own for calls that overlap."""
     rows, cols = _rows("q", q)
-    tokens = _cache("k", k, k_scale, kv_heads, head_dim)
-    if cols != heads * head_dim or _cache("v", v, v_scale, kv_heads, head_dim) != tokens:
-        raise FlashDiffError(f"q has {cols} columns of {heads} heads, or v other tokens than k")
+    if cols != heads * head_dim:
+        raise FlashDiffError(f"q has {cols} columns, needs {heads * head_dim}")
+    tokens = _cache(k, k_scale, v, v_scale, kv_heads, head_dim)
     if cu_q is None or req_tok_off is None or cu_q.numel() < 2 or cu_q.numel() != req_tok_off.numel():
         raise FlashDiffError("cu_q and req_tok_off must both have requests + 1 entries")
     B, kv = cu_q.numel() - 1, tokens * kv_heads
