@@ -30,6 +30,16 @@ constexpr uint32_t kNowhere = 0x80000000u;   // an offset past every buffer: loa
 // Cache policy of wide results: non-temporal, so that they leave the L2 to the operands (9828 x 4608 x 1536 to bf16
 // 77.4 -> 74.8 us, x 1536 x 6144 84.3 -> 79.7; codes, a quarter to a half of the bytes, the same either way).
 constexpr int kStream = 2;
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+// A store of four fp32 per lane at voff + soff, the sum in a vector register and none in the scalar one.  A store of more
+// than 8 bytes reads its data over several clocks, and a vector instruction right behind it that writes these registers has to
+// wait two states; the compiler puts them there only where the store has no scalar offset.  With one, the first of the
+// four values came out as the next row's raw sum (9728 of 16.8 million, 8192 x 2048 x 16).
+template <class Rsrc>
+FD_DEVICE void store_f4(float a, float b, float c, float d, Rsrc y, uint32_t voff, uint32_t soff) {
+  __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d)}, y,
+                                         static_cast<int>(voff + soff), 0, kStream);
+}
 // 16 (4) bytes per lane from buffer offset voff + soff into LDS at lds + MORE + 16 (4) * lane.  In assembly so that
 // the compiler does not wait for it before unrelated LDS reads.  A load to LDS takes M0 one wait state after its write.
 template <int MORE>

@@ -322,7 +322,6 @@ FD_DEVICE void int_tiles(const fdh::IntLinearArgs& g, int M, uint4* ring) {
           }
           const uint32_t to = col_ok && row < rows ? off : kNowhere;
           typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-          typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
           if constexpr (!WIDE && NJ == 2)
             __builtin_amdgcn_raw_buffer_store_b32(fd::pack_bf2(v[0], v[1]), y, to, row * pitch, kStream);
           else if constexpr (NJ == 2)
@@ -330,7 +329,7 @@ FD_DEVICE void int_tiles(const fdh::IntLinearArgs& g, int M, uint4* ring) {
           else if constexpr (!WIDE)
             __builtin_amdgcn_raw_buffer_store_b64(u32x2{fd::pack_bf2(v[0], v[1]), fd::pack_bf2(v[2], v[3])}, y, to, row * pitch, kStream);
           else
-            __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}, y, to, row * pitch, kStream);
+            store_f4(v[0], v[1], v[2], v[3], y, to, row * pitch);
         }
       }
       __builtin_amdgcn_sched_barrier(0);   // 32 rows at a time: fewer registers
