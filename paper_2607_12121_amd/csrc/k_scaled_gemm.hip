@@ -209,7 +209,6 @@ struct Rows32 {
   static_assert(KIND != kToCodes || NJ == 4, "32 lanes hold a block's columns");
   static constexpr int STORES = KIND == kToCodes ? 17 : 16;
   typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
   // The largest of each of 16 rows over the 32 lanes of a half, row r's in the lanes with l32 % 16 == r: at each
   // level a lane hands its partner (mirrored within 16, 8, 4, 2) the half of the rows that the partner keeps.
@@ -268,8 +267,7 @@ struct Rows32 {
         else if constexpr (KIND == kToBf16)
           __builtin_amdgcn_raw_buffer_store_b64(u32x2{fd::pack_bf2(v[0][r], v[1][r]), fd::pack_bf2(v[2][r], v[3][r])}, y, to, row * pitch, kStream);
         else
-          __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(v[0][r]), __float_as_uint(v[1][r]), __float_as_uint(v[2][r]), __float_as_uint(v[3][r])},
-                                                 y, to, row * pitch, kStream);
+          store_f4(v[0][r], v[1][r], v[2][r], v[3][r], y, to, row * pitch);
       }
     }
   }
