@@ -550,7 +550,8 @@ FD_DEVICE void tile_piece(const fdh::CacheAttnArgs& g, int group, float scale_lo
   }
   lds_barrier();   // the rings are filled again by the next piece
   l_run = half_sum(l_run);
-  const float inv = 1.0f / l_run;
+  // a piece whose keys all scored below fp32's range has the weight zero beside the others; alone such a row is NaN
+  const float inv = slot_no >= 0 && l_run == 0.f ? 0.f : 1.0f / l_run;
   if (slot_no < 0) {
     if (me.live) store_o<DH>(g.o + me.at, lg, o, inv);
     return;
@@ -723,7 +724,7 @@ FD_DEVICE void few_piece(const fdh::CacheAttnArgs& g, int group, float scale_log
       l += a * p[1];
       sum.x += a * v.x; sum.y += a * v.y; sum.z += a * v.z; sum.w += a * v.w;
     }
-    const float inv = 1.0f / l;
+    const float inv = slot_no >= 0 && l == 0.f ? 0.f : 1.0f / l;
     sum = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
     if (slot_no < 0) {
       const RowAt to = row_at<DH>(g, group, b, head, tile * C::QF + r);
@@ -812,7 +813,7 @@ struct Joined {
 #pragma unroll
       for (int j = 0; j < AT_ONCE; ++j) {
         if (j0 + j >= pieces) continue;
-        // a piece without a finite score has the sum 0 (or NaN)
+        // a piece without a finite score has the sum 0 and zeros (or NaN)
         const float a = ml[j][0] == -INFINITY ? ml[j][1] : __builtin_amdgcn_exp2f(ml[j][0] - top) * ml[j][1];
         l += a;
 #pragma unroll

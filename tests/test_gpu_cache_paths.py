@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import integer as ref
 from paper_2607_12121_amd import flashdiff as fdl
 from tests import gpu_harness as gh
 from tests.test_gpu_cache import cache, check_attention, run_attention
@@ -141,3 +142,21 @@ def test_recorded():
         assert torch.equal(o, eager)
         case = (q.cpu(), k, ks, v, vs, offsets(q_len), np.array([0, 4000, 5000], np.int32), hq, hk, dh)
         check_attention(o.double().cpu().numpy().reshape(rows, hq, dh), *case)
+
+
+@pytest.mark.parametrize("rows", [5, 300])
+@pytest.mark.parametrize("dh", [16, 64, 128])
+def test_pieces_of_keys_without_weight(rows, dh):
+    """Scores of the first half of the keys below the lowest fp32 value: those keys have the weight zero, also where a piece of the cut range has
+    no others, and the result is that of the second half."""
+    rng = np.random.default_rng([rows, dh])
+    tokens, half, hk = 6000, 3000, 2
+    x = rng.standard_normal((tokens, hk, dh))
+    x[:half, :, 0], x[half:, :, 0] = 448.0, 0.0
+    (k, ks), (v, vs) = ref.head_codes(x), ref.head_codes(rng.standard_normal((tokens, hk, dh)))
+    q = bf16(rng.standard_normal((rows, hk * dh)))
+    k, v, ks, vs = k.reshape(tokens, -1), v.reshape(tokens, -1), ks.T.copy(), vs.T.copy()
+    q[:, ::dh] = -2e38                       # times 448: past fp32's range
+    got = run_attention(q, k, ks, v, vs, offsets([rows]), offsets([tokens]), hk, hk, dh)
+    q[:, ::dh] = 0                           # the second half's values there are zeros
+    check_attention(got, q, k[half:], ks[:, half:].copy(), v[half:], vs[:, half:].copy(), offsets([rows]), offsets([half]), hk, hk, dh)
