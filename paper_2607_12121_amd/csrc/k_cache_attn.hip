@@ -220,10 +220,10 @@ FD_DEVICE Way build_tables(SchedTables& t, const fdh::CacheAttnArgs& g, int grou
 
 template <int DH>
 using Sched = fd::CacheSched<DH>;
-template <int DH>
+template <int DH, bool FEW_ONLY>   // FEW_ONLY: known to be so
 FD_DEVICE Sched<DH> schedule(const SchedTables* t, const fdh::CacheAttnArgs& g, const Way& way) {
   return Sched<DH>(t, g.cu_q, g.tok_off, g.n_req, g.kv_heads, static_cast<int>(gridDim.x), (g.max_req_tokens + KB - 1) / KB,
-                   fd::uniform(static_cast<int>(way.few)) != 0, g.may_cut, fd::uniform(way.extra));
+                   FEW_ONLY || fd::uniform(static_cast<int>(way.few)) != 0, g.may_cut, FEW_ONLY ? 0 : fd::uniform(way.extra));
 }
 
 // The cut item whose first piece a workgroup has, for the join; no pieces: none.  Every workgroup writes its own.
@@ -571,11 +571,16 @@ FD_DEVICE void tile_piece(const fdh::CacheAttnArgs& g, int group, float scale_lo
 
 // Key steps [s0, s1) of 32 rows; the piece's slot holds O / sum [32][DH] and (maximum, sum) [32].
 template <int DH>
-FD_DEVICE void few_piece(const fdh::CacheAttnArgs& g, int group, float scale_log2, const Lane<DH>& ln, uint4* ring, uint32_t lds, int head,
-                         int tile, int b, int s0, int s1, int slot_no) {
+FD_DEVICE void few_piece(const fdh::CacheAttnArgs& g, int group, float scale_log2, uint4* ring, uint32_t lds, int head, int tile, int b, int s0,
+                         int s1, int slot_no) {
   using C = Cfg<DH>;
   constexpr int DT = C::DT, KS = C::KS, KCH = C::KCH;
-  const int tid = threadIdx.x, lane = tid & 63, wave = fd::uniform(tid >> 6), l32 = lane & 31, lg = lane >> 5;
+  // Formed anew for each piece: kept from one to the next, the lane's addresses were spilled, and what read them back waited for
+  // every load under way.
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  const int lane = tid & 63, wave = fd::uniform(tid >> 6), l32 = lane & 31, lg = lane >> 5;
+  const Lane<DH> ln(lane);
   const int k_beg = g.tok_off[b], k_end = g.tok_off[b + 1], ldk = g.kv_heads * DH;
   const RowAt me = row_at<DH>(g, group, b, head, tile * C::QF + l32);
   // A tile's codes come 16 a lane, whole rows side by side.  K's go to LDS as they are and come back as fragments: the
@@ -755,8 +760,8 @@ __global__ __launch_bounds__(Cfg<DH>::THREADS) __attribute__((amdgpu_waves_per_e
       const long long per = static_cast<long long>(g.heads) * DH / 8, end = per * g.cu_q[b + 1];
       for (long long i = per * g.cu_q[b] + tid; i < end; i += C::THREADS) reinterpret_cast<uint4*>(g.o)[i] = make_uint4(0, 0, 0, 0);
     }
-  const bool few = fd::uniform(static_cast<int>(way.few)) != 0;
-  const Sched<DH> sch = schedule<DH>(&tabs, g, way);
+  const bool few = FEW_ONLY || fd::uniform(static_cast<int>(way.few)) != 0;
+  const Sched<DH> sch = schedule<DH, FEW_ONLY>(&tabs, g, way);
   if (tid == 0 && g.may_cut) g_cut_items(g)[blockIdx.x] = CutItem{};
   if (sch.work == 0) return;
   const float scale_log2 = g.scale * 1.4426950408889634f;
@@ -771,12 +776,13 @@ __global__ __launch_bounds__(Cfg<DH>::THREADS) __attribute__((amdgpu_waves_per_e
     long long i_start;
     int n, head, b, first, tau;
     sch.locate(p, i_start, n, head, b, first, tau);
+    b = fd::uniform(b);   // what it indexes comes through the scalar cache
     const int s0 = static_cast<int>(p - i_start), s1 = static_cast<int>(min(p_end, i_start + n) - i_start);
     const int slot = sch.cut ? sch.slot_of(w, s0, s1, n) : -1;
     if (tid == 0 && slot >= 0 && s0 == 0)   // its first piece
       g_cut_items(g)[blockIdx.x] = CutItem{sch.last_share(i_start + n) - w + 1, w, head, b, 2 * (tau - first) + few};
     const int t0 = sch.tile(s0), t1 = sch.tile(s1);
-    if (FEW_ONLY || few) few_piece<DH>(g, group, scale_log2, ln, ring, lds, head, tau - first, b, t0, t1, slot);
+    if (FEW_ONLY || few) few_piece<DH>(g, group, scale_log2, ring, lds, head, tau - first, b, t0, t1, slot);
     else if constexpr (!FEW_ONLY) tile_piece<DH>(g, group, scale_log2, ln, lds, head, tau - first, b, t0, t1, slot);
     p = i_start + s1;
   }
