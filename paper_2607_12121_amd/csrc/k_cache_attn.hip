@@ -352,11 +352,14 @@ struct Lane {   // addressing that does not depend on the work
 // Key tiles [kt0, kt1) of query tile `tile` of request b under key head `head`, to the outputs or, of a cut item, to
 // scratch slot `slot_no`.
 template <int DH>
-FD_DEVICE void tile_piece(const fdh::CacheAttnArgs& g, int group, float scale_log2, const Lane<DH>& ln, uint32_t lds, int head, int tile,
-                          int b, int kt0, int kt1, int slot_no) {
+FD_DEVICE void tile_piece(const fdh::CacheAttnArgs& g, int group, float scale_log2, uint32_t lds, int head, int tile, int b, int kt0, int kt1,
+                          int slot_no) {
   using C = Cfg<DH>;
   constexpr int DT = C::DT, KS = C::KS, KCH = C::KCH;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, lg = lane >> 5;
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  const int lane = tid & 63, wave = tid >> 6, l32 = lane & 31, lg = lane >> 5;
+  const Lane<DH> ln(lane);
   const int k_beg = g.tok_off[b], k_end = g.tok_off[b + 1], nkt = kt1 - kt0, ldk = g.kv_heads * DH;
   const RowAt me = row_at<DH>(g, group, b, head, tile * C::QB + 32 * wave + l32);
   bf16x8_t qf[KS];
@@ -766,7 +769,6 @@ __global__ __launch_bounds__(Cfg<DH>::THREADS) __attribute__((amdgpu_waves_per_e
   if (sch.work == 0) return;
   const float scale_log2 = g.scale * 1.4426950408889634f;
   const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr_t)&ring[0]));
-  const Lane<DH> ln(tid & 63);
   // waves w and w + WAVES / 2 share a SIMD: the second issues first when both are ready, so that the pair drifts apart
   if (__builtin_amdgcn_readfirstlane(tid >> 6) >= C::WAVES / 2) __builtin_amdgcn_s_setprio(1);
   const int w = sch.share(static_cast<int>(blockIdx.x));
@@ -783,7 +785,7 @@ __global__ __launch_bounds__(Cfg<DH>::THREADS) __attribute__((amdgpu_waves_per_e
       g_cut_items(g)[blockIdx.x] = CutItem{sch.last_share(i_start + n) - w + 1, w, head, b, 2 * (tau - first) + few};
     const int t0 = sch.tile(s0), t1 = sch.tile(s1);
     if (FEW_ONLY || few) few_piece<DH>(g, group, scale_log2, ring, lds, head, tau - first, b, t0, t1, slot);
-    else if constexpr (!FEW_ONLY) tile_piece<DH>(g, group, scale_log2, ln, lds, head, tau - first, b, t0, t1, slot);
+    else if constexpr (!FEW_ONLY) tile_piece<DH>(g, group, scale_log2, lds, head, tau - first, b, t0, t1, slot);
     p = i_start + s1;
   }
 }
