@@ -101,12 +101,16 @@ struct Lengths {
   }
 };
 
+// The schedule's tables, and the requests' first rows and tokens: from LDS they are there 1 us before they would be from memory.
+struct Tables : SchedTables {
+  int q0[fd::kMaxSchedRequests + 1], k0[fd::kMaxSchedRequests + 1];
+};
 // What the schedule is built from, by every workgroup alike: the way, and the prefix tables of its items and key steps over the
 // requests.  Up to a wave's lanes of requests, each wave reads them at once and counts in scalar registers (1024 rows of
 // one request 32.7 -> 31.3 us); more: each thread takes a run of requests, the runs' sums are scanned over the waves and the workgroup.
 struct Way { bool few, empty; int extra; };   // empty: a request has rows but no keys; extra: key steps that an item's start counts for
 template <int DH>
-FD_DEVICE Way build_tables(SchedTables& t, const fdh::CacheAttnArgs& g, int group) {
+FD_DEVICE Way build_tables(Tables& t, const fdh::CacheAttnArgs& g, int group) {
   using C = Cfg<DH>;
   constexpr int NW = C::WAVES;
   __shared__ int s_items[2][NW], s_empty[NW];
@@ -115,7 +119,8 @@ FD_DEVICE Way build_tables(SchedTables& t, const fdh::CacheAttnArgs& g, int grou
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (g.n_req <= 64) {
     const bool mine = lane < g.n_req;
-    const int at = mine ? lane : 0, rows = mine ? len.rows(at) : 0, keys = mine ? len.keys(at) : 0;
+    const int at = mine ? lane : 0, q0 = g.cu_q[at], q1 = g.cu_q[at + 1], k0 = g.tok_off[at], k1 = g.tok_off[at + 1];
+    const int rows = mine ? (q1 - q0) * group : 0, keys = mine ? k1 - k0 : 0;
     const bool has = rows > 0 && keys > 0;
     const int few = has ? (rows + C::QF - 1) / C::QF : 0, tiles = has ? (rows + C::QB - 1) / C::QB : 0;
     int all_few = 0, all_tiles = 0;
@@ -140,9 +145,13 @@ FD_DEVICE Way build_tables(SchedTables& t, const fdh::CacheAttnArgs& g, int grou
     if (wave == 0 && mine) {
       t.tpre[lane] = mine_i;
       t.wpre[lane] = mine_s;
-      if (lane == 0) {
+      t.q0[lane] = q0;
+      t.k0[lane] = k0;
+      if (lane == g.n_req - 1) {
         t.tpre[g.n_req] = pi;
         t.wpre[g.n_req] = ps;
+        t.q0[g.n_req] = q1;
+        t.k0[g.n_req] = k1;
       }
     }
     __syncthreads();
@@ -206,6 +215,8 @@ FD_DEVICE Way build_tables(SchedTables& t, const fdh::CacheAttnArgs& g, int grou
   for (int b = b0; b < b1; ++b) {
     t.tpre[b] = pi;
     t.wpre[b] = ps;
+    t.q0[b] = g.cu_q[b];
+    t.k0[b] = g.tok_off[b];
     const int n = len.items(b, qb);
     pi += n;
     ps += static_cast<long long>(n) * ((len.keys(b) + kb - 1) / kb + more);
@@ -213,6 +224,8 @@ FD_DEVICE Way build_tables(SchedTables& t, const fdh::CacheAttnArgs& g, int grou
   if (b0 < b1 && b1 == g.n_req) {
     t.tpre[g.n_req] = pi;
     t.wpre[g.n_req] = ps;
+    t.q0[g.n_req] = g.cu_q[g.n_req];
+    t.k0[g.n_req] = g.tok_off[g.n_req];
   }
   __syncthreads();
   return way;
@@ -230,13 +243,14 @@ FD_DEVICE Sched<DH> schedule(const SchedTables* t, const fdh::CacheAttnArgs& g, 
 struct CutItem { int pieces, share, head, request, tile_few; };
 FD_DEVICE CutItem* g_cut_items(const fdh::CacheAttnArgs& g) { return static_cast<CutItem*>(g.cut_items); }
 
+// A request: its first query and rows under a key head, its first key and the one behind its last.
+struct Request { int q0, rows, k_beg, k_end; };
 // One lane's row of an item: where its query (and result) begins, and whether there is one.
 struct RowAt { size_t at; bool live; };
 template <int DH>
-FD_DEVICE RowAt row_at(const fdh::CacheAttnArgs& g, int group, int b, int head, int r) {
-  const int q0 = g.cu_q[b], rows = (g.cu_q[b + 1] - q0) * group;
+FD_DEVICE RowAt row_at(const fdh::CacheAttnArgs& g, int group, const Request& of, int head, int r) {
   const int query = group == 1 ? r : r / group;
-  return {(static_cast<size_t>(q0 + query) * g.heads + static_cast<size_t>(head) * group + (r - query * group)) * DH, r < rows};
+  return {(static_cast<size_t>(of.q0 + query) * g.heads + static_cast<size_t>(head) * group + (r - query * group)) * DH, r < of.rows};
 }
 
 // This lane's part of O^T blocks as a bf16 row: register 4 r4 + e of block dt is d = 32 dt + 8 r4 + 4 lg + e.
@@ -349,19 +363,19 @@ struct Lane {   // addressing that does not depend on the work
 
 // ---------------------------------------------------------------- tiles
 
-// Key tiles [kt0, kt1) of query tile `tile` of request b under key head `head`, to the outputs or, of a cut item, to
+// Key tiles [kt0, kt1) of query tile `tile` of a request under key head `head`, to the outputs or, of a cut item, to
 // scratch slot `slot_no`.
 template <int DH>
-FD_DEVICE void tile_piece(const fdh::CacheAttnArgs& g, int group, float scale_log2, uint32_t lds, int head, int tile, int b, int kt0, int kt1,
-                          int slot_no) {
+FD_DEVICE void tile_piece(const fdh::CacheAttnArgs& g, int group, float scale_log2, uint32_t lds, int head, int tile, const Request& of, int kt0,
+                          int kt1, int slot_no) {
   using C = Cfg<DH>;
   constexpr int DT = C::DT, KS = C::KS, KCH = C::KCH;
   int tid = threadIdx.x;
   asm volatile("" : "+v"(tid));
   const int lane = tid & 63, wave = tid >> 6, l32 = lane & 31, lg = lane >> 5;
   const Lane<DH> ln(lane);
-  const int k_beg = g.tok_off[b], k_end = g.tok_off[b + 1], nkt = kt1 - kt0, ldk = g.kv_heads * DH;
-  const RowAt me = row_at<DH>(g, group, b, head, tile * C::QB + 32 * wave + l32);
+  const int k_beg = of.k_beg, k_end = of.k_end, nkt = kt1 - kt0, ldk = g.kv_heads * DH;
+  const RowAt me = row_at<DH>(g, group, of, head, tile * C::QB + 32 * wave + l32);
   bf16x8_t qf[KS];
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
@@ -574,8 +588,8 @@ FD_DEVICE void tile_piece(const fdh::CacheAttnArgs& g, int group, float scale_lo
 
 // Key steps [s0, s1) of 32 rows; the piece's slot holds O / sum [32][DH] and (maximum, sum) [32].
 template <int DH>
-FD_DEVICE void few_piece(const fdh::CacheAttnArgs& g, int group, float scale_log2, uint4* ring, uint32_t lds, int head, int tile, int b, int s0,
-                         int s1, int slot_no) {
+FD_DEVICE void few_piece(const fdh::CacheAttnArgs& g, int group, float scale_log2, uint4* ring, uint32_t lds, int head, int tile,
+                         const Request& of, int s0, int s1, int slot_no) {
   using C = Cfg<DH>;
   constexpr int DT = C::DT, KS = C::KS, KCH = C::KCH;
   // Formed anew for each piece: kept from one to the next, the lane's addresses were spilled, and what read them back waited for
@@ -584,8 +598,8 @@ FD_DEVICE void few_piece(const fdh::CacheAttnArgs& g, int group, float scale_log
   asm volatile("" : "+v"(tid));
   const int lane = tid & 63, wave = fd::uniform(tid >> 6), l32 = lane & 31, lg = lane >> 5;
   const Lane<DH> ln(lane);
-  const int k_beg = g.tok_off[b], k_end = g.tok_off[b + 1], ldk = g.kv_heads * DH;
-  const RowAt me = row_at<DH>(g, group, b, head, tile * C::QF + l32);
+  const int k_beg = of.k_beg, k_end = of.k_end, ldk = g.kv_heads * DH;
+  const RowAt me = row_at<DH>(g, group, of, head, tile * C::QF + l32);
   // A tile's codes come 16 a lane, whole rows side by side.  K's go to LDS as they are and come back as fragments: the
   // contraction's order is free, so that a lane's two steps 2 j and 2 j + 1 take its chunk 2 j + lg of the key's row (head dim 16,
   // of one step: 8 codes of the chunk).  V's go there as values, head dim 128 half the keys at a time.
@@ -715,7 +729,7 @@ FD_DEVICE void few_piece(const fdh::CacheAttnArgs& g, int group, float scale_log
     }
   if (lg == 0) ml[wave * 32 + l32] = f32x2_t{m_run, l_run};
   __syncthreads();
-  const int rows = min(C::QF, (g.cu_q[b + 1] - g.cu_q[b]) * group - tile * C::QF);
+  const int rows = min(C::QF, of.rows - tile * C::QF);
   float* slot = g.partial + static_cast<size_t>(max(slot_no, 0)) * C::FEW_SLOT;
   for (int i = tid; i < rows * (DH / 4); i += C::THREADS) {
     const int r = i / (DH / 4), d0 = i % (DH / 4) * 4;
@@ -735,7 +749,7 @@ FD_DEVICE void few_piece(const fdh::CacheAttnArgs& g, int group, float scale_log
     const float inv = slot_no >= 0 && l == 0.f ? 0.f : 1.0f / l;
     sum = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
     if (slot_no < 0) {
-      const RowAt to = row_at<DH>(g, group, b, head, tile * C::QF + r);
+      const RowAt to = row_at<DH>(g, group, of, head, tile * C::QF + r);
       *reinterpret_cast<uint2*>(g.o + to.at + d0) = make_uint2(fd::pack_bf2(sum.x, sum.y), fd::pack_bf2(sum.z, sum.w));
     } else {
       *reinterpret_cast<float4*>(slot + r * DH + d0) = sum;
@@ -753,7 +767,7 @@ __global__ __launch_bounds__(Cfg<DH>::THREADS) __attribute__((amdgpu_waves_per_e
   constexpr int kTileBytes = FEW_ONLY ? 0 : 4 * C::TILE * 16, kFewBytes = C::WAVES * C::FEW_WAVE_BYTES, kJoinBytes = C::WAVES * 32 * ((DH + 4) * 4 + 8);
   constexpr int kMore = kFewBytes > kJoinBytes ? kFewBytes : kJoinBytes, kBytes = kMore > kTileBytes ? kMore : kTileBytes;
   __shared__ __align__(256) uint4 ring[(kBytes + 15) / 16];   // chunk addresses are formed by exclusive or
-  __shared__ SchedTables tabs;
+  __shared__ Tables tabs;
   const int group = fd::uniform(g.heads / g.kv_heads);
   const Way way = build_tables<DH>(tabs, g, group);
   const int tid = threadIdx.x;
@@ -778,14 +792,14 @@ __global__ __launch_bounds__(Cfg<DH>::THREADS) __attribute__((amdgpu_waves_per_e
     long long i_start;
     int n, head, b, first, tau;
     sch.locate(p, i_start, n, head, b, first, tau);
-    b = fd::uniform(b);   // what it indexes comes through the scalar cache
     const int s0 = static_cast<int>(p - i_start), s1 = static_cast<int>(min(p_end, i_start + n) - i_start);
     const int slot = sch.cut ? sch.slot_of(w, s0, s1, n) : -1;
+    const int t0 = sch.tile(s0), t1 = sch.tile(s1), q0 = fd::uniform(tabs.q0[b]);
+    const Request of{q0, (fd::uniform(tabs.q0[b + 1]) - q0) * group, fd::uniform(tabs.k0[b]), fd::uniform(tabs.k0[b + 1])};
+    if (FEW_ONLY || few) few_piece<DH>(g, group, scale_log2, ring, lds, head, tau - first, of, t0, t1, slot);
+    else if constexpr (!FEW_ONLY) tile_piece<DH>(g, group, scale_log2, lds, head, tau - first, of, t0, t1, slot);
     if (tid == 0 && slot >= 0 && s0 == 0)   // its first piece
       g_cut_items(g)[blockIdx.x] = CutItem{sch.last_share(i_start + n) - w + 1, w, head, b, 2 * (tau - first) + few};
-    const int t0 = sch.tile(s0), t1 = sch.tile(s1);
-    if (FEW_ONLY || few) few_piece<DH>(g, group, scale_log2, ring, lds, head, tau - first, b, t0, t1, slot);
-    else if constexpr (!FEW_ONLY) tile_piece<DH>(g, group, scale_log2, lds, head, tau - first, b, t0, t1, slot);
     p = i_start + s1;
   }
 }
@@ -840,21 +854,22 @@ __global__ __launch_bounds__(Cfg<DH>::THREADS) void cache_join_kernel(fdh::Cache
   using C = Cfg<DH>;
   const CutItem it = g_cut_items(g)[blockIdx.x];
   if (it.pieces == 0) return;
-  const int group = g.heads / g.kv_heads, few = it.tile_few & 1, tile = it.tile_few >> 1, head = it.head, b = it.request, x = it.share;
+  const int group = g.heads / g.kv_heads, few = it.tile_few & 1, tile = it.tile_few >> 1, head = it.head, b = it.request, x = it.share, first = g.cu_q[b];
+  const Request of{first, (g.cu_q[b + 1] - first) * group, 0, 0};
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, lg = lane >> 5;
   auto slot = [&](int j, int floats) { return g.partial + static_cast<size_t>(Sched<DH>::slot_at(x, j)) * floats; };
   if (few) {
-    const int rows = min(C::QF, (g.cu_q[b + 1] - g.cu_q[b]) * group - tile * C::QF);
+    const int rows = min(C::QF, of.rows - tile * C::QF);
     for (int i = blockIdx.y * C::THREADS + tid; i < rows * (DH / 4); i += gridDim.y * C::THREADS) {
       const int r = i / (DH / 4), d0 = i % (DH / 4) * 4;
       Joined<1> sum;
       sum.template add<24>(it.pieces, [&](int j) { return reinterpret_cast<const f32x2_t*>(slot(j, C::FEW_SLOT) + 32 * DH)[r]; },
                            [&](int j, int) { return *reinterpret_cast<const float4*>(slot(j, C::FEW_SLOT) + r * DH + d0); });
-      *reinterpret_cast<uint2*>(g.o + row_at<DH>(g, group, b, head, tile * C::QF + r).at + d0) = sum.row(0);
+      *reinterpret_cast<uint2*>(g.o + row_at<DH>(g, group, of, head, tile * C::QF + r).at + d0) = sum.row(0);
     }
     return;
   }
-  const RowAt me = row_at<DH>(g, group, b, head, tile * C::QB + 32 * wave + l32);
+  const RowAt me = row_at<DH>(g, group, of, head, tile * C::QB + 32 * wave + l32);
   if (!me.live) return;
   const int q0 = blockIdx.y * 2;   // this workgroup's quads q0 and q0 + 1: d = 8 q + 4 lg ..
   Joined<2> sum;
