@@ -599,20 +599,11 @@ FD_DEVICE void few_piece(const fdh::CacheAttnArgs& g, int group, float scale_log
   const int lane = tid & 63, wave = fd::uniform(tid >> 6), l32 = lane & 31, lg = lane >> 5;
   const Lane<DH> ln(lane);
   const int k_beg = of.k_beg, k_end = of.k_end, ldk = g.kv_heads * DH;
-  const RowAt me = row_at<DH>(g, group, of, head, tile * C::QF + l32);
   // A tile's codes come 16 a lane, whole rows side by side.  K's go to LDS as they are and come back as fragments: the
   // contraction's order is free, so that a lane's two steps 2 j and 2 j + 1 take its chunk 2 j + lg of the key's row (head dim 16,
   // of one step: 8 codes of the chunk).  V's go there as values, head dim 128 half the keys at a time.
   constexpr int PER_ROW = DH / 16, ROWS = 64 / PER_ROW, N = KB / ROWS;   // ROWS rows a load, N loads
   constexpr int VH = C::VHALVES;
-  bf16x8_t qf[KS];
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks) {
-    u32x4_t t = {0, 0, 0, 0};
-    const int d = DH == 16 ? 8 * lg : 16 * (2 * (ks >> 1) + lg) + 8 * (ks & 1);
-    if (me.live) t = *reinterpret_cast<const u32x4_t*>(g.q + me.at + d);
-    qf[ks] = __builtin_bit_cast(bf16x8_t, t);
-  }
   // The lane's rows of a load are ROWS apart, which leaves the swizzles: addresses are a base and a constant.
   const int lrow = lane / PER_ROW, lc = lane % PER_ROW;
   auto kswz = [](int r) { return PER_ROW == 8 ? (r & 7) : PER_ROW == 4 ? ((r >> 1) & 3) : 0; };
@@ -641,6 +632,7 @@ FD_DEVICE void few_piece(const fdh::CacheAttnArgs& g, int group, float scale_log
   };
   f32x16_t o[DT] = {};
   float m_run = -INFINITY, l_run = 0.f;
+  bf16x8_t qf[KS];
   u32x4_t xk[N], xv[N];
   uint32_t sk, sv;
   auto own_lds = [] { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
@@ -710,6 +702,12 @@ FD_DEVICE void few_piece(const fdh::CacheAttnArgs& g, int group, float scale_log
   int key0 = k_beg + s0 * C::FEW_KEYS + wave * KB;
   if (key0 < key_end) {
     fetch(g.k, ksc, key0, xk, sk);
+    // rows past the last repeat it; without branches, as what stands here costs its fetch from memory (a call of a few MB has the L2
+    // full of something else)
+    const uint16_t* q = g.q + row_at<DH>(g, group, of, head, min(tile * C::QF + l32, of.rows - 1)).at;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      qf[ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(q + (DH == 16 ? 8 * lg : 16 * (2 * (ks >> 1) + lg) + 8 * (ks & 1))));
     fetch(g.v, vsc, key0, xv, sv);
     for (; key0 < key_end; key0 += C::FEW_KEYS) step(key0, min(key0 + C::FEW_KEYS, k_end - 1));   // the last one fetches in vain
   }
