@@ -458,24 +458,26 @@ def _pointers(stream: Optional[torch.cuda.Stream], *args) -> list:
     the current device, the one the call runs on; returns the tensors' addresses and the stream's handle.  One
     pass of cheap tests, as these calls take microseconds on the GPU; what fails is named by the slow path.
     An element count below 0 marks an optional tensor of minus that many elements."""
-    cur = None
-    out = []
+    cur, out, kinds = None, [], _KIND
+    put = out.append
     for name, t, kind, n in args:
         if t is None:
             if n >= 0:
                 raise FlashDiffError(f"{name} is required")
-            out.append(None)
+            put(None)
             continue
+        if n < 0:
+            n = -n
         if cur is None:
             if not t.is_cuda:
-                _need(name, t, kind, abs(n))
+                _need(name, t, kind, n)
             cur = torch.cuda.current_device()
-        if t.get_device() != cur or t.dtype not in _KIND[kind] or t.numel() < (n if n >= 0 else -n) or not t.is_contiguous():
-            _need(name, t, kind, abs(n))
+        if t.get_device() != cur or t.dtype not in kinds[kind] or t.numel() < n or not t.is_contiguous():
+            _need(name, t, kind, n)
             if t.get_device() != cur:
                 raise FlashDiffError(f"{name} is on {t.device}, the current device is {cur}")
             _ptr(t)
-        out.append(t.data_ptr())
+        put(t.data_ptr())
     if stream is None:
         out.append(_current_stream(cur))
     elif stream.device.index != cur:
@@ -497,15 +499,18 @@ def fd_quant_blocks(x, block_rows: int, q, scale, m=None, stream=None) -> None:
 
 def _modulation(h, B: int, D: int, *parts):
     """(row stride, addresses) of a request's gate, shift and scale: fp32 [B, D] on h's device, or None."""
-    stride, mod = 0, [None] * len(parts)
-    given = [(i, t) for i, t in enumerate(parts) if t is not None]
-    if given:
-        stride, dev = given[0][1].stride(0), h.get_device()
-        for i, t in given:
-            if t.shape != (B, D) or t.stride() != (stride, 1) or stride > 1 << 30 or t.dtype != torch.float32 or t.get_device() != dev:
-                raise FlashDiffError(f"gate, shift and mod_scale must be fp32 [{B}, {D}] with contiguous rows of one stride, on {h.device}")
-            mod[i] = t.data_ptr()
-    return stride, mod
+    stride, mod = None, []
+    for t in parts:
+        if t is None:
+            mod.append(None)
+            continue
+        steps = t.stride()
+        if stride is None:
+            stride, dev, want = steps[0], h.get_device(), (B, D)
+        if t.shape != want or steps != (stride, 1) or stride > 1 << 30 or t.dtype is not torch.float32 or t.get_device() != dev:
+            raise FlashDiffError(f"gate, shift and mod_scale must be fp32 [{B}, {D}] with contiguous rows of one stride, on {h.device}")
+        mod.append(t.data_ptr())
+    return stride or 0, mod
 
 
 def fd_rms_quant(h, q, scale, cu_q, m, y=None, gate=None, weight=None, shift=None, mod_scale=None, eps: float = 1e-6,
