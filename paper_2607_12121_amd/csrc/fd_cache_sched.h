@@ -14,11 +14,14 @@ FD_RULE constexpr int cache_tile_rows(int dh) { return dh >= 64 ? 256 : 128; }  
 FD_RULE constexpr int cache_few_keys(int dh) { return 2 * cache_tile_rows(dh); }    // keys of a step of few rows
 
 // Few rows rather than tiles, by the items that each way has: all waves of a workgroup work on the same 32 rows, each on keys of
-// its own, where tiles would leave most waves without rows.  12 heads of 128 over 32760 keys, us, few rows and tiles: 96 rows
-// (3 items and 1 a head) 62 and 72, 128 rows 78 and 71.
-FD_RULE bool cache_few_rows(int few, int tiles) { return few <= 3 * tiles; }
+// its own, where tiles would leave most waves without rows.  One request, us, few rows and tiles: 12 heads of 128 over 32760 keys,
+// 64 rows (2 items of few rows a head, 1 of tiles) 52 and 62, 96 rows (3) 57 and 63, 128 rows (4) 76 and 66; 24 heads of 64 over
+// 20000 keys, 64 rows 45 and 48, 96 rows 53 and 48, and 16 heads over 2 requests of 10000 keys, 128 rows (5 and 2) 25 and 28; 24
+// heads of 16 over 8000 keys, 96 rows 20 and 22, 128 rows 22 and 22.5.
+FD_RULE constexpr int cache_few_half_items(int dh) { return dh == 64 ? 5 : 6; }   // per item of tiles, twice
+FD_RULE bool cache_few_rows(int dh, int few, int tiles) { return 2LL * few <= static_cast<long long>(cache_few_half_items(dh)) * tiles; }
 // Whether every call of at most `rows` rows is of few.
-FD_RULE bool cache_always_few(long long rows) { return rows <= 3 * kFewRows; }
+FD_RULE bool cache_always_few(int dh, long long rows) { return rows <= cache_few_half_items(dh) / 2 * kFewRows; }
 
 // Key tiles that the start of an item of tiles counts for in the shares: its queries and first key tiles on their way.  Every share
 // has one start; where shares have several items, those of short ones would end late (a packed batch 276 -> 254 us).

@@ -128,7 +128,7 @@ FD_DEVICE Way build_tables(Tables& t, const fdh::CacheAttnArgs& g, int group) {
       all_few += __builtin_amdgcn_readlane(few, b);
       all_tiles += __builtin_amdgcn_readlane(tiles, b);
     }
-    const bool is_few = fd::cache_few_rows(all_few, all_tiles);
+    const bool is_few = fd::cache_few_rows(DH, all_few, all_tiles);
     const Way way{is_few, __any(rows > 0 && keys <= 0) != 0, is_few ? 0 : fd::cache_item_steps(static_cast<long long>(all_tiles) * g.kv_heads, static_cast<int>(gridDim.x))};
     const int kb = is_few ? C::FEW_KEYS : KB, items = is_few ? few : tiles, steps = has ? (keys + kb - 1) / kb + way.extra : 0;
     int pi = 0, mine_i = 0;
@@ -179,7 +179,7 @@ FD_DEVICE Way build_tables(Tables& t, const fdh::CacheAttnArgs& g, int group) {
     tiles += s_items[1][w];
     empty |= s_empty[w];
   }
-  const bool is_few = fd::cache_few_rows(few, tiles);
+  const bool is_few = fd::cache_few_rows(DH, few, tiles);
   const Way way{is_few, empty != 0, is_few ? 0 : fd::cache_item_steps(static_cast<long long>(tiles) * g.kv_heads, static_cast<int>(gridDim.x))};
   const int qb = way.few ? C::QF : C::QB, kb = way.few ? C::FEW_KEYS : KB, more = way.extra;
   int it = 0;
@@ -896,7 +896,7 @@ size_t cut_items_bytes(int dh) { return (cache_grid(dh) * sizeof(CutItem) + 255)
 
 size_t cache_attention_scratch_bytes(int n_rows, int heads, int kv_heads, int dh) {
   // two slots per share: 32 rows where no call of these rows runs in tiles
-  const bool few = fd::cache_always_few(static_cast<long long>(n_rows) * (heads / kv_heads));
+  const bool few = fd::cache_always_few(dh, static_cast<long long>(n_rows) * (heads / kv_heads));
   const size_t floats = few ? 32 * (dh + 2) : static_cast<size_t>(2 * fd::cache_tile_rows(dh)) * ((dh + 31) / 32 * 16 + 2);
   return cut_items_bytes(dh) + 2 * static_cast<size_t>(cache_grid(dh)) * floats * sizeof(float);
 }
@@ -908,7 +908,7 @@ hipError_t launch_cache_attention(const CacheAttnArgs& args, hipStream_t s) {
   g.may_cut = g.max_req_tokens > fd::cache_few_keys(g.dh);
   auto run = [&](auto tag) {
     constexpr int DH = decltype(tag)::value;
-    if (fd::cache_always_few(static_cast<long long>(g.n_rows) * (g.heads / g.kv_heads))) cache_attn_kernel<DH, true><<<cache_grid(DH), Cfg<DH>::THREADS, 0, s>>>(g);
+    if (fd::cache_always_few(DH, static_cast<long long>(g.n_rows) * (g.heads / g.kv_heads))) cache_attn_kernel<DH, true><<<cache_grid(DH), Cfg<DH>::THREADS, 0, s>>>(g);
     else cache_attn_kernel<DH, false><<<cache_grid(DH), Cfg<DH>::THREADS, 0, s>>>(g);
     if (g.may_cut) cache_join_kernel<DH><<<dim3(cache_grid(DH), Cfg<DH>::JOIN_PARTS), Cfg<DH>::THREADS, 0, s>>>(g);
   };

@@ -124,7 +124,7 @@ def test_attention_workspace():
         assert size(*bad) == 0
     # calls that only run with few rows need less
     assert 0 < size(96, 2, 2, 128) < size(97, 2, 2, 128) == size(1 << 20, 2, 2, 128)
-    assert size(24, 8, 2, 64) < size(25, 8, 2, 64)
+    assert size(16, 8, 2, 64) < size(17, 8, 2, 64)
 
 
 def test_bindings_refuse():
@@ -201,8 +201,8 @@ int cache_pieces(int dh, int few, int may_cut, const int32_t* cu, const int32_t*
                                                                                                   : pieces<128>(few, may_cut, cu, tok, B, group, H, G, nkv_max, out, cap);
 }
 int slot_at(int x, int j) { return fd::CacheSched<64>::slot_at(x, j); }
-int few_rows(int few, int tiles) { return fd::cache_few_rows(few, tiles); }
-int always_few(long long rows) { return fd::cache_always_few(rows); }
+int few_rows(int dh, int few, int tiles) { return fd::cache_few_rows(dh, few, tiles); }
+int always_few(int dh, long long rows) { return fd::cache_always_few(dh, rows); }
 }
 """
 
@@ -269,13 +269,15 @@ def test_schedule_of_a_video_row(shim):
     assert np.all(np.bincount(rows[:, 0], weights=rows[:, 5] - rows[:, 4]) == 3)
 
 
-def test_few_rows_rule(shim):
-    assert shim.few_rows(3, 1) and not shim.few_rows(4, 1)
+@pytest.mark.parametrize("dh,most", [(16, 3), (64, 2), (128, 3)])
+def test_few_rows_rule(shim, dh, most):
+    assert shim.few_rows(dh, most, 1) and not shim.few_rows(dh, most + 1, 1)
+    assert shim.always_few(dh, ctypes.c_longlong(32 * most)) and not shim.always_few(dh, ctypes.c_longlong(32 * most + 1))
     for rows in range(1, 200):      # always_few: however the rows are spread over requests
         for parts in (1, 2, 5):
             q = [rows // parts + (i < rows % parts) for i in range(parts)]
-            few, tiles = sum(-(-n // 32) for n in q), sum(-(-n // 128) for n in q)
-            assert not shim.always_few(ctypes.c_longlong(rows)) or shim.few_rows(few, tiles)
+            few, tiles = sum(-(-n // 32) for n in q), sum(-(-n // (256 if dh >= 64 else 128)) for n in q)
+            assert not shim.always_few(dh, ctypes.c_longlong(rows)) or shim.few_rows(dh, few, tiles)
 
 
 def test_no_vector_memory_read_of_a_fresh_scalar(tmp_path):
