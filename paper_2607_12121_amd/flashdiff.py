@@ -535,11 +535,14 @@ def rope_axes(dims: Sequence[int], theta=10000.0, step=1.0, halves: bool = False
     n = len(dims)
     if not 1 <= n <= 4:
         raise FlashDiffError(f"{n} axes, not 1 to 4")
-    th, st = ([float(v)] * n if isinstance(v, (int, float)) else [float(u) for u in v] for v in (theta, step))
-    if len(th) != n or len(st) != n:
-        raise FlashDiffError("dims, theta and step must have one entry per axis")
-    pad = (0,) * (4 - n)
-    return FdRope(n, int(bool(halves)), _Axes(*dims, *pad), _Reals(*th, *pad), _Reals(*st, *pad))
+    r = FdRope(n, int(bool(halves)))    # the rest zeros
+    r.dim[:n] = tuple(dims)
+    for field, v in ((r.theta, theta), (r.step, step)):
+        per = (v,) * n if isinstance(v, (int, float)) else [float(u) for u in v]
+        if len(per) != n:
+            raise FlashDiffError("dims, theta and step must have one entry per axis")
+        field[:n] = per
+    return r
 
 
 def fd_rope_axes(qkv, coord, idx, m, q, k_cache, v_cache, heads: int, kv_heads: int, head_dim: int, dims=None, theta=10000.0,
