@@ -47,7 +47,7 @@ def test_search_finds_a_planted_pair():
     assert _overwritten(["buffer_store_dwordx2 v[80:81], v98, s[16:19], s67 offen", write]) == (0, [])
 
 
-@pytest.mark.parametrize("source,stores", [("k_int_gemm.hip", 40), ("k_scaled_gemm.hip", 40)])
+@pytest.mark.parametrize("source,stores", [("k_int_gemm.hip", 40), ("k_scaled_gemm.hip", 40), ("k_int_rows.hip", 40), ("k_rope.hip", 4), ("k_cache_attn.hip", 40)])
 def test_no_early_write_of_a_wide_stores_data(source, stores, tmp_path):
     out = tmp_path / "k.s"
     subprocess.run([build.hipcc(), *[f for f in build.HIPCC_FLAGS if f != "-Wall"], "--cuda-device-only", "-S",
