@@ -4,7 +4,7 @@
 #include <type_traits>
 
 #include "fd_int.h"
-#include "fd_scaled_rules.h"
+#include "fd_int_rules.h"
 #include "fd_tile_loads.h"
 
 namespace {
@@ -100,6 +100,143 @@ __global__ __launch_bounds__(kFewWaves * 64) void int_few_kernel(fdh::IntLinearA
     const size_t at = static_cast<size_t>(row) * g.N + col + 4 * j;
     if constexpr (WIDE) *reinterpret_cast<float4*>(g.y_f32 + at) = make_float4(v[0], v[1], v[2], v[3]);
     else *reinterpret_cast<uint2*>(g.y_bf16 + at) = make_uint2(fd::pack_bf2(v[0], v[1]), fd::pack_bf2(v[2], v[3]));
+  }
+}
+
+// ---------------------------------------------------------------- tiles of their own K-blocks
+
+// Few tiles: every wave of a workgroup has K-blocks of its own, every fourth, and the whole tile's sums of them (32 FI x 32 NJ);
+// the waves' sums, whole numbers, meet in LDS.  Operands come to the wave's own LDS, STAGES blocks ahead, by loads of whole
+// 128-byte rows, and each byte is read from there once: no barrier in the loop.  What bounds it is the loads to LDS (64 bytes a
+// clock and CU; 64 x 1536 x 6144 7.7 us, of which 4 are the start and the end).  The few-row kernel's loads take 16 bytes of 16 rows
+// side by side, which the L1 serves at a quarter of its rate (there 16.2 us); the tiles below, most CUs without one, 17.4.
+// Larger tiles, one stage: 512 x 1536 x 6144 in 64 x 128 20.8, in 128 x 128 31.6, where 64 x 64 take 13.3.
+template <int FI_, int NJ_, int STAGES_>
+struct IntSplit {
+  static constexpr int FI = FI_, NJ = NJ_, STAGES = STAGES_, WAVES = 4, THREADS = 64 * WAVES;
+  static constexpr int BM = 32 * FI, BN = 32 * NJ, LOADS_A = BM / 8, LOADS_W = BN / 8, ISSUED = LOADS_A + LOADS_W;   // 8 rows a wave-load
+  static constexpr int SLOT = (BM + BN) * kBlock;                   // bytes
+  static constexpr int SIDE = WAVES * STAGES * SLOT;                // column scales, bias and row scales, 64 each
+  static constexpr int TOTAL = (SIDE + 3 * 256) / 16;
+  static_assert(BM <= 64 && BN <= 64 && (STAGES - 1) * ISSUED < 64, "one load of scales, the counter's range");
+  static_assert(WAVES * FI * NJ * 4096 <= SIDE, "the waves' sums");
+  static FD_DEVICE int column(int p) { return NJ * (p & 31) + (p >> 5); }   // of LDS row p, so that a lane has NJ consecutive columns
+};
+
+template <bool WIDE, class T>
+__global__ __launch_bounds__(T::THREADS) void int_split_kernel(fdh::IntLinearArgs g) {
+  constexpr int FI = T::FI, NJ = T::NJ, STAGES = T::STAGES, WAVES = T::WAVES;
+  __shared__ uint4 ring[T::TOTAL];
+  const int M = g.m ? min(*g.m, g.n_rows) : g.n_rows, K = g.K, blocks = (K + kBlock - 1) / kBlock;
+  const int m0 = blockIdx.y * T::BM, n0 = blockIdx.x * T::BN;
+  if (m0 >= M) return;
+  const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5, l8 = lane >> 3;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t ring_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_ptr_t)ring)), wave_at = ring_at + wave * STAGES * T::SLOT;
+  const char* lds = reinterpret_cast<const char*>(ring);
+  const i32x4_t ra = buffer_of(g.a + static_cast<size_t>(m0) * K), rw = buffer_of(g.w + static_cast<size_t>(n0) * K);
+  if (wave == 0) {   // ahead of this wave's first stage; of zeros where there is no bias
+    dma4(ring_at + T::SIDE, static_cast<uint32_t>(n0 + lane) * 4, buffer_of(g.w_scale, 4u * g.N), 0);
+    dma4(ring_at + T::SIDE + 256, static_cast<uint32_t>(n0 + lane) * 4, buffer_of(g.bias, g.bias ? 4u * g.N : 0u), 0);
+    dma4(ring_at + T::SIDE + 512, static_cast<uint32_t>(lane) * 4, buffer_of(g.a_scale + m0, 4u * min(T::BM, M - m0)), 0);
+  }
+  // chunk c of LDS row r lies at c ^ swz(r) = c ^ ((r >> 1) & 7); this lane's chunk of the rows 8 q + l8, even q and odd
+  const int chunk = (lane & 7) ^ (l8 >> 1);
+  uint32_t off[T::ISSUED];
+#pragma unroll
+  for (int q = 0; q < T::LOADS_A; ++q) off[q] = static_cast<uint32_t>(min(8 * q + l8, M - m0 - 1)) * static_cast<uint32_t>(K) + 16 * (chunk ^ (4 * (q & 1)));
+#pragma unroll
+  for (int q = 0; q < T::LOADS_W; ++q)
+    off[T::LOADS_A + q] = static_cast<uint32_t>(min(T::column(8 * q + l8), g.N - n0 - 1)) * static_cast<uint32_t>(K) + 16 * (chunk ^ (4 * (q & 1)));
+  auto issue = [&](uint32_t slot_at, int b) {   // K-block b; chunks past K read zeros
+    const bool in[2] = {b * kBlock + 16 * chunk < K, b * kBlock + 16 * (chunk ^ 4) < K};
+    auto go = [&](auto self, auto i) {
+      constexpr int q = decltype(i)::value;
+      if constexpr (q < T::ISSUED) {
+        const uint32_t from = in[(q < T::LOADS_A ? q : q - T::LOADS_A) & 1] ? off[q] : kNowhere;
+        dma16<q * 1024>(wave_at + slot_at, from, q < T::LOADS_A ? ra : rw, static_cast<uint32_t>(b) * kBlock);
+        self(self, std::integral_constant<int, q + 1>{});
+      }
+    };
+    go(go, std::integral_constant<int, 0>{});
+  };
+#pragma unroll
+  for (int p = 0; p < STAGES; ++p) issue(p * T::SLOT, wave + p * WAVES);
+
+  uint32_t at[2][2];   // byte offsets in a slot of this lane's chunks of a half K-block; rows 32 on: 4096 bytes
+#pragma unroll
+  for (int kh = 0; kh < 2; ++kh)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) at[kh][c] = wave * STAGES * T::SLOT + l32 * kBlock + ((4 * kh + 2 * half + c) ^ ((l32 >> 1) & 7)) * 16;
+  auto read = [&](const char* lo_at, const char* hi_at) {
+    const uint4 lo = *reinterpret_cast<const uint4*>(lo_at), hi = *reinterpret_cast<const uint4*>(hi_at);
+    return i32x8_t{static_cast<int>(lo.x), static_cast<int>(lo.y), static_cast<int>(lo.z), static_cast<int>(lo.w),
+                   static_cast<int>(hi.x), static_cast<int>(hi.y), static_cast<int>(hi.z), static_cast<int>(hi.w)};
+  };
+  i32x16_t acc[FI][NJ] = {};
+  uint32_t slot = 0;
+  for (int b = wave; b < blocks; b += WAVES) {
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"((STAGES - 1) * T::ISSUED) : "memory");
+    i32x8_t f[2][FI + NJ];
+#pragma unroll
+    for (int kh = 0; kh < 2; ++kh)
+#pragma unroll
+      for (int i = 0; i < FI + NJ; ++i) f[kh][i] = read(lds + (slot + at[kh][0]) + 4096 * i, lds + (slot + at[kh][1]) + 4096 * i);
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");   // the slot is read
+    issue(slot, b + STAGES * WAVES);
+#pragma unroll
+    for (int kh = 0; kh < 2; ++kh)
+#pragma unroll
+      for (int i = 0; i < FI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = mma(f[kh][i], f[kh][FI + j], acc[i][j]);
+    slot = slot == (STAGES - 1) * T::SLOT ? 0 : slot + T::SLOT;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" : : : "memory");   // loads past the end write zeros
+  __syncthreads();
+  i32x4_t* part = reinterpret_cast<i32x4_t*>(ring);   // [wave][rows 8 r4 + 4 half + 0 .. 3 of fragment i][j][lane], as acc holds them
+#pragma unroll
+  for (int i = 0; i < FI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4)
+        part[((wave * FI * 4 + 4 * i + r4) * NJ + j) * 64 + lane] = i32x4_t{acc[i][j][4 * r4], acc[i][j][4 * r4 + 1], acc[i][j][4 * r4 + 2], acc[i][j][4 * r4 + 3]};
+  __syncthreads();
+  const float* side = reinterpret_cast<const float*>(lds + T::SIDE);
+  const int col = n0 + NJ * l32;
+  float sw[NJ], bias[NJ];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    sw[j] = side[NJ * l32 + j];
+    bias[j] = side[64 + NJ * l32 + j];
+  }
+#pragma unroll
+  for (int i = 0; i < FI; ++i) {   // wave r4 adds up and stores the rows of r4
+    const int at4 = 4 * i + wave, row0 = 8 * at4 + 4 * half;
+    i32x4_t sum[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      sum[j] = part[(at4 * NJ + j) * 64 + lane];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) sum[j] += part[((w * FI * 4 + at4) * NJ + j) * 64 + lane];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float sa = side[128 + row0 + e];
+      float v[NJ];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        v[j] = static_cast<float>(sum[j][e]) * (sa * sw[j]) + bias[j];
+        if (g.gelu) v[j] = fd::gelu(v[j]);
+      }
+      if (m0 + row0 + e >= M || col >= g.N) continue;
+      const size_t to = static_cast<size_t>(m0 + row0 + e) * g.N + col;
+      if constexpr (WIDE && NJ == 2) *reinterpret_cast<float2*>(g.y_f32 + to) = make_float2(v[0], v[1]);
+      else if constexpr (WIDE) g.y_f32[to] = v[0];
+      else if constexpr (NJ == 2) *reinterpret_cast<uint32_t*>(g.y_bf16 + to) = fd::pack_bf2(v[0], v[1]);
+      else g.y_bf16[to] = static_cast<uint16_t>(fd::pack_bf2(v[0], v[0]));
+    }
   }
 }
 
@@ -364,12 +501,13 @@ __global__ __launch_bounds__(T::THREADS, (PER_CU * T::WAVES + 3) / 4) void int_t
 
 namespace fdh {
 
-// The block-scaled product's rules: the loads, the tiles and the rate of the matrix instructions are the same.
+// Beyond few rows and few tiles the block-scaled product's rules: the loads, the tiles and the rate of the matrix instructions
+// are the same.
 hipError_t launch_int_linear(const IntLinearArgs& g, hipStream_t s) {
   auto run = [&](auto wide) {
     constexpr bool WIDE = decltype(wide)::value;
     using std::integral_constant;
-    if (fd::scaled_few(g.n_rows, g.N, g.K, false, false, num_cus())) {
+    if (fd::int_few(g.n_rows, g.N, g.K, num_cus())) {
       auto few = [&](auto fm, auto nf, auto deep) {
         constexpr int FM = decltype(fm)::value, NF = decltype(nf)::value;
         int_few_kernel<WIDE, FM, NF, decltype(deep)::value><<<dim3((g.N + 16 * NF - 1) / (16 * NF), (g.n_rows + 16 * FM - 1) / (16 * FM)), kFewWaves * 64, 0, s>>>(g);
@@ -389,6 +527,16 @@ hipError_t launch_int_linear(const IntLinearArgs& g, hipStream_t s) {
         else few(four, one, one);
       }
       return;
+    }
+    auto split = [&](auto tile) {
+      using T = decltype(tile);
+      int_split_kernel<WIDE, T><<<dim3((g.N + T::BN - 1) / T::BN, (g.n_rows + T::BM - 1) / T::BM), T::THREADS, 0, s>>>(g);
+    };
+    switch (fd::int_split(g.n_rows, g.N, g.K, num_cus())) {
+      case fd::kSplit32: return split(IntSplit<1, 1, 4>{});
+      case fd::kSplit32x64: return split(IntSplit<1, 2, 3>{});
+      case fd::kSplit64: return split(IntSplit<2, 2, 2>{});
+      default: break;
     }
     const int cus = num_cus() / 8 * 8;   // the tile order counts on whole rounds of the 8 XCDs
     const bool both = g.m && fd::scaled_both(g.n_rows, g.N, g.K, false, cus), large = !g.m && fd::scaled_large(g.n_rows, g.N, g.K, false, cus);
