@@ -187,10 +187,12 @@ def test_block_recorded(name):
 
 # (M, N, K): 256 x 256 tiles where the host knows the row count: short sums, last blocks of 16 and of 112 columns, tiles that rows
 # and columns leave part of, one tile a workgroup and two
+# and tiles of split K-blocks: 32 x 32 (from one row to 240; one block and a part, all waves, a last round of some), 32 x 64, 64 x 64
+SPLIT = [(1, 4624, 2320), (17, 16, 1296), (33, 528, 1552), (64, 1536, 6144), (240, 1040, 1408), (250, 1040, 4112), (300, 1552, 1296), (500, 1552, 1808), (513, 1536, 2064)]
 LARGE = [(8192, 2048, 16), (8190, 2032, 240), (8190, 2048, 512), (14999, 2032, 144)]
 
 
-@pytest.mark.parametrize("M,N,K", LARGE + [(3000, 1536, 400), (600, 1040, 4112), (129, 4096, 144)])
+@pytest.mark.parametrize("M,N,K", LARGE + SPLIT + [(3000, 1536, 400), (600, 1040, 4112), (129, 4096, 144)])
 @pytest.mark.parametrize("wide,gelu", [(False, True), (True, False)])
 def test_tiles(M, N, K, wide, gelu):
     """Integer operands of few bits, so that the sum times scales of powers of two, and its bias, are exact: every element's place."""
@@ -201,7 +203,7 @@ def test_tiles(M, N, K, wide, gelu):
     sa, sw = (2.0 ** torch.randint(-6, -3, (n,), generator=g, device="cuda").float() for n in (M, N))
     bias = torch.randint(-8, 9, (N,), generator=g, device="cuda").float() / 4
     z = (a.double() @ w.double().t()) * sa.double()[:, None] * sw.double() + bias.double()
-    for m in (None, M, M - 3):
+    for m in (None, M, max(M - 3, 0)):
         y = torch.full((M, N), 7.0, dtype=torch.float32 if wide else torch.bfloat16, device="cuda")
         fdl.fd_int_linear(a, sa, w, sw, y, bias=bias, gelu=gelu, m=None if m is None else count(m))
         n = M if m is None else m

@@ -280,6 +280,28 @@ def test_few_rows_rule(shim, dh, most):
             assert not shim.always_few(dh, ctypes.c_longlong(rows)) or shim.few_rows(dh, few, tiles)
 
 
+def test_product_rules(tmp_path):
+    """Which kernel a product runs: few rows, tiles of split K-blocks where each has a CU, or neither."""
+    (tmp_path / "r.cpp").write_text("""#include "fd_int_rules.h"
+extern "C" int way(int M, int N, int K, int cus) { return fd::int_few(M, N, K, cus) ? -1 : fd::int_split(M, N, K, cus); }
+""")
+    subprocess.run(["g++", "-std=c++17", "-shared", "-fPIC", f"-I{build.CSRC}", str(tmp_path / "r.cpp"), "-o", str(tmp_path / "r.so")], check=True)
+    way = ctypes.CDLL(str(tmp_path / "r.so")).way
+    few, none, split32, split32x64, split64 = -1, 0, 1, 2, 3
+    for M, N, K, want in ((1, 4608, 1536, few), (1, 4608, 6144, split32), (1, 1536, 6144, few), (16, 1536, 6144, split32), (1, 65536, 4096, few),
+                          (16, 8208, 4096, few), (17, 1536, 1088, few), (17, 1536, 1536, split32), (64, 1536, 1088, few), (64, 1536, 6144, split32),
+                          (129, 1536, 6144, split32), (171, 1536, 6144, split32x64), (256, 1536, 6144, split32x64), (512, 1536, 6144, split64),
+                          (512, 1536, 1536, none), (700, 1536, 6144, none), (1021, 4288, 1088, none), (9828, 6144, 1536, none)):
+        assert way(M, N, K, 256) == want, (M, N, K)
+    rng = np.random.default_rng(0)
+    for M, N, K in zip(*(np.exp(rng.uniform(0, np.log(t), 3000)).astype(int) for t in (40000, 4000, 4000))):
+        M, N, K = int(M), 16 * int(N), 16 * int(K)
+        w = way(M, N, K, 256)
+        if w > 0:      # a round of workgroups
+            bm, bn = {split32: (32, 32), split32x64: (32, 64), split64: (64, 64)}[w]
+            assert -(-M // bm) * -(-N // bn) <= 256
+
+
 def test_no_vector_memory_read_of_a_fresh_scalar(tmp_path):
     """The integer product's loads in inline assembly, searched as those of the bf16 products are."""
     out = tmp_path / "k.s"
