@@ -29,7 +29,7 @@ FD_DEVICE i32x16_t mma(const i32x8_t& a, const i32x8_t& w, i32x16_t c) {
 // workgroup takes the rows' FM fragments and 16 NF columns, its waves the K-blocks in turn, operands straight from memory
 // into registers, DEEP blocks at a time; the waves' sums meet in LDS.  The first operand is the weights, so that a lane
 // holds a row (l & 15) and, of its NF fragments, 4 NF consecutive columns.  1 x 4608 x 1536 4.4 us alone (7.1 MB: launch and two
-// round trips to memory), 64 x 4608 x 1536 7, 1 x 65536 x 4096 52 (5.2 TB/s).
+// round trips to memory), 64 x 4608 x 1088 4.7, 1 x 65536 x 4096 52 (5.2 TB/s).
 constexpr int kFewWaves = 8;
 
 template <bool WIDE, int FM, int NF, int DEEP>
@@ -272,8 +272,9 @@ struct IntTile {
 //
 // TOP/s: 32760 x 1536 x 6144 2230 to 2310 (the library's product alone 2230), 9828 x 1536 x 6144 2190, x 4608 x 1536 1750, x 6144 x
 // 1536 with GELU to bf16 1750 (matrix pipes 43% busy, vector instructions 34%, little of it at once: the results have no product
-// beside them, one workgroup a CU; in 128 x 128 tiles 120 us for 123).  Where workgroups have one tile each the steps count: 0.49
-// us of matrix instructions a wave and K-block (1664 x 1536 x 6144 28 us; 1021 x 4288 x 1088 14, 16 of 256 CUs with two tiles).
+// beside them, one workgroup a CU; in 128 x 128 tiles 120 us for 123).  Where a 128 x 128 workgroup is alone on its CU a K-step
+// takes 0.5 us: 512 clocks of matrix instructions, 900 of LDS (80 KB read, 32 written), with no other wave on the SIMD to fill the
+// waits (1664 x 1536 x 6144 28 us; 1021 x 4288 x 1088 14, 16 of 256 CUs with two tiles).
 template <class T, bool WIDE>
 FD_DEVICE void int_tiles(const fdh::IntLinearArgs& g, int M, uint4* ring) {
   constexpr int FI = T::FI, NJ = T::NJ, STAGES = T::STAGES, kSubs = 2 * NJ, kSize = WIDE ? 4 : 2;
