@@ -1,4 +1,4 @@
-// Which kernels a product of 8-bit integers runs: rules for few rows and few tiles, then those of the block-scaled product.
+// Which kernels a product of 8-bit integers runs.
 // Plain C++, shared by the device code, the host code and a CPU build.
 #pragma once
 
@@ -25,6 +25,24 @@ enum { kSplitNone, kSplit32, kSplit32x64, kSplit64 };
 FD_RULE int int_split(int M, int N, int K, int cus) {
   return int_one_round(M, N, 32, 32, cus) ? kSplit32 : int_one_round(M, N, 32, 64, cus) ? kSplit32x64
          : K > 14 * 128 && int_one_round(M, N, 64, 64, cus) ? kSplit64 : kSplitNone;
+}
+
+// 256 x 256 tiles, one workgroup a CU, rather than 128 x 128, two: the shorter of what their rounds take, in hundredths of a K-block of
+// 128 x 128 tiles on full CUs (0.82 us).  A round of small tiles on half the CUs' places (one each) takes 0.52 a K-block and 2.7 at its
+// ends, of large ones 1.2 on up to half the CUs, 1.9 and more on all of them (power), and 9, 12 with fp32 results.  us, small and
+// large: 5000 x 1600 x 6400 (1.02 rounds and 0.55) 74 and 66, 2048 x 6400 x 6400 (1.56, 0.78) 99 and 80, 2600 rows (2.05, 1.07) 125 and
+// 149, 9828 rows (7.52, 3.81) 423 and 351; 6000 x 4608 x 1536 to fp32 (3.30, 1.69) 52 and 58, 4000 x 3200 x 3200 (1.56, 0.81) 52 and 46.
+FD_RULE bool int_large(int M, int N, int K, bool wide, int cus) {
+  const long long blocks = (K + 127) / 128, ends = wide ? 1200 : 900;
+  const long long small = static_cast<long long>((M + 127) / 128) * ((N + 127) / 128), large = static_cast<long long>((M + 255) / 256) * ((N + 255) / 256);
+  const long long full = large / cus, rest = large % cus, over = 2 * rest > cus ? 2 * rest - cus : 0;
+  return full * (190 * blocks + ends) + (rest ? 120 * blocks + 80 * blocks * over / cus + ends : 0) < (small + cus - 1) / cus * (52 * blocks + 270);
+}
+
+// Whether a call whose row count only the device knows launches both kernels, of which one ends at once (4 to 5 us): where large tiles
+// win at capacity by more than that, or may at a part of it as in the block-scaled product.
+FD_RULE bool int_both(int n_max, int N, int K, bool wide, int cus) {
+  return scaled_both(n_max, N, K, false, cus) || (2.0 * n_max * N * K >= 8e10 && int_large(n_max, N, K, wide, cus));
 }
 
 }  // namespace fd

@@ -494,7 +494,7 @@ __global__ __launch_bounds__(T::THREADS, (PER_CU * T::WAVES + 3) / 4) void int_t
   __shared__ uint4 ring[T::TOTAL];
   static_assert(T::TOTAL * 16 * PER_CU <= 160 * 1024, "the LDS of a CU");
   const int M = g.m ? min(*g.m, g.n_rows) : g.n_rows;
-  if (M <= 0 || (cus > 0 && fd::scaled_large(M, g.N, g.K, false, cus) != (T::BM == TileLarge::BM))) return;
+  if (M <= 0 || (cus > 0 && fd::int_large(M, g.N, g.K, WIDE, cus) != (T::BM == TileLarge::BM))) return;
   int_tiles<T, WIDE>(g, M, ring);
 }
 
@@ -502,8 +502,6 @@ __global__ __launch_bounds__(T::THREADS, (PER_CU * T::WAVES + 3) / 4) void int_t
 
 namespace fdh {
 
-// Beyond few rows and few tiles the block-scaled product's rules: the loads, the tiles and the rate of the matrix instructions
-// are the same.
 hipError_t launch_int_linear(const IntLinearArgs& g, hipStream_t s) {
   auto run = [&](auto wide) {
     constexpr bool WIDE = decltype(wide)::value;
@@ -540,7 +538,7 @@ hipError_t launch_int_linear(const IntLinearArgs& g, hipStream_t s) {
       default: break;
     }
     const int cus = num_cus() / 8 * 8;   // the tile order counts on whole rounds of the 8 XCDs
-    const bool both = g.m && fd::scaled_both(g.n_rows, g.N, g.K, false, cus), large = !g.m && fd::scaled_large(g.n_rows, g.N, g.K, false, cus);
+    const bool both = g.m && fd::int_both(g.n_rows, g.N, g.K, WIDE, cus), large = !g.m && fd::int_large(g.n_rows, g.N, g.K, WIDE, cus);
     auto tiles = [&](auto tile, auto per_cu, int check) {
       using T = decltype(tile);
       constexpr int PER_CU = decltype(per_cu)::value;

@@ -284,9 +284,14 @@ def test_product_rules(tmp_path):
     """Which kernel a product runs: few rows, tiles of split K-blocks where each has a CU, or neither."""
     (tmp_path / "r.cpp").write_text("""#include "fd_int_rules.h"
 extern "C" int way(int M, int N, int K, int cus) { return fd::int_few(M, N, K, cus) ? -1 : fd::int_split(M, N, K, cus); }
+extern "C" int large(int M, int N, int K, int wide, int cus) { return fd::int_large(M, N, K, wide, cus); }
 """)
     subprocess.run(["g++", "-std=c++17", "-shared", "-fPIC", f"-I{build.CSRC}", str(tmp_path / "r.cpp"), "-o", str(tmp_path / "r.so")], check=True)
-    way = ctypes.CDLL(str(tmp_path / "r.so")).way
+    lib = ctypes.CDLL(str(tmp_path / "r.so"))
+    way = lib.way
+    for M, N, K, wide, want in ((5000, 1600, 6400, 0, 1), (2048, 6400, 6400, 0, 1), (2600, 6400, 6400, 0, 0), (9828, 6144, 1536, 0, 1), (9828, 1536, 6144, 0, 1),
+                                (5000, 1536, 6144, 0, 0), (6000, 4608, 1536, 1, 0), (32760, 1536, 6144, 1, 1), (1664, 1536, 6144, 0, 0), (1 << 30, 1 << 20, 65536, 1, 1)):
+        assert lib.large(M, N, K, wide, 256) == want, (M, N, K)
     few, none, split32, split32x64, split64 = -1, 0, 1, 2, 3
     for M, N, K, want in ((1, 4608, 1536, few), (1, 4608, 6144, split32), (1, 1536, 6144, few), (16, 1536, 6144, split32), (1, 65536, 4096, few),
                           (16, 8208, 4096, few), (17, 1536, 1088, few), (17, 1536, 1536, split32), (64, 1536, 1088, few), (64, 1536, 6144, split32),
