@@ -272,9 +272,10 @@ struct IntTile {
 //
 // TOP/s: 32760 x 1536 x 6144 2230 to 2310 (the library's product alone 2230), 9828 x 1536 x 6144 2190, x 4608 x 1536 1750, x 6144 x
 // 1536 with GELU to bf16 1750 (matrix pipes 43% busy, vector instructions 34%, little of it at once: the results have no product
-// beside them, one workgroup a CU; in 128 x 128 tiles 120 us for 123).  Where a 128 x 128 workgroup is alone on its CU a K-step
-// takes 0.5 us: 512 clocks of matrix instructions, 900 of LDS (80 KB read, 32 written), with no other wave on the SIMD to fill the
-// waits (1664 x 1536 x 6144 28 us; 1021 x 4288 x 1088 14, 16 of 256 CUs with two tiles).
+// beside them, one workgroup a CU; in 128 x 128 tiles 120 us for 123).  Where a 128 x 128 workgroup is alone on its CU it has eight
+// waves: more reads of LDS (96 KB a K-block for 80, beside 32 written), which bound it at 0.43 us a K-block, but two waves a SIMD:
+// 1664 x 1536 x 6144 28.1 -> 25.3 us, 700 x 3200 x 3200 16.8 -> 15.9; four waves of 64 x 64 and three or four stages 27.5 and 27.9.
+// 1021 x 4288 x 1088 14: 16 of 256 CUs have two tiles.
 template <class T, bool WIDE>
 FD_DEVICE void int_tiles(const fdh::IntLinearArgs& g, int M, uint4* ring) {
   constexpr int FI = T::FI, NJ = T::NJ, STAGES = T::STAGES, kSubs = 2 * NJ, kSize = WIDE ? 4 : 2;
@@ -486,6 +487,7 @@ FD_DEVICE void int_tiles(const fdh::IntLinearArgs& g, int M, uint4* ring) {
 
 using Tile64 = IntTile<1, 2, 2, 2, 3>;      // 64 x 128, two workgroups per CU
 using Tile128 = IntTile<1, 4, 4, 1, 2>;     // 128 x 128, two
+using TileAlone = IntTile<1, 2, 4, 2, 4>;   // 128 x 128, one, of eight waves
 using TileLarge = IntTile<2, 4, 4, 2, 2>;   // 256 x 256, one
 
 // Where both kernels are launched (cus > 0), the one that the row count does not call for ends at once.
@@ -546,6 +548,7 @@ hipError_t launch_int_linear(const IntLinearArgs& g, hipStream_t s) {
       int_tile_kernel<WIDE, T, PER_CU><<<static_cast<int>(all < most ? (all + 7) / 8 * 8 : most), T::THREADS, 0, s>>>(g, check);
     };
     if (fd::scaled_small(g.n_rows, g.N, cus)) return tiles(Tile64{}, integral_constant<int, 2>{}, 0);
+    if (!both && !large && fd::int_one_round(g.n_rows, g.N, 128, 128, cus)) return tiles(TileAlone{}, integral_constant<int, 1>{}, 0);
     if (both || !large) tiles(Tile128{}, integral_constant<int, 2>{}, both ? cus : 0);
     if (both || large) tiles(TileLarge{}, integral_constant<int, 1>{}, both ? cus : 0);
   };

@@ -192,7 +192,7 @@ SPLIT = [(1, 4624, 2320), (17, 16, 1296), (33, 528, 1552), (64, 1536, 6144), (24
 LARGE = [(8192, 2048, 16), (8190, 2032, 240), (8190, 2048, 512), (14999, 2032, 144)]
 
 
-@pytest.mark.parametrize("M,N,K", LARGE + SPLIT + [(3000, 1536, 400), (600, 1040, 4112), (129, 4096, 144)])
+@pytest.mark.parametrize("M,N,K", LARGE + SPLIT + [(3000, 1536, 400), (600, 1040, 4112), (129, 4096, 144), (1664, 1536, 1104), (1300, 2064, 400)])
 @pytest.mark.parametrize("wide,gelu", [(False, True), (True, False)])
 def test_tiles(M, N, K, wide, gelu):
     """Integer operands of few bits, so that the sum times scales of powers of two, and its bias, are exact: every element's place."""
