@@ -523,8 +523,9 @@ fd_status fd_int_rows(int32_t n_rows, int32_t cols, const uint16_t* x, const int
 
 /*
  * A linear layer on integers:
- *   y[i][j] = act(sum_k a[i][k] w[j][k] * (a_scale[i] * w_scale[j]) + bias[j])  for i < *m,
- * the sum exact, then in fp32; act GELU (tanh form) or none.  -128 is taken as it is.
+ *   y[i][j] = act(sum_k a[i][k] w[j][k] * w_scale[j] * a_scale[i] + bias[j])  for i < *m,
+ * the sum exact, then in fp32 from left to right; act GELU (tanh form) or none.  -128 is taken as it
+ * is.  For w_scale below 2^98 (weights below 2^104) only the result itself can pass fp32's range.
  *   a, a_scale  device int8 [n_rows][n_in], fp32 [n_rows]
  *   w, w_scale  device int8 [n_out][n_in], fp32 [n_out]
  *   bias        device fp32 [n_out] or null

@@ -1,6 +1,8 @@
 // The product of 8-bit integers with a scale per row and per column:
-//   Y[M][N] = act(float(sum_k A[i][k] W[j][k]) * (a_scale[i] * w_scale[j]) + bias[j])
-// on v_mfma_i32_16x16x64_i8 and 32x32x32: the sums are whole numbers of at most 2^30 (K <= 2^16) and exact.
+//   Y[M][N] = act(float(sum_k A[i][k] W[j][k]) * w_scale[j] * a_scale[i] + bias[j])
+// on v_mfma_i32_16x16x64_i8 and 32x32x32: the sums are whole numbers of at most 2^30 (K <= 2^16) and exact.  A sum meets the
+// scales one after the other: 0 or at least 1, it stays a normal number times scales from 2^-107 to 2^98.  The scales' product
+// need not be one: below 2^-126 it loses bits, past 2^128 it makes NaN of a sum of zero.
 #include <type_traits>
 
 #include "fd_int.h"
@@ -90,8 +92,8 @@ __global__ __launch_bounds__(kFewWaves * 64) void int_few_kernel(fdh::IntLinearA
     for (int p = 1; p < kFewWaves; ++p) sum += part[p][wave][j][lane];
     const int c = min(col + 4 * j, g.N - 4);
     const float4 sw = *reinterpret_cast<const float4*>(g.w_scale + c), bias = g.bias ? *reinterpret_cast<const float4*>(g.bias + c) : make_float4(0, 0, 0, 0);
-    float v[4] = {static_cast<float>(sum[0]) * (sa * sw.x) + bias.x, static_cast<float>(sum[1]) * (sa * sw.y) + bias.y,
-                  static_cast<float>(sum[2]) * (sa * sw.z) + bias.z, static_cast<float>(sum[3]) * (sa * sw.w) + bias.w};
+    float v[4] = {static_cast<float>(sum[0]) * sw.x * sa + bias.x, static_cast<float>(sum[1]) * sw.y * sa + bias.y,
+                  static_cast<float>(sum[2]) * sw.z * sa + bias.z, static_cast<float>(sum[3]) * sw.w * sa + bias.w};
     if (g.gelu) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = fd::gelu(v[e]);
@@ -227,7 +229,7 @@ __global__ __launch_bounds__(T::THREADS) void int_split_kernel(fdh::IntLinearArg
       float v[NJ];
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
-        v[j] = static_cast<float>(sum[j][e]) * (sa * sw[j]) + bias[j];
+        v[j] = static_cast<float>(sum[j][e]) * sw[j] * sa + bias[j];
         if (g.gelu) v[j] = fd::gelu(v[j]);
       }
       if (m0 + row0 + e >= M || col >= g.N) continue;
@@ -462,7 +464,7 @@ FD_DEVICE void int_tiles(const fdh::IntLinearArgs& g, int M, uint4* ring) {
           float v[NJ];
 #pragma unroll
           for (int j = 0; j < NJ; ++j) {
-            v[j] = static_cast<float>(acc[i][j][4 * r4 + e]) * (sa[e] * sw[j]) + bias[j];
+            v[j] = static_cast<float>(acc[i][j][4 * r4 + e]) * sw[j] * sa[e] + bias[j];
             if (g.gelu) v[j] = fd::gelu(v[j]);
           }
           const uint32_t to = col_ok && row < rows ? off : kNowhere;

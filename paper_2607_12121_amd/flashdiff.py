@@ -649,7 +649,7 @@ def fd_int_rows(x, q, scale, m=None, stream=None) -> None:
 
 
 def fd_int_linear(a, a_scale, w, w_scale, y, bias=None, gelu: bool = False, m=None, stream=None) -> None:
-    """y = act((a w^T) * a_scale * w_scale + bias) of int8 a [rows, n_in] and w [n_out, n_in] with fp32 scales per row
+    """y = act((a w^T) * w_scale * a_scale + bias) of int8 a [rows, n_in] and w [n_out, n_in] with fp32 scales per row
     and per output channel; y bf16 or fp32."""
     (rows, k), (n, kw) = _rows("a", a), _rows("w", w)
     if k != kw:
