@@ -45,4 +45,22 @@ FD_RULE bool int_both(int n_max, int N, int K, bool wide, int cus) {
   return scaled_both(n_max, N, K, false, cus) || (2.0 * n_max * N * K >= 8e10 && int_large(n_max, N, K, wide, cus));
 }
 
+// The kernel of a call of `rows` rows on a device of `num_cus` CUs: few rows, tiles of split K-blocks, tiles of 64 x 128, 128 x 128
+// alone on their CUs or two, 256 x 256, or (both) whichever of the last two the row count on the device calls for.
+enum IntKernel { kIntFew, kIntSplit32, kIntSplit32x64, kIntSplit64, kInt64, kIntAlone, kInt128, kInt256, kIntBoth };
+FD_RULE IntKernel int_kernel(int rows, int N, int K, bool wide, bool counted_on_device, int num_cus) {
+  if (int_few(rows, N, K, num_cus)) return kIntFew;
+  switch (int_split(rows, N, K, num_cus)) {
+    case kSplit32: return kIntSplit32;
+    case kSplit32x64: return kIntSplit32x64;
+    case kSplit64: return kIntSplit64;
+    default: break;
+  }
+  const int cus = num_cus / 8 * 8;   // the tile order counts on whole rounds of the 8 XCDs
+  if (scaled_small(rows, N, cus)) return kInt64;
+  if (counted_on_device && int_both(rows, N, K, wide, cus)) return kIntBoth;
+  if (!counted_on_device && int_large(rows, N, K, wide, cus)) return kInt256;
+  return int_one_round(rows, N, 128, 128, cus) ? kIntAlone : kInt128;
+}
+
 }  // namespace fd

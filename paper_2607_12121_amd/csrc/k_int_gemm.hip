@@ -510,49 +510,50 @@ hipError_t launch_int_linear(const IntLinearArgs& g, hipStream_t s) {
   auto run = [&](auto wide) {
     constexpr bool WIDE = decltype(wide)::value;
     using std::integral_constant;
-    if (fd::int_few(g.n_rows, g.N, g.K, num_cus())) {
-      auto few = [&](auto fm, auto nf, auto deep) {
-        constexpr int FM = decltype(fm)::value, NF = decltype(nf)::value;
-        int_few_kernel<WIDE, FM, NF, decltype(deep)::value><<<dim3((g.N + 16 * NF - 1) / (16 * NF), (g.n_rows + 16 * FM - 1) / (16 * FM)), kFewWaves * 64, 0, s>>>(g);
-      };
-      const integral_constant<int, 1> one{};
-      const integral_constant<int, 2> two{};
-      const integral_constant<int, 3> three{};
-      const integral_constant<int, 4> four{};
-      const int frags = fd::scaled_few_frags(g.n_rows);
-      if (fd::scaled_few_wide(g.N, num_cus())) {
-        if (frags == 1) few(one, two, two);
-        else if (frags == 2) few(two, two, two);
-        else few(four, two, one);
-      } else {
-        if (frags == 1) few(one, one, three);
-        else if (frags == 2) few(two, one, two);
-        else few(four, one, one);
-      }
-      return;
-    }
+    const integral_constant<int, 1> one{};
+    const integral_constant<int, 2> two{};
+    const integral_constant<int, 3> three{};
+    const integral_constant<int, 4> four{};
+    auto few = [&](auto fm, auto nf, auto deep) {
+      constexpr int FM = decltype(fm)::value, NF = decltype(nf)::value;
+      int_few_kernel<WIDE, FM, NF, decltype(deep)::value><<<dim3((g.N + 16 * NF - 1) / (16 * NF), (g.n_rows + 16 * FM - 1) / (16 * FM)), kFewWaves * 64, 0, s>>>(g);
+    };
     auto split = [&](auto tile) {
       using T = decltype(tile);
       int_split_kernel<WIDE, T><<<dim3((g.N + T::BN - 1) / T::BN, (g.n_rows + T::BM - 1) / T::BM), T::THREADS, 0, s>>>(g);
     };
-    switch (fd::int_split(g.n_rows, g.N, g.K, num_cus())) {
-      case fd::kSplit32: return split(IntSplit<1, 1, 4>{});
-      case fd::kSplit32x64: return split(IntSplit<1, 2, 3>{});
-      case fd::kSplit64: return split(IntSplit<2, 2, 2>{});
-      default: break;
-    }
-    const int cus = num_cus() / 8 * 8;   // the tile order counts on whole rounds of the 8 XCDs
-    const bool both = g.m && fd::int_both(g.n_rows, g.N, g.K, WIDE, cus), large = !g.m && fd::int_large(g.n_rows, g.N, g.K, WIDE, cus);
+    const int cus = num_cus() / 8 * 8;
     auto tiles = [&](auto tile, auto per_cu, int check) {
       using T = decltype(tile);
       constexpr int PER_CU = decltype(per_cu)::value;
       const long long all = static_cast<long long>((g.n_rows + T::BM - 1) / T::BM) * ((g.N + T::BN - 1) / T::BN), most = PER_CU * cus;
       int_tile_kernel<WIDE, T, PER_CU><<<static_cast<int>(all < most ? (all + 7) / 8 * 8 : most), T::THREADS, 0, s>>>(g, check);
     };
-    if (fd::scaled_small(g.n_rows, g.N, cus)) return tiles(Tile64{}, integral_constant<int, 2>{}, 0);
-    if (!both && !large && fd::int_one_round(g.n_rows, g.N, 128, 128, cus)) return tiles(TileAlone{}, integral_constant<int, 1>{}, 0);
-    if (both || !large) tiles(Tile128{}, integral_constant<int, 2>{}, both ? cus : 0);
-    if (both || large) tiles(TileLarge{}, integral_constant<int, 1>{}, both ? cus : 0);
+    const int frags = fd::scaled_few_frags(g.n_rows);
+    switch (fd::int_kernel(g.n_rows, g.N, g.K, WIDE, g.m != nullptr, num_cus())) {
+      case fd::kIntFew:
+        if (fd::scaled_few_wide(g.N, num_cus())) {
+          if (frags == 1) few(one, two, two);
+          else if (frags == 2) few(two, two, two);
+          else few(four, two, one);
+        } else {
+          if (frags == 1) few(one, one, three);
+          else if (frags == 2) few(two, one, two);
+          else few(four, one, one);
+        }
+        break;
+      case fd::kIntSplit32: split(IntSplit<1, 1, 4>{}); break;
+      case fd::kIntSplit32x64: split(IntSplit<1, 2, 3>{}); break;
+      case fd::kIntSplit64: split(IntSplit<2, 2, 2>{}); break;
+      case fd::kInt64: tiles(Tile64{}, two, 0); break;
+      case fd::kIntAlone: tiles(TileAlone{}, one, 0); break;
+      case fd::kInt128: tiles(Tile128{}, two, 0); break;
+      case fd::kInt256: tiles(TileLarge{}, one, 0); break;
+      case fd::kIntBoth:
+        tiles(Tile128{}, two, cus);
+        tiles(TileLarge{}, one, cus);
+        break;
+    }
   };
   if (g.y_f32) run(std::true_type{});
   else run(std::false_type{});
