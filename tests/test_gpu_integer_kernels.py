@@ -16,7 +16,9 @@ CUS = 256
 LISTED = [
     ("few1x1", False, 11, 64, 144), ("few1x1", True, 16, 4096, 1088), ("few1x2", False, 9, 4624, 1088), ("few1x2", True, 16, 8208, 16),
     ("few2x1", True, 20, 528, 272), ("few2x1", False, 32, 4096, 1040),
+    ("few2x2", False, 20, 4624, 1280), ("few2x2", True, 31, 8176, 144), ("few2x2", True, 17, 4608, 1088), ("few2x2", False, 32, 4112, 16),
     ("few4x1", False, 50, 528, 272), ("few4x1", True, 64, 1536, 1088),
+    ("few4x2", False, 33, 4624, 272), ("few4x2", True, 64, 4608, 1088), ("few4x2", True, 63, 8176, 144), ("few4x2", False, 48, 4112, 1264),
     ("split32", True, 33, 528, 1552), ("split32", False, 224, 1040, 1408), ("split32x64", False, 250, 1040, 4112), ("split32x64", True, 300, 1552, 1296),
     ("split64", True, 500, 1552, 1808), ("split64", False, 513, 1536, 2064),
     ("64x128", False, 600, 1040, 400), ("64x128", True, 129, 4096, 144), ("alone", True, 1664, 1536, 1104), ("alone", False, 1300, 2064, 400),

@@ -36,7 +36,7 @@ def test_listed_shapes_run_their_kernels(rules, wide):
         assert kernel(rules, M, N, K, wide, int(counted)) == name, (M, N, K)
         if name == "both":          # the count at capacity picks the large tiles, a third of it the small ones
             assert rules.large(M, N, K, wide, CUS) and not rules.large(M // 3, N, K, wide, CUS)
-    assert {name for name, *_ in LISTED} == {"few1x1", "few1x2", "few2x1", "few4x1"} | set(TILES)
+    assert {name for name, *_ in LISTED} == {f"few{a}x{b}" for a in (1, 2, 4) for b in (1, 2)} | set(TILES)
     tiles = [-(-M // 256) * -(-N // 256) for name, _, M, N, _ in LISTED if name == "256x256"]
     assert min(tiles) <= CUS and any(CUS < t <= 2 * CUS for t in tiles) and any(t > 2 * CUS for t in tiles)
 
