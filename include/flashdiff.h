@@ -585,8 +585,8 @@ fd_status fd_cache_write(int32_t n_rows, int32_t n_tokens, const fd_rope* rope, 
  * Attention of the active rows over every token of their request in an 8-bit cache:
  *   o_i = softmax(scale * q_i K_b^T) V_b   per head, head h with the keys of key head h / (heads / kv_heads),
  * for the rows cu_q[b] <= i < cu_q[b + 1] and the tokens req_tok_off[b] .. req_tok_off[b + 1] - 1 of each
- * request b.  Products of the values that the codes stand for; scores, softmax and sums in fp32, probabilities
- * rounded to bf16.  Rows of a request without tokens are zeros; rows past cu_q[n_requests] are untouched.
+ * request b.  Products of the values that the codes stand for (of scales s = 1 and 2 rounded to multiples of 2^-133,
+ * bf16's least; others exact); scores, softmax and sums in fp32, probabilities rounded to bf16.  Rows of a request without tokens are zeros; rows past cu_q[n_requests] are untouched.
  *   n_rows      row capacity, cu_q[n_requests] <= n_rows
  *   max_request_tokens  the most tokens of a request (as in fd_plan): sizes the launch
  *   heads       a multiple of kv_heads; dh in {16, 64, 128}

@@ -1,6 +1,7 @@
 // Attention of the active rows over every token of their request, keys and values from an 8-bit cache: e4m3 codes
-// with a power-of-two scale per token and key head.  Codes times scales are bf16 values without a rounding, so both
-// contractions run on v_mfma_f32_32x32x16_bf16 as for a bf16 cache; fp32 online softmax, base 2.
+// with a power-of-two scale per token and key head.  Codes times scales are bf16 values without a rounding (but for scales of
+// 2^-126 and 2^-125, whose least codes are below bf16's least value, 2^-133), so both contractions run on
+// v_mfma_f32_32x32x16_bf16 as for a bf16 cache; fp32 online softmax, base 2.
 //
 // The query heads that share a key head are rows of one problem: row r of a request under key head kh is query
 // r / group, head kh * group + r % group.  A wave computes S^T = K Q^T (64 keys x 32 rows), so that a lane owns one
