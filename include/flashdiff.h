@@ -567,6 +567,7 @@ fd_status fd_norm_residual(int32_t n_rows, int32_t D, int32_t n_requests, float*
  * of every token of every block; the paper does not prescribe their format): keys and values as
  * e4m3 codes, one scale byte per token and key head.  A value is code * 2^(s - 127) as for the 8-bit
  * rows, its block the head's dh values; s is 1 .. 247, or 255 for a head that holds an infinity or a NaN.
+ * Outputs overlap neither inputs nor each other.
  *   k, v              device e4m3 [n_tokens][kv_heads dh], 16-byte aligned
  *   k_scale, v_scale  device uint8 [kv_heads][n_tokens] (a head's bytes side by side)
  */

@@ -25,7 +25,8 @@
 //
 // Measured, both kernels: 9828 rows of 12 heads of 128 over 32760 keys 1.72 to 1.80 ms (1.1 PFLOP/s; matrix pipes 53% busy at 1.9
 // GHz: power), 8937 rows of 8 requests, 24 heads of 64 on 8 key heads, 249 us (0.77 PFLOP/s; matrix pipes 35%, vector
-// instructions 58%: two exponentials a pair of scores and their packing take as long as the products), one row of 12 heads over
+// instructions 58%: two exponentials a pair of scores and their packing take as long as the products), 4000 rows of 64 heads of 16 over
+// 8000 keys 475 us (0.28 PFLOP/s; vector instructions 72%, matrix pipes 17%), one row of 12 heads over
 // 32760 keys 34 us (101 MB: 16 us of reads at 6.5 TB/s behind 5 us of schedule and first loads, 4 us of joining the waves, 5 us of
 // joining the pieces).
 #include <type_traits>

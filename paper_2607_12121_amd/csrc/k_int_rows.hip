@@ -79,7 +79,7 @@ enum { kNone, kBf16, kCodes, kInts };
 // A team of LANES lanes (16, 32 or whole waves) takes a run of rows, lane t the 8 columns at 8 * (t + LANES * j), j < VEC, and
 // keeps a request's factors of a value (gate * post_weight, weight * (1 + scale), shift) in registers while the request stays;
 // the next row is on its way while one is summed.  Bound by HBM: 4 bytes of h read and 4 written, 2 of y, 1 or 2 of the result
-// per value; 8937 x 1536 with y to codes 27 us alone, 32 among other calls (4.7 TB/s).
+// per value; 8937 x 1536 with y to codes 27 us alone, 32 among other calls (4.7 TB/s), to integers 29, h alone 23.
 template <int VEC, int LANES, int OUT>
 __global__ __launch_bounds__(team_threads<LANES>()) void norm_residual_kernel(fdh::ResidualArgs g) {
   constexpr int TEAMS = team_threads<LANES>() / LANES, WAVES = (LANES + 63) / 64;
@@ -262,6 +262,11 @@ hipError_t launch_int_rows(const uint16_t* x, int n_rows, int cols, const int32_
     const int groups = (n_rows + TEAMS - 1) / TEAMS, most = 16 * num_cus();
     int_rows_kernel<VEC, LANES><<<groups < most ? groups : most, team_threads<LANES>(), 0, s>>>(x, n_rows, cols, m, q, scale);
   };
+  // Teams by width.  Some 60 million values, us, these and the fastest of 16 to 1024 lanes with 8 to 64 columns each: up to 128
+  // columns these (64 columns 51, 128 34.6; on 32 lanes 49), 208 columns 37.3 and 35.7 (16 lanes of 16), 512 36.1 and 33.8 (16 of 64), 768 35.2 and
+  // 33.9 (16 of 64), 1024 34.6 and 33.9 (32 of 64; three waves of 8 would be 36), 1088 46.0 and 33.8 (32 of 64), 1536 37.7 and 34.0 (32 of
+  // 64), 2048 36 and 33.8 (64 of 64), 4096 34.7 and 34.3 (64 of 64), 6144 34.6 and 34.1 (512 of 32), 8192 34.3 and 33.2 (256 of 64), 12288 47.7 and
+  // 33.5 (512 of 32), 16384 44.4 and 34.2 (1024 of 16), 32768 41.5 and 37.1 (512 of 64).  1021 rows take the same 6.3 to 6.6 with any, up to 8192 columns.
   const integral_constant<int, 1> one{};
   const integral_constant<int, 2> two{};
   const integral_constant<int, 4> four{};
@@ -290,7 +295,10 @@ hipError_t launch_norm_residual(const ResidualArgs& g, hipStream_t s) {
       norm_residual_kernel<VEC, LANES, OUT><<<groups < most ? groups : most, team_threads<LANES>(), 0, s>>>(g);
     };
     // eight columns a lane, up to eight waves; as many workgroups as are resident, whose runs are read with the
-    // next row on its way
+    // next row on its way.  13.7 million values with y to bf16, us, these and the next best of 16 to 512 lanes with 8 to 24 columns
+    // each: 128 columns 34.5 and 42.0, 256 34.4 and 37.1, 512 35.5 and 41.8, 1024 33.9 and 35.9 (192 lanes; 64 of 16 columns 40.0), 1536 34.2 and
+    // 36.1, 2048 34.5 and 38.1, 4096 34.2 and 39.3, 8192 43.3 and 44.0; another is ahead at 640 (40.5 and 40.1, 32 lanes of 24),
+    // 2560 (39.3 and 39.1, 128 of 24) and 6144 (44.9 and 40.4, 256 of 24); to integers in the same order
     const integral_constant<int, 1> one{};
     const integral_constant<int, 512> widest{};
     if (g.D <= 128) run(one, integral_constant<int, 16>{});
